@@ -1,0 +1,384 @@
+"""Operators of token models, as cases that can be timed and compared: plain torch, and the kernel-level entry points.
+
+A case is a dict of plain values; ``kind`` says which operator it is about:
+
+  embedding  ``cdp_k_embedding``: rows of a table scaled, and the table's gradient (fp32) by sorted tokens
+  norm       ``cdp_k_residual_norm``, ``cdp_k_residual_norm_backward``: norm after a block, gate, residual scale, norm before the next
+  attention  ``cdp_k_attention_packed``: causal attention over packed sequences of different lengths, grouped heads
+  clip       ``cdp_k_grad_clip``: the norm over all gradients of a model, and the clipped gradients
+
+Where ``own`` is false, ``run`` is elementary torch operations in 32 bits, rounded once; ``exact`` is the same from the definitions in 64.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+DTYPES = {"f32": (0, torch.float32, 4), "bf16": (1, torch.bfloat16, 2)}
+EPS = 1e-6
+
+
+def listed():
+    return [
+        # A toy vocabulary, fp32: what a call costs when there is next to nothing to do.
+        dict(name="embedding_small_f32", kind="embedding", dtype="f32", rows=64, vocab=1000, width=64, scale=1.0, padding=0.0, backward=True),
+        # Eight packed sequences of 1024 tokens with a little padding, a vocabulary of no round size, ViT-B's width.
+        dict(name="embedding_words_bf16", kind="embedding", dtype="bf16", rows=8192, vocab=50257, width=768, scale=27.7, padding=0.05, backward=True),
+        # A large vocabulary under a large batch: the gradient's table is what costs.
+        dict(name="embedding_large_bf16", kind="embedding", dtype="bf16", rows=32768, vocab=128000, width=2048, scale=1.0, padding=0.0, backward=True),
+        # One micro-batch of the smallest width.
+        dict(name="norm_small_f32", kind="norm", dtype="f32", rows=64, width=64, post=True, gate=True, scale=0.5, backward=True),
+        # 32 x 196 tokens of ViT-B's width: forward and backward of one block's end.
+        dict(name="norm_vit_bf16", kind="norm", dtype="bf16", rows=6272, width=768, post=True, gate=True, scale=0.25, backward=True),
+        # A large model's width.
+        dict(name="norm_wide_bf16", kind="norm", dtype="bf16", rows=16384, width=4096, post=True, gate=True, scale=0.125, backward=True),
+        # Three short sequences, one of them a single token, some rows behind the last: launch costs.
+        dict(name="attention_small_f32", kind="attention", dtype="f32", tokens=64, sequences=3, split=1, tail=5, heads=4, kv_heads=2, width=16, backward=True),
+        # 24 sequences of different lengths packed into 8192 rows, three query heads to a key head.
+        dict(name="attention_packed_bf16", kind="attention", dtype="bf16", tokens=8192, sequences=24, split=2, tail=100, heads=12, kv_heads=4, width=64, backward=True),
+        # One whole prompt of a large model, four query heads to a key head.
+        dict(name="attention_long_bf16", kind="attention", dtype="bf16", tokens=8192, sequences=1, split=0, tail=0, heads=32, kv_heads=8, width=128, backward=True),
+        # Odd lengths and head width, as many key heads as query heads, fp32.
+        dict(name="attention_odd_f32", kind="attention", dtype="f32", tokens=2500, sequences=5, split=3, tail=0, heads=8, kv_heads=8, width=80, backward=True),
+        # The gradients of the smallest model: six small tensors.
+        dict(name="clip_small_f32", kind="clip", dtype="f32", tensors=6, elements=20000, split=1, max_norm=1.0),
+        # The fp32 gradients of a model of 400 million parameters in 300 tensors.
+        dict(name="clip_model_f32", kind="clip", dtype="f32", tensors=300, elements=400_000_000, split=2, max_norm=1.0),
+    ]
+
+
+def _log(rng, lo, hi, step=1):
+    """Log-uniform multiple of `step` in [lo, hi]."""
+    v = math.exp(rng.uniform(math.log(lo), math.log(hi)))
+    return int(min(hi // step * step, max(-(-lo // step) * step, round(v / step) * step)))
+
+
+def draw(rng):
+    kind = rng.choice(["embedding", "norm", "attention", "attention", "clip"])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    if kind == "embedding":
+        width = _log(rng, 16, 4096, rng.choice([8, 8, 1]))
+        return dict(kind=kind, dtype=dtype, rows=_log(rng, 1, 32768), vocab=_log(rng, 2, min(128000, 250_000_000 // width)), width=width,
+                    scale=rng.choice([1.0, width ** 0.5]), padding=rng.choice([0.0, 0.1]), backward=rng.random() < 0.8)
+    if kind == "norm":
+        width = _log(rng, 16, 8192, rng.choice([8, 8, 1]))
+        return dict(kind=kind, dtype=dtype, rows=_log(rng, 1, 60_000_000 // width // (2 if dtype == "f32" else 1)), width=width, post=rng.random() < 0.7,
+                    gate=rng.random() < 0.7, scale=rng.choice([1.0, 0.25]), backward=rng.random() < 0.7)
+    if kind == "attention":
+        kv_heads = rng.choice([1, 2, 4, 8])
+        heads = kv_heads * rng.choice([1, 2, 3, 4])
+        tokens = _log(rng, 1, 8192 if dtype == "bf16" else 4096)
+        return dict(kind=kind, dtype=dtype, tokens=tokens, sequences=min(tokens, _log(rng, 1, 64)), split=rng.randint(0, 1000), tail=rng.choice([0, 0, tokens // 10]),
+                    heads=heads, kv_heads=kv_heads, width=rng.choice([16, 32, 40, 64, 64, 80, 96, 128, 128]), backward=rng.random() < 0.7)
+    return dict(kind=kind, dtype=dtype, tensors=_log(rng, 1, 400), elements=_log(rng, 1000, 300_000_000), split=rng.randint(0, 1000), max_norm=rng.choice([1.0, 1e6]))
+
+
+def _offsets(case):
+    """Starts of the sequences, and the last one's end: lengths of a spread of 1 to 20, a few of them zero where there are many."""
+    n, total = case["sequences"], case["tokens"] - case["tail"]
+    rng = random.Random(case["split"])
+    weights = [0.0 if n >= 16 and rng.random() < 0.05 else math.exp(rng.uniform(0.0, 3.0)) for _ in range(n)]
+    if not sum(weights):
+        weights[0] = 1.0
+    at, far = [0], 0.0
+    for w in weights:
+        far += w
+        at.append(round(total * far / sum(weights)))
+    at[-1] = total
+    return at
+
+
+def _counts(case):
+    """Elements of each tensor: matrices and vectors side by side, a spread of 1 to 1000."""
+    rng = random.Random(case["split"])
+    weights = [math.exp(rng.uniform(0.0, 7.0)) for _ in range(case["tensors"])]
+    return [max(1, int(case["elements"] * w / sum(weights))) for w in weights]
+
+
+def prepare(case, seed):
+    code, t, e = DTYPES[case["dtype"]]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    empty = lambda *shape: torch.empty(shape, dtype=t, device="cuda")  # noqa: E731
+    s = dict(case=case, code=code, dtype=t)
+    if case["kind"] == "embedding":
+        R, V, C = case["rows"], case["vocab"], case["width"]
+        s.update(table=normal(V, C).to(t), dout=normal(R, C).to(t), out=empty(R, C), dtable=torch.empty((V, C), device="cuda"))
+        # words come by rank: a few of them make up much of a text
+        ids = torch.exp(torch.rand(R, generator=g, device="cuda") * math.log(V)).floor().clamp(max=V) - 1
+        s["ids"] = torch.where(torch.rand(R, generator=g, device="cuda") < case["padding"], torch.full_like(ids, -1.0), ids).to(torch.int32)
+        s["ws"] = torch.empty(16 * R + 8 * C * -(-R // 32) + 512, dtype=torch.uint8, device="cuda")
+    elif case["kind"] == "norm":
+        R, C = case["rows"], case["width"]
+        s.update(x=normal(R, C).to(t), h=(3 * normal(R, C)).to(t), gate=normal(R, C).to(t) if case["gate"] else None, pre=1 + 0.1 * normal(C),
+                 post=1 + 0.1 * normal(C) if case["post"] else None, r=empty(R, C), y=empty(R, C))
+        if case["backward"]:
+            s.update(dr=normal(R, C).to(t), dy=normal(R, C).to(t), dx=empty(R, C), dh=empty(R, C), dgate=empty(R, C) if case["gate"] else None,
+                     dpre=torch.empty(C, device="cuda"), dpost=torch.empty(C, device="cuda") if case["post"] else None,
+                     ws=torch.empty(8 * C * min(512, R) + 256, dtype=torch.uint8, device="cuda"))
+    elif case["kind"] == "attention":
+        T, H, K, W = case["tokens"], case["heads"], case["kv_heads"], case["width"]
+        s.update(qkv=normal(T, (H + 2 * K) * W).to(t), offsets=torch.tensor(_offsets(case), dtype=torch.int32, device="cuda"),
+                 # rows behind the last sequence stay as they are
+                 out=torch.zeros((T, H * W), dtype=t, device="cuda"), lse=torch.zeros((H, T), device="cuda"))
+        if case["backward"]:
+            parts = 8 * K * T * W * min(H // K, 4) if H > K else 0
+            s.update(dout=normal(T, H * W).to(t), dqkv=torch.zeros((T, (H + 2 * K) * W), dtype=t, device="cuda"),
+                     ws=torch.empty(4 * H * T + parts + 512, dtype=torch.uint8, device="cuda"))
+    else:
+        # tensors of one arena, each on a 64-element border, zeros between them
+        starts = np.cumsum([0] + [-(-n // 64) * 64 for n in _counts(case)])
+        s.update(grads=torch.zeros(int(starts[-1]), dtype=t, device="cuda"), outs=torch.zeros(int(starts[-1]), dtype=t, device="cuda"))
+        for at, n in zip(starts, _counts(case)):
+            s["grads"][at:at + n] = 0.02 * normal(n)
+        s["norm"] = torch.empty(1, device="cuda")
+        s["ws"] = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+        s["grad_at"], s["out_at"] = (s[k].data_ptr() + starts[:-1].astype(np.int64) * s[k].element_size() for k in ("grads", "outs"))
+        s["counts"] = np.array(_counts(case), dtype=np.int64)
+    return s
+
+
+def run(s):
+    if own:
+        return {"embedding": _embedding_own, "norm": _norm_own, "attention": _attention_own, "clip": _clip_own}[s["case"]["kind"]](s)
+    return {"embedding": _embedding, "norm": _norm, "attention": _attention, "clip": _clip}[s["case"]["kind"]](s)
+
+
+# ---- plain forms ------------------------------------------------------------------------------------------------------
+def _embedding(s):
+    c = s["case"]
+    inside = (s["ids"] >= 0) & (s["ids"] < c["vocab"])
+    at = torch.where(inside, s["ids"], 0).long()
+    res = {"out": (s["table"][at].float() * c["scale"] * inside[:, None]).to(s["dtype"])}
+    if c["backward"]:
+        d = s["dout"].float() * c["scale"] * inside[:, None]
+        res["dtable"] = torch.zeros((c["vocab"], c["width"]), device="cuda").index_add_(0, at, d)
+    return res
+
+
+def _norm(s):
+    c, t = s["case"], s["dtype"]
+    h = s["h"].float()
+    eta = (h.square().mean(1, keepdim=True) + EPS).rsqrt()
+    n = h * eta
+    u = n * s["post"] if c["post"] else h
+    sig = 1 / (1 + torch.exp(-s["gate"].float())) if c["gate"] else 1.0
+    r = s["x"].float() + c["scale"] * sig * u
+    y = r * (r.square().mean(1, keepdim=True) + EPS).rsqrt() * s["pre"]
+    res = {"r": r.to(t), "y": y.to(t)}
+    if c["backward"]:
+        rho = (r.square().mean(1, keepdim=True) + EPS).rsqrt()
+        rhat, dy = r * rho, s["dy"].float()
+        a = dy * s["pre"]
+        d = s["dr"].float() + rho * (a - rhat * (a * rhat).mean(1, keepdim=True))
+        du = c["scale"] * sig * d
+        b = du * s["post"] if c["post"] else du
+        dh = eta * (b - n * (b * n).mean(1, keepdim=True)) if c["post"] else b
+        res.update(dx=d.to(t), dh=dh.to(t), dpre=(dy * rhat).sum(0))
+        if c["gate"]:
+            res["dgate"] = (c["scale"] * u * d * sig * (1 - sig)).to(t)
+        if c["post"]:
+            res["dpost"] = (du * n).sum(0)
+    return res
+
+
+def _attention(s):
+    c, t = s["case"], s["dtype"]
+    T, H, K, W = c["tokens"], c["heads"], c["kv_heads"], c["width"]
+    scale = W ** -0.5
+    q, k, v = (a.float().reshape(T, -1, W).transpose(0, 1).contiguous() for a in s["qkv"].split([H * W, K * W, K * W], 1))
+    k, v = k.repeat_interleave(H // K, 0), v.repeat_interleave(H // K, 0)
+    row = torch.arange(T, device="cuda")
+    sequence = (row[:, None] >= s["offsets"][None, 1:]).sum(1)
+    used = row < s["offsets"][-1]
+    seen = (sequence[:, None] == sequence[None, :]) & (row[:, None] >= row[None, :])
+    a = torch.matmul(q, k.transpose(1, 2).contiguous()).mul_(scale).masked_fill_(~seen, -math.inf)
+    m = a.amax(2, keepdim=True)
+    p = a.sub_(m).exp_()
+    z = p.sum(2, keepdim=True)
+    p = p.div_(z)
+    o = torch.matmul(p, v)
+    flat = lambda x: x.transpose(0, 1).reshape(T, -1)  # noqa: E731
+    res = {"out": (flat(o) * used[:, None]).to(t), "lse": (m + torch.log(z))[:, :, 0] * used}
+    if c["backward"]:
+        do = (s["dout"].float() * used[:, None]).reshape(T, H, W).transpose(0, 1).contiguous()
+        dv = torch.matmul(p.transpose(1, 2).contiguous(), do)
+        ds = torch.matmul(do, v.transpose(1, 2).contiguous()).sub_((do * o).sum(2, keepdim=True)).mul_(p).mul_(scale)
+        dq, dk = torch.matmul(ds, k), torch.matmul(ds.transpose(1, 2).contiguous(), q)
+        dk, dv = (x.reshape(K, H // K, T, W).sum(1) for x in (dk, dv))
+        res["dqkv"] = (torch.cat([flat(dq), flat(dk), flat(dv)], 1) * used[:, None]).to(t)
+    return res
+
+
+def _clip(s):
+    g = s["grads"].float()
+    norm = g.square().sum().sqrt()
+    factor = torch.where(norm > s["case"]["max_norm"], s["case"]["max_norm"] / norm, torch.ones_like(norm))
+    return {"norm": norm.reshape(1), "grads": (g * factor).to(s["dtype"])}
+
+
+# ---- the framework's calls --------------------------------------------------------------------------------------------
+def _at(x):
+    return 0 if x is None else x.data_ptr()
+
+
+def _embedding_own(s):
+    from paper_2403_08837_amd import binding as cdp
+    c = s["case"]
+    R, V, C = c["rows"], c["vocab"], c["width"]
+    cdp.cdp_k_embedding(s["code"], 0, _at(s["table"]), _at(s["ids"]), 0, _at(s["out"]), c["scale"], 0, 0, R, V, C)
+    res = {"out": s["out"]}
+    if c["backward"]:
+        cdp.cdp_k_embedding(s["code"], 1, 0, _at(s["ids"]), _at(s["dout"]), _at(s["dtable"]), c["scale"], _at(s["ws"]), s["ws"].numel(), R, V, C)
+        res["dtable"] = s["dtable"]
+    return res
+
+
+def _norm_own(s):
+    from paper_2403_08837_amd import binding as cdp
+    c = s["case"]
+    R, C = c["rows"], c["width"]
+    cdp.cdp_k_residual_norm(s["code"], _at(s["x"]), _at(s["h"]), _at(s["gate"]), _at(s["post"]), _at(s["pre"]), _at(s["r"]), _at(s["y"]), c["scale"], EPS, R, C)
+    res = {"r": s["r"], "y": s["y"]}
+    if c["backward"]:
+        cdp.cdp_k_residual_norm_backward(s["code"], 0, _at(s["h"]), _at(s["gate"]), _at(s["post"]), _at(s["pre"]), _at(s["r"]), _at(s["dr"]), _at(s["dy"]), _at(s["dx"]),
+                                         _at(s["dh"]), _at(s["dgate"]), _at(s["dpost"]), _at(s["dpre"]), c["scale"], EPS, _at(s["ws"]), s["ws"].numel(), R, C)
+        res.update(dx=s["dx"], dh=s["dh"], dpre=s["dpre"])
+        if c["gate"]:
+            res["dgate"] = s["dgate"]
+        if c["post"]:
+            res["dpost"] = s["dpost"]
+    return res
+
+
+def _attention_own(s):
+    from paper_2403_08837_amd import binding as cdp
+    c = s["case"]
+    sizes = (c["tokens"], c["sequences"], c["heads"], c["kv_heads"], c["width"], c["width"] ** -0.5)
+    cdp.cdp_k_attention_packed(s["code"], 0, _at(s["qkv"]), _at(s["offsets"]), _at(s["out"]), _at(s["lse"]), 0, 0, 0, 0, *sizes)
+    res = {"out": s["out"], "lse": s["lse"]}
+    if c["backward"]:
+        cdp.cdp_k_attention_packed(s["code"], 1, _at(s["qkv"]), _at(s["offsets"]), _at(s["out"]), _at(s["lse"]), _at(s["dout"]), _at(s["dqkv"]), _at(s["ws"]),
+                                   s["ws"].numel(), *sizes)
+        res["dqkv"] = s["dqkv"]
+    return res
+
+
+def _clip_own(s):
+    from paper_2403_08837_amd import binding as cdp
+    c = s["case"]
+    cdp.cdp_k_grad_clip(s["code"], len(s["counts"]), s["grad_at"].ctypes.data, s["out_at"].ctypes.data, s["counts"].ctypes.data, c["max_norm"], _at(s["norm"]),
+                        _at(s["ws"]), s["ws"].numel())
+    return {"norm": s["norm"], "grads": s["outs"]}
+
+
+# ---- what a pass cannot do without ------------------------------------------------------------------------------------
+def work(case):
+    e = DTYPES[case["dtype"]][2]
+    if case["kind"] == "embedding":
+        R, V, C = case["rows"], case["vocab"], case["width"]
+        return {"bytes": e * min(R, V) * C + 4 * R + e * R * C + ((e * R * C + 4 * V * C) if case["backward"] else 0), "flops": R * C * (2 if case["backward"] else 1)}
+    if case["kind"] == "norm":
+        n, gate = case["rows"] * case["width"], int(case["gate"])
+        return {"bytes": e * n * (4 + gate + ((6 + 2 * gate) if case["backward"] else 0)), "flops": n * (10 + (30 if case["backward"] else 0))}
+    if case["kind"] == "attention":
+        T, H, K, W = case["tokens"], case["heads"], case["kv_heads"], case["width"]
+        at = _offsets(case)
+        pairs = sum((b - a) * (b - a + 1) // 2 for a, b in zip(at, at[1:]))
+        T = at[-1]
+        b = e * T * W * (2 * H + 2 * K) + 4 * T * H
+        if case["backward"]:
+            b += e * T * W * (2 * (H + 2 * K) + 2 * H) + 4 * T * H
+        return {"bytes": b, "flops": (14 if case["backward"] else 4) * W * H * pairs}
+    n = sum(_counts(case))
+    return {"bytes": 2 * e * n, "flops": 3 * n}
+
+
+# ---- the definitions in 64 bits ---------------------------------------------------------------------------------------
+def exact(case, seed):
+    s = prepare(case, seed)
+    return {"embedding": _embedding_exact, "norm": _norm_exact, "attention": _attention_exact, "clip": _clip_exact}[case["kind"]](s)
+
+
+def _embedding_exact(s):
+    c, ids = s["case"], s["ids"].long()
+    keep = torch.nonzero((ids >= 0) & (ids < c["vocab"]))[:, 0]
+    out = torch.zeros((c["rows"], c["width"]), dtype=torch.float64, device="cuda")
+    out[keep] = c["scale"] * s["table"].index_select(0, ids[keep]).double()
+    res = {"out": out}
+    if c["backward"]:
+        # tokens in the order of their words; a word's sum is the difference of two running sums over its run
+        order = keep[torch.argsort(ids[keep], stable=True)]
+        words, runs = torch.unique_consecutive(ids[order], return_counts=True)
+        d = torch.zeros((c["vocab"], c["width"]), dtype=torch.float64, device="cuda")
+        far = torch.zeros((len(order) + 1, c["width"]), dtype=torch.float64, device="cuda")
+        far[1:] = torch.cumsum(s["dout"][order].double(), 0)
+        end = torch.cumsum(runs, 0)
+        d[words] = c["scale"] * (far[end] - far[end - runs])
+        res["dtable"] = d
+    return res
+
+
+def _norm_exact(s):
+    """By the chain rule, from the forward's own definition."""
+    c = s["case"]
+    leaf = lambda v: v.double().requires_grad_(c["backward"])  # noqa: E731
+    x, h, pre = leaf(s["x"]), leaf(s["h"]), leaf(s["pre"])
+    gate, post = (leaf(s[k]) if s[k] is not None else None for k in ("gate", "post"))
+
+    def normed(v):
+        return v / torch.sqrt((v * v).sum(1, keepdim=True) / c["width"] + EPS)
+    u = normed(h) * post if post is not None else h
+    r = x + c["scale"] * (u * torch.sigmoid(gate) if gate is not None else u)
+    y = normed(r) * pre
+    res = {"r": r.detach(), "y": y.detach()}
+    if c["backward"]:
+        torch.autograd.backward([r, y], [s["dr"].double(), s["dy"].double()])
+        res.update(dx=x.grad, dh=h.grad, dpre=pre.grad)
+        if gate is not None:
+            res["dgate"] = gate.grad
+        if post is not None:
+            res["dpost"] = post.grad
+    return res
+
+
+def _attention_exact(s):
+    """One sequence and one key head after the other."""
+    c, at = s["case"], _offsets(s["case"])
+    T, H, K, W = c["tokens"], c["heads"], c["kv_heads"], c["width"]
+    zeros = lambda *n: torch.zeros(n, dtype=torch.float64, device="cuda")  # noqa: E731
+    out, lse, dqkv = zeros(T, H, W), zeros(H, T), zeros(T, H + 2 * K, W)
+    qkv = s["qkv"].reshape(T, H + 2 * K, W)
+    for a, b in zip(at, at[1:]):
+        later = torch.ones((b - a, b - a), dtype=torch.bool, device="cuda").triu(1)
+        for j in range(K if b > a else 0):
+            heads = slice(j * (H // K), (j + 1) * (H // K))
+            q, k, v = qkv[a:b, heads].double(), qkv[a:b, H + j].double(), qkv[a:b, H + K + j].double()
+            q = q.transpose(0, 1).reshape(-1, W)  # the heads of the group below each other
+            x = (q @ k.t().contiguous() / math.sqrt(W)).reshape(-1, b - a, b - a).masked_fill(later, -math.inf)
+            z = torch.logsumexp(x, 2)
+            p = torch.exp(x - z[:, :, None]).reshape(-1, b - a)
+            o = p @ v
+            out[a:b, heads] = o.reshape(-1, b - a, W).transpose(0, 1)
+            lse[heads, a:b] = z
+            if c["backward"]:
+                do = s["dout"].reshape(T, H, W)[a:b, heads].double().transpose(0, 1).reshape(-1, W)
+                ds = p * (do @ v.t().contiguous() - (do * o).sum(1, keepdim=True)) / math.sqrt(W)
+                dqkv[a:b, heads] = (ds @ k).reshape(-1, b - a, W).transpose(0, 1)
+                dqkv[a:b, H + j] = ds.t().contiguous() @ q
+                dqkv[a:b, H + K + j] = p.t().contiguous() @ do
+    res = {"out": out.reshape(T, -1), "lse": lse}
+    if c["backward"]:
+        res["dqkv"] = dqkv.reshape(T, -1)
+    return res
+
+
+def _clip_exact(s):
+    g = s["grads"].double()
+    norm = float(torch.linalg.vector_norm(g))
+    factor = min(1.0, s["case"]["max_norm"] / norm) if norm else 1.0
+    return {"norm": torch.tensor([norm], dtype=torch.float64), "grads": g * factor}
