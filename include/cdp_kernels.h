@@ -91,6 +91,64 @@ int cdp_k_gelu(int dtype, int backward, const void* x, const void* dy, void* out
 int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const void* dout, void* out, void* workspace,
                     size_t workspace_bytes, int B, int T, int D, int heads, void* stream);
 
+/* ---- token models on packed batches ----------------------------------------------------------------------------
+ * Rows are tokens.  Tensors are row-major and packed; nothing but what is said to be written is touched.  Outputs must not alias
+ * inputs except where it is said.  Sizes of zero are CDP_EINVAL like negative ones.  The device of the pointers and of `stream` has to be
+ * the current one.  Every call may be captured into a graph; calls that overlap in time need workspaces of their own.  The same inputs give
+ * the same bits.
+ *
+ * Embedding: rows of table[vocab][C] by ids[rows].  A token whose id is outside [0, vocab) (padding) has a row of zeros and no gradient.
+ *   backward 0: out[rows][C] (elem type) = scale * table[ids]   (dout, workspace unused)
+ *   backward 1: out = dtable[vocab][C] (fp32) = scale * sum over the tokens of a row of dout[rows][C] (table unused), zero for
+ *               rows without a token; the tokens of a row are summed in a fixed order
+ *   backward 2: as 1, but added to dtable; rows without a token are not touched
+ * workspace (backward): 16 * rows + 8 * C * ceil(rows / 32) + 512 bytes (CDP_EINVAL if smaller). */
+int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* ids, const void* dout, void* out, float scale,
+                    void* workspace, size_t workspace_bytes, int rows, int vocab, int C, void* stream);
+
+/* The end of one block and the start of the next, over rows of C <= 16384 channels, norm(v) = v / sqrt(mean(v^2) + eps):
+ *   u = norm(h) * gamma_post       h[rows][C]: what the block computed; gamma_post NULL: u = h
+ *   r = x + scale * sigmoid(gate) * u       gate[rows][C]; NULL: no gate.  h NULL: r = x, and gate and gamma_post are NULL
+ *   y = norm(r) * gamma_pre        gamma_pre NULL: no y
+ * x, h, gate, r, y in the element type, gamma_* fp32[C].  r may be NULL (not wanted) if y is not; r may be x. */
+int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gate, const float* gamma_post, const float* gamma_pre,
+                        void* r, void* y, float scale, float eps, int rows, int C, void* stream);
+
+/* Its gradients from dr[rows][C] (the gradient of r beside the one through y; NULL: none) and dy[rows][C] (with gamma_pre; NULL without):
+ *   dx = d r in all, dh, dgate (elem type, written; dh and dgate with h and gate);
+ *   dgamma_post[C], dgamma_pre[C] (fp32, with gamma_post and gamma_pre): overwritten, with accumulate != 0 added to.
+ * r: as the forward wrote it (NULL without gamma_pre).  dx may be dr.
+ * workspace: 8 * C * min(rows, 512) + 256 bytes (CDP_EINVAL if smaller). */
+int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const void* gate, const float* gamma_post,
+                                 const float* gamma_pre, const void* r, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
+                                 float* dgamma_post, float* dgamma_pre, float scale, float eps, void* workspace, size_t workspace_bytes,
+                                 int rows, int C, void* stream);
+
+/* Causal self-attention of sequences of different lengths packed behind each other: sequence s is the rows offsets[s] ..
+ * offsets[s + 1] - 1 (device int32 [sequences + 1], ascending, within [0, tokens]; a length may be zero), and a token sees its own
+ * sequence up to itself.  qkv[tokens][(heads + 2 * kv_heads) * width]: q heads | k heads | v heads per token; query head h goes with key
+ * head h / (heads / kv_heads).  width: a multiple of 8 up to 128; heads a multiple of kv_heads; tensors 16-byte aligned.
+ *   backward 0: out[tokens][heads * width] = softmax(scale * q k^T) v, lse[heads][tokens] (fp32) = log of the sum that the softmax divides
+ *               by, sum exp(scale * q k^T)   (dout, dqkv, workspace unused)
+ *   backward 1: dqkv from dout[tokens][heads * width] and the forward's out and lse
+ * Rows outside all sequences are neither read for another's sake nor written.  Offsets that are not as said give wrong results, within
+ * the tensors.
+ * workspace (backward): 4 * heads * tokens + 512 bytes (CDP_EINVAL if smaller).  Where it holds P times 8 * kv_heads * tokens * width
+ * bytes more, launches of few key tiles share the query heads of a key head over up to P workgroups: faster, other roundings. */
+int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32_t* offsets, void* out, float* lse, const void* dout,
+                           void* dqkv, void* workspace, size_t workspace_bytes, int tokens, int sequences, int heads, int kv_heads,
+                           int width, float scale, void* stream);
+
+/* The norm over all elements of `tensors` gradients, and the gradients scaled so that it is at most max_norm:
+ *   norm[0] (device fp32) = sqrt(sum of squares), summed in 64 bits
+ *   outs[i][0 .. counts[i]) = norm > max_norm ? grads[i] * (max_norm / norm) : grads[i]   (elem type; outs[i] may be grads[i])
+ * grads, outs, counts: HOST arrays of device pointers and element counts (0: nothing there), read during the call.  outs NULL: the norm alone.
+ * A norm that is NaN leaves the gradients as they are; one that is infinite scales by zero.
+ * workspace: CDP_CLIP_BYTES, 8-byte aligned; nothing in it has to be cleared. */
+#define CDP_CLIP_BYTES 65536u
+int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm,
+                    float* norm, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -23,7 +23,8 @@ CDP_F32, CDP_BF16 = 0, 1
 EXPORTS = ["cdp_arena_bytes", "cdp_init", "cdp_set_weights", "cdp_param_count", "cdp_tick", "cdp_step",
            "cdp_drain", "cdp_get_weights", "cdp_get_losses", "cdp_get_trace", "cdp_get_live_counts",
            "cdp_get_live_bytes", "cdp_get_stats", "cdp_last_error", "cdp_destroy", "cdp_profile_gemm", "cdp_get_gemm_profile",
-           "cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention"]
+           "cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention",
+           "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip"]
 
 
 class cdp_layer_desc(C.Structure):
@@ -73,7 +74,7 @@ def lib() -> C.CDLL:
             raise ImportError("libcdp.so is not built: run `python -m paper_2403_08837_amd.build` "
                               "(or __graft_entry__.build()); there is no fallback path")
         L = C.CDLL(LIB_PATH)
-        vp, i32, sz = C.c_void_p, C.c_int, C.c_size_t
+        vp, i32, sz, f32 = C.c_void_p, C.c_int, C.c_size_t, C.c_float
         L.cdp_arena_bytes.argtypes = [C.POINTER(cdp_stage_desc), i32, i32, i32, i32, C.POINTER(cdp_opts), C.POINTER(sz)]
         L.cdp_init.argtypes = [C.POINTER(vp), C.POINTER(cdp_stage_desc), i32, i32, i32, C.c_float, i32, C.POINTER(cdp_opts)]
         L.cdp_set_weights.argtypes = [vp, i32, C.POINTER(C.c_float), sz]
@@ -99,6 +100,11 @@ def lib() -> C.CDLL:
         L.cdp_k_layernorm.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, vp]
         L.cdp_k_gelu.argtypes = [i32, i32, vp, vp, vp, C.c_int64, vp]
         L.cdp_k_attention.argtypes = [i32, i32, vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, vp]
+        L.cdp_k_embedding.argtypes = [i32, i32, vp, vp, vp, vp, f32, vp, sz, i32, i32, i32, vp]
+        L.cdp_k_residual_norm.argtypes = [i32, vp, vp, vp, vp, vp, vp, vp, f32, f32, i32, i32, vp]
+        L.cdp_k_residual_norm_backward.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, f32, f32, vp, sz, i32, i32, vp]
+        L.cdp_k_attention_packed.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, i32, f32, vp]
+        L.cdp_k_grad_clip.argtypes = [i32, i32, vp, vp, vp, f32, vp, vp, sz, vp]
         for name in EXPORTS:
             if name not in ("cdp_last_error", "cdp_destroy"):
                 getattr(L, name).restype = C.c_int
@@ -106,7 +112,8 @@ def lib() -> C.CDLL:
     return _lib
 
 
-_CALLS = ("cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention")
+_CALLS = ("cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention",
+          "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip")
 
 
 def _calls():
@@ -121,7 +128,7 @@ def _calls():
 
 
 def _entry(name: str):
-    """Kernel-level entry point `name` of _calls.so: a call whose arguments are plain integers costs 0.3 us there and
+    """Kernel-level entry point `name` of _calls.so: a call whose arguments are plain integers and floats costs 0.3 us there and
     one to two through ctypes.  None: an argument is something else, or there is no _calls.so; the caller goes through ctypes then.
     Loaded with the first call."""
     def first(*args):
@@ -131,7 +138,8 @@ def _entry(name: str):
     return first
 
 
-_cdp_k_gemm, _cdp_k_conv, _cdp_k_conv_wgrad_static, _cdp_k_layernorm, _cdp_k_gelu, _cdp_k_attention = map(_entry, _CALLS)
+_cdp_k_gemm, _cdp_k_conv, _cdp_k_conv_wgrad_static, _cdp_k_layernorm, _cdp_k_gelu, _cdp_k_attention, \
+    _cdp_k_embedding, _cdp_k_residual_norm, _cdp_k_residual_norm_backward, _cdp_k_attention_packed, _cdp_k_grad_clip = map(_entry, _CALLS)
 
 
 def _check(rc: int, ctx=None) -> None:
@@ -330,6 +338,63 @@ def cdp_k_attention(dtype, backward, qkv_ptr, P_ptr, dout_ptr, out_ptr, ws_ptr, 
         rc = lib().cdp_k_attention(*args)
     if rc != CDP_OK:
         raise CdpError(rc, "cdp_k_attention")
+
+
+def cdp_k_embedding(dtype, backward, table_ptr, ids_ptr, dout_ptr, out_ptr, scale, ws_ptr, ws_bytes, rows, vocab, C_, stream=0) -> None:
+    """scale * table[ids] (backward = 0), or the table's gradient, overwritten (1) or added to (2)."""
+    args = (dtype, backward, table_ptr or None, ids_ptr, dout_ptr or None, out_ptr, scale, ws_ptr or None, ws_bytes, rows, vocab, C_,
+            stream or None)
+    rc = _cdp_k_embedding(*args)
+    if rc is None:
+        rc = lib().cdp_k_embedding(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_embedding")
+
+
+def cdp_k_residual_norm(dtype, x_ptr, h_ptr, gate_ptr, gamma_post_ptr, gamma_pre_ptr, r_ptr, y_ptr, scale, eps, rows, C_, stream=0) -> None:
+    """r = x + scale * sigmoid(gate) * norm(h) * gamma_post and y = norm(r) * gamma_pre."""
+    args = (dtype, x_ptr, h_ptr or None, gate_ptr or None, gamma_post_ptr or None, gamma_pre_ptr or None, r_ptr or None, y_ptr or None, scale, eps,
+            rows, C_, stream or None)
+    rc = _cdp_k_residual_norm(*args)
+    if rc is None:
+        rc = lib().cdp_k_residual_norm(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_residual_norm")
+
+
+def cdp_k_residual_norm_backward(dtype, accumulate, h_ptr, gate_ptr, gamma_post_ptr, gamma_pre_ptr, r_ptr, dr_ptr, dy_ptr, dx_ptr, dh_ptr, dgate_ptr,
+                                 dgamma_post_ptr, dgamma_pre_ptr, scale, eps, ws_ptr, ws_bytes, rows, C_, stream=0) -> None:
+    """Gradients of cdp_k_residual_norm from those of r and y."""
+    args = (dtype, accumulate, h_ptr or None, gate_ptr or None, gamma_post_ptr or None, gamma_pre_ptr or None, r_ptr or None, dr_ptr or None,
+            dy_ptr or None, dx_ptr, dh_ptr or None, dgate_ptr or None, dgamma_post_ptr or None, dgamma_pre_ptr or None, scale, eps, ws_ptr or None,
+            ws_bytes, rows, C_, stream or None)
+    rc = _cdp_k_residual_norm_backward(*args)
+    if rc is None:
+        rc = lib().cdp_k_residual_norm_backward(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_residual_norm_backward")
+
+
+def cdp_k_attention_packed(dtype, backward, qkv_ptr, offsets_ptr, out_ptr, lse_ptr, dout_ptr, dqkv_ptr, ws_ptr, ws_bytes, tokens, sequences, heads,
+                           kv_heads, width, scale, stream=0) -> None:
+    """Causal attention over packed sequences, forward (backward = 0: out and lse) or backward (1: dqkv)."""
+    args = (dtype, backward, qkv_ptr, offsets_ptr, out_ptr, lse_ptr, dout_ptr or None, dqkv_ptr or None, ws_ptr or None, ws_bytes, tokens, sequences,
+            heads, kv_heads, width, scale, stream or None)
+    rc = _cdp_k_attention_packed(*args)
+    if rc is None:
+        rc = lib().cdp_k_attention_packed(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_attention_packed")
+
+
+def cdp_k_grad_clip(dtype, tensors, grads_ptr, outs_ptr, counts_ptr, max_norm, norm_ptr, ws_ptr, ws_bytes, stream=0) -> None:
+    """grads_ptr, outs_ptr, counts_ptr: addresses of host arrays (numpy int64: ``a.ctypes.data``), read before this returns."""
+    args = (dtype, tensors, grads_ptr, outs_ptr or None, counts_ptr, max_norm, norm_ptr, ws_ptr, ws_bytes, stream or None)
+    rc = _cdp_k_grad_clip(*args)
+    if rc is None:
+        rc = lib().cdp_k_grad_clip(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_grad_clip")
 
 
 # ---- convenience wrapper used by tests and bench -------------------------------------------

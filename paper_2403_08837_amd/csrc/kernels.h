@@ -360,4 +360,43 @@ int attention_launches(bool backward, int B, int NT, int D, int heads, int dtype
 // T -> f32 copy (cdp_get_weights of a ring copy).
 hipError_t launch_to_f32(const void* src, float* dst, int64_t n, int dtype, hipStream_t stream);
 
+// Operators of token models on packed batches (embedding_kernels.hip, residual_norm.hip, packed_attention.hip, grad_clip.hip): the entry points of
+// cdp_kernels.h after their checks.
+hipError_t launch_embedding_fwd(const void* table, const int32_t* ids, void* out, float scale, int rows, int vocab, int C, int dtype,
+                                hipStream_t stream);
+int64_t embedding_bwd_workspace_bytes(int rows, int C);
+hipError_t launch_embedding_bwd(const int32_t* ids, const void* dout, float* dtable, float scale, void* workspace, bool accumulate, int rows,
+                                int vocab, int C, int dtype, hipStream_t stream);
+struct ResidualNorm {
+  const void *x, *h, *gate;
+  const float *gamma_post, *gamma_pre;
+  void *r, *y;                         // forward: written
+  const void *rin, *dr, *dy;           // backward: r, d r, d y
+  void *dx, *dh, *dgate;
+  float *dgamma_post, *dgamma_pre, *part;
+  int rows, C, accumulate;
+  float scale, eps;
+};
+constexpr int RNORM_MAX_C = 16384, RNORM_MAX_PARTS = 512;
+int64_t residual_norm_bwd_workspace_bytes(int rows, int C);
+hipError_t launch_residual_norm_fwd(const ResidualNorm& a, int dtype, hipStream_t stream);
+hipError_t launch_residual_norm_bwd(const ResidualNorm& a, int dtype, hipStream_t stream);
+struct PackedAttention {
+  const void* qkv;
+  const int32_t* offsets;
+  void* out;
+  float* lse;
+  const void* dout;
+  void* dqkv;
+  float* delta;                        // backward: [heads][tokens]
+  float* parts;                        // backward: room for `max_parts` times [2][tokens][kv_heads][width] sums
+  int64_t max_parts;
+  int tokens, sequences, heads, kv_heads, width;
+  float scale;
+};
+hipError_t launch_packed_attention_fwd(const PackedAttention& a, int dtype, hipStream_t stream);
+hipError_t launch_packed_attention_bwd(const PackedAttention& a, int dtype, hipStream_t stream);
+hipError_t launch_grad_clip(int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm, float* norm,
+                            void* workspace, int dtype, hipStream_t stream);
+
 }  // namespace cdp

@@ -27,6 +27,8 @@ bool cdp::gemm_wgrad_tiles_wanted(int tile_shape, int M, int N, int K, int lda, 
 
 static_assert((int64_t)CDP_CONV_SHARE_BYTES == CONV_SPLIT_WS_BYTES + CONV_SPLIT_SLOTS * 4, "partial tiles, then counters");
 
+static bool aligned_to(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
 extern "C" {
 
 int cdp_k_gemm(int dtype, int tile_shape, int a_kmajor, int b_kmajor, const void* A, const void* B, float* C, int M, int N,
@@ -189,6 +191,102 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
   if (!dout || (int64_t)workspace_bytes < dp_bytes + tt * (dtype == DT_BF16 ? 2 : 4)) return CDP_EINVAL;
   return launch_attention_bwd(qkv, P, dout, out, static_cast<float*>(workspace), static_cast<char*>(workspace) + dp_bytes, B, T, D,
                               heads, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+}
+
+int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* ids, const void* dout, void* out, float scale,
+                    void* workspace, size_t workspace_bytes, int rows, int vocab, int C, void* stream) {
+  if (!ids || !out || rows <= 0 || vocab <= 0 || C <= 0 || backward < 0 || backward > 2 || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  const int eb = dtype == DT_BF16 ? 2 : 4;
+  if (!aligned_to(ids, 4) || !aligned_to(out, backward ? 4 : eb)) return CDP_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!backward) {
+    if (!table || !aligned_to(table, eb)) return CDP_EINVAL;
+    return launch_embedding_fwd(table, ids, out, scale, rows, vocab, C, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+  }
+  if (!dout || !aligned_to(dout, eb) || !workspace || !aligned_to(workspace, 16) ||
+      workspace_bytes < (size_t)embedding_bwd_workspace_bytes(rows, C))
+    return CDP_EINVAL;
+  return launch_embedding_bwd(ids, dout, static_cast<float*>(out), scale, workspace, backward == 2, rows, vocab, C, dtype, st) == hipSuccess
+             ? CDP_OK : CDP_EHIP;
+}
+
+int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gate, const float* gamma_post, const float* gamma_pre,
+                        void* r, void* y, float scale, float eps, int rows, int C, void* stream) {
+  if (!x || (!r && !y) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!y != !gamma_pre || (!h && (gate || gamma_post))) return CDP_EINVAL;
+  const int eb = dtype == DT_BF16 ? 2 : 4;
+  if (!aligned_to(x, eb) || !aligned_to(h, eb) || !aligned_to(gate, eb) || !aligned_to(r, eb) || !aligned_to(y, eb) ||
+      !aligned_to(gamma_post, 4) || !aligned_to(gamma_pre, 4))
+    return CDP_EINVAL;
+  ResidualNorm a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.h = h; a.gate = gate; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
+  a.r = r; a.y = y; a.rows = rows; a.C = C; a.scale = scale; a.eps = eps;
+  return launch_residual_norm_fwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;
+}
+
+int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const void* gate, const float* gamma_post,
+                                 const float* gamma_pre, const void* r, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
+                                 float* dgamma_post, float* dgamma_pre, float scale, float eps, void* workspace, size_t workspace_bytes,
+                                 int rows, int C, void* stream) {
+  if (!dx || (!dr && !dy) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!dy != !gamma_pre || !dgamma_pre != !gamma_pre || !r != !gamma_pre) return CDP_EINVAL;
+  if (!h != !dh || !gate != !dgate || !gamma_post != !dgamma_post || (!h && (gate || gamma_post))) return CDP_EINVAL;
+  const int eb = dtype == DT_BF16 ? 2 : 4;
+  for (const void* p : {h, gate, r, dr, dy, (const void*)dx, (const void*)dh, (const void*)dgate})
+    if (!aligned_to(p, eb)) return CDP_EINVAL;
+  for (const float* p : {gamma_post, gamma_pre, (const float*)dgamma_post, (const float*)dgamma_pre})
+    if (!aligned_to(p, 4)) return CDP_EINVAL;
+  if ((gamma_post || gamma_pre) &&
+      (!workspace || !aligned_to(workspace, 16) || workspace_bytes < (size_t)residual_norm_bwd_workspace_bytes(rows, C)))
+    return CDP_EINVAL;
+  ResidualNorm a;
+  memset(&a, 0, sizeof(a));
+  a.h = h; a.gate = gate; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
+  a.rin = r; a.dr = dr; a.dy = dy; a.dx = dx; a.dh = dh; a.dgate = dgate; a.dgamma_post = dgamma_post; a.dgamma_pre = dgamma_pre;
+  a.part = static_cast<float*>(workspace);
+  a.rows = rows; a.C = C; a.accumulate = accumulate != 0; a.scale = scale; a.eps = eps;
+  return launch_residual_norm_bwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;
+}
+
+int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32_t* offsets, void* out, float* lse, const void* dout,
+                           void* dqkv, void* workspace, size_t workspace_bytes, int tokens, int sequences, int heads, int kv_heads,
+                           int width, float scale, void* stream) {
+  if (!qkv || !offsets || !out || !lse || tokens <= 0 || sequences <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || width <= 0 ||
+      width % 8 || width > 128 || (dtype != DT_F32 && dtype != DT_BF16))
+    return CDP_EINVAL;
+  // tiles of 32 rows at least, and one more for every sequence: what a launch can number, and the rows' addresses in 63 bits
+  if (heads > 65536 || kv_heads > 65536 || ((int64_t)tokens / 32 + sequences + 1) * heads > INT_MAX / 2) return CDP_EINVAL;
+  if (!aligned_to(qkv, 16) || !aligned_to(out, 16) || !aligned_to(lse, 4) || !aligned_to(offsets, 4)) return CDP_EINVAL;
+  PackedAttention a;
+  memset(&a, 0, sizeof(a));
+  a.qkv = qkv; a.offsets = offsets; a.out = out; a.lse = lse;
+  a.tokens = tokens; a.sequences = sequences; a.heads = heads; a.kv_heads = kv_heads; a.width = width; a.scale = scale;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!backward) return launch_packed_attention_fwd(a, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+  const size_t rows = (size_t)heads * tokens, need = 4 * rows + 512;
+  if (!dout || !dqkv || !aligned_to(dout, 16) || !aligned_to(dqkv, 16) || !workspace || !aligned_to(workspace, 16) || workspace_bytes < need)
+    return CDP_EINVAL;
+  a.dout = dout; a.dqkv = dqkv;
+  a.delta = static_cast<float*>(workspace);
+  a.parts = a.delta + (rows + 63) / 64 * 64;
+  a.max_parts = (int64_t)((workspace_bytes - need) / (8 * (size_t)kv_heads * tokens * width));
+  return launch_packed_attention_bwd(a, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+}
+
+int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm,
+                    float* norm, void* workspace, size_t workspace_bytes, void* stream) {
+  if (tensors <= 0 || !grads || !counts || !norm || !(max_norm >= 0.f) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!workspace || workspace_bytes < CDP_CLIP_BYTES || !aligned_to(workspace, 8) || !aligned_to(norm, 4)) return CDP_EINVAL;
+  const int eb = dtype == DT_BF16 ? 2 : 4;
+  int64_t total = 0;
+  for (int i = 0; i < tensors; ++i) {
+    if (counts[i] < 0 || counts[i] > (INT64_MAX >> 4) - total) return CDP_EINVAL;
+    total += counts[i];
+    if (counts[i] && (!grads[i] || !aligned_to(grads[i], eb) || (outs && (!outs[i] || !aligned_to(outs[i], eb))))) return CDP_EINVAL;
+  }
+  return launch_grad_clip(tensors, grads, outs, counts, max_norm, norm, workspace, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? CDP_OK : CDP_EHIP;
 }
 
 }  // extern "C"

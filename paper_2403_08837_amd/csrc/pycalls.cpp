@@ -1,8 +1,8 @@
 // The kernel-level entry points as Python calls without ctypes (`_calls`, built beside libcdp.so).
 //
 // A small layer is a launch of a few microseconds, and converting a dozen arguments through ctypes takes one to two of them.  Here an
-// argument is read with one PyLong conversion.  What is accepted is what ctypes accepts for the same prototypes in plain integers: None or 0
-// for a null pointer, integers of any size for an int (the low bits, as C would take them).  Anything else makes the call
+// argument is read with one PyLong conversion.  What is accepted is what ctypes accepts for the same prototypes in plain integers and floats: None or 0
+// for a null pointer, integers of any size for an int (the low bits, as C would take them), a float for a float.  Anything else makes the call
 // return None without doing anything, and the caller goes through ctypes, which converts it or says what is wrong with it.  The interpreter lock
 // is released for the call, as ctypes does.
 //
@@ -28,6 +28,13 @@ template <typename T> bool read(PyObject* o, T& v) {
       return true;
     }
   }
+  if constexpr (std::is_floating_point_v<T>) {
+    if (PyFloat_CheckExact(o)) {
+      v = static_cast<T>(PyFloat_AS_DOUBLE(o));
+      return true;
+    }
+    return false;
+  }
   if (!PyLong_CheckExact(o)) return false;
   const unsigned long long u = PyLong_AsUnsignedLongLongMask(o);
   if constexpr (std::is_pointer_v<T>) v = reinterpret_cast<T>(static_cast<uintptr_t>(u));
@@ -50,7 +57,7 @@ template <typename... A> PyObject* checked(int (*f)(A...), PyObject* const* args
   return call(f, args, std::index_sequence_for<A...>{});
 }
 
-enum Entry { GEMM, CONV, CONV_WGRAD_STATIC, LAYERNORM, GELU, ATTENTION, ENTRIES };
+enum Entry { GEMM, CONV, CONV_WGRAD_STATIC, LAYERNORM, GELU, ATTENTION, EMBEDDING, RESIDUAL_NORM, RESIDUAL_NORM_BACKWARD, ATTENTION_PACKED, GRAD_CLIP, ENTRIES };
 void* address[ENTRIES];  // null: not told yet
 
 template <int E, typename F> PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -76,6 +83,11 @@ PyMethodDef methods[] = {method("cdp_k_gemm", &entry<GEMM, decltype(&cdp_k_gemm)
                          method("cdp_k_layernorm", &entry<LAYERNORM, decltype(&cdp_k_layernorm)>),
                          method("cdp_k_gelu", &entry<GELU, decltype(&cdp_k_gelu)>),
                          method("cdp_k_attention", &entry<ATTENTION, decltype(&cdp_k_attention)>),
+                         method("cdp_k_embedding", &entry<EMBEDDING, decltype(&cdp_k_embedding)>),
+                         method("cdp_k_residual_norm", &entry<RESIDUAL_NORM, decltype(&cdp_k_residual_norm)>),
+                         method("cdp_k_residual_norm_backward", &entry<RESIDUAL_NORM_BACKWARD, decltype(&cdp_k_residual_norm_backward)>),
+                         method("cdp_k_attention_packed", &entry<ATTENTION_PACKED, decltype(&cdp_k_attention_packed)>),
+                         method("cdp_k_grad_clip", &entry<GRAD_CLIP, decltype(&cdp_k_grad_clip)>),
                          method("use", &use),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
