@@ -127,7 +127,8 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const
 /* Causal self-attention of sequences of different lengths packed behind each other: sequence s is the rows offsets[s] ..
  * offsets[s + 1] - 1 (device int32 [sequences + 1], ascending, within [0, tokens]; a length may be zero), and a token sees its own
  * sequence up to itself.  qkv[tokens][(heads + 2 * kv_heads) * width]: q heads | k heads | v heads per token; query head h goes with key
- * head h / (heads / kv_heads).  width: a multiple of 8 up to 128; heads a multiple of kv_heads; tensors 16-byte aligned.
+ * head h / (heads / kv_heads).  width: a multiple of 8 up to 128; heads a multiple of kv_heads, heads + 2 * kv_heads up to 4096; tensors 16-byte
+ * aligned.
  *   backward 0: out[tokens][heads * width] = softmax(scale * q k^T) v, lse[heads][tokens] (fp32) = log of the sum that the softmax divides
  *               by, sum exp(scale * q k^T)   (dout, dqkv, workspace unused)
  *   backward 1: dqkv from dout[tokens][heads * width] and the forward's out and lse

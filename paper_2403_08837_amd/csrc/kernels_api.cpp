@@ -255,8 +255,8 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
   if (!qkv || !offsets || !out || !lse || tokens <= 0 || sequences <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || width <= 0 ||
       width % 8 || width > 128 || (dtype != DT_F32 && dtype != DT_BF16))
     return CDP_EINVAL;
-  // tiles of 32 rows at least, and one more for every sequence: what a launch can number, and the rows' addresses in 63 bits
-  if (heads > 65536 || kv_heads > 65536 || ((int64_t)tokens / 32 + sequences + 1) * heads > INT_MAX / 2) return CDP_EINVAL;
+  // a tile of rows within 32-bit offsets of its first; tiles of 32 rows at least, and one more for every sequence, within what a launch can number
+  if (heads > 4096 || (int64_t)heads + 2ll * kv_heads > 4096 || ((int64_t)tokens / 32 + sequences + 1) * heads > INT_MAX / 2) return CDP_EINVAL;
   if (!aligned_to(qkv, 16) || !aligned_to(out, 16) || !aligned_to(lse, 4) || !aligned_to(offsets, 4)) return CDP_EINVAL;
   PackedAttention a;
   memset(&a, 0, sizeof(a));
