@@ -95,14 +95,17 @@ __device__ __forceinline__ void across_product(const char* tile, int r0, const v
   }
 }
 
-// A tile's loads into LDS.  Lane offsets are the same for every tile; the buffer's base and bounds move.
+// A tile's loads into LDS.  Lane offsets are the same for every tile; the buffer's base and bounds move.  Where 4 KB of the tile are whole rows whose
+// swizzle repeats, load i differs from load 0 by rows alone, which go into the base: one offset register instead of one per load.
 template <typename T, int DW> struct TileLoads {
   using Tl = Tile<T, DW>;
-  unsigned off[Tl::LOADS];
+  static constexpr int STEP_ROWS = 256 / Tl::CPR;  // rows of 4 KB
+  static constexpr bool BY_ROWS = Tl::E == 2 && 256 % Tl::CPR == 0;
+  unsigned off[BY_ROWS ? 1 : Tl::LOADS];
   __device__ __forceinline__ void start(int wave, int lane, unsigned row_bytes, int width) {
 #pragma unroll
-    for (int i = 0; i < Tl::LOADS; ++i) {
-      const int e = (wave * Tl::LOADS + i) * 64 + lane, r = e / Tl::CPR, c = (e % Tl::CPR) ^ Tl::swz(r);
+    for (int i = 0; i < (BY_ROWS ? 1 : Tl::LOADS); ++i) {
+      const int e = (4 * i + wave) * 64 + lane, r = e / Tl::CPR, c = (e % Tl::CPR) ^ Tl::swz(r);
       off[i] = c * Tl::VEC < width ? r * row_bytes + 16 * c : ~0u;  // past the width: out of bounds, zero
     }
   }
@@ -110,18 +113,19 @@ template <typename T, int DW> struct TileLoads {
   __device__ __forceinline__ void issue(unsigned at, int wave, const char* base, int rows, unsigned row_bytes, int width) const {
     typedef unsigned v4u __attribute__((ext_vector_type(4)));
     rows = min(rows, Tl::OTHER);
-    const unsigned records = rows > 0 ? (rows - 1) * row_bytes + width * Tl::E : 0u;
-    const uintptr_t p = (uintptr_t)base;
     auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
-    const v4u buffer = {uniform((unsigned)p), uniform((unsigned)(p >> 32)), uniform(records), 0x00020000u};
 #pragma unroll
     for (int i = 0; i < Tl::LOADS; ++i) {
-      const unsigned lds = at + (wave * Tl::LOADS + i) * 1024;
+      const int skip = BY_ROWS ? i * STEP_ROWS : 0;
+      const unsigned records = rows > skip ? (rows - 1 - skip) * row_bytes + width * Tl::E : 0u;
+      const uintptr_t p = (uintptr_t)base + (uintptr_t)skip * row_bytes;
+      const v4u buffer = {uniform((unsigned)p), uniform((unsigned)(p >> 32)), uniform(records), 0x00020000u};
+      const unsigned lds = at + (4 * i + wave) * 1024;
       // the wait states of this are ours: one between the write of m0 and the load, five between a write of a descriptor word by the vector unit
       // (the readfirstlane above) and the load; s_mov_b32 is one, s_nop 3 four
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off[i]), "s"(buffer) : "m0");
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off[BY_ROWS ? 0 : i]), "s"(buffer) : "m0");
 #pragma clang diagnostic pop
     }
   }
@@ -359,14 +363,15 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------------------------
-// The tiles are those of the query heads of the key head, one head after the other, each from the workgroup's first key on.
-template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 64 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a) {
+// The tiles are those of the query heads of the key head, one head after the other, each from the workgroup's first key on.  Where that leaves
+// the chip short of workgroups the heads are shared by `shares` of them, whose sums (fp32, in the workspace) packed_bwd_fold_kernel adds in a fixed order.
+template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 64 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
   using Tl = Tile<T, DW>;
   __shared__ __attribute__((aligned(1024))) char smem[4 * Tl::BYTES];
   __shared__ __attribute__((aligned(16))) float stats[2][2][Tl::OTHER];  // per stage: lse (in log2), delta
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
-  const int kv = blockIdx.x % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
-  const Span span = find_span(a, blockIdx.x / a.kv_heads, lane);
+  const int share = blockIdx.x % shares, kv = blockIdx.x / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
+  const Span span = find_span(a, blockIdx.x / (shares * a.kv_heads), lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E, out_bytes = a.heads * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -385,9 +390,9 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
   qloads.start(wave, lane, row_bytes, W);
   oloads.start(wave, lane, out_bytes, W);
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem;
-  const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * group;
+  const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
   // the next tile: head and first query; what its statistics were
-  int head = kv * group, q0 = span.first;
+  int head = kv * group + share * (group / shares), q0 = span.first;
   float stat = 0.f;
   auto issue = [&](int i) {
     const unsigned to = lds + (i & 1) * 2 * Tl::BYTES;
@@ -421,7 +426,7 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
     tile_barrier();
     if (i + 1 < tiles) issue(i + 1);
     const char* Qs = smem + (i & 1) * 2 * Tl::BYTES;
-#pragma unroll
+#pragma unroll 1
     for (int b = 0; b < Tl::NB; ++b) {
       const int b0 = t0 + 32 * b;
       if (b0 + 31 < first || b0 >= span.len) continue;
@@ -454,9 +459,37 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
     if (t0 >= span.len) t0 = span.first;
   }
   if (key >= span.len) return;
+  if (shares > 1) {
+    float* row = a.parts + (((int64_t)share * 2 * a.tokens + span.begin + key) * a.kv_heads + kv) * W;
+    store_own<float, DW>(row, dk, a.scale, hi, W);
+    store_own<float, DW>(row + (int64_t)a.tokens * a.kv_heads * W, dv, 1.f, hi, W);
+    return;
+  }
   T* row = static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W;
   store_own<T, DW>(row, dk, a.scale, hi, W);
   store_own<T, DW>(row + a.kv_heads * W, dv, 1.f, hi, W);
+}
+
+// Sums of the shares: [share][dk, dv][tokens][kv_heads][width] -> the rows of dqkv that belong to a sequence, eight columns a thread.
+template <typename T> __global__ __launch_bounds__(256) void packed_bwd_fold_kernel(const PackedAttention a, const int shares) {
+  const int n8 = a.kv_heads * a.width / 8, begin = min(max(a.offsets[0], 0), a.tokens), end = min(max(a.offsets[a.sequences], 0), a.tokens);
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / n8;
+  if (row < begin || row >= end) return;
+  const int64_t stride = (int64_t)a.tokens * a.kv_heads * a.width;
+  const int col = (int)(i - row * n8) * 8;
+  const float* p = a.parts + row * a.kv_heads * a.width + col + blockIdx.y * stride;
+  float s[8] = {};
+  for (int k = 0; k < shares; ++k, p += 2 * stride) {
+    const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+    s[0] += x.x; s[1] += x.y; s[2] += x.z; s[3] += x.w;
+    s[4] += y.x; s[5] += y.y; s[6] += y.z; s[7] += y.w;
+  }
+  T* out = static_cast<T*>(a.dqkv) + row * (a.heads + 2 * a.kv_heads) * a.width + (a.heads + blockIdx.y * a.kv_heads) * a.width + col;
+  Chunk16<T> c[8 / Elem<T>::VEC];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) c[e / Elem<T>::VEC].e[e % Elem<T>::VEC] = Elem<T>::from_f32(s[e]);
+#pragma unroll
+  for (int e = 0; e < 8 / Elem<T>::VEC; ++e) reinterpret_cast<uint4*>(out)[e] = c[e].v;
 }
 
 #define CDP_WIDTHS(CALL)                                 \
@@ -469,17 +502,33 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
 
 int tiles_of(const PackedAttention& a) { return a.tokens / OWN + a.sequences; }
 
+// Workgroups that share a key tile's query heads: as few as make 2048 workgroups, four rounds of two per CU (a causal launch's workgroups differ in
+// length by as much as their tiles are many, and the longest, which start first, have to be short against the whole).
+int shares_of(const PackedAttention& a) {
+  const int group = a.heads / a.kv_heads;
+  const int64_t have = (int64_t)tiles_of(a) * a.kv_heads;
+  int shares = 1;
+  for (int n = 2; n <= group && have * shares < 2048; ++n)
+    if (group % n == 0 && n <= a.max_parts) shares = n;
+  return shares;
+}
+
 template <typename T> hipError_t forward(const PackedAttention& a, hipStream_t stream) {
   const dim3 grid((unsigned)tiles_of(a) * a.heads);
   CDP_WIDTHS(hipLaunchKernelGGL((packed_fwd_kernel<T, DW>), grid, dim3(256), 0, stream, a));
   return hipGetLastError();
 }
 template <typename T> hipError_t backward(const PackedAttention& a, hipStream_t stream) {
-  const dim3 qgrid((unsigned)tiles_of(a) * a.heads), kgrid((unsigned)tiles_of(a) * a.kv_heads);
+  const dim3 qgrid((unsigned)tiles_of(a) * a.heads);
+  const unsigned kgrid = (unsigned)tiles_of(a) * a.kv_heads;
   CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_q_kernel<T, DW>), qgrid, dim3(256), 0, stream, a));
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, DW>), kgrid, dim3(256), 0, stream, a));
+  const int shares = shares_of(a);
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, DW>), dim3(kgrid * shares), dim3(256), 0, stream, a, shares));
+  if ((e = hipGetLastError()) != hipSuccess || shares == 1) return e;
+  const int64_t n = (int64_t)a.tokens * a.kv_heads * a.width / 8;
+  hipLaunchKernelGGL((packed_bwd_fold_kernel<T>), dim3((unsigned)((n + 255) / 256), 2), dim3(256), 0, stream, a, shares);
   return hipGetLastError();
 }
 
