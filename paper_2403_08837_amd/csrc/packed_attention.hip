@@ -3,16 +3,20 @@
 //   backward: P = exp(S - lse), delta = rowsum(dout out), dP = dout v^T, dS = P (dP - delta), dq = scale dS k, dk = scale dS^T q, dv = P^T dout.
 //
 // One pass over the keys with the running maximum and sum of the softmax; nothing of S or P goes through memory.  A workgroup is four wavefronts
-// of 32 rows each (queries forward and for dq, keys for dk and dv) of one head of one sequence and walks tiles of the other side, which two
+// of 32 rows (ROWS = 128) each (queries forward and for dq, keys for dk and dv) of one head of one sequence and walks tiles of the other side, which two
 // stages of LDS hold: the next tile's loads (straight into LDS, zeros past the sequence from the buffer's bounds) are in flight under the products
 // of the current one.  Score blocks are contracted so that a lane holds one of the wavefront's own rows, 16 rows of the other side in its
 // registers: row sums and maxima stay in the lane (and lane +- 32), and the probabilities are, in the registers they are in, the column operand of the next
 // product, whose row operand is read from LDS across rows (bf16: transposing reads) in that same order.
+// SPLIT, for launches of few workgroups: all four wavefronts have the same 32 rows, each walks every fourth tile of the other side, filled by itself
+// into LDS of its own (no barrier), and they join their sums at the end.
 // Work is found on the device: sequence s takes offsets[s + 1] / ROWS - offsets[s] / ROWS + 1 workgroups per head, which is what it needs or one more, so
 // that workgroup t's sequence is the last with offsets[s] / ROWS + s <= t: no table, no launch ahead.
 // fp32: the same on 32x32x2 products, tiles of 32 rows instead of 64.
 #include "elem.h"
 #include "kernels.h"
+
+#include <type_traits>
 
 namespace cdp {
 
@@ -21,16 +25,18 @@ namespace {
 typedef short att_v4s __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
-constexpr int OWN = 128;  // rows of a workgroup
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // Tile of `OTHER` rows of one head, DW columns (the width rounded up, zeros behind it), in LDS.  16-byte chunk c of row r sits in slot c ^ swz(r) of the
 // row: 16 consecutive rows' chunk c are 16 different slots modulo 256 bytes, and so are the pieces that a read across rows takes.
-template <typename T, int DW> struct Tile {
+template <typename T, int DW, bool SPLIT> struct Tile {
   static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = CPR / 2;  // steps: 16-byte reads of a row by either lane half
-  static constexpr int OTHER = E == 2 ? 64 : 32, NB = OTHER / 32, OB = DW / 32;
-  static constexpr int BYTES = OTHER * DW * E, LOADS = BYTES / 1024 / 4;              // per wavefront
-  static_assert(LOADS * 4 * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
+  static constexpr int OWN = SPLIT ? 32 : 128, OTHER = SPLIT || E == 4 ? 32 : 64, NB = OTHER / 32, OB = DW / 32;
+  static constexpr int BYTES = OTHER * DW * E, FILLERS = SPLIT ? 1 : 4, LOADS = BYTES / 1024 / FILLERS;  // wavefronts that fill a tile, loads of each
+  static_assert(LOADS * FILLERS * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
+  static constexpr int STAGES = SPLIT && E == 4 && DW > 64 ? 1 : 2;                   // what fits LDS
+  static constexpr int LDS = (SPLIT ? 4 : 1) * STAGES * 2 * BYTES;
+  static_assert(!SPLIT || LDS >= 2 * 4 * 32 * DW * 4, "room for what the wavefronts join");
   __device__ static __forceinline__ int swz(int r) {
     if constexpr (E == 2) return CPR == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : CPR == 8 ? ((r & 2) << 1) | ((r >> 2) & 3) : (r >> 2) & 3;
     else return CPR % 16 == 0 ? (r & 3) | ((r & 4) << 1) | ((r & 8) >> 1) : (r >> 1) & 7;
@@ -39,8 +45,8 @@ template <typename T, int DW> struct Tile {
 };
 
 // Operand rows r0 .. r0 + 31 of the tile, 16-byte step ks of them.
-template <typename T, int DW> __device__ __forceinline__ uint4 rows_frag(const char* tile, int r0, int ks, int l31, int hi) {
-  return *reinterpret_cast<const uint4*>(tile + Tile<T, DW>::slot(r0 + l31, 2 * ks + hi));
+template <typename Tl> __device__ __forceinline__ uint4 rows_frag(const char* tile, int r0, int ks, int l31, int hi) {
+  return *reinterpret_cast<const uint4*>(tile + Tl::slot(r0 + l31, 2 * ks + hi));
 }
 // acc += rows x columns over one 16-byte step of both.
 template <typename T> __device__ __forceinline__ v16f_t step_product(uint4 a, uint4 b, v16f_t c) {
@@ -61,9 +67,8 @@ __device__ __forceinline__ v16f_t zero16() {
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); }
 
 // out[ob] += (columns 32 ob .. of the tile's rows r0 .. r0 + 31)^T x p, p as a score block's accumulator holds it (rounded to the element type).
-template <typename T, int DW>
-__device__ __forceinline__ void across_product(const char* tile, int r0, const v16f_t& p, v16f_t (&out)[DW / 32], int lane) {
-  using Tl = Tile<T, DW>;
+template <typename T, typename Tl, int OB>
+__device__ __forceinline__ void across_product(const char* tile, int r0, const v16f_t& p, v16f_t (&out)[OB], int lane) {
   const int hi = lane >> 5;
   if constexpr (sizeof(T) == 2) {
     const int rho = lane & 15, cl = 16 * ((lane >> 4) & 1) + 4 * (rho & 3);
@@ -73,7 +78,7 @@ __device__ __forceinline__ void across_product(const char* tile, int r0, const v
       const uint4 w = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]), pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
       const int r = r0 + 16 * t + 4 * hi + (rho >> 2);
 #pragma unroll
-      for (int ob = 0; ob < Tl::OB; ++ob) {
+      for (int ob = 0; ob < OB; ++ob) {
         const int c = 32 * ob + cl;
         union { att_v4s v[2]; uint4 u; } f;
         f.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(tile + Tl::slot(r, c >> 3) + 2 * (c & 7)));
@@ -86,7 +91,7 @@ __device__ __forceinline__ void across_product(const char* tile, int r0, const v
     for (int v = 0; v < 16; ++v) {
       const int r = r0 + 8 * (v >> 2) + 4 * hi + (v & 3);
 #pragma unroll
-      for (int ob = 0; ob < Tl::OB; ++ob) {
+      for (int ob = 0; ob < OB; ++ob) {
         const int c = 32 * ob + (lane & 31);
         const float x = *reinterpret_cast<const float*>(tile + Tl::slot(r, c >> 2) + 4 * (c & 3));
         out[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[v], out[ob], 0, 0, 0);
@@ -95,17 +100,17 @@ __device__ __forceinline__ void across_product(const char* tile, int r0, const v
   }
 }
 
-// A tile's loads into LDS.  Lane offsets are the same for every tile; the buffer's base and bounds move.  Where 4 KB of the tile are whole rows whose
+// A tile's loads into LDS.  Lane offsets are the same for every tile; the buffer's base and bounds move.  Where one load of every wavefront is whole rows whose
 // swizzle repeats, load i differs from load 0 by rows alone, which go into the base: one offset register instead of one per load.
-template <typename T, int DW> struct TileLoads {
-  using Tl = Tile<T, DW>;
-  static constexpr int STEP_ROWS = 256 / Tl::CPR;  // rows of 4 KB
-  static constexpr bool BY_ROWS = Tl::E == 2 && 256 % Tl::CPR == 0;
+template <typename Tl> struct TileLoads {
+  static constexpr int STEP = Tl::FILLERS * 64, STEP_ROWS = STEP / Tl::CPR;  // chunks and rows of a load by every filler
+  static constexpr bool BY_ROWS = Tl::E == 2 && STEP % Tl::CPR == 0 && STEP_ROWS % 16 == 0;
   unsigned off[BY_ROWS ? 1 : Tl::LOADS];
+  // wave: of the wavefronts that fill the tile
   __device__ __forceinline__ void start(int wave, int lane, unsigned row_bytes, int width) {
 #pragma unroll
     for (int i = 0; i < (BY_ROWS ? 1 : Tl::LOADS); ++i) {
-      const int e = (4 * i + wave) * 64 + lane, r = e / Tl::CPR, c = (e % Tl::CPR) ^ Tl::swz(r);
+      const int e = i * STEP + wave * 64 + lane, r = e / Tl::CPR, c = (e % Tl::CPR) ^ Tl::swz(r);
       off[i] = c * Tl::VEC < width ? r * row_bytes + 16 * c : ~0u;  // past the width: out of bounds, zero
     }
   }
@@ -120,7 +125,7 @@ template <typename T, int DW> struct TileLoads {
       const unsigned records = rows > skip ? (rows - 1 - skip) * row_bytes + width * Tl::E : 0u;
       const uintptr_t p = (uintptr_t)base + (uintptr_t)skip * row_bytes;
       const v4u buffer = {uniform((unsigned)p), uniform((unsigned)(p >> 32)), uniform(records), 0x00020000u};
-      const unsigned lds = at + (4 * i + wave) * 1024;
+      const unsigned lds = at + i * STEP * 16 + wave * 1024;
       // the wait states of this are ours: one between the write of m0 and the load, five between a write of a descriptor word by the vector unit
       // (the readfirstlane above) and the load; s_mov_b32 is one, s_nop 3 four
 #pragma clang diagnostic push
@@ -130,19 +135,21 @@ template <typename T, int DW> struct TileLoads {
     }
   }
 };
-// This wavefront's loads have landed and its LDS reads and writes are done; then everyone's, and everyone has left the other stage.
-__device__ __forceinline__ void tile_barrier() {
+// This wavefront's loads have landed and its LDS reads and writes are done; where tiles are shared, everyone's, and everyone has left the other stage.
+template <bool SPLIT> __device__ __forceinline__ void tile_wait() {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0) lgkmcnt(0)
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_barrier();
-  asm volatile("" ::: "memory");
+  if constexpr (!SPLIT) {
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  }
   __builtin_amdgcn_sched_barrier(0);
 }
 
 struct Span { int begin, len, first; };  // rows of a sequence, and the workgroup's first row in it; len 0: nothing to do
 // Offsets that are not as they should be give some span within the tensor.
-__device__ __forceinline__ Span find_span(const PackedAttention& a, int t, int lane) {
+template <int OWN> __device__ __forceinline__ Span find_span(const PackedAttention& a, int t, int lane) {
   auto at = [&](int s) { return min(max(a.offsets[s], 0), a.tokens); };
   int lo = 0, n = a.sequences;
   for (;;) {
@@ -196,19 +203,43 @@ __device__ __forceinline__ float both_halves(float v, bool maximum) {
 // is taken by turning the sign of one operand, so that the largest product is the largest score.
 __device__ __forceinline__ float score_factor(float scale) { return fmaxf(fabsf(scale) * LOG2E, 1.17549435e-38f); }
 
+// SPLIT: four wavefronts' accumulators of the same 32 rows through LDS, [wavefront][column][row], and the sum of them for DW / 8 columns of a lane's row.
+template <int OB> __device__ __forceinline__ void put_share(float* mine, const v16f_t (&acc)[OB], float f, int l31, int hi) {
+#pragma unroll
+  for (int ob = 0; ob < OB; ++ob)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) mine[(32 * ob + 8 * (v >> 2) + 4 * hi + (v & 3)) * 32 + l31] = acc[ob][v] * f;
+}
+template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row, const float* shares, float f, int wave, int l31, int hi, int width) {
+  const int d0 = (2 * wave + hi) * (DW / 8);
+#pragma unroll
+  for (int d = d0; d < d0 + DW / 8; d += 4) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float* p = shares + (d + e) * 32 + l31;
+      v[e] = ((p[0] + p[DW * 32]) + (p[2 * DW * 32] + p[3 * DW * 32])) * f;
+    }
+    if (d >= width) continue;
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(row + d) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+    else *reinterpret_cast<float4*>(row + d) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+}
+
 // ---- forward ----------------------------------------------------------------------------------------------------------
-template <typename T, int DW> __global__ __launch_bounds__(256, 2) void packed_fwd_kernel(const PackedAttention a) {
-  using Tl = Tile<T, DW>;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * Tl::BYTES];
+template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
+  using Tl = Tile<T, DW, SPLIT>;
+  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
-  const Span span = find_span(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
+  const Span span = find_span<Tl::OWN>(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
   const char* kbase = base + (int64_t)(a.heads + kv) * W * Tl::E;
   const char* vbase = kbase + (int64_t)a.kv_heads * W * Tl::E;
-  const int q = span.first + 32 * wave + l31, last = span.first + 32 * wave + 31;
+  const int q = span.first + 32 * rows_of + l31, last = span.first + 32 * rows_of + 31;
   uint4 qf[Tl::STEPS];
   load_own<T>(qf, base + (int64_t)min(q, span.len - 1) * row_bytes + (int64_t)head * W * Tl::E, hi, W);
   if (a.scale < 0.f) {
@@ -216,34 +247,37 @@ template <typename T, int DW> __global__ __launch_bounds__(256, 2) void packed_f
     for (int ks = 0; ks < Tl::STEPS; ++ks) qf[ks] = flip<T>(qf[ks]);
   }
   const float c = score_factor(a.scale);
-  TileLoads<T, DW> loads;
-  loads.start(wave, lane, row_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem;
-  auto issue = [&](int i) {
+  TileLoads<Tl> loads;
+  loads.start(filler, lane, row_bytes, W);
+  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
+  auto issue = [&](int i, int stage) {
     const int k0 = i * Tl::OTHER;
-    const unsigned at = lds + (i & 1) * 2 * Tl::BYTES;
-    loads.issue(at, wave, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
-    loads.issue(at + Tl::BYTES, wave, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    const unsigned at = lds + stage * 2 * Tl::BYTES;
+    loads.issue(at, filler, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    loads.issue(at + Tl::BYTES, filler, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
-  const int tiles = (min(span.len, span.first + OWN) + Tl::OTHER - 1) / Tl::OTHER;
+  const int tiles = (min(span.len, span.first + Tl::OWN) + Tl::OTHER - 1) / Tl::OTHER;
   v16f_t o[Tl::OB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) o[ob] = zero16();
   float m = -INFINITY, z = 0.f;
-  issue(0);
-  for (int i = 0; i < tiles; ++i) {
-    tile_barrier();
-    if (i + 1 < tiles) issue(i + 1);
+  const int from = SPLIT ? wave : 0;
+  if (from < tiles) issue(from, 0);
+  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
+    tile_wait<SPLIT>();
+    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
     const int k0 = i * Tl::OTHER;
     if (k0 > last) continue;
-    const char* Ks = smem + (i & 1) * 2 * Tl::BYTES;
+    const char* Ks = tiles_at + stage * 2 * Tl::BYTES;
     v16f_t s[Tl::NB];
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) s[b] = zero16();
 #pragma unroll
     for (int ks = 0; ks < Tl::STEPS; ++ks)
 #pragma unroll
-      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<T, DW>(Ks, 32 * b, ks, l31, hi), qf[ks], s[b]);
+      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<Tl>(Ks, 32 * b, ks, l31, hi), qf[ks], s[b]);
     if (k0 + Tl::OTHER - 1 > last - 31) {
 #pragma unroll
       for (int b = 0; b < Tl::NB; ++b)
@@ -275,27 +309,51 @@ template <typename T, int DW> __global__ __launch_bounds__(256, 2) void packed_f
         z += s[b][v];
       }
 #pragma unroll
-    for (int b = 0; b < Tl::NB; ++b) across_product<T, DW>(Ks + Tl::BYTES, 32 * b, s[b], o, lane);
+    for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(Ks + Tl::BYTES, 32 * b, s[b], o, lane);
+    if (Tl::STAGES == 1 && i + NEXT < tiles) {
+      tile_wait<SPLIT>();
+      issue(i + NEXT, 0);
+    }
   }
-  if (q >= span.len) return;
   z = both_halves(z, false);
-  store_own<T, DW>(static_cast<T*>(a.out) + ((int64_t)(span.begin + q) * a.heads + head) * W, o, 1.f / z, hi, W);
+  T* const out = static_cast<T*>(a.out) + ((int64_t)(span.begin + q) * a.heads + head) * W;
+  if constexpr (SPLIT) {
+    // every wavefront's maximum, then its sums relative to the largest (one without tiles has a maximum of -inf and a factor of 0)
+    __shared__ float ms[4][32], zs[4][32];
+    if (hi == 0) ms[wave][l31] = m;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(ms[0][l31], ms[1][l31]), fmaxf(ms[2][l31], ms[3][l31])), f = __builtin_amdgcn_exp2f(m - top);
+    if (hi == 0) zs[wave][l31] = z * f;
+    float* shares = reinterpret_cast<float*>(smem);
+    put_share(shares + wave * DW * 32, o, f, l31, hi);
+    __syncthreads();
+    if (q >= span.len) return;
+    z = (zs[0][l31] + zs[1][l31]) + (zs[2][l31] + zs[3][l31]);
+    m = top;
+    join_shares<T, DW>(out, shares, 1.f / z, wave, l31, hi, W);
+    if (wave) return;
+  } else {
+    if (q >= span.len) return;
+    store_own<T, DW>(out, o, 1.f / z, hi, W);
+  }
   if (hi == 0) a.lse[(int64_t)head * a.tokens + span.begin + q] = (m + __builtin_amdgcn_logf(z)) * LN2;
 }
 
 // ---- backward: dq, and delta for the other kernel ---------------------------------------------------------------------
-template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 96 ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
-  using Tl = Tile<T, DW>;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * Tl::BYTES];
+template <typename T, int DW, bool SPLIT>
+__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
+  using Tl = Tile<T, DW, SPLIT>;
+  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
-  const Span span = find_span(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
+  const Span span = find_span<Tl::OWN>(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
   const char* kbase = base + (int64_t)(a.heads + kv) * W * Tl::E;
   const char* vbase = kbase + (int64_t)a.kv_heads * W * Tl::E;
-  const int q = span.first + 32 * wave + l31, last = span.first + 32 * wave + 31, qc = min(q, span.len - 1);
+  const int q = span.first + 32 * rows_of + l31, last = span.first + 32 * rows_of + 31, qc = min(q, span.len - 1);
   uint4 qf[Tl::STEPS], df[Tl::STEPS];
   load_own<T>(qf, base + (int64_t)qc * row_bytes + (int64_t)head * W * Tl::E, hi, W);
   if (a.scale < 0.f) {
@@ -319,26 +377,29 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
     delta = both_halves(delta, false);
   }
   const float lse = a.lse[at] * LOG2E;
-  if (hi == 0 && q < span.len) a.delta[at] = delta;
+  if (hi == 0 && q < span.len && (!SPLIT || wave == 0)) a.delta[at] = delta;
   const float c = score_factor(a.scale);
-  TileLoads<T, DW> loads;
-  loads.start(wave, lane, row_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem;
-  auto issue = [&](int i) {
+  TileLoads<Tl> loads;
+  loads.start(filler, lane, row_bytes, W);
+  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
+  auto issue = [&](int i, int stage) {
     const int k0 = i * Tl::OTHER;
-    const unsigned to = lds + (i & 1) * 2 * Tl::BYTES;
-    loads.issue(to, wave, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
-    loads.issue(to + Tl::BYTES, wave, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    const unsigned to = lds + stage * 2 * Tl::BYTES;
+    loads.issue(to, filler, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    loads.issue(to + Tl::BYTES, filler, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
-  const int tiles = (min(span.len, span.first + OWN) + Tl::OTHER - 1) / Tl::OTHER;
+  const int tiles = (min(span.len, span.first + Tl::OWN) + Tl::OTHER - 1) / Tl::OTHER;
   v16f_t dq[Tl::OB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) dq[ob] = zero16();
-  issue(0);
-  for (int i = 0; i < tiles; ++i) {
-    tile_barrier();
-    if (i + 1 < tiles) issue(i + 1);
-    const char* Ks = smem + (i & 1) * 2 * Tl::BYTES;
+  const int from = SPLIT ? wave : 0;
+  if (from < tiles) issue(from, 0);
+  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
+    tile_wait<SPLIT>();
+    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
+    const char* Ks = tiles_at + stage * 2 * Tl::BYTES;
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) {
       const int k0 = i * Tl::OTHER + 32 * b;
@@ -346,8 +407,8 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
       v16f_t s = zero16(), dp = zero16();
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<T, DW>(Ks, 32 * b, ks, l31, hi), qf[ks], s);
-        dp = step_product<T>(rows_frag<T, DW>(Ks + Tl::BYTES, 32 * b, ks, l31, hi), df[ks], dp);
+        s = step_product<T>(rows_frag<Tl>(Ks, 32 * b, ks, l31, hi), qf[ks], s);
+        dp = step_product<T>(rows_frag<Tl>(Ks + Tl::BYTES, 32 * b, ks, l31, hi), df[ks], dp);
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * (dp[v] - delta);
@@ -356,27 +417,42 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
         for (int v = 0; v < 16; ++v)
           if (k0 + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[v] = 0.f;
       }
-      across_product<T, DW>(Ks, 32 * b, s, dq, lane);
+      across_product<T, Tl>(Ks, 32 * b, s, dq, lane);
+    }
+    if (Tl::STAGES == 1 && i + NEXT < tiles) {
+      tile_wait<SPLIT>();
+      issue(i + NEXT, 0);
     }
   }
-  if (q < span.len) store_own<T, DW>(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + q) * (a.heads + 2 * a.kv_heads) * W + head * W, dq, a.scale, hi, W);
+  T* const row = static_cast<T*>(a.dqkv) + (int64_t)(span.begin + q) * (a.heads + 2 * a.kv_heads) * W + head * W;
+  if constexpr (SPLIT) {
+    float* shares = reinterpret_cast<float*>(smem);
+    __syncthreads();
+    put_share(shares + wave * DW * 32, dq, 1.f, l31, hi);
+    __syncthreads();
+    if (q < span.len) join_shares<T, DW>(row, shares, a.scale, wave, l31, hi, W);
+  } else if (q < span.len) {
+    store_own<T, DW>(row, dq, a.scale, hi, W);
+  }
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------------------------
 // The tiles are those of the query heads of the key head, one head after the other, each from the workgroup's first key on.  Where that leaves
 // the chip short of workgroups the heads are shared by `shares` of them, whose sums (fp32, in the workspace) packed_bwd_fold_kernel adds in a fixed order.
-template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 64 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
-  using Tl = Tile<T, DW>;
-  __shared__ __attribute__((aligned(1024))) char smem[4 * Tl::BYTES];
-  __shared__ __attribute__((aligned(16))) float stats[2][2][Tl::OTHER];  // per stage: lse (in log2), delta
+template <typename T, int DW, bool SPLIT>
+__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+  using Tl = Tile<T, DW, SPLIT>;
+  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
+  __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 1][2][2][Tl::OTHER];  // per stage: lse (in log2), delta
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int share = blockIdx.x % shares, kv = blockIdx.x / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
-  const Span span = find_span(a, blockIdx.x / (shares * a.kv_heads), lane);
+  const Span span = find_span<Tl::OWN>(a, blockIdx.x / (shares * a.kv_heads), lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E, out_bytes = a.heads * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
   const char* obase = static_cast<const char*>(a.dout) + (int64_t)span.begin * out_bytes;
-  const int key = span.first + 32 * wave + l31, first = span.first + 32 * wave, kc = min(key, span.len - 1);
+  const int key = span.first + 32 * rows_of + l31, first = span.first + 32 * rows_of, kc = min(key, span.len - 1);
   uint4 kf[Tl::STEPS], vf[Tl::STEPS];
   const char* krow = base + (int64_t)kc * row_bytes + (int64_t)(a.heads + kv) * W * Tl::E;
   load_own<T>(kf, krow, hi, W);
@@ -386,46 +462,44 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
     for (int ks = 0; ks < Tl::STEPS; ++ks) kf[ks] = flip<T>(kf[ks]);
   }
   const float c = score_factor(a.scale);
-  TileLoads<T, DW> qloads, oloads;
-  qloads.start(wave, lane, row_bytes, W);
-  oloads.start(wave, lane, out_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem;
+  TileLoads<Tl> qloads, oloads;
+  qloads.start(filler, lane, row_bytes, W);
+  oloads.start(filler, lane, out_bytes, W);
+  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
-  // the next tile: head and first query; what its statistics were
-  int head = kv * group + share * (group / shares), q0 = span.first;
-  float stat = 0.f;
-  auto issue = [&](int i) {
-    const unsigned to = lds + (i & 1) * 2 * Tl::BYTES;
+  const int head0 = kv * group + share * (group / shares);
+  constexpr int STATS = 2 * Tl::OTHER, LOADERS = SPLIT ? 64 : 256;
+  static_assert(STATS <= LOADERS, "a statistic per thread");
+  const int id = SPLIT ? lane : (int)threadIdx.x;
+  float stat = 0.f;  // of the tile under way
+  auto issue = [&](int i, int stage) {
+    const unsigned to = lds + stage * 2 * Tl::BYTES;
+    const int head = head0 + i / per_head, q0 = span.first + i % per_head * Tl::OTHER;
     const int64_t col = (int64_t)head * W * Tl::E;
-    qloads.issue(to, wave, base + (int64_t)q0 * row_bytes + col, span.len - q0, row_bytes, W);
-    oloads.issue(to + Tl::BYTES, wave, obase + (int64_t)q0 * out_bytes + col, span.len - q0, out_bytes, W);
-    if (threadIdx.x < 2 * Tl::OTHER) {
+    qloads.issue(to, filler, base + (int64_t)q0 * row_bytes + col, span.len - q0, row_bytes, W);
+    oloads.issue(to + Tl::BYTES, filler, obase + (int64_t)q0 * out_bytes + col, span.len - q0, out_bytes, W);
+    if (id < STATS) {
       // rows past the sequence: exp(score - inf) is a probability of zero
-      const bool is_lse = threadIdx.x < Tl::OTHER;
-      const int q = q0 + threadIdx.x % Tl::OTHER;
-      const float* from = (is_lse ? a.lse : a.delta) + (int64_t)head * a.tokens + span.begin;
-      const float x = from[min(q, span.len - 1)];
+      const bool is_lse = id < Tl::OTHER;
+      const int q = q0 + id % Tl::OTHER;
+      const float x = ((is_lse ? a.lse : a.delta) + (int64_t)head * a.tokens + span.begin)[min(q, span.len - 1)];
       stat = is_lse ? (q < span.len ? x * LOG2E : INFINITY) : (q < span.len ? x : 0.f);
     }
-    q0 += Tl::OTHER;
-    if (q0 >= span.len) {
-      q0 = span.first;
-      ++head;
-    }
-  };
-  auto put = [&](int i) {
-    if (threadIdx.x < 2 * Tl::OTHER) stats[i & 1][threadIdx.x / Tl::OTHER][threadIdx.x % Tl::OTHER] = stat;
   };
   v16f_t dk[Tl::OB], dv[Tl::OB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) dk[ob] = dv[ob] = zero16();
-  issue(0);
-  int t0 = span.first;  // first query of the current tile
-  for (int i = 0; i < tiles; ++i) {
-    put(i);
-    tile_barrier();
-    if (i + 1 < tiles) issue(i + 1);
-    const char* Qs = smem + (i & 1) * 2 * Tl::BYTES;
+  const int from = SPLIT ? wave : 0;
+  if (from < tiles) issue(from, 0);
+  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
+    float(*const st)[Tl::OTHER] = stats[SPLIT ? wave : 0][stage];
+    if (id < STATS) st[id / Tl::OTHER][id % Tl::OTHER] = stat;
+    tile_wait<SPLIT>();
+    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
+    const char* Qs = tiles_at + stage * 2 * Tl::BYTES;
+    const int t0 = span.first + i % per_head * Tl::OTHER;
 #pragma unroll 1
     for (int b = 0; b < Tl::NB; ++b) {
       const int b0 = t0 + 32 * b;
@@ -433,13 +507,13 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
       v16f_t s = zero16(), dp = zero16();
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<T, DW>(Qs, 32 * b, ks, l31, hi), kf[ks], s);
-        dp = step_product<T>(rows_frag<T, DW>(Qs + Tl::BYTES, 32 * b, ks, l31, hi), vf[ks], dp);
+        s = step_product<T>(rows_frag<Tl>(Qs, 32 * b, ks, l31, hi), kf[ks], s);
+        dp = step_product<T>(rows_frag<Tl>(Qs + Tl::BYTES, 32 * b, ks, l31, hi), vf[ks], dp);
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const float4 lse = *reinterpret_cast<const float4*>(&stats[i & 1][0][32 * b + 8 * g + 4 * hi]);
-        const float4 delta = *reinterpret_cast<const float4*>(&stats[i & 1][1][32 * b + 8 * g + 4 * hi]);
+        const float4 lse = *reinterpret_cast<const float4*>(&st[0][32 * b + 8 * g + 4 * hi]);
+        const float4 delta = *reinterpret_cast<const float4*>(&st[1][32 * b + 8 * g + 4 * hi]);
         const float l[4] = {lse.x, lse.y, lse.z, lse.w}, d[4] = {delta.x, delta.y, delta.z, delta.w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -452,22 +526,36 @@ template <typename T, int DW> __global__ __launch_bounds__(256, sizeof(T) == 2 |
         for (int v = 0; v < 16; ++v)
           if (b0 + 8 * (v >> 2) + 4 * hi + (v & 3) < key) s[v] = dp[v] = 0.f;
       }
-      across_product<T, DW>(Qs + Tl::BYTES, 32 * b, s, dv, lane);
-      across_product<T, DW>(Qs, 32 * b, dp, dk, lane);
+      across_product<T, Tl>(Qs + Tl::BYTES, 32 * b, s, dv, lane);
+      across_product<T, Tl>(Qs, 32 * b, dp, dk, lane);
     }
-    t0 += Tl::OTHER;
-    if (t0 >= span.len) t0 = span.first;
+    if (Tl::STAGES == 1 && i + NEXT < tiles) {
+      tile_wait<SPLIT>();
+      issue(i + NEXT, 0);
+    }
   }
-  if (key >= span.len) return;
-  if (shares > 1) {
-    float* row = a.parts + (((int64_t)share * 2 * a.tokens + span.begin + key) * a.kv_heads + kv) * W;
-    store_own<float, DW>(row, dk, a.scale, hi, W);
-    store_own<float, DW>(row + (int64_t)a.tokens * a.kv_heads * W, dv, 1.f, hi, W);
-    return;
-  }
-  T* row = static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W;
-  store_own<T, DW>(row, dk, a.scale, hi, W);
-  store_own<T, DW>(row + a.kv_heads * W, dv, 1.f, hi, W);
+  // to dqkv, or to the share's sums
+  auto write = [&](auto* row, int64_t v_from_k) {
+    using R = std::remove_reference_t<decltype(*row)>;
+    if constexpr (SPLIT) {
+      float* joined = reinterpret_cast<float*>(smem);
+      __syncthreads();
+      put_share(joined + wave * DW * 32, dk, 1.f, l31, hi);
+      put_share(joined + (4 + wave) * DW * 32, dv, 1.f, l31, hi);
+      __syncthreads();
+      if (key >= span.len) return;
+      join_shares<R, DW>(row, joined, a.scale, wave, l31, hi, W);
+      join_shares<R, DW>(row + v_from_k, joined + 4 * DW * 32, 1.f, wave, l31, hi, W);
+    } else {
+      if (key >= span.len) return;
+      store_own<R, DW>(row, dk, a.scale, hi, W);
+      store_own<R, DW>(row + v_from_k, dv, 1.f, hi, W);
+    }
+  };
+  if (shares > 1)
+    write(a.parts + (((int64_t)share * 2 * a.tokens + span.begin + key) * a.kv_heads + kv) * W, (int64_t)a.tokens * a.kv_heads * W);
+  else
+    write(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W, (int64_t)a.kv_heads * W);
 }
 
 // Sums of the shares: [share][dk, dv][tokens][kv_heads][width] -> the rows of dqkv that belong to a sequence, eight columns a thread.
@@ -492,44 +580,66 @@ template <typename T> __global__ __launch_bounds__(256) void packed_bwd_fold_ker
   for (int e = 0; e < 8 / Elem<T>::VEC; ++e) reinterpret_cast<uint4*>(out)[e] = c[e].v;
 }
 
-#define CDP_WIDTHS(CALL)                                 \
-  do {                                                   \
-    if (a.width <= 32) { constexpr int DW = 32; CALL; }  \
+#define CDP_WIDTHS(CALL)                                     \
+  do {                                                       \
+    if (a.width <= 32) { constexpr int DW = 32; CALL; }      \
     else if (a.width <= 64) { constexpr int DW = 64; CALL; } \
     else if (a.width <= 96) { constexpr int DW = 96; CALL; } \
-    else { constexpr int DW = 128; CALL; }               \
+    else { constexpr int DW = 128; CALL; }                   \
   } while (0)
 
-int tiles_of(const PackedAttention& a) { return a.tokens / OWN + a.sequences; }
+int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int64_t)a.tokens / own + a.sequences) * heads; }
 
+// Whether the wavefronts of a workgroup share 32 rows' other side (SPLIT) instead of having 32 rows each: a quarter of the way through the longest sequence
+// for the few workgroups that there are, against filling LDS four times as often.  Worth it while the workgroups of 128 rows do not fill the chip; to
+// what count grows with the split workgroups that a CU's LDS holds.  us, 128 rows / split, one sequence or more as said:
+//   bf16 forward, width 32: 72 workgroups 14.4 / 8.2, 384 10.9 / 8.9, 528 46.1 / 46.7; 64: 72 17.5 / 9.8, 272 31.5 / 25.8, 384 13.3 / 13.3, 528
+//   61.6 / 72.4; 128: 72 24.3 / 14.0, 144 24.6 / 19.3, 192 34.1 / 34.6, 528 95.8 / 163.2 (dq crosses at the same counts);
+//   dk and dv, 64: 272 98 / 79, 384 37 / 36, 528 207 / 212; 128: 272 191 / 161, 384 77 / 76, 528 420 / 477;
+//   fp32 forward, 32: 528 218 / 170, 1056 341 / 330; 128: 384 111 / 72, 640 259 / 211, 1056 1202 / 1364; dq, 128: 384 -26, 528 +98; dk and dv -31, +222.
+template <typename T> bool split_wanted(const PackedAttention& a, bool kv) {
+  const int resident = sizeof(T) == 2 ? (a.width <= 32 ? 4 : a.width <= 64 ? 2 : 1) : (a.width <= 32 ? 2 : 1);
+  const int most = sizeof(T) == 4 ? 400 * resident : kv ? 256 + 64 * resident : 48 + 128 * resident;
+  return a.tokens > 64 && workgroups(a, 128, a.heads) <= most;  // (one tile of 64 rows has nothing to share: one token, backward, 9.1 / 10.9)
+}
 // Workgroups that share a key tile's query heads: as few as make 2048 workgroups, four rounds of two per CU (a causal launch's workgroups differ in
 // length by as much as their tiles are many, and the longest, which start first, have to be short against the whole).
-int shares_of(const PackedAttention& a) {
+int shares_of(const PackedAttention& a, int own) {
   const int group = a.heads / a.kv_heads;
-  const int64_t have = (int64_t)tiles_of(a) * a.kv_heads;
+  const int64_t have = workgroups(a, own, a.kv_heads);
   int shares = 1;
   for (int n = 2; n <= group && have * shares < 2048; ++n)
     if (group % n == 0 && n <= a.max_parts) shares = n;
   return shares;
 }
 
-template <typename T> hipError_t forward(const PackedAttention& a, hipStream_t stream) {
-  const dim3 grid((unsigned)tiles_of(a) * a.heads);
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_fwd_kernel<T, DW>), grid, dim3(256), 0, stream, a));
+template <typename T, bool SPLIT> hipError_t forward(const PackedAttention& a, hipStream_t stream) {
+  const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.heads));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_fwd_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a));
   return hipGetLastError();
 }
-template <typename T> hipError_t backward(const PackedAttention& a, hipStream_t stream) {
-  const dim3 qgrid((unsigned)tiles_of(a) * a.heads);
-  const unsigned kgrid = (unsigned)tiles_of(a) * a.kv_heads;
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_q_kernel<T, DW>), qgrid, dim3(256), 0, stream, a));
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int shares = shares_of(a);
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, DW>), dim3(kgrid * shares), dim3(256), 0, stream, a, shares));
-  if ((e = hipGetLastError()) != hipSuccess || shares == 1) return e;
+template <typename T, bool SPLIT> hipError_t backward_q(const PackedAttention& a, hipStream_t stream) {
+  const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.heads));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_q_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a));
+  return hipGetLastError();
+}
+template <typename T, bool SPLIT> hipError_t backward_kv(const PackedAttention& a, hipStream_t stream) {
+  const int shares = shares_of(a, SPLIT ? 32 : 128);
+  const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.kv_heads) * shares);
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a, shares));
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || shares == 1) return e;
   const int64_t n = (int64_t)a.tokens * a.kv_heads * a.width / 8;
   hipLaunchKernelGGL((packed_bwd_fold_kernel<T>), dim3((unsigned)((n + 255) / 256), 2), dim3(256), 0, stream, a, shares);
   return hipGetLastError();
+}
+template <typename T> hipError_t backward(const PackedAttention& a, hipStream_t stream) {
+  const hipError_t e = split_wanted<T>(a, false) ? backward_q<T, true>(a, stream) : backward_q<T, false>(a, stream);
+  if (e != hipSuccess) return e;
+  return split_wanted<T>(a, true) ? backward_kv<T, true>(a, stream) : backward_kv<T, false>(a, stream);
+}
+template <typename T> hipError_t forward(const PackedAttention& a, hipStream_t stream) {
+  return split_wanted<T>(a, false) ? forward<T, true>(a, stream) : forward<T, false>(a, stream);
 }
 
 }  // namespace
