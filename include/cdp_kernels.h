@@ -93,11 +93,12 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
 
 /* ---- token models on packed batches ----------------------------------------------------------------------------
  * Rows are tokens.  Tensors are row-major and packed; nothing but what is said to be written is touched.  Outputs must not alias
- * inputs except where it is said.  Sizes of zero are CDP_EINVAL like negative ones.  The device of the pointers and of `stream` has to be
+ * inputs except where it is said.  Sizes of zero are CDP_EINVAL like negative ones, and so
+ * are scales that are not finite.  The device of the pointers and of `stream` has to be
  * the current one.  Every call may be captured into a graph; calls that overlap in time need workspaces of their own.  The same inputs give
  * the same bits.
  *
- * Embedding: rows of table[vocab][C] by ids[rows].  A token whose id is outside [0, vocab) (padding) has a row of zeros and no gradient.
+ * Embedding: rows of table[vocab][C] (C <= 2^24) by ids[rows].  A token whose id is outside [0, vocab) (padding) has a row of zeros and no gradient.
  *   backward 0: out[rows][C] (elem type) = scale * table[ids]   (dout, workspace unused)
  *   backward 1: out = dtable[vocab][C] (fp32) = scale * sum over the tokens of a row of dout[rows][C] (table unused), zero for
  *               rows without a token; the tokens of a row are summed in a fixed order

@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstring>
 
 #include "../../include/cdp.h"
@@ -195,7 +196,7 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
 
 int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* ids, const void* dout, void* out, float scale,
                     void* workspace, size_t workspace_bytes, int rows, int vocab, int C, void* stream) {
-  if (!ids || !out || rows <= 0 || vocab <= 0 || C <= 0 || backward < 0 || backward > 2 || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!ids || !out || rows <= 0 || vocab <= 0 || C <= 0 || C > (1 << 24) || !std::isfinite(scale) || backward < 0 || backward > 2 || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
   const int eb = dtype == DT_BF16 ? 2 : 4;
   if (!aligned_to(ids, 4) || !aligned_to(out, backward ? 4 : eb)) return CDP_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
@@ -212,7 +213,7 @@ int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* i
 
 int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gate, const float* gamma_post, const float* gamma_pre,
                         void* r, void* y, float scale, float eps, int rows, int C, void* stream) {
-  if (!x || (!r && !y) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!x || (!r && !y) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || !std::isfinite(scale) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
   if (!y != !gamma_pre || (!h && (gate || gamma_post))) return CDP_EINVAL;
   const int eb = dtype == DT_BF16 ? 2 : 4;
   if (!aligned_to(x, eb) || !aligned_to(h, eb) || !aligned_to(gate, eb) || !aligned_to(r, eb) || !aligned_to(y, eb) ||
@@ -229,7 +230,7 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const
                                  const float* gamma_pre, const void* r, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
                                  float* dgamma_post, float* dgamma_pre, float scale, float eps, void* workspace, size_t workspace_bytes,
                                  int rows, int C, void* stream) {
-  if (!dx || (!dr && !dy) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
+  if (!dx || (!dr && !dy) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || !std::isfinite(scale) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
   if (!dy != !gamma_pre || !dgamma_pre != !gamma_pre || !r != !gamma_pre) return CDP_EINVAL;
   if (!h != !dh || !gate != !dgate || !gamma_post != !dgamma_post || (!h && (gate || gamma_post))) return CDP_EINVAL;
   const int eb = dtype == DT_BF16 ? 2 : 4;
@@ -253,7 +254,7 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
                            void* dqkv, void* workspace, size_t workspace_bytes, int tokens, int sequences, int heads, int kv_heads,
                            int width, float scale, void* stream) {
   if (!qkv || !offsets || !out || !lse || tokens <= 0 || sequences <= 0 || heads <= 0 || kv_heads <= 0 || heads % kv_heads || width <= 0 ||
-      width % 8 || width > 128 || (dtype != DT_F32 && dtype != DT_BF16))
+      width % 8 || width > 128 || !std::isfinite(scale) || (dtype != DT_F32 && dtype != DT_BF16))
     return CDP_EINVAL;
   // a tile of rows within 32-bit offsets of its first; tiles of 32 rows at least, and one more for every sequence, within what a launch can number
   if (heads > 4096 || (int64_t)heads + 2ll * kv_heads > 4096 || ((int64_t)tokens / 32 + sequences + 1) * heads > INT_MAX / 2) return CDP_EINVAL;

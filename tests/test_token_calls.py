@@ -21,20 +21,20 @@ ONE = {n: np.array([v], dtype=np.int64) for n, v in (("at", P), ("odd", P + 2), 
 CLIP = dict(dtype=0, tensors=1, grads=ONE["at"].ctypes.data, outs=ONE["at"].ctypes.data, counts=ONE["count"].ctypes.data, max_norm=1.0, norm=P, ws=P, ws_bytes=65536)
 
 REFUSED = [("cdp_k_embedding", EMBED, w) for w in (
-    dict(dtype=2), dict(dtype=-1), dict(backward=3), dict(backward=-1), dict(rows=0), dict(rows=-1), dict(vocab=0), dict(C=0), dict(table=0), dict(ids=0), dict(out=0),
+    dict(dtype=2), dict(dtype=-1), dict(backward=3), dict(backward=-1), dict(rows=0), dict(rows=-1), dict(vocab=0), dict(C=0), dict(C=(1 << 24) + 1), dict(scale=float("inf")), dict(scale=float("nan")), dict(table=0), dict(ids=0), dict(out=0),
     dict(table=P + 2), dict(out=P + 1), dict(ids=P + 2), dict(dtype=1, out=P + 1))]
 REFUSED += [("cdp_k_embedding", EMBED_B, w) for w in (
     dict(dout=0), dict(ws=0), dict(ws_bytes=16 * 8 + 8 * 8 + 511), dict(backward=2, ws_bytes=8), dict(ws=P + 8), dict(dout=P + 2), dict(dtype=1, out=P + 2))]
 REFUSED += [("cdp_k_residual_norm", NORM, w) for w in (
     dict(dtype=2), dict(x=0), dict(r=0, y=0, pre=0), dict(y=0), dict(pre=0), dict(h=0), dict(h=0, gate=0), dict(h=0, post=0), dict(rows=0), dict(C=0), dict(C=16385),
-    dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(x=P + 2), dict(post=P + 1), dict(dtype=1, gate=P + 1))]
+    dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(scale=float("nan")), dict(x=P + 2), dict(post=P + 1), dict(dtype=1, gate=P + 1))]
 REFUSED += [("cdp_k_residual_norm_backward", NORM_B, w) for w in (
     dict(dtype=2), dict(dx=0), dict(dr=0, dy=0, pre=0, dpre=0, r=0), dict(dy=0), dict(pre=0), dict(dpre=0), dict(r=0), dict(h=0), dict(dh=0), dict(dgate=0), dict(gate=0),
-    dict(dpost=0), dict(post=0), dict(h=0, dh=0, post=0, dpost=0), dict(rows=0), dict(C=16385), dict(eps=0.0), dict(ws=0), dict(ws=P + 4), dict(ws_bytes=8 * 8 * 4 + 255),
+    dict(dpost=0), dict(post=0), dict(h=0, dh=0, post=0, dpost=0), dict(rows=0), dict(C=16385), dict(eps=0.0), dict(scale=float("inf")), dict(ws=0), dict(ws=P + 4), dict(ws_bytes=8 * 8 * 4 + 255),
     dict(dh=P + 2), dict(dpre=P + 2))]
 REFUSED += [("cdp_k_attention_packed", ATT, w) for w in (
     dict(dtype=2), dict(qkv=0), dict(offsets=0), dict(out=0), dict(lse=0), dict(tokens=0), dict(sequences=0), dict(heads=0), dict(kv_heads=0), dict(heads=5), dict(kv_heads=-2),
-    dict(width=0), dict(width=12), dict(width=136), dict(width=-8), dict(qkv=P + 8), dict(out=P + 4), dict(lse=P + 2), dict(offsets=P + 1), dict(heads=131072, kv_heads=1),
+    dict(width=0), dict(width=12), dict(width=136), dict(width=-8), dict(scale=float("nan")), dict(qkv=P + 8), dict(out=P + 4), dict(lse=P + 2), dict(offsets=P + 1), dict(heads=4095, kv_heads=1), dict(heads=2048, kv_heads=2048),
     dict(tokens=2 ** 31 - 1, heads=32))]
 REFUSED += [("cdp_k_attention_packed", ATT_B, w) for w in (
     dict(dout=0), dict(dqkv=0), dict(ws=0), dict(ws_bytes=4 * 4 * 8 + 511), dict(ws=P + 8), dict(dout=P + 8), dict(dqkv=P + 8))]
