@@ -5,9 +5,9 @@
 // Backward: dtable[v] = scale * sum of the rows of dout whose token is v, in fp32 and in a fixed order, without atomics.  The least it has to do is to read dout
 // and write the table; what makes it more than a copy is that a few words are a large part of a text, so that a row of the table is the sum
 // of anything from none to thousands of rows.  The tokens are sorted by word (stably: a word's tokens stay in order):
-//   1. runs of 2048 in LDS; in the same launch, under the sort, all other workgroups write the zeros of the table;
+//   1. runs of 2048 in registers and LDS; in the same launch, under the sort, all other workgroups write the zeros of the table (half of them under 2.);
 //   2. sixteen runs to one, repeated: a token's place is the sum of its ranks in the sixteen, each a binary search;
-//   3. a wavefront per 32 sorted tokens and 64 pieces of their rows: words that begin and end among them are finished there; of one
+//   3. a workgroup per 32 sorted tokens and 512 columns of their rows (fp32: 256): words that begin and end among them are finished there; of one
 //      that goes on, the sums before the first and after the last border go to the workspace;
 //   4. those sums, a workgroup per word that crosses a border.
 // Up to 256 tokens are looked for by comparison instead: every row of the table is matched against all ids, which are in registers, in one launch.
@@ -24,56 +24,46 @@ constexpr int RUN = 2048, WAYS = 16, CHUNK = 32, FEW = 256;
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-// What a lane of a wavefront holds of a row: piece `p` of 64 pieces of V neighbouring columns, or (V = 1, rows that are not whole 16-byte
-// pieces) eight columns 64 apart.
+// What a lane of a wavefront holds of a row, columns p * SPAN ..: K groups of V neighbouring columns, 64 V apart (V = 4: what makes 16 bytes of the table
+// per lane, so that a wavefront writes whole lines; V = 1 for rows that are not whole groups).
 template <typename T, int V> struct Piece {
-  static constexpr int K = V == 1 ? 8 : 1, N = V * K, SPAN = 64 * N;
-  __device__ static __forceinline__ int col(int p, int k, int lane) { return p * SPAN + (V == 1 ? 64 * k + lane : lane * V); }
+  static constexpr int K = V == 1 ? 8 : 4 / (int)sizeof(T), N = V * K, SPAN = 64 * N;
+  __device__ static __forceinline__ int col(int p, int k, int lane) { return p * SPAN + (64 * k + lane) * V; }
   // the bits: a conversion is a use, which waits for the load
-  struct Bits { uint4 v; uint32_t e[K]; };
+  typedef typename std::conditional<V == 1, T, typename std::conditional<sizeof(T) == 2, uint2, uint4>::type>::type Group;
+  struct Bits { Group g[K]; };
   __device__ static __forceinline__ void load(Bits& b, const T* row, int p, int lane, int C) {
-    if constexpr (V > 1) b.v = *reinterpret_cast<const uint4*>(row + min(col(p, 0, lane), C - V));
-    else
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const T x = row[min(col(p, k, lane), C - 1)];
-        if constexpr (sizeof(T) == 2) b.e[k] = x;
-        else b.e[k] = __float_as_uint(x);
-      }
+    for (int k = 0; k < K; ++k) b.g[k] = *reinterpret_cast<const Group*>(row + min(col(p, k, lane), C - V));
   }
-  __device__ static __forceinline__ void values(const Bits& b, float (&x)[N]) {
-    if constexpr (V > 1) {
-      Chunk16<T> c;
-      c.v = b.v;
+  __device__ static __forceinline__ void add(float (&sum)[N], const Bits& b) {
 #pragma unroll
-      for (int e = 0; e < V; ++e) x[e] = Elem<T>::to_f32(c.e[e]);
-    } else {
+    for (int k = 0; k < K; ++k) {
+      union { Group g; T e[V]; } c;
+      c.g = b.g[k];
 #pragma unroll
-      for (int k = 0; k < K; ++k) x[k] = __uint_as_float(sizeof(T) == 2 ? b.e[k] << 16 : b.e[k]);
+      for (int e = 0; e < V; ++e) sum[V * k + e] += Elem<T>::to_f32(c.e[e]);
     }
   }
   // fp32 rows of the table and of the workspace
+  typedef typename std::conditional<V == 1, float, float4>::type Group32;
   __device__ static __forceinline__ void load32(float (&x)[N], const float* row, int p, int lane, int C) {
-    if constexpr (V > 1) {
-      const float* r = row + min(col(p, 0, lane), C - V);
 #pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const float4 f = *reinterpret_cast<const float4*>(r + e);
-        x[e] = f.x; x[e + 1] = f.y; x[e + 2] = f.z; x[e + 3] = f.w;
-      }
-    } else {
+    for (int k = 0; k < K; ++k) {
+      union { Group32 g; float e[V]; } c;
+      c.g = *reinterpret_cast<const Group32*>(row + min(col(p, k, lane), C - V));
 #pragma unroll
-      for (int k = 0; k < K; ++k) x[k] = row[min(col(p, k, lane), C - 1)];
+      for (int e = 0; e < V; ++e) x[V * k + e] = c.e[e];
     }
   }
   __device__ static __forceinline__ void store32(const float (&x)[N], float* row, int p, int lane, int C) {
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (col(p, k, lane) < C) {
-        if constexpr (V > 1) {
+        union { Group32 g; float e[V]; } c;
 #pragma unroll
-          for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(row + col(p, 0, lane) + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
-        } else row[col(p, k, lane)] = x[k];
+        for (int e = 0; e < V; ++e) c.e[e] = x[V * k + e];
+        *reinterpret_cast<Group32*>(row + col(p, k, lane)) = c.g;
       }
   }
 };
@@ -151,135 +141,180 @@ __global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const int32_t* i
 #pragma unroll
       for (int j = 0; j < 8; ++j) P::load(b[j], dout + (int64_t)list[wave][min(j0 + j, n - 1)] * C, p, lane, C);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float x[P::N];
-        P::values(b[j], x);
-        if (j0 + j < n)
-#pragma unroll
-          for (int e = 0; e < P::N; ++e) sum[e] += x[e];
-      }
+      for (int j = 0; j < 8; ++j)
+        if (j0 + j < n) P::add(sum, b[j]);
     }
     finish_row<T, V>(sum, dtable + v * C, scale, accumulate, p, lane, C);
   }
 }
 
 // ---- backward, sorted ---------------------------------------------------------------------------------------------------
-// Workgroups 0 .. runs - 1 sort a run each (ids that are no word come last, as ~0); the others clear the table, 64 KB each.
-__global__ __launch_bounds__(1024) void embedding_sort_kernel(const int32_t* ids, uint32_t* word, int* token, float* dtable, int64_t elements, int rows, int vocab, int runs) {
+// Zeros to the part of the table that is `THREADS` * 64 bytes of workgroup `block`'s.
+constexpr int CLEAR = 16384;  // elements of a workgroup of 1024; of one of 256 a quarter
+template <int THREADS> __device__ __forceinline__ void clear_table(float* table, int64_t elements, int64_t block) {
   const int t = threadIdx.x;
-  if ((int)blockIdx.x >= runs) {
-    const int64_t head = min((int64_t)((16 - reinterpret_cast<uintptr_t>(dtable) % 16) % 16 / 4), elements), pieces = (elements - head) / 4;
-    float4* const to = reinterpret_cast<float4*>(dtable + head);
-    const int64_t e = (int64_t)(blockIdx.x - runs) * 4096 + t;
+  const int64_t head = min((int64_t)((16 - reinterpret_cast<uintptr_t>(table) % 16) % 16 / 4), elements), pieces = (elements - head) / 4;
+  float4* const to = reinterpret_cast<float4*>(table + head);
+  const int64_t e = block * (THREADS * 4) + t;
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (e + 1024 * u < pieces) to[e + 1024 * u] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if ((int)blockIdx.x == runs) {
-      if (t < head) dtable[t] = 0.f;
-      const int64_t tail = head + 4 * pieces + t;
-      if (tail < elements) dtable[tail] = 0.f;
-    }
-    return;
+  for (int u = 0; u < 4; ++u)
+    if (e + THREADS * u < pieces) to[e + THREADS * u] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (block == 0) {
+    if (t < head) table[t] = 0.f;
+    const int64_t tail = head + 4 * pieces + t;
+    if (tail < elements) table[tail] = 0.f;
   }
-  __shared__ uint64_t key[RUN];
+}
+// Workgroups 0 .. runs - 1 sort a run each (ids that are no word come last); the others clear the table.  A key is the word and the place in the run, two
+// keys a thread; keys 2 to 64 apart are exchanged between lanes, farther ones through LDS (every step through LDS with a barrier: 14 us instead of 6).
+template <typename Key>
+__global__ __launch_bounds__(1024) void embedding_sort_kernel(const int32_t* ids, uint32_t* word, int* token, float* dtable, int64_t elements, int rows, int vocab, int runs) {
+  if ((int)blockIdx.x >= runs) return clear_table<1024>(dtable, elements, blockIdx.x - runs);
+  constexpr int BITS = 11;
+  static_assert(RUN == 1 << BITS, "a place in the run");
+  __shared__ Key keys[RUN];
+  const int i = 2 * threadIdx.x;
   const uint32_t base = blockIdx.x * RUN;
+  Key k[2];
 #pragma unroll
-  for (int i = t; i < RUN; i += 1024) {
-    const uint32_t at = base + i;
-    const uint32_t id = at < (uint32_t)rows ? (uint32_t)ids[at] : ~0u;
-    key[i] = ((uint64_t)(id < (uint32_t)vocab ? id : ~0u) << 32) | at;
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t at = base + i + u, id = at < (uint32_t)rows ? (uint32_t)ids[at] : ~0u;
+    k[u] = ((Key)min(id, (uint32_t)vocab) << BITS) | (i + u);
   }
-  for (int size = 2; size <= RUN; size <<= 1)
-    for (int stride = size >> 1; stride > 0; stride >>= 1) {
-      __syncthreads();
-      const int i = 2 * t - (t & (stride - 1)), j = i + stride;
-      const uint64_t x = key[i], y = key[j];
-      if ((x > y) == ((i & size) == 0)) {
-        key[i] = y;
-        key[j] = x;
+  auto keep = [](Key mine, Key other, bool low) { return low == (mine < other) ? mine : other; };
+#pragma unroll
+  for (int size = 2; size <= RUN; size <<= 1) {
+    const bool up = (i & size) == 0;
+#pragma unroll
+    for (int stride = size >> 1; stride > 1; stride >>= 1) {
+      const bool low = ((i & stride) == 0) == up;
+      if (stride <= 64) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          Key other;
+          if constexpr (sizeof(Key) == 4) other = __shfl_xor(k[u], stride >> 1, 64);
+          else other = (Key)(unsigned long long)__shfl_xor((unsigned long long)k[u], stride >> 1, 64);
+          k[u] = keep(k[u], other, low);
+        }
+      } else {
+        __syncthreads();
+        keys[i] = k[0];
+        keys[i + 1] = k[1];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 2; ++u) k[u] = keep(k[u], keys[(i ^ stride) + u], low);
       }
     }
-  __syncthreads();
+    const Key x = k[0], y = k[1];
+    k[0] = keep(x, y, up);
+    k[1] = keep(y, x, !up);
+  }
 #pragma unroll
-  for (int i = t; i < RUN; i += 1024)
-    if (base + i < (uint32_t)rows) {
-      word[base + i] = (uint32_t)(key[i] >> 32);
-      token[base + i] = (int)(uint32_t)key[i];
-    }
-}
-// Sorted runs of `run` (a power of two) to runs of WAYS times that.  Equal words: an earlier run's come first.
-__global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* word, const int* token, uint32_t* word_out, int* token_out, int rows, int run) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= rows) return;
-  const int64_t own = e / run, group = own / WAYS * WAYS;
-  const uint32_t w = word[e];
-  int below[WAYS] = {};
-  for (int s = run; s > 0; s >>= 1) {
-    uint32_t x[WAYS];
-#pragma unroll
-    for (int q = 0; q < WAYS; ++q) x[q] = word[min((group + q) * run + below[q] + s - 1, (int64_t)rows - 1)];
-#pragma unroll
-    for (int q = 0; q < WAYS; ++q) {
-      const bool inside = below[q] + s <= run && (group + q) * run + below[q] + s <= rows;
-      if (inside && (group + q < own ? x[q] <= w : x[q] < w)) below[q] += s;
+  for (int u = 0; u < 2; ++u) {
+    const uint32_t w = (uint32_t)(k[u] >> BITS);
+    if (base + i + u < (uint32_t)rows) {
+      word[base + i + u] = w < (uint32_t)vocab ? w : ~0u;
+      token[base + i + u] = (int)(base + (uint32_t)(k[u] & (RUN - 1)));
     }
   }
-  int64_t to = group * run + (e - own * run);
-#pragma unroll
-  for (int q = 0; q < WAYS; ++q)
-    if (group + q != own) to += below[q];
-  word_out[to] = w;
-  token_out[to] = token[e];
 }
-// part[chunk][0]: of a word that began before the chunk; [1]: of one that began in it and goes on.
+// Sorted runs of `run` (a power of two) to runs of WAYS times that: sixteen lanes search an element's place in sixteen runs, which is equal words of
+// earlier runs and smaller ones of later runs before it.  Workgroups past `merging` clear the rest of the table.
+__global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* word, const int* token, uint32_t* word_out, int* token_out, int rows, int run, float* dtable,
+                                                              int64_t elements, int64_t merging, int64_t cleared) {
+  if (blockIdx.x >= merging) return clear_table<256>(dtable, elements, blockIdx.x - merging + cleared);
+  const int64_t e = (int64_t)blockIdx.x * (256 / WAYS) + threadIdx.x / WAYS;
+  if (e >= rows) return;
+  const int q = threadIdx.x % WAYS;
+  const int64_t own = e / run, other = own / WAYS * WAYS + q, start = other * run;
+  const uint32_t w = word[e];
+  const int len = (int)max(min((int64_t)run, rows - start), (int64_t)0);
+  int below = 0;
+  if (other == own) below = (int)(e - start);
+  else
+    for (int s = run; s > 0; s >>= 1) {
+      if (below + s > len) continue;
+      const uint32_t x = word[start + below + s - 1];
+      if (x < w || (x == w && other < own)) below += s;
+    }
+#pragma unroll
+  for (int s = 1; s < WAYS; s <<= 1) below += __shfl_xor(below, s, 64);
+  if (q) return;
+  word_out[start + below] = w;  // (start of the group's first run)
+  token_out[start + below] = token[e];
+}
+// A workgroup per 32 sorted tokens and piece of their rows, eight tokens a wavefront, all of them requested at once.  What a word has in a wavefront goes to the
+// table where it begins and ends there, else to LDS: heads (it began before) and tails (it began here and goes on), which the wavefront where it
+// began adds up.  part[chunk][0]: of a word that began before the chunk; [1]: of one that began in it and goes on.
 template <typename T, int V>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const uint32_t* word, const int* token, const T* dout, float* dtable, float* part, float scale, int accumulate,
                                                             int rows, int C) {
   using P = Piece<T, V>;
-  const int lane = threadIdx.x & 63, p = blockIdx.y;
-  const int64_t chunk = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), e0 = chunk * CHUNK;
-  if (e0 >= rows) return;
+  constexpr int U = CHUNK / 4;
+  __shared__ float heads[4][P::N][64], tails[4][P::N][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), p = blockIdx.y;
+  const int64_t chunk = blockIdx.x, e0 = chunk * CHUNK;
   const int there = (int)min((int64_t)CHUNK, rows - e0);
   const uint32_t w = lane < there ? word[e0 + lane] : ~0u;
   const int at = lane < there ? token[e0 + lane] : 0;
   const uint32_t before = e0 > 0 ? word[e0 - 1] : ~0u, after = e0 + there < rows ? word[e0 + there] : ~0u;
-  const int n = __popcll(__ballot(w != ~0u));
+  const int n = __popcll(__ballot(w != ~0u)), j0 = wave * U;
   if (n == 0) return;
-  const uint32_t next = __shfl_down(w, 1, 64);
-  const uint64_t ends = __ballot(lane == n - 1 || (lane < n && next != w));
+  typename P::Bits b[U];
+  if (j0 < n)
+#pragma unroll
+    for (int j = 0; j < U; ++j) P::load(b[j], dout + (int64_t)__builtin_amdgcn_readlane(at, min(j0 + j, n - 1)) * C, p, lane, C);
+  uint32_t next = __shfl_down(w, 1, 64), previous = __shfl_up(w, 1, 64);
+  if (lane == there - 1) next = after;
+  if (lane == 0) previous = before;
+  const uint32_t begins = (uint32_t)__ballot(lane < n && previous != w), ends = (uint32_t)__ballot(lane < n && next != w);
   float sum[P::N] = {};
-  bool first = true;
-  for (int j0 = 0; j0 < n; j0 += 8) {
-    typename P::Bits b[8];
+  bool began = (begins >> j0) & 1, going = false;  // this wavefront's last word begins in it and goes on
+  if (j0 < n)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) P::load(b[j], dout + (int64_t)__builtin_amdgcn_readlane(at, min(j0 + j, n - 1)) * C, p, lane, C);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
+    for (int j = 0; j < U; ++j) {
       if (j0 + j >= n) break;
-      float x[P::N];
-      P::values(b[j], x);
+      P::add(sum, b[j]);
+      const bool end = (ends >> (j0 + j)) & 1;
+      if (!end && j < U - 1 && j0 + j < n - 1) continue;
+      going = began && !end;
+      if (began && end) finish_row<T, V>(sum, dtable + (int64_t)__builtin_amdgcn_readlane(w, j0 + j) * C, scale, accumulate, p, lane, C);
+      else {
+        float(*const to)[64] = began ? tails[wave] : heads[wave];
 #pragma unroll
-      for (int e = 0; e < P::N; ++e) sum[e] += x[e];
-      if ((ends >> (j0 + j)) & 1) {
-        const uint32_t here = __builtin_amdgcn_readlane(w, j0 + j);
-        if (first && here == before) P::store32(sum, part + 2 * chunk * C, p, lane, C);
-        else if (j0 + j == there - 1 && here == after) P::store32(sum, part + (2 * chunk + 1) * C, p, lane, C);
-        else finish_row<T, V>(sum, dtable + (int64_t)here * C, scale, accumulate, p, lane, C);
-#pragma unroll
-        for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-        first = false;
+        for (int e = 0; e < P::N; ++e) to[e][lane] = sum[e];
       }
+#pragma unroll
+      for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
+      began = true;
     }
+  __syncthreads();
+  const bool lead = wave == 0 && !(begins & 1);  // the chunk's first word began before it
+#pragma unroll 1
+  for (int k = 0; k < 2; ++k) {  // the word that began before the chunk, the one that began in this wavefront
+    if (k ? !going : !lead) continue;
+    bool open = true;
+#pragma unroll
+    for (int e = 0; e < P::N; ++e) sum[e] = k ? tails[wave][e][lane] : 0.f;
+    for (int u = k ? wave + 1 : 0; open && u * U < n; ++u) {
+#pragma unroll
+      for (int e = 0; e < P::N; ++e) sum[e] += heads[u][e][lane];
+      open = !((ends >> (u * U)) & ((1u << U) - 1));
+    }
+    if (!k) P::store32(sum, part + 2 * chunk * C, p, lane, C);
+    else if (open) P::store32(sum, part + (2 * chunk + 1) * C, p, lane, C);
+    else finish_row<T, V>(sum, dtable + (int64_t)__builtin_amdgcn_readlane(w, j0 + U - 1) * C, scale, accumulate, p, lane, C);
   }
 }
+constexpr int JOIN = 8;  // wavefronts that share a word's chunks
 template <typename T, int V>
-__global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* word, float* dtable, const float* part, float scale, int accumulate, int rows, int C) {
+__global__ __launch_bounds__(64 * JOIN) void embedding_join_kernel(const uint32_t* word, float* dtable, const float* part, float scale, int accumulate, int rows, int C) {
   using P = Piece<T, V>;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, p = blockIdx.y;
   const int64_t chunk = blockIdx.x, e0 = chunk * CHUNK;
   // (the last chunk is not launched: nothing goes on behind it)
-  const uint32_t w = word[e0 + CHUNK - 1];
-  if (w == ~0u || word[e0 + CHUNK] != w || (word[e0] == w && e0 > 0 && word[e0 - 1] == w)) return;
+  const uint32_t w = word[e0 + CHUNK - 1], next = word[e0 + CHUNK], first = word[e0], before = word[max(e0 - 1, (int64_t)0)];
+  if (w == ~0u || next != w || (first == w && e0 > 0 && before == w)) return;
   // tokens of the word behind the chunk: the last of them by a search of 64 ways
   int64_t lo = e0 + CHUNK, n = rows - lo;  // word[lo] is w
   while (n > 1) {
@@ -294,24 +329,27 @@ __global__ __launch_bounds__(256) void embedding_join_kernel(const uint32_t* wor
   else
 #pragma unroll
     for (int e = 0; e < P::N; ++e) sum[e] = 0.f;
-  for (int64_t k0 = chunk + 1 + wave; k0 <= last; k0 += 16) {
-    float x[4][P::N];
+  for (int64_t k0 = chunk + 1 + wave; k0 <= last; k0 += 8 * JOIN) {
+    float x[8][P::N];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) P::load32(x[j], part + 2 * min(k0 + 4 * j, last) * C, p, lane, C);
+    for (int j = 0; j < 8; ++j) P::load32(x[j], part + 2 * min(k0 + JOIN * j, last) * C, p, lane, C);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (k0 + 4 * j <= last)
+    for (int j = 0; j < 8; ++j)
+      if (k0 + JOIN * j <= last)
 #pragma unroll
         for (int e = 0; e < P::N; ++e) sum[e] += x[j][e];
   }
-  __shared__ float shares[3][P::N][64];
-  if (wave)
+  __shared__ float shares[JOIN][P::N][64];
 #pragma unroll
-    for (int e = 0; e < P::N; ++e) shares[wave - 1][e][lane] = sum[e];
+  for (int e = 0; e < P::N; ++e) shares[wave][e][lane] = sum[e];
   __syncthreads();
   if (wave) return;
 #pragma unroll
-  for (int e = 0; e < P::N; ++e) sum[e] = (sum[e] + shares[0][e][lane]) + (shares[1][e][lane] + shares[2][e][lane]);
+  for (int e = 0; e < P::N; ++e) {
+    sum[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < JOIN; ++k) sum[e] += shares[k][e][lane];
+  }
   finish_row<T, V>(sum, dtable + (int64_t)w * C, scale, accumulate, p, lane, C);
 }
 
@@ -327,7 +365,8 @@ template <typename T> hipError_t forward(const T* table, const int32_t* ids, T* 
 template <typename T, int V>
 hipError_t backward(const int32_t* ids, const T* dout, float* dtable, float scale, void* workspace, int accumulate, int rows, int vocab, int C, hipStream_t stream) {
   const unsigned pieces = (C + Piece<T, V>::SPAN - 1) / Piece<T, V>::SPAN;
-  if (rows <= FEW) {
+  // (a large table is cleared faster by itself: 200 tokens, 100000 x 2048 177 us here)
+  if (rows <= FEW && (accumulate || (int64_t)vocab * C <= (8 << 20))) {
     const int per = 8;
     hipLaunchKernelGGL((embedding_bwd_few_kernel<T, V>), dim3((unsigned)((vocab + 4ll * per - 1) / (4 * per)), pieces), dim3(256), 0, stream, ids, dout, dtable, scale,
                        accumulate, rows, vocab, C, per);
@@ -337,26 +376,31 @@ hipError_t backward(const int32_t* ids, const T* dout, float* dtable, float scal
   int* token[2] = {reinterpret_cast<int*>(word[1] + rows), reinterpret_cast<int*>(word[1] + rows) + rows};
   float* part = static_cast<float*>(workspace) + (4ll * rows + 63) / 64 * 64;
   const int runs = (int)((rows + (int64_t)RUN - 1) / RUN);
-  const int64_t elements = (int64_t)vocab * C, clear = accumulate ? 0 : (elements + 16383) / 16384;
-  hipLaunchKernelGGL(embedding_sort_kernel, dim3((unsigned)(runs + clear)), dim3(1024), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
+  // the table is cleared beside the sort and, where there is one, the first merge, half each: neither fills the chip
+  const int64_t elements = (int64_t)vocab * C, clear = accumulate ? 0 : (elements + CLEAR - 1) / CLEAR, beside_sort = runs > 1 ? (clear + 1) / 2 : clear;
+  const dim3 sorting((unsigned)(runs + beside_sort));
+  if (vocab < (1 << 20)) hipLaunchKernelGGL((embedding_sort_kernel<uint32_t>), sorting, dim3(1024), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
+  else hipLaunchKernelGGL((embedding_sort_kernel<uint64_t>), sorting, dim3(1024), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
   hipError_t e = hipGetLastError();
   int at = 0;
   for (int64_t run = RUN; run < rows && e == hipSuccess; run *= WAYS, at ^= 1) {
-    hipLaunchKernelGGL(embedding_merge_kernel, dim3((unsigned)((rows + 255ll) / 256)), dim3(256), 0, stream, word[at], token[at], word[at ^ 1], token[at ^ 1], rows, (int)run);
+    const int64_t merging = ((int64_t)rows * WAYS + 255) / 256, clearing = run == RUN ? 4 * (clear - beside_sort) : 0;
+    hipLaunchKernelGGL(embedding_merge_kernel, dim3((unsigned)(merging + clearing)), dim3(256), 0, stream, word[at], token[at], word[at ^ 1], token[at ^ 1], rows, (int)run, dtable,
+                       elements, merging, 4 * beside_sort);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
   const int64_t chunks = (rows + (int64_t)CHUNK - 1) / CHUNK;
-  hipLaunchKernelGGL((embedding_sum_kernel<T, V>), dim3((unsigned)((chunks + 3) / 4), pieces), dim3(256), 0, stream, word[at], token[at], dout, dtable, part, scale, accumulate,
+  hipLaunchKernelGGL((embedding_sum_kernel<T, V>), dim3((unsigned)chunks, pieces), dim3(256), 0, stream, word[at], token[at], dout, dtable, part, scale, accumulate,
                      rows, C);
   if ((e = hipGetLastError()) != hipSuccess || chunks == 1) return e;
-  hipLaunchKernelGGL((embedding_join_kernel<T, V>), dim3((unsigned)(chunks - 1), pieces), dim3(256), 0, stream, word[at], dtable, part, scale, accumulate, rows, C);
+  hipLaunchKernelGGL((embedding_join_kernel<T, V>), dim3((unsigned)(chunks - 1), pieces), dim3(64 * JOIN), 0, stream, word[at], dtable, part, scale, accumulate, rows, C);
   return hipGetLastError();
 }
 template <typename T>
 hipError_t backward(const int32_t* ids, const T* dout, float* dtable, float scale, void* workspace, int accumulate, int rows, int vocab, int C, hipStream_t stream) {
-  const bool vec = C % Elem<T>::VEC == 0 && aligned16(dout) && aligned16(dtable);
-  return vec ? backward<T, Elem<T>::VEC>(ids, dout, dtable, scale, workspace, accumulate, rows, vocab, C, stream)
+  const bool vec = C % 4 == 0 && reinterpret_cast<uintptr_t>(dout) % (4 * sizeof(T)) == 0 && aligned16(dtable);
+  return vec ? backward<T, 4>(ids, dout, dtable, scale, workspace, accumulate, rows, vocab, C, stream)
              : backward<T, 1>(ids, dout, dtable, scale, workspace, accumulate, rows, vocab, C, stream);
 }
 
