@@ -144,7 +144,8 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
 /* The norm over all elements of `tensors` gradients, and the gradients scaled so that it is at most max_norm:
  *   norm[0] (device fp32) = sqrt(sum of squares), summed in 64 bits
  *   outs[i][0 .. counts[i]) = norm > max_norm ? grads[i] * (max_norm / norm) : grads[i]   (elem type; outs[i] may be grads[i])
- * grads, outs, counts: HOST arrays of device pointers and element counts (0: nothing there), read during the call.  outs NULL: the norm alone.
+ * grads, outs, counts: HOST arrays of device pointers and element counts (0: nothing there; up
+ * to 2^40 in all), read during the call.  outs NULL: the norm alone.
  * A norm that is NaN leaves the gradients as they are; one that is infinite scales by zero.
  * workspace: CDP_CLIP_BYTES, 8-byte aligned; nothing in it has to be cleared. */
 #define CDP_CLIP_BYTES 65536u

@@ -1,67 +1,151 @@
 // The norm over all gradients of a model, and the gradients scaled to at most a given norm.
+//
+// Two passes, bound by memory: every gradient is read for the norm, and read and written for the result.  The tensors are cut into units of 32 KB, which workgroups
+// take in strides: eight 16-byte loads in flight in every thread.  Squares are summed in 64 bits (any fp32 value's square is there, and the
+// order hardly matters), the workgroups' sums go to the workspace, and every workgroup of the second pass adds them up for itself in the same
+// order: no third launch, no atomics.  The second pass goes through the units backwards: what the first read last is still cached.
+// The tensors' addresses travel in the kernel arguments, 128 of them a launch; a wavefront finds the tensor of a unit by comparing all of them at once.
 #include "elem.h"
 #include "kernels.h"
 
 #include <algorithm>
+#include <cstring>
 
 namespace cdp {
 
 namespace {
 
-constexpr int CLIP_GROUPS = 1024, CLIP_TENSORS = 128;
+constexpr int CLIP_TENSORS = 128, CLIP_GROUPS = 2048, UNIT_BYTES = 32768, LOADS = UNIT_BYTES / 16 / 256;
 
 struct ClipTable {
   const void* g[CLIP_TENSORS];
   void* out[CLIP_TENSORS];
   int64_t count[CLIP_TENSORS];
-  int n;
+  int32_t units[CLIP_TENSORS];  // of the tensors before it; past the last tensor all units (2^31 of them are 64 TB)
+  int32_t total;
+};
+static_assert(sizeof(ClipTable) <= 3600, "kernel arguments are 4 KB at most");
+
+template <typename T> struct Unit {
+  static constexpr int V = Elem<T>::VEC, SIZE = UNIT_BYTES / (int)sizeof(T);
+  const T* g;
+  T* out;
+  int n;        // elements, up to SIZE
+  bool whole;   // 16-byte pieces
+  __device__ __forceinline__ Unit(const ClipTable& t, int u, bool scaling) {
+    const int lane = threadIdx.x & 63;
+    const int i = __popcll(__ballot(t.units[lane] <= u)) + __popcll(__ballot(t.units[lane + 64] <= u)) - 1;
+    const int64_t first = (int64_t)(u - t.units[i]) * SIZE;
+    g = static_cast<const T*>(t.g[i]) + first;
+    out = scaling ? static_cast<T*>(t.out[i]) + first : nullptr;
+    n = (int)min((int64_t)SIZE, t.count[i] - first);
+    whole = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+  }
 };
 
-// Sum of squares of a workgroup's elements of all tensors of the table, added to part[workgroup] (the first table's: written).
+__device__ __forceinline__ double group_sum(double s, double* lds) {
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k, 64);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
+  __syncthreads();
+  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+}
+
+// Sum of squares of a workgroup's units, written to part[workgroup], or, past the first table, added to it.
 template <typename T> __global__ __launch_bounds__(256) void grad_norm_kernel(const ClipTable t, double* part, int first) {
-  __shared__ double lds[256];
+  __shared__ double lds[4];
   double s = 0;
-  for (int i = 0; i < t.n; ++i)
-    for (int64_t e = blockIdx.x * 256ll + threadIdx.x; e < t.count[i]; e += CLIP_GROUPS * 256ll) {
-      const double v = ld_f32<T>(static_cast<const T*>(t.g[i]), e);
+  for (int u = blockIdx.x; u < t.total; u += gridDim.x) {
+    const Unit<T> w(t, u, false);
+    const int pieces = w.whole ? w.n / Unit<T>::V : 0;
+    Chunk16<T> c[LOADS];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k)
+      if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min((int)threadIdx.x + 256 * k, pieces - 1)];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k)
+      if ((int)threadIdx.x + 256 * k < pieces)
+#pragma unroll
+        for (int e = 0; e < Unit<T>::V; ++e) {
+          const double v = Elem<T>::to_f32(c[k].e[e]);
+          s += v * v;
+        }
+    for (int e = pieces * Unit<T>::V + threadIdx.x; e < w.n; e += 256) {
+      const double v = Elem<T>::to_f32(w.g[e]);
       s += v * v;
     }
-  lds[threadIdx.x] = s;
-  __syncthreads();
-  for (int n = 128; n > 0; n >>= 1) {
-    if ((int)threadIdx.x < n) lds[threadIdx.x] += lds[threadIdx.x + n];
-    __syncthreads();
   }
-  if (threadIdx.x == 0) part[blockIdx.x] = lds[0] + (first ? 0.0 : part[blockIdx.x]);
+  s = group_sum(s, lds);
+  if (threadIdx.x == 0) part[blockIdx.x] = first ? s : part[blockIdx.x] + s;
 }
-template <typename T> __global__ __launch_bounds__(256) void grad_scale_kernel(const ClipTable t, const double* part, float* norm, float max_norm, int scale) {
+
+template <typename T> __global__ __launch_bounds__(256) void grad_scale_kernel(const ClipTable t, const double* part, int parts, float* norm, float max_norm, int scaling) {
+  __shared__ double lds[4];
   double s = 0;
-  for (int i = 0; i < CLIP_GROUPS; ++i) s += part[i];
-  const double r = sqrt(s);
+#pragma unroll
+  for (int k = 0; k < CLIP_GROUPS / 256; ++k) {
+    const int i = threadIdx.x + 256 * k;
+    const double v = part[min(i, parts - 1)];
+    s += i < parts ? v : 0.0;
+  }
+  const double r = sqrt(group_sum(s, lds));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
-  if (!scale) return;
-  const float c = r > max_norm ? (float)(max_norm / r) : 1.f;
-  for (int i = 0; i < t.n; ++i)
-    for (int64_t e = blockIdx.x * 256ll + threadIdx.x; e < t.count[i]; e += gridDim.x * 256ll)
-      st_f32<T>(static_cast<T*>(t.out[i]), e, c * ld_f32<T>(static_cast<const T*>(t.g[i]), e));
+  if (!scaling) return;
+  const bool over = r > max_norm;  // (not a number: no)
+  const float f = over ? (float)(max_norm / r) : 1.f;
+  for (int v = blockIdx.x; v < t.total; v += gridDim.x) {
+    const Unit<T> w(t, t.total - 1 - v, true);
+    if (!over && w.out == w.g) continue;  // in place, nothing to do
+    const int pieces = w.whole ? w.n / Unit<T>::V : 0;
+    Chunk16<T> c[LOADS];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k)
+      if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min((int)threadIdx.x + 256 * k, pieces - 1)];
+#pragma unroll
+    for (int k = 0; k < LOADS; ++k) {
+      if ((int)threadIdx.x + 256 * k >= pieces) continue;
+      if (over)
+#pragma unroll
+        for (int e = 0; e < Unit<T>::V; ++e) c[k].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k].e[e]));
+      reinterpret_cast<uint4*>(w.out)[threadIdx.x + 256 * k] = c[k].v;
+    }
+    for (int e = pieces * Unit<T>::V + threadIdx.x; e < w.n; e += 256) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
+  }
 }
 
 template <typename T>
 hipError_t clip(int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm, float* norm, double* part, hipStream_t stream) {
-  for (int pass = 0; pass < 2; ++pass)
-    for (int i0 = 0; i0 < tensors; i0 += CLIP_TENSORS) {
-      ClipTable t;
-      t.n = std::min(CLIP_TENSORS, tensors - i0);
-      for (int i = 0; i < t.n; ++i) {
-        t.g[i] = grads[i0 + i];
-        t.out[i] = outs ? outs[i0 + i] : nullptr;
-        t.count[i] = counts[i0 + i];
-      }
-      if (!pass) hipLaunchKernelGGL((grad_norm_kernel<T>), dim3(CLIP_GROUPS), dim3(256), 0, stream, t, part, i0 == 0);
-      else hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(outs ? 2048 : 1), dim3(256), 0, stream, t, part, norm, max_norm, outs != nullptr);
-      const hipError_t e = hipGetLastError();
-      if (e != hipSuccess) return e;
+  auto table = [&](int i0) {
+    ClipTable t;
+    int32_t units = 0;
+    for (int i = 0; i < CLIP_TENSORS; ++i) {
+      const bool there = i0 + i < tensors && counts[i0 + i] > 0;
+      t.g[i] = there ? grads[i0 + i] : nullptr;
+      t.out[i] = there && outs ? outs[i0 + i] : nullptr;
+      t.count[i] = there ? counts[i0 + i] : 0;
+      t.units[i] = units;  // (of tensors with the same one, only the last has units)
+      if (there) units += (int32_t)((t.count[i] + Unit<T>::SIZE - 1) / Unit<T>::SIZE);
     }
+    t.total = units;
+    return t;
+  };
+  int64_t most = 1;
+  for (int i0 = 0; i0 < tensors; i0 += CLIP_TENSORS) {
+    int64_t units = 0;
+    for (int i = i0; i < std::min(tensors - i0, CLIP_TENSORS) + i0; ++i) units += (counts[i] + Unit<T>::SIZE - 1) / Unit<T>::SIZE;
+    most = std::max(most, units);
+  }
+  const int groups = (int)std::min<int64_t>(most, CLIP_GROUPS);
+  for (int i0 = 0; i0 < tensors; i0 += CLIP_TENSORS) {
+    hipLaunchKernelGGL((grad_norm_kernel<T>), dim3(groups), dim3(256), 0, stream, table(i0), part, i0 == 0);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  for (int i0 = (tensors - 1) / CLIP_TENSORS * CLIP_TENSORS; i0 >= 0; i0 -= CLIP_TENSORS) {
+    hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(outs ? groups : 1), dim3(256), 0, stream, table(i0), part, groups, norm, max_norm, outs != nullptr);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !outs) return e;
+  }
   return hipSuccess;
 }
 

@@ -282,7 +282,7 @@ int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* cons
   const int eb = dtype == DT_BF16 ? 2 : 4;
   int64_t total = 0;
   for (int i = 0; i < tensors; ++i) {
-    if (counts[i] < 0 || counts[i] > (INT64_MAX >> 4) - total) return CDP_EINVAL;
+    if (counts[i] < 0 || counts[i] > (1ll << 40) - total) return CDP_EINVAL;
     total += counts[i];
     if (counts[i] && (!grads[i] || !aligned_to(grads[i], eb) || (outs && (!outs[i] || !aligned_to(outs[i], eb))))) return CDP_EINVAL;
   }

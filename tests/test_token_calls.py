@@ -17,7 +17,7 @@ NORM_B = dict(dtype=0, accumulate=0, h=P, gate=P, post=P, pre=P, r=P, dr=P, dy=P
               ws_bytes=8 * 8 * 4 + 256, rows=4, C=8)
 ATT = dict(dtype=0, backward=0, qkv=P, offsets=P, out=P, lse=P, dout=0, dqkv=0, ws=0, ws_bytes=0, tokens=8, sequences=2, heads=4, kv_heads=2, width=16, scale=0.25)
 ATT_B = dict(ATT, backward=1, dout=P, dqkv=P, ws=P, ws_bytes=4 * 4 * 8 + 512)
-ONE = {n: np.array([v], dtype=np.int64) for n, v in (("at", P), ("odd", P + 2), ("count", 5), ("none", 0), ("less", -1))}
+ONE = {n: np.array([v], dtype=np.int64) for n, v in (("at", P), ("odd", P + 2), ("count", 5), ("none", 0), ("less", -1), ("lots", (1 << 40) + 1))}
 CLIP = dict(dtype=0, tensors=1, grads=ONE["at"].ctypes.data, outs=ONE["at"].ctypes.data, counts=ONE["count"].ctypes.data, max_norm=1.0, norm=P, ws=P, ws_bytes=65536)
 
 REFUSED = [("cdp_k_embedding", EMBED, w) for w in (
@@ -41,7 +41,7 @@ REFUSED += [("cdp_k_attention_packed", ATT_B, w) for w in (
 REFUSED += [("cdp_k_grad_clip", CLIP, w) for w in (
     dict(dtype=2), dict(tensors=0), dict(tensors=-1), dict(grads=0), dict(counts=0), dict(norm=0), dict(ws=0), dict(ws_bytes=65535), dict(ws=P + 4), dict(norm=P + 2),
     dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(grads=ONE["none"].ctypes.data), dict(outs=ONE["none"].ctypes.data), dict(grads=ONE["odd"].ctypes.data),
-    dict(outs=ONE["odd"].ctypes.data), dict(counts=ONE["less"].ctypes.data))]
+    dict(outs=ONE["odd"].ctypes.data), dict(counts=ONE["less"].ctypes.data), dict(counts=ONE["lots"].ctypes.data))]
 
 
 @pytest.mark.parametrize("name,good,change", REFUSED, ids=lambda v: v if isinstance(v, str) else ",".join("%s=%s" % p for p in v.items()) if len(v) < 7 else "")
