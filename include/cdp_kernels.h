@@ -118,10 +118,10 @@ int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gat
 /* Its gradients from dr[rows][C] (the gradient of r beside the one through y; NULL: none) and dy[rows][C] (with gamma_pre; NULL without):
  *   dx = d r in all, dh, dgate (elem type, written; dh and dgate with h and gate);
  *   dgamma_post[C], dgamma_pre[C] (fp32, with gamma_post and gamma_pre): overwritten, with accumulate != 0 added to.
- * r: as the forward wrote it (NULL without gamma_pre).  dx may be dr.
+ * x, h, gate, gammas: as the forward had them (x NULL without gamma_pre); r and y are made again.  dx may be dr.
  * workspace: 8 * C * min(rows, 512) + 256 bytes (CDP_EINVAL if smaller). */
-int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const void* gate, const float* gamma_post,
-                                 const float* gamma_pre, const void* r, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
+int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const void* h, const void* gate, const float* gamma_post,
+                                 const float* gamma_pre, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
                                  float* dgamma_post, float* dgamma_pre, float scale, float eps, void* workspace, size_t workspace_bytes,
                                  int rows, int C, void* stream);
 

@@ -362,10 +362,10 @@ def cdp_k_residual_norm(dtype, x_ptr, h_ptr, gate_ptr, gamma_post_ptr, gamma_pre
         raise CdpError(rc, "cdp_k_residual_norm")
 
 
-def cdp_k_residual_norm_backward(dtype, accumulate, h_ptr, gate_ptr, gamma_post_ptr, gamma_pre_ptr, r_ptr, dr_ptr, dy_ptr, dx_ptr, dh_ptr, dgate_ptr,
+def cdp_k_residual_norm_backward(dtype, accumulate, x_ptr, h_ptr, gate_ptr, gamma_post_ptr, gamma_pre_ptr, dr_ptr, dy_ptr, dx_ptr, dh_ptr, dgate_ptr,
                                  dgamma_post_ptr, dgamma_pre_ptr, scale, eps, ws_ptr, ws_bytes, rows, C_, stream=0) -> None:
     """Gradients of cdp_k_residual_norm from those of r and y."""
-    args = (dtype, accumulate, h_ptr or None, gate_ptr or None, gamma_post_ptr or None, gamma_pre_ptr or None, r_ptr or None, dr_ptr or None,
+    args = (dtype, accumulate, x_ptr or None, h_ptr or None, gate_ptr or None, gamma_post_ptr or None, gamma_pre_ptr or None, dr_ptr or None,
             dy_ptr or None, dx_ptr, dh_ptr or None, dgate_ptr or None, dgamma_post_ptr or None, dgamma_pre_ptr or None, scale, eps, ws_ptr or None,
             ws_bytes, rows, C_, stream or None)
     rc = _cdp_k_residual_norm_backward(*args)

@@ -371,7 +371,7 @@ struct ResidualNorm {
   const void *x, *h, *gate;
   const float *gamma_post, *gamma_pre;
   void *r, *y;                         // forward: written
-  const void *rin, *dr, *dy;           // backward: r, d r, d y
+  const void *dr, *dy;                 // backward
   void *dx, *dh, *dgate;
   float *dgamma_post, *dgamma_pre, *part;
   int rows, C, accumulate;

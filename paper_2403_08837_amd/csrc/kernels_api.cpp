@@ -226,15 +226,15 @@ int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gat
   return launch_residual_norm_fwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;
 }
 
-int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const void* gate, const float* gamma_post,
-                                 const float* gamma_pre, const void* r, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
+int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const void* h, const void* gate, const float* gamma_post,
+                                 const float* gamma_pre, const void* dr, const void* dy, void* dx, void* dh, void* dgate,
                                  float* dgamma_post, float* dgamma_pre, float scale, float eps, void* workspace, size_t workspace_bytes,
                                  int rows, int C, void* stream) {
   if (!dx || (!dr && !dy) || rows <= 0 || C <= 0 || C > RNORM_MAX_C || !(eps > 0.f) || !std::isfinite(scale) || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
-  if (!dy != !gamma_pre || !dgamma_pre != !gamma_pre || !r != !gamma_pre) return CDP_EINVAL;
+  if (!dy != !gamma_pre || !dgamma_pre != !gamma_pre || !x != !gamma_pre) return CDP_EINVAL;
   if (!h != !dh || !gate != !dgate || !gamma_post != !dgamma_post || (!h && (gate || gamma_post))) return CDP_EINVAL;
   const int eb = dtype == DT_BF16 ? 2 : 4;
-  for (const void* p : {h, gate, r, dr, dy, (const void*)dx, (const void*)dh, (const void*)dgate})
+  for (const void* p : {x, h, gate, dr, dy, (const void*)dx, (const void*)dh, (const void*)dgate})
     if (!aligned_to(p, eb)) return CDP_EINVAL;
   for (const float* p : {gamma_post, gamma_pre, (const float*)dgamma_post, (const float*)dgamma_pre})
     if (!aligned_to(p, 4)) return CDP_EINVAL;
@@ -243,8 +243,8 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* h, const
     return CDP_EINVAL;
   ResidualNorm a;
   memset(&a, 0, sizeof(a));
-  a.h = h; a.gate = gate; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
-  a.rin = r; a.dr = dr; a.dy = dy; a.dx = dx; a.dh = dh; a.dgate = dgate; a.dgamma_post = dgamma_post; a.dgamma_pre = dgamma_pre;
+  a.x = x; a.h = h; a.gate = gate; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
+  a.dr = dr; a.dy = dy; a.dx = dx; a.dh = dh; a.dgate = dgate; a.dgamma_post = dgamma_post; a.dgamma_pre = dgamma_pre;
   a.part = static_cast<float*>(workspace);
   a.rows = rows; a.C = C; a.accumulate = accumulate != 0; a.scale = scale; a.eps = eps;
   return launch_residual_norm_bwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;

@@ -5,8 +5,9 @@
 //
 // Bound by memory: five tensors forward, eight backward, each once.  A row stays in the registers of the lanes that share it (8 to 1024 of them, eight values
 // in each, sixteen past 8192 channels), read in one round of buffer loads: a tensor that is not there is a buffer of no bytes, which reads zeros and drops stores,
-// so that one kernel without branches serves every form.  Forward a row needs two sums, one after the other.  Backward one round of six sums is
-// enough: mean(b n) falls into sums that do not wait for rho and eta,
+// so that one kernel without branches serves every form.  Forward a row needs two sums, one after the other (eta, then rho of what it makes).  So does backward:
+// r is made again from x, in fp32 as the forward had it (from the rounded r the gradient of gamma_pre would be off by half a step of bf16), and
+// mean(b n) falls into sums that do not wait for rho,
 //   sum b h = sum sg dr h + rho sum sg a h - rho^2 mean(a rhat) sum sg r h,   sg = scale sig gamma_post.
 // Column sums stay in registers over a workgroup's rows; what the workgroups have is added up by residual_norm_fold_kernel in a fixed order.
 #include "elem.h"
@@ -152,7 +153,7 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_fwd_kernel(
   s[0] = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    r[i] = x[i] + f * (h[i] * post[i]) * (a.gate ? sigmoid(g[i]) : 1.f);
+    r[i] = x[i] + f * (h[i] * post[i]) * (a.gate ? sigmoid(g[i]) : 1.f);  // (as the backward makes it)
     s[0] += r[i] * r[i];
   }
   store_row<T, typename Ly::Group, K>(a.r, at, off, r);
@@ -170,8 +171,8 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
   using Ly = Lay<T, V, K, LR>;
   using Vals = Values<T, typename Ly::Group, K>;
   typedef typename Ly::Group Group;
-  constexpr int N = Ly::N, NS = 6;
-  __shared__ float lds[2][Ly::THREADS / 64 * NS];
+  constexpr int N = Ly::N, NS = 5;
+  __shared__ float lds[2][Ly::THREADS / 64 * NS], lds_eta[2][Ly::THREADS / 64];
   const int slot = threadIdx.x / LR, idx = threadIdx.x % LR, C = a.C;
   const int64_t groups = ((int64_t)a.rows + Ly::SLOTS - 1) / Ly::SLOTS;
   int col[K];
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
   if constexpr (!Ly::HEAVY) gammas();
 #pragma unroll
   for (int i = 0; i < N; ++i) sum_of(0, i) = sum_of(1, i) = 0.f;
-  struct Row { Vals h, g, r, dr, dy; };
+  struct Row { Vals x, h, g, dr, dy; };
   auto offsets = [&](int64_t group, unsigned (&off)[K]) {
 #pragma unroll
     for (int k = 0; k < K; ++k) off[k] = col[k] < C && group * Ly::SLOTS + slot < a.rows ? (unsigned)(slot * C + col[k]) * (unsigned)sizeof(T) : ~0u;
@@ -200,9 +201,9 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     const int64_t at = group * Ly::SLOTS * C * (int)sizeof(T);
     unsigned off[K];
     offsets(group, off);
+    w.x.load(a.x, at, off);
     w.h.load(a.h, at, off);
     w.g.load(a.gate, at, off);
-    w.r.load(a.rin, at, off);
     w.dr.load(a.dr, at, off);
     w.dy.load(a.dy, at, off);
   };
@@ -211,28 +212,32 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     const int64_t at = group * Ly::SLOTS * C * (int)sizeof(T);
     unsigned off[K];
     offsets(group, off);
-    float s[NS] = {}, sig[N];
+    float e[1] = {0.f}, s[NS] = {}, sig[N], r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[0] += w.h[i] * w.h[i];
+    row_sums<LR>(e, lds_eta[parity]);
+    const float eta = a.gamma_post ? rsqrtf(e[0] * inv + a.eps) : 1.f, f = a.scale * eta;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       sig[i] = a.gate ? sigmoid(w.g[i]) : 1.f;
-      const float h = w.h[i], r = w.r[i], ad = w.dy[i] * pre[i], sgh = a.scale * sig[i] * post[i] * h;
-      s[0] += r * r;
-      s[1] += r * ad;
-      s[2] += h * h;
-      s[3] += sgh * w.dr[i];
-      s[4] += sgh * ad;
-      s[5] += sgh * r;
+      const float hp = w.h[i] * post[i], ad = w.dy[i] * pre[i], sgh = a.scale * sig[i] * hp;
+      r[i] = w.x[i] + f * hp * sig[i];
+      s[0] += r[i] * r[i];
+      s[1] += r[i] * ad;
+      s[2] += sgh * w.dr[i];
+      s[3] += sgh * ad;
+      s[4] += sgh * r[i];
     }
     row_sums<LR>(s, lds[parity]);
-    const float rho = a.gamma_pre ? rsqrtf(s[0] * inv + a.eps) : 0.f, eta = a.gamma_post ? rsqrtf(s[2] * inv + a.eps) : 1.f;
+    const float rho = a.gamma_pre ? rsqrtf(s[0] * inv + a.eps) : 0.f;
     const float across = rho * rho * rho * (s[1] * inv);  // rho rho mean(a rhat): what a value of r takes from d
-    const float dot = a.gamma_post ? eta * eta * eta * inv * (s[3] + rho * s[4] - across * s[5]) : 0.f;
+    const float dot = a.gamma_post ? eta * eta * eta * inv * (s[2] + rho * s[3] - across * s[4]) : 0.f;
     float d[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float dy = w.dy[i], r = w.r[i];
-      d[i] = w.dr[i] + (rho * (dy * pre[i]) - across * r);
-      sum_of(1, i) += dy * (r * rho);
+      const float dy = w.dy[i];
+      d[i] = w.dr[i] + (rho * (dy * pre[i]) - across * r[i]);
+      sum_of(1, i) += dy * (r[i] * rho);
     }
     store_row<T, Group, K>(a.dx, at, off, d);
     float dg[N];
@@ -340,7 +345,7 @@ template <typename T, int V, int K, int LR = 8> hipError_t dispatch(const Residu
 }
 template <typename T> hipError_t any(const ResidualNorm& a, bool backward, hipStream_t stream) {
   uintptr_t all = (uintptr_t)(a.C % Elem<T>::VEC);
-  for (const void* p : {a.x, a.h, a.gate, (const void*)a.r, (const void*)a.y, a.rin, a.dr, a.dy, (const void*)a.dx, (const void*)a.dh, (const void*)a.dgate})
+  for (const void* p : {a.x, a.h, a.gate, (const void*)a.r, (const void*)a.y, a.dr, a.dy, (const void*)a.dx, (const void*)a.dh, (const void*)a.dgate})
     all |= reinterpret_cast<uintptr_t>(p) & 15;
   if (all == 0)
     return a.C <= 8192 ? dispatch<T, Elem<T>::VEC, 8 / Elem<T>::VEC>(a, backward, stream) : launch<T, Elem<T>::VEC, 16 / Elem<T>::VEC, 1024>(a, backward, stream);

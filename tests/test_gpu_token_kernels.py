@@ -161,9 +161,8 @@ def test_embedding_table_past_2_to_the_31():
 
 
 # ---- norms around a block ---------------------------------------------------------------------------------------------
-def norm_reference(x, h, gate, post, pre, dr, dy, scale, eps, dtype, r_given=None):
-    """Values and sizes of the terms.  r_given: what the backward reads."""
-    half_t = half(dtype)
+def norm_reference(x, h, gate, post, pre, dr, dy, scale, eps):
+    """Values and sizes of the terms."""
     res, size = {}, {}
     if h is not None:
         eta = (h.square().mean(1, keepdim=True) + eps).rsqrt() if post is not None else torch.ones_like(h[:, :1])
@@ -181,18 +180,16 @@ def norm_reference(x, h, gate, post, pre, dr, dy, scale, eps, dtype, r_given=Non
         res["y"] = r * rho * pre
         # r's error moves every y of the row through rho, and its own
         size["y"] = (size["r"] + r.abs() * (1 + size["r"].norm(dim=1, keepdim=True) / r.norm(dim=1, keepdim=True).clamp(min=1e-30))) * rho * pre.abs()
-    if r_given is None:
-        return res, size
     d, d_size = torch.zeros_like(r), torch.zeros_like(r)
     if dr is not None:
         d, d_size = d + dr, d_size + dr.abs()
     if pre is not None:
-        r = r_given
-        rho = (r.square().mean(1, keepdim=True) + eps).rsqrt()
         rhat, a = r * rho, dy * pre
+        # the size of a value of rhat: r's own terms, and what the whole row's do to rho
+        rhat_size = size["y"] / pre.abs().clamp(min=1e-30)
         d = d + rho * (a - rhat * (a * rhat).mean(1, keepdim=True))
-        d_size = d_size + rho * (a.abs() + rhat.abs() * (a * rhat).abs().mean(1, keepdim=True))
-        res["dpre"], size["dpre"] = (dy * rhat).sum(0), (dy * rhat).abs().sum(0)
+        d_size = d_size + rho * (a.abs() * (1 + size["r"].norm(dim=1, keepdim=True) / r.norm(dim=1, keepdim=True).clamp(min=1e-30)) + 2 * rhat_size * (a.abs() * rhat_size).mean(1, keepdim=True))
+        res["dpre"], size["dpre"] = (dy * rhat).sum(0), (dy.abs() * rhat_size).sum(0)
     res["dx"], size["dx"] = d, d_size
     if h is not None:
         du, du_size = scale * sig * d, scale * sig * d_size
@@ -209,7 +206,7 @@ def norm_reference(x, h, gate, post, pre, dr, dy, scale, eps, dtype, r_given=Non
 
 
 def norm_tolerance(name, res, size, dtype, rows):
-    """A sum over a row is at most 16 values in a lane, then a tree of at most 10 levels: 27 roundings with the squares; eta and rho are roots of such
+    """What `size` holds is the sum of the terms' sizes.  A sum over a row is at most 16 values in a lane, then a tree of at most 10 levels: 27 roundings with the squares; eta and rho are roots of such
     sums (half their relative error), with an error of the reciprocal root of 2 units and one product with 1/C; sigmoid costs 6 units.  r: 14 + 3 +
     6 + 4 < 32.  y: twice that and its own 20: < 96.  The gradients chain two norms and their means, each mean another 27: < 160.  Column sums: rows
     of a workgroup one after the other, then its share with the others', at most rows + 16 more."""
@@ -260,12 +257,12 @@ def test_residual_norm(dtype, rows, C, form):
     need = 8 * C * min(rows, 512) + 256
     ws = workspace(need)
     for accumulate in (0, 1):
-        b.cdp_k_residual_norm_backward(dtype, accumulate, p(dev["h"]), p(dev["gate"]), p(dev["post"]), p(dev["pre"]), p(r) if v["pre"] is not None else 0, p(dev["dr"]),
+        b.cdp_k_residual_norm_backward(dtype, accumulate, p(dev["x"]) if v["pre"] is not None else 0, p(dev["h"]), p(dev["gate"]), p(dev["post"]), p(dev["pre"]), p(dev["dr"]),
                                        p(dev["dy"]), p(got["dx"]), p(got["dh"]), p(got["dgate"]), p(grads[accumulate]["post"]), p(grads[accumulate]["pre"]), scale, eps,
                                        p(ws), need, rows, C)
     args = [dbl(v[k]) for k in ("x", "h", "gate", "post", "pre", "dr", "dy")]
     eps = float(np.float32(eps))
-    res, size = norm_reference(*args, scale, eps, dtype, r_given=r.cpu().double())
+    res, size = norm_reference(*args, scale, eps)
     for k in got:
         if got[k] is not None:
             near(got[k], res[k], norm_tolerance(k, res, size, dtype, rows), k)
@@ -298,7 +295,7 @@ def test_residual_norm_in_place_without_r_and_of_zeros(dtype):
     for inplace in (False, True):
         dr = v["dr"].clone()
         outs = [dr if inplace else torch.empty_like(dr), torch.empty_like(dr), torch.empty_like(dr), torch.empty(C, device="cuda"), torch.empty(C, device="cuda")]
-        b.cdp_k_residual_norm_backward(dtype, 0, p(v["h"]), p(v["gate"]), p(v["post"]), p(v["pre"]), p(r), p(dr), p(v["dy"]), *[p(o) for o in outs[:3]], p(outs[3]),
+        b.cdp_k_residual_norm_backward(dtype, 0, p(v["x"]), p(v["h"]), p(v["gate"]), p(v["post"]), p(v["pre"]), p(dr), p(v["dy"]), *[p(o) for o in outs[:3]], p(outs[3]),
                                        p(outs[4]), 0.5, 1e-6, p(workspace(need)), need, rows, C)
         results.append(outs)
     for one, two in zip(*results):
@@ -311,7 +308,7 @@ def test_residual_norm_of_extreme_gates():
     x, h = torch.ones_like(gate), 2 * torch.ones_like(gate)
     r, dx, dh, dg = (torch.empty_like(gate) for _ in range(4))
     b.cdp_k_residual_norm(F32, p(x), p(h), p(gate), 0, 0, p(r), 0, 1.0, 1e-6, 1, 8)
-    b.cdp_k_residual_norm_backward(F32, 0, p(h), p(gate), 0, 0, 0, p(x), 0, p(dx), p(dh), p(dg), 0, 0, 1.0, 1e-6, 0, 0, 1, 8)
+    b.cdp_k_residual_norm_backward(F32, 0, 0, p(h), p(gate), 0, 0, p(x), 0, p(dx), p(dh), p(dg), 0, 0, 1.0, 1e-6, 0, 0, 1, 8)
     sig = torch.sigmoid(gate.double())
     near(r, (1 + 2 * sig).cpu(), 16 * U * 3, "r")
     near(dh, sig.cpu(), 16 * U, "dh")
@@ -583,7 +580,7 @@ class Step:
         gemm(1, 1, B["n1"], w["wg"], B["gate"], T, C, C, C, C)
         b.cdp_k_residual_norm(F32, p(B["x"]), p(B["h"]), p(B["gate"]), p(w["post"]), p(w["g2"]), p(B["r"]), p(B["y"]), 0.5, self.EPS, T, C, stream)
         torch.sub(B["y"], self.target_d, out=B["dy"])   # the gradient of half the squared error
-        b.cdp_k_residual_norm_backward(F32, 0, p(B["h"]), p(B["gate"]), p(w["post"]), p(w["g2"]), p(B["r"]), 0, p(B["dy"]), p(B["dx"]), p(B["dh"]), p(B["dgate"]), p(g["post"]),
+        b.cdp_k_residual_norm_backward(F32, 0, p(B["x"]), p(B["h"]), p(B["gate"]), p(w["post"]), p(w["g2"]), 0, p(B["dy"]), p(B["dx"]), p(B["dh"]), p(B["dgate"]), p(g["post"]),
                                        p(g["g2"]), 0.5, self.EPS, p(ws["norm"]), size("norm"), T, C, stream)
         gemm(0, 0, B["dh"], B["att"], g["wo"], C, A, T, C, A)
         gemm(0, 0, B["dgate"], B["n1"], g["wg"], C, C, T, C, C)
@@ -593,7 +590,7 @@ class Step:
         gemm(1, 0, B["dqkv"], w["wqkv"], B["dn1"], T, C, Q, Q, C)
         gemm(1, 0, B["dgate"], w["wg"], B["dn1b"], T, C, C, C, C)
         B["dn1"].add_(B["dn1b"])
-        b.cdp_k_residual_norm_backward(F32, 0, 0, 0, 0, p(w["g1"]), p(B["x"]), p(B["dx"]), p(B["dn1"]), p(B["dx0"]), 0, 0, 0, p(g["g1"]), 1.0, self.EPS, p(ws["norm"]),
+        b.cdp_k_residual_norm_backward(F32, 0, p(B["x"]), 0, 0, 0, p(w["g1"]), p(B["dx"]), p(B["dn1"]), p(B["dx0"]), 0, 0, 0, p(g["g1"]), 1.0, self.EPS, p(ws["norm"]),
                                        size("norm"), T, C, stream)
         b.cdp_k_embedding(F32, 1, 0, p(self.ids_d), p(B["dx0"]), p(g["table"]), 1.5, p(ws["emb"]), size("emb"), T, self.V, C, stream)
         b.cdp_k_grad_clip(F32, len(g), *[v.ctypes.data for v in self.lists], 1.0, p(self.norm), p(ws["clip"]), 65536, stream)

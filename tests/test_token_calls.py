@@ -13,7 +13,7 @@ BIG = 1 << 40     # workspace enough
 EMBED = dict(dtype=0, backward=0, table=P, ids=P, dout=0, out=P, scale=1.0, ws=0, ws_bytes=0, rows=8, vocab=8, C=8)
 EMBED_B = dict(EMBED, backward=1, table=0, dout=P, ws=P, ws_bytes=16 * 8 + 8 * 8 + 512)
 NORM = dict(dtype=0, x=P, h=P, gate=P, post=P, pre=P, r=P, y=P, scale=1.0, eps=1e-6, rows=4, C=8)
-NORM_B = dict(dtype=0, accumulate=0, h=P, gate=P, post=P, pre=P, r=P, dr=P, dy=P, dx=P, dh=P, dgate=P, dpost=P, dpre=P, scale=1.0, eps=1e-6, ws=P,
+NORM_B = dict(dtype=0, accumulate=0, x=P, h=P, gate=P, post=P, pre=P, dr=P, dy=P, dx=P, dh=P, dgate=P, dpost=P, dpre=P, scale=1.0, eps=1e-6, ws=P,
               ws_bytes=8 * 8 * 4 + 256, rows=4, C=8)
 ATT = dict(dtype=0, backward=0, qkv=P, offsets=P, out=P, lse=P, dout=0, dqkv=0, ws=0, ws_bytes=0, tokens=8, sequences=2, heads=4, kv_heads=2, width=16, scale=0.25)
 ATT_B = dict(ATT, backward=1, dout=P, dqkv=P, ws=P, ws_bytes=4 * 4 * 8 + 512)
@@ -29,7 +29,7 @@ REFUSED += [("cdp_k_residual_norm", NORM, w) for w in (
     dict(dtype=2), dict(x=0), dict(r=0, y=0, pre=0), dict(y=0), dict(pre=0), dict(h=0), dict(h=0, gate=0), dict(h=0, post=0), dict(rows=0), dict(C=0), dict(C=16385),
     dict(eps=0.0), dict(eps=-1.0), dict(eps=float("nan")), dict(scale=float("nan")), dict(x=P + 2), dict(post=P + 1), dict(dtype=1, gate=P + 1))]
 REFUSED += [("cdp_k_residual_norm_backward", NORM_B, w) for w in (
-    dict(dtype=2), dict(dx=0), dict(dr=0, dy=0, pre=0, dpre=0, r=0), dict(dy=0), dict(pre=0), dict(dpre=0), dict(r=0), dict(h=0), dict(dh=0), dict(dgate=0), dict(gate=0),
+    dict(dtype=2), dict(dx=0), dict(dr=0, dy=0, pre=0, dpre=0, x=0), dict(dy=0), dict(pre=0), dict(dpre=0), dict(x=0), dict(h=0), dict(dh=0), dict(dgate=0), dict(gate=0),
     dict(dpost=0), dict(post=0), dict(h=0, dh=0, post=0, dpost=0), dict(rows=0), dict(C=16385), dict(eps=0.0), dict(scale=float("inf")), dict(ws=0), dict(ws=P + 4), dict(ws_bytes=8 * 8 * 4 + 255),
     dict(dh=P + 2), dict(dpre=P + 2))]
 REFUSED += [("cdp_k_attention_packed", ATT, w) for w in (
