@@ -245,7 +245,7 @@ def _norm_own(s):
     cdp.cdp_k_residual_norm(s["code"], _at(s["x"]), _at(s["h"]), _at(s["gate"]), _at(s["post"]), _at(s["pre"]), _at(s["r"]), _at(s["y"]), c["scale"], EPS, R, C)
     res = {"r": s["r"], "y": s["y"]}
     if c["backward"]:
-        cdp.cdp_k_residual_norm_backward(s["code"], 0, _at(s["h"]), _at(s["gate"]), _at(s["post"]), _at(s["pre"]), _at(s["r"]), _at(s["dr"]), _at(s["dy"]), _at(s["dx"]),
+        cdp.cdp_k_residual_norm_backward(s["code"], 0, _at(s["x"]), _at(s["h"]), _at(s["gate"]), _at(s["post"]), _at(s["pre"]), _at(s["dr"]), _at(s["dy"]), _at(s["dx"]),
                                          _at(s["dh"]), _at(s["dgate"]), _at(s["dpost"]), _at(s["dpre"]), c["scale"], EPS, _at(s["ws"]), s["ws"].numel(), R, C)
         res.update(dx=s["dx"], dh=s["dh"], dpre=s["dpre"])
         if c["gate"]:
