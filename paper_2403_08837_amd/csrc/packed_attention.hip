@@ -64,7 +64,12 @@ __device__ __forceinline__ v16f_t zero16() {
   for (int v = 0; v < 16; ++v) a[v] = 0.f;
   return a;
 }
-__device__ __forceinline__ uint32_t pack2(float lo, float hi) { return (uint32_t)f32_to_bf16(lo) | ((uint32_t)f32_to_bf16(hi) << 16); }
+// Both halves in one conversion (to nearest even); put together from two it is four instructions.
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  typedef float v2f __attribute__((ext_vector_type(2)));
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
+}
 
 // out[ob] += (columns 32 ob .. of the tile's rows r0 .. r0 + 31)^T x p, p as a score block's accumulator holds it (rounded to the element type).
 template <typename T, typename Tl, int OB>
@@ -302,12 +307,15 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
         for (int v = 0; v < 16; ++v) o[ob][v] *= f;
     }
 #pragma unroll
-    for (int b = 0; b < Tl::NB; ++b)
+    for (int b = 0; b < Tl::NB; ++b) {
+      float y[4] = {};
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         s[b][v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[b][v], c, -m));
-        z += s[b][v];
+        y[v & 3] += s[b][v];
       }
+      z += (y[0] + y[1]) + (y[2] + y[3]);
+    }
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(Ks + Tl::BYTES, 32 * b, s[b], o, lane);
     if (Tl::STAGES == 1 && i + NEXT < tiles) {
