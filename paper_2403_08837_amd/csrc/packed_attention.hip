@@ -42,11 +42,24 @@ template <typename T, int DW, bool SPLIT> struct Tile {
     else return CPR % 16 == 0 ? (r & 3) | ((r & 4) << 1) | ((r & 8) >> 1) : (r >> 1) & 7;
   }
   __device__ static __forceinline__ int slot(int r, int c) { return (r * CPR + (c ^ swz(r))) * 16; }  // bytes
+  // Where chunk c + `more` is, given where chunk c is: the bits of a chunk's number that the swizzle turns are turned in the address (tile rows are
+  // aligned to them), the others are added.  (more: a constant that c has no bits of)
+  static constexpr int TURNED = (CPR & (CPR - 1)) == 0 ? CPR - 1 : E == 2 ? 3 : 7;
+  __device__ static __forceinline__ unsigned chunk(unsigned at, int more) { return (at ^ ((more & TURNED) << 4)) + ((more & ~TURNED) << 4); }
+};
+template <typename V> __device__ __forceinline__ V lds_at(unsigned at) { return *(__attribute__((address_space(3))) const V*)(uintptr_t)at; }
+// The lane's place in what it reads of a tile, kept where it is: the addresses that a loop reads from differ from it by a constant turn, made
+// where they are used (all of them at hand, as the compiler would have it, are registers that wide heads need for data).
+struct Lane {
+  unsigned at;
+  __device__ __forceinline__ Lane(unsigned a) : at(a) { asm volatile("" : "+v"(at)); }
 };
 
-// Operand rows r0 .. r0 + 31 of the tile, 16-byte step ks of them.
-template <typename Tl> __device__ __forceinline__ uint4 rows_frag(const char* tile, int r0, int ks, int l31, int hi) {
-  return *reinterpret_cast<const uint4*>(tile + Tl::slot(r0 + l31, 2 * ks + hi));
+// Operand rows r0 .. r0 + 31 (r0 a multiple of 32) of the tile at LDS address `at`, 16-byte step ks of them.
+template <typename Tl> __device__ __forceinline__ unsigned rows_place(int l31, int hi) { return Tl::slot(l31, hi); }
+template <typename Tl> __device__ __forceinline__ uint4 rows_frag(Lane at, int r0, int ks) {
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint4, lds_at<v4u>(Tl::chunk(at.at, 2 * ks) + r0 * Tl::CPR * 16));
 }
 // acc += rows x columns over one 16-byte step of both.
 template <typename T> __device__ __forceinline__ v16f_t step_product(uint4 a, uint4 b, v16f_t c) {
@@ -72,35 +85,39 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 // out[ob] += (columns 32 ob .. of the tile's rows r0 .. r0 + 31)^T x p, p as a score block's accumulator holds it (rounded to the element type).
-template <typename T, typename Tl, int OB>
-__device__ __forceinline__ void across_product(const char* tile, int r0, const v16f_t& p, v16f_t (&out)[OB], int lane) {
+// bf16: a 16-lane group's addresses are 4 rows by 16 columns, and lane i gets column i of them; `at` of rows 4 hi + .. and `at8` of those 8 on.
+template <typename Tl> __device__ __forceinline__ unsigned across_place(int lane, int rows_on) {
   const int hi = lane >> 5;
+  if constexpr (Tl::E == 2) {
+    const int rho = lane & 15, c = 16 * ((lane >> 4) & 1) + 4 * (rho & 3);
+    return Tl::slot(4 * hi + (rho >> 2) + rows_on, c >> 3) + 2 * (c & 7);
+  } else {
+    return Tl::slot(4 * hi, (lane & 31) >> 2) + 4 * (lane & 3);
+  }
+}
+template <typename T, typename Tl, int OB>
+__device__ __forceinline__ void across_product(Lane at, Lane at8, int r0, const v16f_t& p, v16f_t (&out)[OB]) {
+  constexpr int PITCH = Tl::CPR * 16;
   if constexpr (sizeof(T) == 2) {
-    const int rho = lane & 15, cl = 16 * ((lane >> 4) & 1) + 4 * (rho & 3);
     typedef __attribute__((address_space(3))) att_v4s* v4s_ptr;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const uint4 w = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]), pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
-      const int r = r0 + 16 * t + 4 * hi + (rho >> 2);
 #pragma unroll
       for (int ob = 0; ob < OB; ++ob) {
-        const int c = 32 * ob + cl;
         union { att_v4s v[2]; uint4 u; } f;
-        f.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(tile + Tl::slot(r, c >> 3) + 2 * (c & 7)));
-        f.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(tile + Tl::slot(r + 8, c >> 3) + 2 * (c & 7)));
+        f.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at.at, 4 * ob) + (r0 + 16 * t) * PITCH));
+        f.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at8.at, 4 * ob) + (r0 + 16 * t) * PITCH));
         out[ob] = mfma_bf16(f.u, w, out[ob]);
       }
     }
   } else {
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
-      const int r = r0 + 8 * (v >> 2) + 4 * hi + (v & 3);
+      const int r = 8 * (v >> 2) + (v & 3);  // + 4 hi: bits of their own
 #pragma unroll
-      for (int ob = 0; ob < OB; ++ob) {
-        const int c = 32 * ob + (lane & 31);
-        const float x = *reinterpret_cast<const float*>(tile + Tl::slot(r, c >> 2) + 4 * (c & 3));
-        out[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[v], out[ob], 0, 0, 0);
-      }
+      for (int ob = 0; ob < OB; ++ob)
+        out[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_at<float>((Tl::chunk(at.at, 8 * ob) ^ (Tl::swz(r) << 4)) + (r0 + r) * PITCH), p[v], out[ob], 0, 0, 0);
     }
   }
 }
@@ -255,7 +272,7 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
   TileLoads<Tl> loads;
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
-  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   auto issue = [&](int i, int stage) {
     const int k0 = i * Tl::OTHER;
@@ -275,14 +292,15 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
     if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
     const int k0 = i * Tl::OTHER;
     if (k0 > last) continue;
-    const char* Ks = tiles_at + stage * 2 * Tl::BYTES;
+    const unsigned to = stage * 2 * Tl::BYTES;
     v16f_t s[Tl::NB];
+    const Lane rows(rows_of_tile + to);
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) s[b] = zero16();
 #pragma unroll
     for (int ks = 0; ks < Tl::STEPS; ++ks)
 #pragma unroll
-      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<Tl>(Ks, 32 * b, ks, l31, hi), qf[ks], s[b]);
+      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<Tl>(rows, 32 * b, ks), qf[ks], s[b]);
     if (k0 + Tl::OTHER - 1 > last - 31) {
 #pragma unroll
       for (int b = 0; b < Tl::NB; ++b)
@@ -316,8 +334,9 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
       }
       z += (y[0] + y[1]) + (y[2] + y[3]);
     }
+    const Lane across(across_tile + to + Tl::BYTES), across8(across_tile8 + to + Tl::BYTES);
 #pragma unroll
-    for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(Ks + Tl::BYTES, 32 * b, s[b], o, lane);
+    for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(across, across8, 32 * b, s[b], o);
     if (Tl::STAGES == 1 && i + NEXT < tiles) {
       tile_wait<SPLIT>();
       issue(i + NEXT, 0);
@@ -390,7 +409,7 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
   TileLoads<Tl> loads;
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
-  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   auto issue = [&](int i, int stage) {
     const int k0 = i * Tl::OTHER;
@@ -407,16 +426,17 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
   for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
     tile_wait<SPLIT>();
     if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
-    const char* Ks = tiles_at + stage * 2 * Tl::BYTES;
+    const unsigned to = stage * 2 * Tl::BYTES;
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) {
       const int k0 = i * Tl::OTHER + 32 * b;
       if (k0 > last) continue;
       v16f_t s = zero16(), dp = zero16();
+      const Lane rows(rows_of_tile + to);
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<Tl>(Ks, 32 * b, ks, l31, hi), qf[ks], s);
-        dp = step_product<T>(rows_frag<Tl>(Ks + Tl::BYTES, 32 * b, ks, l31, hi), df[ks], dp);
+        s = step_product<T>(rows_frag<Tl>(rows, 32 * b, ks), qf[ks], s);
+        dp = step_product<T>(rows_frag<Tl>(rows, 32 * b + Tl::OTHER, ks), df[ks], dp);  // (v's tile lies behind k's)
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * (dp[v] - delta);
@@ -425,7 +445,7 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
         for (int v = 0; v < 16; ++v)
           if (k0 + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[v] = 0.f;
       }
-      across_product<T, Tl>(Ks, 32 * b, s, dq, lane);
+      across_product<T, Tl>(Lane(across_tile + to), Lane(across_tile8 + to), 32 * b, s, dq);
     }
     if (Tl::STAGES == 1 && i + NEXT < tiles) {
       tile_wait<SPLIT>();
@@ -474,7 +494,7 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
   qloads.start(filler, lane, row_bytes, W);
   oloads.start(filler, lane, out_bytes, W);
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
-  const char* const tiles_at = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
   const int head0 = kv * group + share * (group / shares);
@@ -506,17 +526,18 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
     if (id < STATS) st[id / Tl::OTHER][id % Tl::OTHER] = stat;
     tile_wait<SPLIT>();
     if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
-    const char* Qs = tiles_at + stage * 2 * Tl::BYTES;
+    const unsigned to = stage * 2 * Tl::BYTES;
     const int t0 = span.first + i % per_head * Tl::OTHER;
 #pragma unroll 1
     for (int b = 0; b < Tl::NB; ++b) {
       const int b0 = t0 + 32 * b;
       if (b0 + 31 < first || b0 >= span.len) continue;
       v16f_t s = zero16(), dp = zero16();
+      const Lane rows(rows_of_tile + to + 32 * b * Tl::CPR * 16);
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<Tl>(Qs, 32 * b, ks, l31, hi), kf[ks], s);
-        dp = step_product<T>(rows_frag<Tl>(Qs + Tl::BYTES, 32 * b, ks, l31, hi), vf[ks], dp);
+        s = step_product<T>(rows_frag<Tl>(rows, 0, ks), kf[ks], s);
+        dp = step_product<T>(rows_frag<Tl>(rows, Tl::OTHER, ks), vf[ks], dp);  // (dout's tile lies behind q's)
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -534,8 +555,9 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
         for (int v = 0; v < 16; ++v)
           if (b0 + 8 * (v >> 2) + 4 * hi + (v & 3) < key) s[v] = dp[v] = 0.f;
       }
-      across_product<T, Tl>(Qs + Tl::BYTES, 32 * b, s, dv, lane);
-      across_product<T, Tl>(Qs, 32 * b, dp, dk, lane);
+      const Lane across(across_tile + to + 32 * b * Tl::CPR * 16), across8(across_tile8 + to + 32 * b * Tl::CPR * 16);
+      across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
+      across_product<T, Tl>(across, across8, 0, dp, dk);
     }
     if (Tl::STAGES == 1 && i + NEXT < tiles) {
       tile_wait<SPLIT>();
