@@ -4,6 +4,7 @@
 // take in strides: eight 16-byte loads in flight in every thread.  Squares are summed in 64 bits (any fp32 value's square is there, and the
 // order hardly matters), the workgroups' sums go to the workspace, and every workgroup of the second pass adds them up for itself in the same
 // order: no third launch, no atomics.  The second pass goes through the units backwards: what the first read last is still cached.
+// Sets of up to 64 pieces of 4 KB are one launch of one workgroup, whose wavefronts keep their pieces in registers between the two.
 // The tensors' addresses travel in the kernel arguments, 128 of them a launch; a wavefront finds the tensor of a unit by comparing all of them at once.
 #include "elem.h"
 #include "kernels.h"
@@ -15,7 +16,8 @@ namespace cdp {
 
 namespace {
 
-constexpr int CLIP_TENSORS = 128, CLIP_GROUPS = 2048, UNIT_BYTES = 32768, LOADS = UNIT_BYTES / 16 / 256;
+constexpr int CLIP_TENSORS = 128, CLIP_GROUPS = 2048, UNIT_BYTES = 32768;
+constexpr int SOLE = 1024, SOLE_BYTES = 4096, SOLE_EACH = 4, SOLE_UNITS = SOLE / 64 * SOLE_EACH;  // one workgroup: threads, bytes of a piece, pieces of a wavefront, of all
 
 struct ClipTable {
   const void* g[CLIP_TENSORS];
@@ -26,8 +28,8 @@ struct ClipTable {
 };
 static_assert(sizeof(ClipTable) <= 3600, "kernel arguments are 4 KB at most");
 
-template <typename T> struct Unit {
-  static constexpr int V = Elem<T>::VEC, SIZE = UNIT_BYTES / (int)sizeof(T);
+template <typename T, int BYTES = UNIT_BYTES> struct Unit {
+  static constexpr int V = Elem<T>::VEC, SIZE = BYTES / (int)sizeof(T);
   const T* g;
   T* out;
   int n;        // elements, up to SIZE
@@ -43,42 +45,66 @@ template <typename T> struct Unit {
   }
 };
 
-__device__ __forceinline__ double group_sum(double s, double* lds) {
+template <int THREADS> __device__ __forceinline__ double group_sum(double s, double* lds) {
 #pragma unroll
   for (int k = 32; k > 0; k >>= 1) s += __shfl_xor(s, k, 64);
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = s;
   __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
+  s = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) s += lds[w];
+  return s;
+}
+// A thread's part of the sum of squares of a unit.
+template <typename T, int THREADS> __device__ __forceinline__ double unit_squares(const Unit<T>& w) {
+  constexpr int L = UNIT_BYTES / 16 / THREADS;
+  const int t = threadIdx.x, pieces = w.whole ? w.n / Unit<T>::V : 0;
+  double s = 0;
+  Chunk16<T> c[L];
+#pragma unroll
+  for (int k = 0; k < L; ++k)
+    if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min(t + THREADS * k, pieces - 1)];
+#pragma unroll
+  for (int k = 0; k < L; ++k)
+    if (t + THREADS * k < pieces)
+#pragma unroll
+      for (int e = 0; e < Unit<T>::V; ++e) {
+        const double v = Elem<T>::to_f32(c[k].e[e]);
+        s += v * v;
+      }
+  for (int e = pieces * Unit<T>::V + t; e < w.n; e += THREADS) {
+    const double v = Elem<T>::to_f32(w.g[e]);
+    s += v * v;
+  }
+  return s;
+}
+template <typename T, int THREADS> __device__ __forceinline__ void unit_scale(const Unit<T>& w, bool over, float f) {
+  if (!over && w.out == w.g) return;  // in place, nothing to do
+  constexpr int L = UNIT_BYTES / 16 / THREADS;
+  const int t = threadIdx.x, pieces = w.whole ? w.n / Unit<T>::V : 0;
+  Chunk16<T> c[L];
+#pragma unroll
+  for (int k = 0; k < L; ++k)
+    if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min(t + THREADS * k, pieces - 1)];
+#pragma unroll
+  for (int k = 0; k < L; ++k) {
+    if (t + THREADS * k >= pieces) continue;
+    if (over)
+#pragma unroll
+      for (int e = 0; e < Unit<T>::V; ++e) c[k].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k].e[e]));
+    reinterpret_cast<uint4*>(w.out)[t + THREADS * k] = c[k].v;
+  }
+  for (int e = pieces * Unit<T>::V + t; e < w.n; e += THREADS) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
 }
 
 // Sum of squares of a workgroup's units, written to part[workgroup], or, past the first table, added to it.
 template <typename T> __global__ __launch_bounds__(256) void grad_norm_kernel(const ClipTable t, double* part, int first) {
   __shared__ double lds[4];
   double s = 0;
-  for (int u = blockIdx.x; u < t.total; u += gridDim.x) {
-    const Unit<T> w(t, u, false);
-    const int pieces = w.whole ? w.n / Unit<T>::V : 0;
-    Chunk16<T> c[LOADS];
-#pragma unroll
-    for (int k = 0; k < LOADS; ++k)
-      if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min((int)threadIdx.x + 256 * k, pieces - 1)];
-#pragma unroll
-    for (int k = 0; k < LOADS; ++k)
-      if ((int)threadIdx.x + 256 * k < pieces)
-#pragma unroll
-        for (int e = 0; e < Unit<T>::V; ++e) {
-          const double v = Elem<T>::to_f32(c[k].e[e]);
-          s += v * v;
-        }
-    for (int e = pieces * Unit<T>::V + threadIdx.x; e < w.n; e += 256) {
-      const double v = Elem<T>::to_f32(w.g[e]);
-      s += v * v;
-    }
-  }
-  s = group_sum(s, lds);
+  for (int u = blockIdx.x; u < t.total; u += gridDim.x) s += unit_squares<T, 256>(Unit<T>(t, u, false));
+  s = group_sum<256>(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = first ? s : part[blockIdx.x] + s;
 }
-
 template <typename T> __global__ __launch_bounds__(256) void grad_scale_kernel(const ClipTable t, const double* part, int parts, float* norm, float max_norm, int scaling) {
   __shared__ double lds[4];
   double s = 0;
@@ -88,34 +114,73 @@ template <typename T> __global__ __launch_bounds__(256) void grad_scale_kernel(c
     const double v = part[min(i, parts - 1)];
     s += i < parts ? v : 0.0;
   }
-  const double r = sqrt(group_sum(s, lds));
+  const double r = sqrt(group_sum<256>(s, lds));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
   if (!scaling) return;
   const bool over = r > max_norm;  // (not a number: no)
   const float f = over ? (float)(max_norm / r) : 1.f;
-  for (int v = blockIdx.x; v < t.total; v += gridDim.x) {
-    const Unit<T> w(t, t.total - 1 - v, true);
-    if (!over && w.out == w.g) continue;  // in place, nothing to do
-    const int pieces = w.whole ? w.n / Unit<T>::V : 0;
-    Chunk16<T> c[LOADS];
+  for (int v = blockIdx.x; v < t.total; v += gridDim.x) unit_scale<T, 256>(Unit<T>(t, t.total - 1 - v, true), over, f);
+}
+// Both for a set of one table and few pieces; a wavefront has the pieces wave, wave + 16, ..
+template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(const ClipTable t, float* norm, float max_norm, int scaling) {
+  typedef Unit<T, SOLE_BYTES> U;
+  constexpr int L = SOLE_BYTES / 16 / 64;
+  __shared__ double lds[SOLE / 64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  Chunk16<T> c[SOLE_EACH][L];
+  double s = 0;
 #pragma unroll
-    for (int k = 0; k < LOADS; ++k)
-      if (pieces) c[k].v = reinterpret_cast<const uint4*>(w.g)[min((int)threadIdx.x + 256 * k, pieces - 1)];
+  for (int k = 0; k < SOLE_EACH; ++k) {
+    if (wave + k * (SOLE / 64) >= t.total) break;
+    const U w(t, wave + k * (SOLE / 64), scaling);
+    if (!w.whole || w.n < U::V) continue;
 #pragma unroll
-    for (int k = 0; k < LOADS; ++k) {
-      if ((int)threadIdx.x + 256 * k >= pieces) continue;
+    for (int l = 0; l < L; ++l) c[k][l].v = reinterpret_cast<const uint4*>(w.g)[min(lane + 64 * l, w.n / U::V - 1)];
+  }
+#pragma unroll
+  for (int k = 0; k < SOLE_EACH; ++k) {
+    if (wave + k * (SOLE / 64) >= t.total) break;
+    const U w(t, wave + k * (SOLE / 64), scaling);
+    const int pieces = w.whole ? w.n / U::V : 0;
+#pragma unroll
+    for (int l = 0; l < L; ++l)
+      if (lane + 64 * l < pieces)
+#pragma unroll
+        for (int e = 0; e < U::V; ++e) {
+          const double v = Elem<T>::to_f32(c[k][l].e[e]);
+          s += v * v;
+        }
+    for (int e = pieces * U::V + lane; e < w.n; e += 64) {
+      const double v = Elem<T>::to_f32(w.g[e]);
+      s += v * v;
+    }
+  }
+  const double r = sqrt(group_sum<SOLE>(s, lds));
+  if (threadIdx.x == 0) *norm = (float)r;
+  if (!scaling) return;
+  const bool over = r > max_norm;
+  const float f = over ? (float)(max_norm / r) : 1.f;
+#pragma unroll
+  for (int k = 0; k < SOLE_EACH; ++k) {
+    if (wave + k * (SOLE / 64) >= t.total) break;
+    const U w(t, wave + k * (SOLE / 64), true);
+    if (!over && w.out == w.g) continue;
+    const int pieces = w.whole ? w.n / U::V : 0;
+#pragma unroll
+    for (int l = 0; l < L; ++l) {
+      if (lane + 64 * l >= pieces) continue;
       if (over)
 #pragma unroll
-        for (int e = 0; e < Unit<T>::V; ++e) c[k].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k].e[e]));
-      reinterpret_cast<uint4*>(w.out)[threadIdx.x + 256 * k] = c[k].v;
+        for (int e = 0; e < U::V; ++e) c[k][l].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k][l].e[e]));
+      reinterpret_cast<uint4*>(w.out)[lane + 64 * l] = c[k][l].v;
     }
-    for (int e = pieces * Unit<T>::V + threadIdx.x; e < w.n; e += 256) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
+    for (int e = pieces * U::V + lane; e < w.n; e += 64) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
   }
 }
 
 template <typename T>
 hipError_t clip(int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm, float* norm, double* part, hipStream_t stream) {
-  auto table = [&](int i0) {
+  auto table = [&](int i0, int size) {
     ClipTable t;
     int32_t units = 0;
     for (int i = 0; i < CLIP_TENSORS; ++i) {
@@ -124,7 +189,7 @@ hipError_t clip(int tensors, const void* const* grads, void* const* outs, const 
       t.out[i] = there && outs ? outs[i0 + i] : nullptr;
       t.count[i] = there ? counts[i0 + i] : 0;
       t.units[i] = units;  // (of tensors with the same one, only the last has units)
-      if (there) units += (int32_t)((t.count[i] + Unit<T>::SIZE - 1) / Unit<T>::SIZE);
+      if (there) units += (int32_t)((t.count[i] + size - 1) / size);
     }
     t.total = units;
     return t;
@@ -135,14 +200,21 @@ hipError_t clip(int tensors, const void* const* grads, void* const* outs, const 
     for (int i = i0; i < std::min(tensors - i0, CLIP_TENSORS) + i0; ++i) units += (counts[i] + Unit<T>::SIZE - 1) / Unit<T>::SIZE;
     most = std::max(most, units);
   }
+  if (tensors <= CLIP_TENSORS && most <= SOLE_UNITS) {
+    const ClipTable t = table(0, Unit<T, SOLE_BYTES>::SIZE);
+    if (t.total <= SOLE_UNITS) {
+      hipLaunchKernelGGL((grad_sole_kernel<T>), dim3(1), dim3(SOLE), 0, stream, t, norm, max_norm, outs != nullptr);
+      return hipGetLastError();
+    }
+  }
   const int groups = (int)std::min<int64_t>(most, CLIP_GROUPS);
   for (int i0 = 0; i0 < tensors; i0 += CLIP_TENSORS) {
-    hipLaunchKernelGGL((grad_norm_kernel<T>), dim3(groups), dim3(256), 0, stream, table(i0), part, i0 == 0);
+    hipLaunchKernelGGL((grad_norm_kernel<T>), dim3(groups), dim3(256), 0, stream, table(i0, Unit<T>::SIZE), part, i0 == 0);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   for (int i0 = (tensors - 1) / CLIP_TENSORS * CLIP_TENSORS; i0 >= 0; i0 -= CLIP_TENSORS) {
-    hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(outs ? groups : 1), dim3(256), 0, stream, table(i0), part, groups, norm, max_norm, outs != nullptr);
+    hipLaunchKernelGGL((grad_scale_kernel<T>), dim3(outs ? groups : 1), dim3(256), 0, stream, table(i0, Unit<T>::SIZE), part, groups, norm, max_norm, outs != nullptr);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !outs) return e;
   }

@@ -38,6 +38,19 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v) {
   }
   return v;
 }
+// Sum over the lanes that are a multiple of L apart, in every one of them.
+template <int L> __device__ __forceinline__ float groups_sum(float v) {
+  if constexpr (L <= 8) v += dpp<0x128>(v);  // (eight on, around sixteen)
+  if constexpr (L <= 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  if constexpr (L <= 32) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
+  return v;
+}
 // Sums over the LR lanes of a row, n of them at once; rows of more than a wavefront through LDS (`lds`: not in use by the sums before).
 template <int LR, int NS> __device__ __forceinline__ void row_sums(float (&v)[NS], float* lds) {
 #pragma unroll
@@ -274,26 +287,28 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     }
   }
   if (!a.dgamma_post && !a.dgamma_pre) return;
-  // the sums of the rows that the workgroup has at once, one vector after the other
-  __shared__ float join[Ly::SLOTS > 1 ? Ly::THREADS * N : 1];
+  // the sums of the rows that the workgroup has at once, one vector after the other: those of a wavefront between its lanes, the others through LDS
+  constexpr int SHARES = LR < 64 ? Ly::THREADS / 64 : Ly::SLOTS;
+  const int share = LR < 64 ? (int)threadIdx.x >> 6 : slot;
+  __shared__ float join[SHARES > 1 ? SHARES * LR * N : 1];
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float* const out = which ? a.dgamma_pre : a.dgamma_post;
     if (!out) continue;
     float v[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = sum_of(which, i);
-    if constexpr (Ly::SLOTS > 1) {
+    for (int i = 0; i < N; ++i) v[i] = groups_sum<LR>(sum_of(which, i));
+    if constexpr (SHARES > 1) {
       __syncthreads();
 #pragma unroll
-      for (int i = 0; i < N; ++i) join[(i * Ly::SLOTS + slot) * LR + idx] = v[i];
+      for (int i = 0; i < N; ++i) join[(i * SHARES + share) * LR + idx] = v[i];  // (the same from every group of a wavefront)
       __syncthreads();
       if (slot) continue;
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         v[i] = 0.f;
-#pragma unroll 4
-        for (int q = 0; q < Ly::SLOTS; ++q) v[i] += join[(i * Ly::SLOTS + q) * LR + idx];
+#pragma unroll
+        for (int q = 0; q < SHARES; ++q) v[i] += join[(i * SHARES + q) * LR + idx];
       }
     }
     float* const to = gridDim.x == 1 ? out : a.part + ((int64_t)which * gridDim.x + blockIdx.x) * C;
@@ -330,7 +345,8 @@ template <typename T, int V, int K, int LR> hipError_t launch(const ResidualNorm
     hipLaunchKernelGGL((residual_norm_fwd_kernel<T, V, K, LR>), dim3((unsigned)groups), dim3(Ly::THREADS), 0, stream, a);
     return hipGetLastError();
   }
-  const int parts = (int)std::min<int64_t>(groups, RNORM_MAX_PARTS);
+  // (a few row groups are one workgroup's: a second launch for the sums costs more than it saves)
+  const int parts = groups <= 4 ? 1 : (int)std::min<int64_t>(groups, RNORM_MAX_PARTS);
   hipLaunchKernelGGL((residual_norm_bwd_kernel<T, V, K, LR>), dim3(parts), dim3(Ly::THREADS), 0, stream, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1 || !(a.dgamma_post || a.dgamma_pre)) return e;
