@@ -48,6 +48,7 @@ template <typename T, int DW, bool SPLIT> struct Tile {
   __device__ static __forceinline__ unsigned chunk(unsigned at, int more) { return (at ^ ((more & TURNED) << 4)) + ((more & ~TURNED) << 4); }
 };
 template <typename V> __device__ __forceinline__ V lds_at(unsigned at) { return *(__attribute__((address_space(3))) const V*)(uintptr_t)at; }
+__device__ __forceinline__ void lds_put(unsigned at, float v) { *(__attribute__((address_space(3))) float*)(uintptr_t)at = v; }
 // The lane's place in what it reads of a tile, kept where it is: the addresses that a loop reads from differ from it by a constant turn, made
 // where they are used (all of them at hand, as the compiler would have it, are registers that wide heads need for data).
 struct Lane {
@@ -226,21 +227,22 @@ __device__ __forceinline__ float both_halves(float v, bool maximum) {
 __device__ __forceinline__ float score_factor(float scale) { return fmaxf(fabsf(scale) * LOG2E, 1.17549435e-38f); }
 
 // SPLIT: four wavefronts' accumulators of the same 32 rows through LDS, [wavefront][column][row], and the sum of them for DW / 8 columns of a lane's row.
-template <int OB> __device__ __forceinline__ void put_share(float* mine, const v16f_t (&acc)[OB], float f, int l31, int hi) {
+// `mine`, `shares`: LDS addresses of [column][row] and of four of those.
+template <int OB> __device__ __forceinline__ void put_share(unsigned mine, const v16f_t (&acc)[OB], float f, int l31, int hi) {
 #pragma unroll
   for (int ob = 0; ob < OB; ++ob)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) mine[(32 * ob + 8 * (v >> 2) + 4 * hi + (v & 3)) * 32 + l31] = acc[ob][v] * f;
+    for (int v = 0; v < 16; ++v) lds_put(mine + 4 * ((32 * ob + 8 * (v >> 2) + 4 * hi + (v & 3)) * 32 + l31), acc[ob][v] * f);
 }
-template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row, const float* shares, float f, int wave, int l31, int hi, int width) {
+template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row, unsigned shares, float f, int wave, int l31, int hi, int width) {
   const int d0 = (2 * wave + hi) * (DW / 8);
 #pragma unroll
   for (int d = d0; d < d0 + DW / 8; d += 4) {
     float v[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float* p = shares + (d + e) * 32 + l31;
-      v[e] = ((p[0] + p[DW * 32]) + (p[2 * DW * 32] + p[3 * DW * 32])) * f;
+      const unsigned p = shares + 4 * ((d + e) * 32 + l31);
+      v[e] = ((lds_at<float>(p) + lds_at<float>(p + DW * 128)) + (lds_at<float>(p + 2 * DW * 128) + lds_at<float>(p + 3 * DW * 128))) * f;
     }
     if (d >= width) continue;
     if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(row + d) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
@@ -251,7 +253,8 @@ template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row
 // ---- forward ----------------------------------------------------------------------------------------------------------
 template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
   using Tl = Tile<T, DW, SPLIT>;
-  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
+  __shared__ __attribute__((aligned(1024))) char memory[Tl::LDS];
+  const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
@@ -271,7 +274,7 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
   const float c = score_factor(a.scale);
   TileLoads<Tl> loads;
   loads.start(filler, lane, row_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   auto issue = [&](int i, int stage) {
@@ -351,13 +354,12 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
     __syncthreads();
     const float top = fmaxf(fmaxf(ms[0][l31], ms[1][l31]), fmaxf(ms[2][l31], ms[3][l31])), f = __builtin_amdgcn_exp2f(m - top);
     if (hi == 0) zs[wave][l31] = z * f;
-    float* shares = reinterpret_cast<float*>(smem);
-    put_share(shares + wave * DW * 32, o, f, l31, hi);
+    put_share(smem + wave * DW * 128, o, f, l31, hi);
     __syncthreads();
     if (q >= span.len) return;
     z = (zs[0][l31] + zs[1][l31]) + (zs[2][l31] + zs[3][l31]);
     m = top;
-    join_shares<T, DW>(out, shares, 1.f / z, wave, l31, hi, W);
+    join_shares<T, DW>(out, smem, 1.f / z, wave, l31, hi, W);
     if (wave) return;
   } else {
     if (q >= span.len) return;
@@ -367,14 +369,13 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
 }
 
 // ---- backward: dq, and delta for the other kernel ---------------------------------------------------------------------
-template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
+// id: of the workgroups for queries, of which there are `all`.
+template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
   using Tl = Tile<T, DW, SPLIT>;
-  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
-  const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
-  const Span span = find_span<Tl::OWN>(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
+  const int head = id % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
+  const Span span = find_span<Tl::OWN>(a, all / a.heads - 1 - id / a.heads, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -404,11 +405,11 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
     delta = both_halves(delta, false);
   }
   const float lse = a.lse[at] * LOG2E;
-  if (hi == 0 && q < span.len && (!SPLIT || wave == 0)) a.delta[at] = delta;
+  if (write_delta && hi == 0 && q < span.len && (!SPLIT || wave == 0)) a.delta[at] = delta;
   const float c = score_factor(a.scale);
   TileLoads<Tl> loads;
   loads.start(filler, lane, row_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   auto issue = [&](int i, int stage) {
@@ -454,28 +455,33 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
   }
   T* const row = static_cast<T*>(a.dqkv) + (int64_t)(span.begin + q) * (a.heads + 2 * a.kv_heads) * W + head * W;
   if constexpr (SPLIT) {
-    float* shares = reinterpret_cast<float*>(smem);
     __syncthreads();
-    put_share(shares + wave * DW * 32, dq, 1.f, l31, hi);
+    put_share(smem + wave * DW * 128, dq, 1.f, l31, hi);
     __syncthreads();
-    if (q < span.len) join_shares<T, DW>(row, shares, a.scale, wave, l31, hi, W);
+    if (q < span.len) join_shares<T, DW>(row, smem, a.scale, wave, l31, hi, W);
   } else if (q < span.len) {
     store_own<T, DW>(row, dq, a.scale, hi, W);
   }
+}
+template <typename T, int DW, bool SPLIT>
+__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
+  const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
+  bwd_q<T, DW, SPLIT>(a, smem, blockIdx.x, gridDim.x, true);
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------------------------
 // The tiles are those of the query heads of the key head, one head after the other, each from the workgroup's first key on.  Where that leaves
 // the chip short of workgroups the heads are shared by `shares` of them, whose sums (fp32, in the workspace) packed_bwd_fold_kernel adds in a fixed order.
-template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+// OWN: delta is not in memory yet; the workgroup makes that of all the rows it will meet first (up to OWN_ROWS of them: no span is longer than the tensor).
+constexpr int OWN_ROWS = 512;
+template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ void bwd_kv(const PackedAttention& a, unsigned smem, unsigned wg, int shares) {
   using Tl = Tile<T, DW, SPLIT>;
-  __shared__ __attribute__((aligned(1024))) char smem[Tl::LDS];
   __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 1][2][2][Tl::OTHER];  // per stage: lse (in log2), delta
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
-  const int share = blockIdx.x % shares, kv = blockIdx.x / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
-  const Span span = find_span<Tl::OWN>(a, blockIdx.x / (shares * a.kv_heads), lane);
+  const int share = wg % shares, kv = wg / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
+  const Span span = find_span<Tl::OWN>(a, wg / (shares * a.kv_heads), lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E, out_bytes = a.heads * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -493,7 +499,7 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
   TileLoads<Tl> qloads, oloads;
   qloads.start(filler, lane, row_bytes, W);
   oloads.start(filler, lane, out_bytes, W);
-  const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
+  const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
   constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
   const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
@@ -502,6 +508,33 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
   static_assert(STATS <= LOADERS, "a statistic per thread");
   const int id = SPLIT ? lane : (int)threadIdx.x;
   float stat = 0.f;  // of the tile under way
+  __shared__ float own_memory[OWN ? OWN_ROWS : 1];  // [head of the group][query - first]
+  const unsigned own = (unsigned)(uintptr_t)(lds_ptr)own_memory;
+  const int own_rows = span.len - span.first;
+  if constexpr (OWN) {
+    // eight lanes a row
+    const int n = group * own_rows, l8 = threadIdx.x & 7;
+    for (int r = threadIdx.x >> 3; r < n; r += 32) {
+      const int64_t row = ((int64_t)(span.begin + span.first + r % own_rows) * a.heads + head0 + r / own_rows) * W * Tl::E;
+      const char* const o = static_cast<const char*>(a.out) + row;
+      const char* const d = static_cast<const char*>(a.dout) + row;
+      float x = 0.f;
+#pragma unroll
+      for (int k = 0; k < (Tl::CPR + 7) / 8; ++k) {
+        const int c = l8 + 8 * k;
+        if (c * Tl::VEC >= W) continue;
+        Chunk16<T> p, g;
+        p.v = *reinterpret_cast<const uint4*>(o + 16 * c);
+        g.v = *reinterpret_cast<const uint4*>(d + 16 * c);
+#pragma unroll
+        for (int e = 0; e < Tl::VEC; ++e) x += Elem<T>::to_f32(p.e[e]) * Elem<T>::to_f32(g.e[e]);
+      }
+#pragma unroll
+      for (int k = 4; k > 0; k >>= 1) x += __shfl_xor(x, k, 64);
+      if (l8 == 0) lds_put(own + 4 * r, x);
+    }
+    __syncthreads();
+  }
   auto issue = [&](int i, int stage) {
     const unsigned to = lds + stage * 2 * Tl::BYTES;
     const int head = head0 + i / per_head, q0 = span.first + i % per_head * Tl::OTHER;
@@ -512,7 +545,10 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
       // rows past the sequence: exp(score - inf) is a probability of zero
       const bool is_lse = id < Tl::OTHER;
       const int q = q0 + id % Tl::OTHER;
-      const float x = ((is_lse ? a.lse : a.delta) + (int64_t)head * a.tokens + span.begin)[min(q, span.len - 1)];
+      const int qc = min(q, span.len - 1);
+      float x;
+      if (OWN && !is_lse) x = lds_at<float>(own + 4 * ((head - head0) * own_rows + qc - span.first));
+      else x = ((is_lse ? a.lse : a.delta) + (int64_t)head * a.tokens + span.begin)[qc];
       stat = is_lse ? (q < span.len ? x * LOG2E : INFINITY) : (q < span.len ? x : 0.f);
     }
   };
@@ -568,14 +604,13 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
   auto write = [&](auto* row, int64_t v_from_k) {
     using R = std::remove_reference_t<decltype(*row)>;
     if constexpr (SPLIT) {
-      float* joined = reinterpret_cast<float*>(smem);
       __syncthreads();
-      put_share(joined + wave * DW * 32, dk, 1.f, l31, hi);
-      put_share(joined + (4 + wave) * DW * 32, dv, 1.f, l31, hi);
+      put_share(smem + wave * DW * 128, dk, 1.f, l31, hi);
+      put_share(smem + (4 + wave) * DW * 128, dv, 1.f, l31, hi);
       __syncthreads();
       if (key >= span.len) return;
-      join_shares<R, DW>(row, joined, a.scale, wave, l31, hi, W);
-      join_shares<R, DW>(row + v_from_k, joined + 4 * DW * 32, 1.f, wave, l31, hi, W);
+      join_shares<R, DW>(row, smem, a.scale, wave, l31, hi, W);
+      join_shares<R, DW>(row + v_from_k, smem + 4 * DW * 128, 1.f, wave, l31, hi, W);
     } else {
       if (key >= span.len) return;
       store_own<R, DW>(row, dk, a.scale, hi, W);
@@ -586,6 +621,19 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1)
     write(a.parts + (((int64_t)share * 2 * a.tokens + span.begin + key) * a.kv_heads + kv) * W, (int64_t)a.tokens * a.kv_heads * W);
   else
     write(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W, (int64_t)a.kv_heads * W);
+}
+template <typename T, int DW, bool SPLIT>
+__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
+  const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
+  bwd_kv<T, DW, SPLIT, false>(a, smem, blockIdx.x, shares);
+}
+// Both in one launch, for few rows: the workgroups past `queries` are those for keys.
+template <typename T, int DW> __global__ __launch_bounds__(256, 1) void packed_bwd_both_kernel(const PackedAttention a, const unsigned queries) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, true>::LDS];
+  const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
+  if (blockIdx.x < queries) bwd_q<T, DW, true>(a, smem, blockIdx.x, queries, false);
+  else bwd_kv<T, DW, true, true>(a, smem, blockIdx.x - queries, 1);
 }
 
 // Sums of the shares: [share][dk, dv][tokens][kv_heads][width] -> the rows of dqkv that belong to a sequence, eight columns a thread.
@@ -663,7 +711,20 @@ template <typename T, bool SPLIT> hipError_t backward_kv(const PackedAttention& 
   hipLaunchKernelGGL((packed_bwd_fold_kernel<T>), dim3((unsigned)((n + 255) / 256), 2), dim3(256), 0, stream, a, shares);
   return hipGetLastError();
 }
+// One launch for queries and keys: where what it saves, a launch and a half-empty chip, is more than the deltas that every workgroup for keys makes for
+// itself (us, two launches / one: bf16 width 64, 64 tokens, 4 heads over 2 11.4 / 6.7, 256 tokens, 8 heads 13.5 / 11.1, 128 tokens, 16 heads
+// over 4 14.8 / 17.3; fp32 width 128, 512 tokens, 8 heads 82.6 / 57.9, 32 heads 119 / 137, 256 tokens in 8 sequences, 32 heads 62 / 60).
+bool both_wanted(const PackedAttention& a) {
+  const int64_t rows = (int64_t)a.tokens * (a.heads / a.kv_heads);
+  return rows <= (a.heads == a.kv_heads ? OWN_ROWS : OWN_ROWS / 2) && workgroups(a, 32, a.heads + a.kv_heads) <= 512;
+}
+template <typename T> hipError_t backward_both(const PackedAttention& a, hipStream_t stream) {
+  const unsigned queries = (unsigned)workgroups(a, 32, a.heads), keys = (unsigned)workgroups(a, 32, a.kv_heads);
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_both_kernel<T, DW>), dim3(queries + keys), dim3(256), 0, stream, a, queries));
+  return hipGetLastError();
+}
 template <typename T> hipError_t backward(const PackedAttention& a, hipStream_t stream) {
+  if (both_wanted(a)) return backward_both<T>(a, stream);
   const hipError_t e = split_wanted<T>(a, false) ? backward_q<T, true>(a, stream) : backward_q<T, false>(a, stream);
   if (e != hipSuccess) return e;
   return split_wanted<T>(a, true) ? backward_kv<T, true>(a, stream) : backward_kv<T, false>(a, stream);
