@@ -12,7 +12,7 @@
 // into LDS of its own (no barrier), and they join their sums at the end.
 // Work is found on the device: sequence s takes offsets[s + 1] / ROWS - offsets[s] / ROWS + 1 workgroups per head, which is what it needs or one more, so
 // that workgroup t's sequence is the last with offsets[s] / ROWS + s <= t: no table, no launch ahead.
-// fp32: the same on 32x32x2 products, tiles of 32 rows instead of 64.
+// fp32: the same with every operand as three bf16 planes (Part), tiles of 32 rows instead of 64.
 #include "elem.h"
 #include "kernels.h"
 
@@ -30,7 +30,7 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 // Tile of `OTHER` rows of one head, DW columns (the width rounded up, zeros behind it), in LDS.  16-byte chunk c of row r sits in slot c ^ swz(r) of the
 // row: 16 consecutive rows' chunk c are 16 different slots modulo 256 bytes, and so are the pieces that a read across rows takes.
 template <typename T, int DW, bool SPLIT> struct Tile {
-  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = CPR / 2;  // steps: 16-byte reads of a row by either lane half
+  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = DW / 16, CHUNKS = CPR / 2;  // products along a row; 16-byte reads of it by either lane half
   static constexpr int OWN = SPLIT ? 32 : 128, OTHER = SPLIT || E == 4 ? 32 : 64, NB = OTHER / 32, OB = DW / 32;
   static constexpr int BYTES = OTHER * DW * E, FILLERS = SPLIT ? 1 : 4, LOADS = BYTES / 1024 / FILLERS;  // wavefronts that fill a tile, loads of each
   static_assert(LOADS * FILLERS * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
@@ -56,20 +56,51 @@ struct Lane {
   __device__ __forceinline__ Lane(unsigned a) : at(a) { asm volatile("" : "+v"(at)); }
 };
 
-// Operand rows r0 .. r0 + 31 (r0 a multiple of 32) of the tile at LDS address `at`, 16-byte step ks of them.
-template <typename Tl> __device__ __forceinline__ unsigned rows_place(int l31, int hi) { return Tl::slot(l31, hi); }
-template <typename Tl> __device__ __forceinline__ uint4 rows_frag(Lane at, int r0, int ks) {
+// Eight values of a lane as an operand of 32x32x16 products.  fp32: three bf16 planes, the upper 8 bits of the significand, the next 8, the last 8,
+// cut and not rounded, so that their sum is the value.  A product of two such operands is six of planes, from the smallest; the three that are left
+// out are below 2^-23 of it, as a rounding of an fp32 product is.  Six at the rate of bf16 are 192 cycles, one on 32x32x2 in fp32 512.
+// (What is infinite has no planes: it gives NaN.)
+template <typename T> struct Part {
+  uint4 v;
+  __device__ __forceinline__ Part() {}
+  __device__ __forceinline__ explicit Part(const uint4* raw) : v(raw[0]) {}
+};
+template <> struct Part<float> {
+  uint32_t w[3][4];
+  __device__ __forceinline__ Part() {}
+  __device__ __forceinline__ explicit Part(const uint4* raw) {
+    const uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) set(i / 2, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+  }
+  __device__ __forceinline__ void set(int pair, float a, float b) {
+#pragma unroll
+    for (int p = 0; p < 3; ++p) {
+      w[p][pair] = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302);  // both upper halves
+      a -= __uint_as_float(__float_as_uint(a) & 0xffff0000u);
+      b -= __uint_as_float(__float_as_uint(b) & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ uint4 plane(int p) const { return make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]); }
+};
+// Operand rows r0 .. r0 + 31 (r0 a multiple of 32) of the tile at LDS address `at`, columns 16 ks .. of them.
+template <typename Tl> __device__ __forceinline__ unsigned rows_place(int l31, int hi) { return Tl::slot(l31, Tl::E == 2 ? hi : 2 * hi); }
+template <typename T, typename Tl> __device__ __forceinline__ Part<T> rows_frag(Lane at, int r0, int ks) {
   typedef unsigned v4u __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(uint4, lds_at<v4u>(Tl::chunk(at.at, 2 * ks) + r0 * Tl::CPR * 16));
+  constexpr int N = Tl::E / 2;
+  uint4 raw[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) raw[i] = __builtin_bit_cast(uint4, lds_at<v4u>(Tl::chunk(at.at, 2 * N * ks + i) + r0 * Tl::CPR * 16));
+  return Part<T>(raw);
 }
-// acc += rows x columns over one 16-byte step of both.
-template <typename T> __device__ __forceinline__ v16f_t step_product(uint4 a, uint4 b, v16f_t c) {
-  if constexpr (sizeof(T) == 2) return mfma_bf16(a, b, c);
+// acc += rows x columns over 16 of both.
+template <typename T> __device__ __forceinline__ v16f_t step_product(const Part<T>& a, const Part<T>& b, v16f_t c) {
+  if constexpr (sizeof(T) == 2) return mfma_bf16(a.v, b.v, c);
   else {
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.x), __uint_as_float(b.x), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.y), __uint_as_float(b.y), c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.z), __uint_as_float(b.z), c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a.w), __uint_as_float(b.w), c, 0, 0, 0);
+    constexpr int order[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};
+#pragma unroll
+    for (int i = 0; i < 6; ++i) c = mfma_bf16(a.plane(order[i][0]), b.plane(order[i][1]), c);
+    return c;
   }
 }
 __device__ __forceinline__ v16f_t zero16() {
@@ -85,7 +116,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((v2f){lo, hi}, v2bf));
 }
 
-// out[ob] += (columns 32 ob .. of the tile's rows r0 .. r0 + 31)^T x p, p as a score block's accumulator holds it (rounded to the element type).
+// out[ob] += (columns 32 ob .. of the tile's rows r0 .. r0 + 31)^T x p, p as a score block's accumulator holds it.
 // bf16: a 16-lane group's addresses are 4 rows by 16 columns, and lane i gets column i of them; `at` of rows 4 hi + .. and `at8` of those 8 on.
 template <typename Tl> __device__ __forceinline__ unsigned across_place(int lane, int rows_on) {
   const int hi = lane >> 5;
@@ -99,26 +130,34 @@ template <typename Tl> __device__ __forceinline__ unsigned across_place(int lane
 template <typename T, typename Tl, int OB>
 __device__ __forceinline__ void across_product(Lane at, Lane at8, int r0, const v16f_t& p, v16f_t (&out)[OB]) {
   constexpr int PITCH = Tl::CPR * 16;
-  if constexpr (sizeof(T) == 2) {
-    typedef __attribute__((address_space(3))) att_v4s* v4s_ptr;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint4 w = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]), pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
+  for (int t = 0; t < 2; ++t) {
+    Part<T> w;  // rounded to the element type
+    if constexpr (sizeof(T) == 2)
+      w.v = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]), pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
+    else
 #pragma unroll
-      for (int ob = 0; ob < OB; ++ob) {
-        union { att_v4s v[2]; uint4 u; } f;
-        f.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at.at, 4 * ob) + (r0 + 16 * t) * PITCH));
-        f.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at8.at, 4 * ob) + (r0 + 16 * t) * PITCH));
-        out[ob] = mfma_bf16(f.u, w, out[ob]);
+      for (int i = 0; i < 4; ++i) w.set(i, p[8 * t + 2 * i], p[8 * t + 2 * i + 1]);
+#pragma unroll
+    for (int ob = 0; ob < OB; ++ob) {
+      Part<T> f;
+      if constexpr (sizeof(T) == 2) {
+        typedef __attribute__((address_space(3))) att_v4s* v4s_ptr;
+        union { att_v4s v[2]; uint4 u; } x;
+        x.v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at.at, 4 * ob) + (r0 + 16 * t) * PITCH));
+        x.v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((v4s_ptr)(uintptr_t)(Tl::chunk(at8.at, 4 * ob) + (r0 + 16 * t) * PITCH));
+        f.v = x.u;
+      } else {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int r = 16 * t + 8 * (i >> 2) + (i & 3);  // + 4 hi: bits of their own
+          x[i] = lds_at<float>((Tl::chunk(at.at, 8 * ob) ^ (Tl::swz(r) << 4)) + (r0 + r) * PITCH);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f.set(i, x[2 * i], x[2 * i + 1]);
       }
-    }
-  } else {
-#pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      const int r = 8 * (v >> 2) + (v & 3);  // + 4 hi: bits of their own
-#pragma unroll
-      for (int ob = 0; ob < OB; ++ob)
-        out[ob] = __builtin_amdgcn_mfma_f32_32x32x2f32(lds_at<float>((Tl::chunk(at.at, 8 * ob) ^ (Tl::swz(r) << 4)) + (r0 + r) * PITCH), p[v], out[ob], 0, 0, 0);
+      out[ob] = step_product<T>(f, w, out[ob]);
     }
   }
 }
@@ -195,14 +234,28 @@ template <typename T> __device__ __forceinline__ uint4 flip(uint4 u) {
   const uint32_t m = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
   return make_uint4(u.x ^ m, u.y ^ m, u.z ^ m, u.w ^ m);
 }
-// One of the wavefront's own rows as a column operand: a lane half's chunks of it, zeros past the width.
-template <typename T, int STEPS> __device__ __forceinline__ void load_own(uint4 (&f)[STEPS], const char* row, int hi, int width) {
+// One of the wavefront's own rows, a lane half's chunks of it, zeros past the width; and as column operands.
+template <typename Tl> struct Own {
+  uint4 raw[Tl::CHUNKS];
+  __device__ __forceinline__ Own(const char* row, int hi, int width) {
+    constexpr int N = Tl::E / 2;
 #pragma unroll
-  for (int ks = 0; ks < STEPS; ++ks) {
-    const int c = 2 * ks + hi;
-    f[ks] = c * Elem<T>::VEC < width ? *reinterpret_cast<const uint4*>(row + 16 * c) : make_uint4(0, 0, 0, 0);
+    for (int k = 0; k < Tl::CHUNKS; ++k) {
+      const int c = 2 * N * (k / N) + N * hi + k % N;
+      raw[k] = c * Tl::VEC < width ? *reinterpret_cast<const uint4*>(row + 16 * c) : make_uint4(0, 0, 0, 0);
+    }
   }
-}
+  template <typename T> __device__ __forceinline__ void parts(Part<T> (&f)[Tl::STEPS], bool turned) const {
+#pragma unroll
+    for (int ks = 0; ks < Tl::STEPS; ++ks) {
+      constexpr int N = Tl::E / 2;
+      uint4 x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = turned ? flip<T>(raw[N * ks + i]) : raw[N * ks + i];
+      f[ks] = Part<T>(x);
+    }
+  }
+};
 // A transposed result (rows = columns 32 ob .., column = the lane's own row) times f -> the row.
 template <typename T, int DW> __device__ __forceinline__ void store_own(T* row, const v16f_t (&acc)[DW / 32], float f, int hi, int width) {
 #pragma unroll
@@ -251,7 +304,8 @@ template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLIT ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
+template <typename T, int DW, bool SPLIT>
+__global__ __launch_bounds__(256, SPLIT || (sizeof(T) == 4 && DW > 96) ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
   using Tl = Tile<T, DW, SPLIT>;
   __shared__ __attribute__((aligned(1024))) char memory[Tl::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
@@ -265,12 +319,8 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
   const char* kbase = base + (int64_t)(a.heads + kv) * W * Tl::E;
   const char* vbase = kbase + (int64_t)a.kv_heads * W * Tl::E;
   const int q = span.first + 32 * rows_of + l31, last = span.first + 32 * rows_of + 31;
-  uint4 qf[Tl::STEPS];
-  load_own<T>(qf, base + (int64_t)min(q, span.len - 1) * row_bytes + (int64_t)head * W * Tl::E, hi, W);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int ks = 0; ks < Tl::STEPS; ++ks) qf[ks] = flip<T>(qf[ks]);
-  }
+  Part<T> qf[Tl::STEPS];
+  Own<Tl>(base + (int64_t)min(q, span.len - 1) * row_bytes + (int64_t)head * W * Tl::E, hi, W).parts(qf, a.scale < 0.f);
   const float c = score_factor(a.scale);
   TileLoads<Tl> loads;
   loads.start(filler, lane, row_bytes, W);
@@ -303,7 +353,7 @@ template <typename T, int DW, bool SPLIT> __global__ __launch_bounds__(256, SPLI
 #pragma unroll
     for (int ks = 0; ks < Tl::STEPS; ++ks)
 #pragma unroll
-      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<Tl>(rows, 32 * b, ks), qf[ks], s[b]);
+      for (int b = 0; b < Tl::NB; ++b) s[b] = step_product<T>(rows_frag<T, Tl>(rows, 32 * b, ks), qf[ks], s[b]);
     if (k0 + Tl::OTHER - 1 > last - 31) {
 #pragma unroll
       for (int b = 0; b < Tl::NB; ++b)
@@ -382,23 +432,18 @@ template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(
   const char* kbase = base + (int64_t)(a.heads + kv) * W * Tl::E;
   const char* vbase = kbase + (int64_t)a.kv_heads * W * Tl::E;
   const int q = span.first + 32 * rows_of + l31, last = span.first + 32 * rows_of + 31, qc = min(q, span.len - 1);
-  uint4 qf[Tl::STEPS], df[Tl::STEPS];
-  load_own<T>(qf, base + (int64_t)qc * row_bytes + (int64_t)head * W * Tl::E, hi, W);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int ks = 0; ks < Tl::STEPS; ++ks) qf[ks] = flip<T>(qf[ks]);
-  }
+  Part<T> qf[Tl::STEPS], df[Tl::STEPS];
+  Own<Tl>(base + (int64_t)qc * row_bytes + (int64_t)head * W * Tl::E, hi, W).parts(qf, a.scale < 0.f);
   const int64_t orow = ((int64_t)(span.begin + qc) * a.heads + head) * W, at = (int64_t)head * a.tokens + span.begin + qc;
-  load_own<T>(df, static_cast<const char*>(a.dout) + orow * Tl::E, hi, W);
   float delta = 0.f;
   {
-    uint4 of[Tl::STEPS];
-    load_own<T>(of, static_cast<const char*>(a.out) + orow * Tl::E, hi, W);
+    const Own<Tl> d(static_cast<const char*>(a.dout) + orow * Tl::E, hi, W), o(static_cast<const char*>(a.out) + orow * Tl::E, hi, W);
+    d.parts(df, false);
 #pragma unroll
-    for (int ks = 0; ks < Tl::STEPS; ++ks) {
+    for (int k = 0; k < Tl::CHUNKS; ++k) {
       Chunk16<T> x, y;
-      x.v = of[ks];
-      y.v = df[ks];
+      x.v = o.raw[k];
+      y.v = d.raw[k];
 #pragma unroll
       for (int e = 0; e < Tl::VEC; ++e) delta += Elem<T>::to_f32(x.e[e]) * Elem<T>::to_f32(y.e[e]);
     }
@@ -436,8 +481,8 @@ template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(
       const Lane rows(rows_of_tile + to);
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<Tl>(rows, 32 * b, ks), qf[ks], s);
-        dp = step_product<T>(rows_frag<Tl>(rows, 32 * b + Tl::OTHER, ks), df[ks], dp);  // (v's tile lies behind k's)
+        s = step_product<T>(rows_frag<T, Tl>(rows, 32 * b, ks), qf[ks], s);
+        dp = step_product<T>(rows_frag<T, Tl>(rows, 32 * b + Tl::OTHER, ks), df[ks], dp);  // (v's tile lies behind k's)
       }
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * (dp[v] - delta);
@@ -487,14 +532,10 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
   const char* obase = static_cast<const char*>(a.dout) + (int64_t)span.begin * out_bytes;
   const int key = span.first + 32 * rows_of + l31, first = span.first + 32 * rows_of, kc = min(key, span.len - 1);
-  uint4 kf[Tl::STEPS], vf[Tl::STEPS];
+  Part<T> kf[Tl::STEPS], vf[Tl::STEPS];
   const char* krow = base + (int64_t)kc * row_bytes + (int64_t)(a.heads + kv) * W * Tl::E;
-  load_own<T>(kf, krow, hi, W);
-  load_own<T>(vf, krow + (int64_t)a.kv_heads * W * Tl::E, hi, W);
-  if (a.scale < 0.f) {
-#pragma unroll
-    for (int ks = 0; ks < Tl::STEPS; ++ks) kf[ks] = flip<T>(kf[ks]);
-  }
+  Own<Tl>(krow, hi, W).parts(kf, a.scale < 0.f);
+  Own<Tl>(krow + (int64_t)a.kv_heads * W * Tl::E, hi, W).parts(vf, false);
   const float c = score_factor(a.scale);
   TileLoads<Tl> qloads, oloads;
   qloads.start(filler, lane, row_bytes, W);
@@ -572,8 +613,8 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
       const Lane rows(rows_of_tile + to + 32 * b * Tl::CPR * 16);
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<Tl>(rows, 0, ks), kf[ks], s);
-        dp = step_product<T>(rows_frag<Tl>(rows, Tl::OTHER, ks), vf[ks], dp);  // (dout's tile lies behind q's)
+        s = step_product<T>(rows_frag<T, Tl>(rows, 0, ks), kf[ks], s);
+        dp = step_product<T>(rows_frag<T, Tl>(rows, Tl::OTHER, ks), vf[ks], dp);  // (dout's tile lies behind q's)
       }
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
