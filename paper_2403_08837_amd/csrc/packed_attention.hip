@@ -23,6 +23,7 @@ namespace cdp {
 namespace {
 
 typedef short att_v4s __attribute__((ext_vector_type(4)));
+typedef float att_v4f __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
@@ -34,9 +35,8 @@ template <typename T, int DW, bool SPLIT> struct Tile {
   static constexpr int OWN = SPLIT ? 32 : 128, OTHER = SPLIT || E == 4 ? 32 : 64, NB = OTHER / 32, OB = DW / 32;
   static constexpr int BYTES = OTHER * DW * E, FILLERS = SPLIT ? 1 : 4, LOADS = BYTES / 1024 / FILLERS;  // wavefronts that fill a tile, loads of each
   static_assert(LOADS * FILLERS * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
-  static constexpr int STAGES = SPLIT && E == 4 && DW > 64 ? 1 : 2;                   // what fits LDS
-  static constexpr int LDS = (SPLIT ? 4 : 1) * STAGES * 2 * BYTES;
-  static_assert(!SPLIT || LDS >= 2 * 4 * 32 * DW * 4, "room for what the wavefronts join");
+  static constexpr int LDS = (SPLIT ? 4 : 2) * 2 * BYTES;                             // two stages, or one for each wavefront, of two tiles
+  static_assert(!SPLIT || LDS >= 4 * 32 * DW * 4, "room for what the wavefronts join");
   __device__ static __forceinline__ int swz(int r) {
     if constexpr (E == 2) return CPR == 16 ? ((r & 3) << 2) | ((r >> 2) & 3) : CPR == 8 ? ((r & 2) << 1) | ((r >> 2) & 3) : (r >> 2) & 3;
     else return CPR % 16 == 0 ? (r & 3) | ((r & 4) << 1) | ((r & 8) >> 1) : (r >> 1) & 7;
@@ -197,15 +197,30 @@ template <typename Tl> struct TileLoads {
     }
   }
 };
-// This wavefront's loads have landed and its LDS reads and writes are done; where tiles are shared, everyone's, and everyone has left the other stage.
-template <bool SPLIT> __device__ __forceinline__ void tile_wait() {
+// Up to 64 floats from `from` (`rows` of them are there) to LDS address `at`; what is not there is zero.
+__device__ __forceinline__ void issue_floats(unsigned at, const float* from, int rows, int lane) {
+  typedef unsigned v4u __attribute__((ext_vector_type(4)));
+  auto uniform = [](unsigned x) { return (unsigned)__builtin_amdgcn_readfirstlane((int)x); };
+  const uintptr_t p = (uintptr_t)from;
+  const v4u buffer = {uniform((unsigned)p), uniform((unsigned)(p >> 32)), uniform(4u * max(rows, 0)), 0x00020000u};
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(4u * lane), "s"(buffer) : "m0");
+#pragma clang diagnostic pop
+}
+// This wavefront's loads but for the newest N have landed (63: no matter), and its LDS reads and writes are done.
+template <int N> __device__ __forceinline__ void wait_newest() {
+  static_assert(N < 64, "vmcnt");
   asm volatile("" ::: "memory");
-  __builtin_amdgcn_s_waitcnt(7 << 4);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));  // vmcnt(N) lgkmcnt(0)
   asm volatile("" ::: "memory");
-  if constexpr (!SPLIT) {
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+// Shared tiles: everyone's loads have landed, and everyone has left the other stage.
+__device__ __forceinline__ void tile_barrier() {
+  wait_newest<0>();
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -305,7 +320,7 @@ template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
 template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, SPLIT || (sizeof(T) == 4 && DW > 96) ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
   using Tl = Tile<T, DW, SPLIT>;
   __shared__ __attribute__((aligned(1024))) char memory[Tl::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
@@ -326,28 +341,18 @@ __global__ __launch_bounds__(256, SPLIT || (sizeof(T) == 4 && DW > 96) ? 1 : 2) 
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
-  auto issue = [&](int i, int stage) {
+    auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
     const int k0 = i * Tl::OTHER;
-    const unsigned at = lds + stage * 2 * Tl::BYTES;
-    loads.issue(at, filler, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
-    loads.issue(at + Tl::BYTES, filler, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    loads.issue(lds + (2 * stage + v) * Tl::BYTES, filler, (v ? vbase : kbase) + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
   const int tiles = (min(span.len, span.first + Tl::OWN) + Tl::OTHER - 1) / Tl::OTHER;
-  v16f_t o[Tl::OB];
+  v16f_t o[Tl::OB], s[Tl::NB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) o[ob] = zero16();
   float m = -INFINITY, z = 0.f;
-  const int from = SPLIT ? wave : 0;
-  if (from < tiles) issue(from, 0);
-  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
-    tile_wait<SPLIT>();
-    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
+  auto scores = [&](int i, int stage) {
     const int k0 = i * Tl::OTHER;
-    if (k0 > last) continue;
-    const unsigned to = stage * 2 * Tl::BYTES;
-    v16f_t s[Tl::NB];
-    const Lane rows(rows_of_tile + to);
+    const Lane rows(rows_of_tile + 2 * stage * Tl::BYTES);
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) s[b] = zero16();
 #pragma unroll
@@ -361,6 +366,8 @@ __global__ __launch_bounds__(256, SPLIT || (sizeof(T) == 4 && DW > 96) ? 1 : 2) 
         for (int v = 0; v < 16; ++v)
           if (k0 + 32 * b + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[b][v] = -INFINITY;
     }
+  };
+  auto probabilities = [&] {
     float mt = s[0][0];
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b)
@@ -387,12 +394,45 @@ __global__ __launch_bounds__(256, SPLIT || (sizeof(T) == 4 && DW > 96) ? 1 : 2) 
       }
       z += (y[0] + y[1]) + (y[2] + y[3]);
     }
-    const Lane across(across_tile + to + Tl::BYTES), across8(across_tile8 + to + Tl::BYTES);
+  };
+  auto values = [&](int stage) {
+    const unsigned to = (2 * stage + 1) * Tl::BYTES;
+    const Lane across(across_tile + to), across8(across_tile8 + to);
 #pragma unroll
     for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(across, across8, 32 * b, s[b], o);
-    if (Tl::STAGES == 1 && i + NEXT < tiles) {
-      tile_wait<SPLIT>();
-      issue(i + NEXT, 0);
+  };
+  if constexpr (SPLIT) {
+    // one tile of each in LDS: the next one of k is under way from the scores on, the next one of v from their product on
+    if (wave < tiles) {
+      issue(wave, 0, false);
+      issue(wave, 0, true);
+    }
+    for (int i = wave; i < tiles; i += 4) {
+      const bool more = i + 4 < tiles;
+      wait_newest<Tl::LOADS>();
+      scores(i, 0);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, false);
+      probabilities();
+      if (more) wait_newest<Tl::LOADS>();
+      else wait_newest<0>();
+      values(0);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, true);
+    }
+  } else {
+    issue(0, 0, false);
+    issue(0, 0, true);
+    for (int i = 0, stage = 0; i < tiles; ++i, stage ^= 1) {
+      tile_barrier();
+      if (i + 1 < tiles) {
+        issue(i + 1, stage ^ 1, false);
+        issue(i + 1, stage ^ 1, true);
+      }
+      if (i * Tl::OTHER > last) continue;
+      scores(i, stage);
+      probabilities();
+      values(stage);
     }
   }
   z = both_halves(z, false);
@@ -456,46 +496,75 @@ template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
-  auto issue = [&](int i, int stage) {
+    auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
     const int k0 = i * Tl::OTHER;
-    const unsigned to = lds + stage * 2 * Tl::BYTES;
-    loads.issue(to, filler, kbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
-    loads.issue(to + Tl::BYTES, filler, vbase + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
+    loads.issue(lds + (2 * stage + v) * Tl::BYTES, filler, (v ? vbase : kbase) + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
   const int tiles = (min(span.len, span.first + Tl::OWN) + Tl::OTHER - 1) / Tl::OTHER;
   v16f_t dq[Tl::OB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) dq[ob] = zero16();
-  const int from = SPLIT ? wave : 0;
-  if (from < tiles) issue(from, 0);
-  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
-    tile_wait<SPLIT>();
-    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
-    const unsigned to = stage * 2 * Tl::BYTES;
+  auto dprobabilities = [&](v16f_t& dp, int b, int stage) {
+    const Lane rows(rows_of_tile + (2 * stage + 1) * Tl::BYTES);
+    dp = zero16();
 #pragma unroll
-    for (int b = 0; b < Tl::NB; ++b) {
-      const int k0 = i * Tl::OTHER + 32 * b;
-      if (k0 > last) continue;
-      v16f_t s = zero16(), dp = zero16();
-      const Lane rows(rows_of_tile + to);
+    for (int ks = 0; ks < Tl::STEPS; ++ks) dp = step_product<T>(rows_frag<T, Tl>(rows, 32 * b, ks), df[ks], dp);
+  };
+  auto scores = [&](v16f_t& s, int b, int stage) {
+    const Lane rows(rows_of_tile + 2 * stage * Tl::BYTES);
+    s = zero16();
 #pragma unroll
-      for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<T, Tl>(rows, 32 * b, ks), qf[ks], s);
-        dp = step_product<T>(rows_frag<T, Tl>(rows, 32 * b + Tl::OTHER, ks), df[ks], dp);  // (v's tile lies behind k's)
-      }
+    for (int ks = 0; ks < Tl::STEPS; ++ks) s = step_product<T>(rows_frag<T, Tl>(rows, 32 * b, ks), qf[ks], s);
+  };
+  auto finish = [&](v16f_t& s, const v16f_t& dp, int k0, int b, int stage) {  // dS, and dq from it
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * (dp[v] - delta);
-      if (k0 + 31 > last - 31) {
+    for (int v = 0; v < 16; ++v) s[v] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[v], c, -lse)) * (dp[v] - delta);
+    if (k0 + 31 > last - 31) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (k0 + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[v] = 0.f;
-      }
-      across_product<T, Tl>(Lane(across_tile + to), Lane(across_tile8 + to), 32 * b, s, dq);
+      for (int v = 0; v < 16; ++v)
+        if (k0 + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[v] = 0.f;
     }
-    if (Tl::STAGES == 1 && i + NEXT < tiles) {
-      tile_wait<SPLIT>();
-      issue(i + NEXT, 0);
+    const unsigned to = 2 * stage * Tl::BYTES;
+    across_product<T, Tl>(Lane(across_tile + to), Lane(across_tile8 + to), 32 * b, s, dq);
+  };
+  if constexpr (SPLIT) {
+    // v's tile is read first and given back first: the next one of it is under way while k's is in use, and k's under the next product with v
+    if (wave < tiles) {
+      issue(wave, 0, true);
+      issue(wave, 0, false);
+    }
+    for (int i = wave; i < tiles; i += 4) {
+      const bool more = i + 4 < tiles;
+      v16f_t s, dp;
+      wait_newest<Tl::LOADS>();
+      dprobabilities(dp, 0, 0);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, true);
+      if (more) wait_newest<Tl::LOADS>();
+      else wait_newest<0>();
+      scores(s, 0, 0);
+      finish(s, dp, 32 * i, 0, 0);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, false);
+    }
+  } else {
+    issue(0, 0, false);
+    issue(0, 0, true);
+    for (int i = 0, stage = 0; i < tiles; ++i, stage ^= 1) {
+      tile_barrier();
+      if (i + 1 < tiles) {
+        issue(i + 1, stage ^ 1, false);
+        issue(i + 1, stage ^ 1, true);
+      }
+#pragma unroll
+      for (int b = 0; b < Tl::NB; ++b) {
+        const int k0 = i * Tl::OTHER + 32 * b;
+        if (k0 > last) continue;
+        v16f_t s, dp;
+        scores(s, b, stage);
+        dprobabilities(dp, b, stage);
+        finish(s, dp, k0, b, stage);
+      }
     }
   }
   T* const row = static_cast<T*>(a.dqkv) + (int64_t)(span.begin + q) * (a.heads + 2 * a.kv_heads) * W + head * W;
@@ -509,7 +578,7 @@ template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(
   }
 }
 template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 96 ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   bwd_q<T, DW, SPLIT>(a, smem, blockIdx.x, gridDim.x, true);
@@ -522,7 +591,7 @@ __global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 96) ? 2 : 1)
 constexpr int OWN_ROWS = 512;
 template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ void bwd_kv(const PackedAttention& a, unsigned smem, unsigned wg, int shares) {
   using Tl = Tile<T, DW, SPLIT>;
-  __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 1][2][2][Tl::OTHER];  // per stage: lse (in log2), delta
+  __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 2][2][64];  // per wavefront or stage: lse and delta of the tile's rows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int share = wg % shares, kv = wg / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
@@ -542,13 +611,8 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   oloads.start(filler, lane, out_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-  constexpr int NEXT = SPLIT ? 4 : 1;  // tiles from one of the wavefront's to its next
-  const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
+    const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
   const int head0 = kv * group + share * (group / shares);
-  constexpr int STATS = 2 * Tl::OTHER, LOADERS = SPLIT ? 64 : 256;
-  static_assert(STATS <= LOADERS, "a statistic per thread");
-  const int id = SPLIT ? lane : (int)threadIdx.x;
-  float stat = 0.f;  // of the tile under way
   __shared__ float own_memory[OWN ? OWN_ROWS : 1];  // [head of the group][query - first]
   const unsigned own = (unsigned)(uintptr_t)(lds_ptr)own_memory;
   const int own_rows = span.len - span.first;
@@ -576,69 +640,95 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
     }
     __syncthreads();
   }
-  auto issue = [&](int i, int stage) {
-    const unsigned to = lds + stage * 2 * Tl::BYTES;
-    const int head = head0 + i / per_head, q0 = span.first + i % per_head * Tl::OTHER;
+  const unsigned stats_at = (unsigned)(uintptr_t)(lds_ptr)stats + (SPLIT ? 512 * wave : 0);
+  // tiles of q, then of dout, with it what is kept of its rows.  Rows past the sequence are zeros in all of them, which add nothing.
+  auto issue = [&](int i, int stage, bool o) {
+    const unsigned to = lds + (2 * stage + o) * Tl::BYTES;
+    const int head = head0 + i / per_head, q0 = span.first + i % per_head * Tl::OTHER, rows = span.len - q0;
     const int64_t col = (int64_t)head * W * Tl::E;
-    qloads.issue(to, filler, base + (int64_t)q0 * row_bytes + col, span.len - q0, row_bytes, W);
-    oloads.issue(to + Tl::BYTES, filler, obase + (int64_t)q0 * out_bytes + col, span.len - q0, out_bytes, W);
-    if (id < STATS) {
-      // rows past the sequence: exp(score - inf) is a probability of zero
-      const bool is_lse = id < Tl::OTHER;
-      const int q = q0 + id % Tl::OTHER;
-      const int qc = min(q, span.len - 1);
-      float x;
-      if (OWN && !is_lse) x = lds_at<float>(own + 4 * ((head - head0) * own_rows + qc - span.first));
-      else x = ((is_lse ? a.lse : a.delta) + (int64_t)head * a.tokens + span.begin)[qc];
-      stat = is_lse ? (q < span.len ? x * LOG2E : INFINITY) : (q < span.len ? x : 0.f);
+    if (!o) return qloads.issue(to, filler, base + (int64_t)q0 * row_bytes + col, rows, row_bytes, W);
+    const int64_t at = (int64_t)head * a.tokens + span.begin + q0;
+    const unsigned st = stats_at + 512 * stage;
+    if (SPLIT || wave == 0) issue_floats(st, a.lse + at, min(rows, Tl::OTHER), lane);
+    if constexpr (OWN) {
+      if (lane < Tl::OTHER) lds_put(st + 256 + 4 * lane, lane < rows ? lds_at<float>(own + 4 * ((head - head0) * own_rows + q0 - span.first + lane)) : 0.f);
+    } else if (SPLIT || wave == 1) {
+      issue_floats(st + 256, a.delta + at, min(rows, Tl::OTHER), lane);
     }
+    oloads.issue(to, filler, obase + (int64_t)q0 * out_bytes + col, rows, out_bytes, W);
   };
   v16f_t dk[Tl::OB], dv[Tl::OB];
 #pragma unroll
   for (int ob = 0; ob < Tl::OB; ++ob) dk[ob] = dv[ob] = zero16();
-  const int from = SPLIT ? wave : 0;
-  if (from < tiles) issue(from, 0);
-  for (int i = from, stage = 0; i < tiles; i += NEXT, stage ^= Tl::STAGES - 1) {
-    float(*const st)[Tl::OTHER] = stats[SPLIT ? wave : 0][stage];
-    if (id < STATS) st[id / Tl::OTHER][id % Tl::OTHER] = stat;
-    tile_wait<SPLIT>();
-    if (Tl::STAGES == 2 && i + NEXT < tiles) issue(i + NEXT, stage ^ 1);
-    const unsigned to = stage * 2 * Tl::BYTES;
-    const int t0 = span.first + i % per_head * Tl::OTHER;
-#pragma unroll 1
-    for (int b = 0; b < Tl::NB; ++b) {
-      const int b0 = t0 + 32 * b;
-      if (b0 + 31 < first || b0 >= span.len) continue;
-      v16f_t s = zero16(), dp = zero16();
-      const Lane rows(rows_of_tile + to + 32 * b * Tl::CPR * 16);
+  auto statistics = [&](int which, int row, int stage) { return lds_at<att_v4f>(stats_at + 512 * stage + 256 * which + 4 * row); };
+  // P from the scores, dS from dP
+  auto finish = [&](v16f_t& s, v16f_t& dp, int b0, int b, int stage) {
 #pragma unroll
-      for (int ks = 0; ks < Tl::STEPS; ++ks) {
-        s = step_product<T>(rows_frag<T, Tl>(rows, 0, ks), kf[ks], s);
-        dp = step_product<T>(rows_frag<T, Tl>(rows, Tl::OTHER, ks), vf[ks], dp);  // (dout's tile lies behind q's)
+    for (int g = 0; g < 4; ++g) {
+      const att_v4f l = statistics(0, 32 * b + 8 * g + 4 * hi, stage), d = statistics(1, 32 * b + 8 * g + 4 * hi, stage);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[4 * g + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + e], c, -LOG2E * l[e]));
+        dp[4 * g + e] = s[4 * g + e] * (dp[4 * g + e] - d[e]);
       }
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const float4 lse = *reinterpret_cast<const float4*>(&st[0][32 * b + 8 * g + 4 * hi]);
-        const float4 delta = *reinterpret_cast<const float4*>(&st[1][32 * b + 8 * g + 4 * hi]);
-        const float l[4] = {lse.x, lse.y, lse.z, lse.w}, d[4] = {delta.x, delta.y, delta.z, delta.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[4 * g + e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[4 * g + e], c, -l[e]));
-          dp[4 * g + e] = s[4 * g + e] * (dp[4 * g + e] - d[e]);
-        }
-      }
-      if (b0 < first + 31) {
-#pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (b0 + 8 * (v >> 2) + 4 * hi + (v & 3) < key) s[v] = dp[v] = 0.f;
-      }
-      const Lane across(across_tile + to + 32 * b * Tl::CPR * 16), across8(across_tile8 + to + 32 * b * Tl::CPR * 16);
-      across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
-      across_product<T, Tl>(across, across8, 0, dp, dk);
     }
-    if (Tl::STAGES == 1 && i + NEXT < tiles) {
-      tile_wait<SPLIT>();
-      issue(i + NEXT, 0);
+    if (b0 < first + 31) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (b0 + 8 * (v >> 2) + 4 * hi + (v & 3) < key) s[v] = dp[v] = 0.f;
+    }
+  };
+  if constexpr (SPLIT) {
+    // dout's tile is read first and given back first, as v's in the kernel for queries
+    if (wave < tiles) {
+      issue(wave, 0, true);
+      issue(wave, 0, false);
+    }
+    for (int i = wave; i < tiles; i += 4) {
+      const bool more = i + 4 < tiles;
+      const Lane rows(rows_of_tile), across(across_tile), across8(across_tile8);
+      v16f_t s = zero16(), dp = zero16();
+      wait_newest<Tl::LOADS>();
+#pragma unroll
+      for (int ks = 0; ks < Tl::STEPS; ++ks) dp = step_product<T>(rows_frag<T, Tl>(rows, Tl::OTHER, ks), vf[ks], dp);
+      wait_newest<0>();
+#pragma unroll
+      for (int ks = 0; ks < Tl::STEPS; ++ks) s = step_product<T>(rows_frag<T, Tl>(rows, 0, ks), kf[ks], s);
+      finish(s, dp, span.first + i % per_head * 32, 0, 0);
+      across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, true);
+      across_product<T, Tl>(across, across8, 0, dp, dk);
+      wait_newest<63>();
+      if (more) issue(i + 4, 0, false);
+    }
+  } else {
+    issue(0, 0, false);
+    issue(0, 0, true);
+    for (int i = 0, stage = 0; i < tiles; ++i, stage ^= 1) {
+      tile_barrier();
+      if (i + 1 < tiles) {
+        issue(i + 1, stage ^ 1, false);
+        issue(i + 1, stage ^ 1, true);
+      }
+      const int t0 = span.first + i % per_head * Tl::OTHER;
+#pragma unroll 1
+      for (int b = 0; b < Tl::NB; ++b) {
+        const int b0 = t0 + 32 * b;
+        if (b0 + 31 < first || b0 >= span.len) continue;
+        v16f_t s = zero16(), dp = zero16();
+        const unsigned to = 2 * stage * Tl::BYTES + 32 * b * Tl::CPR * 16;
+        const Lane rows(rows_of_tile + to);
+#pragma unroll
+        for (int ks = 0; ks < Tl::STEPS; ++ks) {
+          s = step_product<T>(rows_frag<T, Tl>(rows, 0, ks), kf[ks], s);
+          dp = step_product<T>(rows_frag<T, Tl>(rows, Tl::OTHER, ks), vf[ks], dp);  // (dout's tile lies behind q's)
+        }
+        finish(s, dp, b0, b, stage);
+        const Lane across(across_tile + to), across8(across_tile8 + to);
+        across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
+        across_product<T, Tl>(across, across8, 0, dp, dk);
+      }
     }
   }
   // to dqkv, or to the share's sums
@@ -647,11 +737,12 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
     if constexpr (SPLIT) {
       __syncthreads();
       put_share(smem + wave * DW * 128, dk, 1.f, l31, hi);
-      put_share(smem + (4 + wave) * DW * 128, dv, 1.f, l31, hi);
       __syncthreads();
-      if (key >= span.len) return;
-      join_shares<R, DW>(row, smem, a.scale, wave, l31, hi, W);
-      join_shares<R, DW>(row + v_from_k, smem + 4 * DW * 128, 1.f, wave, l31, hi, W);
+      if (key < span.len) join_shares<R, DW>(row, smem, a.scale, wave, l31, hi, W);
+      __syncthreads();
+      put_share(smem + wave * DW * 128, dv, 1.f, l31, hi);
+      __syncthreads();
+      if (key < span.len) join_shares<R, DW>(row + v_from_k, smem, 1.f, wave, l31, hi, W);
     } else {
       if (key >= span.len) return;
       store_own<R, DW>(row, dk, a.scale, hi, W);
@@ -664,7 +755,7 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
     write(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W, (int64_t)a.kv_heads * W);
 }
 template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, !SPLIT && (sizeof(T) == 2 || DW < 64) ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && (DW < 128 || !SPLIT)) || DW < 64 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   bwd_kv<T, DW, SPLIT, false>(a, smem, blockIdx.x, shares);
