@@ -801,24 +801,31 @@ template <typename T> __global__ __launch_bounds__(256) void packed_bwd_fold_ker
 int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int64_t)a.tokens / own + a.sequences) * heads; }
 
 // Whether the wavefronts of a workgroup share 32 rows' other side (SPLIT) instead of having 32 rows each: a quarter of the way through the longest sequence
-// for the few workgroups that there are, against filling LDS four times as often.  Worth it while the workgroups of 128 rows do not fill the chip; to
-// what count grows with the split workgroups that a CU's LDS holds.  us, 128 rows / split, one sequence or more as said:
-//   bf16 forward, width 32: 72 workgroups 14.4 / 8.2, 384 10.9 / 8.9, 528 46.1 / 46.7; 64: 72 17.5 / 9.8, 272 31.5 / 25.8, 384 13.3 / 13.3, 528
-//   61.6 / 72.4; 128: 72 24.3 / 14.0, 144 24.6 / 19.3, 192 34.1 / 34.6, 528 95.8 / 163.2 (dq crosses at the same counts);
-//   dk and dv, 64: 272 98 / 79, 384 37 / 36, 528 207 / 212; 128: 272 191 / 161, 384 77 / 76, 528 420 / 477;
-//   fp32 forward, 32: 528 218 / 170, 1056 341 / 330; 128: 384 111 / 72, 640 259 / 211, 1056 1202 / 1364; dq, 128: 384 -26, 528 +98; dk and dv -31, +222.
+// for the few workgroups that there are, against filling LDS four times as often.  Worth it while the workgroups of 128 rows do not fill the chip; up to
+// what count goes by the workgroups that a CU holds, which registers and LDS of wide heads and of fp32 keep down.  us, 128 rows / split, at so many
+// workgroups of 128 rows:
+//   forward, bf16 width 64: 272 28.9 / 19.5, 384 18.6 / 13.4, 528 59.7 / 64.0; 128: 272 41.7 / 33.4, 384 17.8 / 17.8, 528 94 / 111; fp32 64: 528 265 / 230,
+//   792 345 / 345; 128: 264 408 / 271, 384 73 / 63, 528 463 / 531 (dq crosses at the same counts);
+//   backward by its kernel for keys, bf16 64: 528 204 / 185, 768 57.6 / 53.2, 896 93 / 98; 96: 528 255 / 255; 128: 192 115 / 106, 272 152 / 153, 384 60 / 73;
+//   fp32 64: 384 123 / 114, 528 889 / 927; 128: 264 1488 / 1441, 384 240 / 254.
 template <typename T> bool split_wanted(const PackedAttention& a, bool kv) {
-  const int resident = sizeof(T) == 2 ? (a.width <= 32 ? 4 : a.width <= 64 ? 2 : 1) : (a.width <= 32 ? 2 : 1);
-  const int most = sizeof(T) == 4 ? 400 * resident : kv ? 256 + 64 * resident : 48 + 128 * resident;
-  return a.tokens > 64 && workgroups(a, 128, a.heads) <= most;  // (one tile of 64 rows has nothing to share: one token, backward, 9.1 / 10.9)
+  int most;
+  if (!kv) most = sizeof(T) == 2 ? (a.width <= 64 ? 500 : 330) : (a.width <= 64 ? 800 : 400);
+  else if (sizeof(T) == 2) most = a.width <= 64 ? 768 : a.width <= 96 ? 500 : 230;
+  else most = a.width <= 32 ? 800 : a.width <= 96 ? 450 : 260;
+  return a.tokens > 64 && workgroups(a, 128, a.heads) <= most;  // (one tile of 64 rows has nothing to share)
 }
-// Workgroups that share a key tile's query heads: as few as make 2048 workgroups, four rounds of two per CU (a causal launch's workgroups differ in
-// length by as much as their tiles are many, and the longest, which start first, have to be short against the whole).
+// Workgroups that share a key tile's query heads: as few as make 1024 workgroups, two rounds of two per CU (a causal launch's workgroups differ in
+// length by as much as their tiles are many, and the longest, which start first, have to be short against the whole).  Not where sequences are
+// shorter than a tile on average: there is nothing to share.  us, backward in bf16, unshared / at 512 / 1024 / 2048: 8192 tokens, 32 heads of 128 over 8
+// 2150 / 2147 / 1785 / 1791; 4096 tokens, 16 heads of 64 over 4 215 / 215 / 175 / 178, in 16 sequences 65 / 65 / 57 / 62; 500 tokens in 60, 32 heads over 8
+// 20 / 25 / 29 / 29.
 int shares_of(const PackedAttention& a, int own) {
   const int group = a.heads / a.kv_heads;
   const int64_t have = workgroups(a, own, a.kv_heads);
   int shares = 1;
-  for (int n = 2; n <= group && have * shares < 2048; ++n)
+  if (a.tokens / 32 < a.sequences) return shares;
+  for (int n = 2; n <= group && have * shares < 1024; ++n)
     if (group % n == 0 && n <= a.max_parts) shares = n;
   return shares;
 }
