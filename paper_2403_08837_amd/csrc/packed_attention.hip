@@ -807,12 +807,14 @@ int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int6
 //   forward, bf16 width 64: 272 28.9 / 19.5, 384 18.6 / 13.4, 528 59.7 / 64.0; 128: 272 41.7 / 33.4, 384 17.8 / 17.8, 528 94 / 111; fp32 64: 528 265 / 230,
 //   792 345 / 345; 128: 264 408 / 271, 384 73 / 63, 528 463 / 531 (dq crosses at the same counts);
 //   backward by its kernel for keys, bf16 64: 528 204 / 185, 768 57.6 / 53.2, 896 93 / 98; 96: 528 255 / 255; 128: 192 115 / 106, 272 152 / 153, 384 60 / 73;
-//   fp32 64: 384 123 / 114, 528 889 / 927; 128: 264 1488 / 1441, 384 240 / 254.
+//   fp32 64: 384 123 / 114, 528 889 / 927; 128: 264 1488 / 1441, 384 240 / 254.  Where query heads share a key head, 128 rows need their shares' fold too:
+//   bf16 128: 2048 tokens, 16 heads over 2 216 / 150, 4096 tokens, 16 over 4 329 / 455.
 template <typename T> bool split_wanted(const PackedAttention& a, bool kv) {
   int most;
   if (!kv) most = sizeof(T) == 2 ? (a.width <= 64 ? 500 : 330) : (a.width <= 64 ? 800 : 400);
-  else if (sizeof(T) == 2) most = a.width <= 64 ? 768 : a.width <= 96 ? 500 : 230;
-  else most = a.width <= 32 ? 800 : a.width <= 96 ? 450 : 260;
+  else if (a.width > 96) most = a.heads > a.kv_heads ? 380 : 240;
+  else if (sizeof(T) == 2) most = a.width <= 64 ? 768 : 500;
+  else most = a.width <= 32 ? 800 : 450;
   return a.tokens > 64 && workgroups(a, 128, a.heads) <= most;  // (one tile of 64 rows has nothing to share)
 }
 // Workgroups that share a key tile's query heads: as few as make 1024 workgroups, two rounds of two per CU (a causal launch's workgroups differ in
