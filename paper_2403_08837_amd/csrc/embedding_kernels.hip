@@ -149,68 +149,86 @@ __global__ __launch_bounds__(256) void embedding_bwd_few_kernel(const int32_t* i
 }
 
 // ---- backward, sorted ---------------------------------------------------------------------------------------------------
-// Zeros to the part of the table that is `THREADS` * 64 bytes of workgroup `block`'s.
-constexpr int CLEAR = 16384;  // elements of a workgroup of 1024; of one of 256 a quarter
-template <int THREADS> __device__ __forceinline__ void clear_table(float* table, int64_t elements, int64_t block) {
-  const int t = threadIdx.x;
-  const int64_t head = min((int64_t)((16 - reinterpret_cast<uintptr_t>(table) % 16) % 16 / 4), elements), pieces = (elements - head) / 4;
-  float4* const to = reinterpret_cast<float4*>(table + head);
-  const int64_t e = block * (THREADS * 4) + t;
-#pragma unroll
-  for (int u = 0; u < 4; ++u)
-    if (e + THREADS * u < pieces) to[e + THREADS * u] = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (block == 0) {
-    if (t < head) table[t] = 0.f;
-    const int64_t tail = head + 4 * pieces + t;
+// Zeros to a workgroup's part of the table, one 16-byte piece a thread (1 GB so 152 us in workgroups of 256 and 166 in workgroups of 1024, four pieces a
+// thread 171 and 190, a grid that walks the table 208 and more).  Pieces are counted from `first`.
+__device__ __forceinline__ void clear_table(float* table, int64_t elements, int64_t first) {
+  const int64_t head = min((int64_t)((16 - reinterpret_cast<uintptr_t>(table) % 16) % 16 / 4), elements), pieces = (elements - head) / 4, e = first + threadIdx.x;
+  if (e < pieces) reinterpret_cast<float4*>(table + head)[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (first == 0) {
+    if ((int)threadIdx.x < head) table[threadIdx.x] = 0.f;
+    const int64_t tail = head + 4 * pieces + threadIdx.x;
     if (tail < elements) table[tail] = 0.f;
   }
 }
-// Workgroups 0 .. runs - 1 sort a run each (ids that are no word come last); the others clear the table.  A key is the word and the place in the run, two
-// keys a thread; keys 2 to 64 apart are exchanged between lanes, farther ones through LDS (every step through LDS with a barrier: 14 us instead of 6).
+// The value of lane `lane ^ M`.
+template <int M> __device__ __forceinline__ uint32_t across_lanes(uint32_t v, int lane) {
+  if constexpr (M == 1) return __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xf, 0xf, false);
+  else if constexpr (M == 2) return __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xf, 0xf, false);
+  else if constexpr (M == 4) {  // four on for the lower four of eight, four back for the upper
+    const uint32_t x = __builtin_amdgcn_update_dpp(0, v, 0x104, 0xf, 0x5, false);
+    return __builtin_amdgcn_update_dpp(x, v, 0x114, 0xf, 0xa, false);
+  } else if constexpr (M == 8) return __builtin_amdgcn_update_dpp(0, v, 0x128, 0xf, 0xf, false);
+  else if constexpr (M == 16) {
+    const auto x = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    return lane & 16 ? x[0] : x[1];
+  } else {
+    const auto x = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return lane & 32 ? x[0] : x[1];
+  }
+}
+template <int M> __device__ __forceinline__ uint64_t across_lanes(uint64_t v, int lane) {
+  return (uint64_t)across_lanes<M>((uint32_t)(v >> 32), lane) << 32 | across_lanes<M>((uint32_t)v, lane);
+}
+// Workgroups 0 .. runs - 1 sort a run each (ids that are no word come last); the others clear the table.  A key is the word and the place in the run,
+// two neighbours a thread; keys less than 128 apart are exchanged between lanes without LDS, ten steps of 66 go through LDS (every one of them 14 us; eight keys
+// a thread of 256, where three steps are left, 11).
+constexpr int SORTERS = 1024;
 template <typename Key>
-__global__ __launch_bounds__(1024) void embedding_sort_kernel(const int32_t* ids, uint32_t* word, int* token, float* dtable, int64_t elements, int rows, int vocab, int runs) {
-  if ((int)blockIdx.x >= runs) return clear_table<1024>(dtable, elements, blockIdx.x - runs);
-  constexpr int BITS = 11;
+__global__ __launch_bounds__(SORTERS) void embedding_sort_kernel(const int32_t* ids, uint32_t* word, int* token, float* dtable, int64_t elements, int rows, int vocab, int runs) {
+  if ((int)blockIdx.x >= runs) return clear_table(dtable, elements, (int64_t)(blockIdx.x - runs) * SORTERS);
+  constexpr int BITS = 11, K = RUN / SORTERS;
   static_assert(RUN == 1 << BITS, "a place in the run");
   __shared__ Key keys[RUN];
-  const int i = 2 * threadIdx.x;
+  const int lane = threadIdx.x & 63, i = K * threadIdx.x;
   const uint32_t base = blockIdx.x * RUN;
-  Key k[2];
+  Key k[K];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
+  for (int u = 0; u < K; ++u) {
     const uint32_t at = base + i + u, id = at < (uint32_t)rows ? (uint32_t)ids[at] : ~0u;
     k[u] = ((Key)min(id, (uint32_t)vocab) << BITS) | (i + u);
   }
   auto keep = [](Key mine, Key other, bool low) { return low == (mine < other) ? mine : other; };
+  static_for<BITS>([&](auto s) {
+    constexpr int size = 2 << decltype(s)::value;
+    static_for<decltype(s)::value + 1>([&](auto d) {
+      constexpr int stride = size >> (decltype(d)::value + 1);
+      if constexpr (stride >= K) {
+        const bool low = ((i & stride) == 0) == ((i & size) == 0);
+        if constexpr (stride < 64 * K) {
 #pragma unroll
-  for (int size = 2; size <= RUN; size <<= 1) {
-    const bool up = (i & size) == 0;
+          for (int u = 0; u < K; ++u) k[u] = keep(k[u], across_lanes<stride / K>(k[u], lane), low);
+        } else {
+          __syncthreads();
 #pragma unroll
-    for (int stride = size >> 1; stride > 1; stride >>= 1) {
-      const bool low = ((i & stride) == 0) == up;
-      if (stride <= 64) {
+          for (int u = 0; u < K; ++u) keys[u * SORTERS + threadIdx.x] = k[u];
+          __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Key other;
-          if constexpr (sizeof(Key) == 4) other = __shfl_xor(k[u], stride >> 1, 64);
-          else other = (Key)(unsigned long long)__shfl_xor((unsigned long long)k[u], stride >> 1, 64);
-          k[u] = keep(k[u], other, low);
+          for (int u = 0; u < K; ++u) k[u] = keep(k[u], keys[u * SORTERS + (threadIdx.x ^ (stride / K))], low);
         }
       } else {
-        __syncthreads();
-        keys[i] = k[0];
-        keys[i + 1] = k[1];
-        __syncthreads();
 #pragma unroll
-        for (int u = 0; u < 2; ++u) k[u] = keep(k[u], keys[(i ^ stride) + u], low);
+        for (int u = 0; u < K; ++u)
+          if (!(u & stride)) {
+            const bool up = size < K ? (u & size) == 0 : (i & size) == 0;
+            const Key x = k[u], y = k[u | stride];
+            k[u] = keep(x, y, up);
+            k[u | stride] = keep(y, x, !up);
+          }
       }
-    }
-    const Key x = k[0], y = k[1];
-    k[0] = keep(x, y, up);
-    k[1] = keep(y, x, !up);
-  }
+    });
+  });
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
+  for (int u = 0; u < K; ++u) {
     const uint32_t w = (uint32_t)(k[u] >> BITS);
     if (base + i + u < (uint32_t)rows) {
       word[base + i + u] = w < (uint32_t)vocab ? w : ~0u;
@@ -222,7 +240,7 @@ __global__ __launch_bounds__(1024) void embedding_sort_kernel(const int32_t* ids
 // earlier runs and smaller ones of later runs before it.  Workgroups past `merging` clear the rest of the table.
 __global__ __launch_bounds__(256) void embedding_merge_kernel(const uint32_t* word, const int* token, uint32_t* word_out, int* token_out, int rows, int run, float* dtable,
                                                               int64_t elements, int64_t merging, int64_t cleared) {
-  if (blockIdx.x >= merging) return clear_table<256>(dtable, elements, blockIdx.x - merging + cleared);
+  if (blockIdx.x >= merging) return clear_table(dtable, elements, (blockIdx.x - merging) * 256 + cleared);
   const int64_t e = (int64_t)blockIdx.x * (256 / WAYS) + threadIdx.x / WAYS;
   if (e >= rows) return;
   const int q = threadIdx.x % WAYS;
@@ -376,17 +394,18 @@ hipError_t backward(const int32_t* ids, const T* dout, float* dtable, float scal
   int* token[2] = {reinterpret_cast<int*>(word[1] + rows), reinterpret_cast<int*>(word[1] + rows) + rows};
   float* part = static_cast<float*>(workspace) + (4ll * rows + 63) / 64 * 64;
   const int runs = (int)((rows + (int64_t)RUN - 1) / RUN);
-  // the table is cleared beside the sort and, where there is one, the first merge, half each: neither fills the chip
-  const int64_t elements = (int64_t)vocab * C, clear = accumulate ? 0 : (elements + CLEAR - 1) / CLEAR, beside_sort = runs > 1 ? (clear + 1) / 2 : clear;
-  const dim3 sorting((unsigned)(runs + beside_sort));
-  if (vocab < (1 << 20)) hipLaunchKernelGGL((embedding_sort_kernel<uint32_t>), sorting, dim3(1024), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
-  else hipLaunchKernelGGL((embedding_sort_kernel<uint64_t>), sorting, dim3(1024), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
+  // the table is cleared beside the sort and, where there is one, the first merge, whose workgroups are smaller: a third and two thirds
+  const int64_t elements = (int64_t)vocab * C, clear = accumulate ? 0 : elements / 4 + 1, beside_sort = (runs > 1 ? (clear + 2) / 3 : clear) + SORTERS - 1;
+  const int64_t first = beside_sort / SORTERS * SORTERS * (clear > 0);  // pieces
+  const dim3 sorting((unsigned)(runs + first / SORTERS));
+  if (vocab < (1 << 20)) hipLaunchKernelGGL((embedding_sort_kernel<uint32_t>), sorting, dim3(SORTERS), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
+  else hipLaunchKernelGGL((embedding_sort_kernel<uint64_t>), sorting, dim3(SORTERS), 0, stream, ids, word[0], token[0], dtable, elements, rows, vocab, runs);
   hipError_t e = hipGetLastError();
   int at = 0;
   for (int64_t run = RUN; run < rows && e == hipSuccess; run *= WAYS, at ^= 1) {
-    const int64_t merging = ((int64_t)rows * WAYS + 255) / 256, clearing = run == RUN ? 4 * (clear - beside_sort) : 0;
+    const int64_t merging = ((int64_t)rows * WAYS + 255) / 256, clearing = run == RUN ? (std::max<int64_t>(clear - first, 0) + 255) / 256 : 0;
     hipLaunchKernelGGL(embedding_merge_kernel, dim3((unsigned)(merging + clearing)), dim3(256), 0, stream, word[at], token[at], word[at ^ 1], token[at ^ 1], rows, (int)run, dtable,
-                       elements, merging, 4 * beside_sort);
+                       elements, merging, first);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
