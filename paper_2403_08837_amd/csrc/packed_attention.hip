@@ -127,15 +127,24 @@ template <typename Tl> __device__ __forceinline__ unsigned across_place(int lane
     return Tl::slot(4 * hi, (lane & 31) >> 2) + 4 * (lane & 3);
   }
 }
-template <typename T, typename Tl, int OB>
+// FINE (bf16): p not rounded to bf16 but in two planes, its rounding and what that leaves.
+template <typename T, typename Tl, bool FINE, int OB>
 __device__ __forceinline__ void across_product(Lane at, Lane at8, int r0, const v16f_t& p, v16f_t (&out)[OB]) {
   constexpr int PITCH = Tl::CPR * 16;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    Part<T> w;  // rounded to the element type
-    if constexpr (sizeof(T) == 2)
-      w.v = make_uint4(pack2(p[8 * t], p[8 * t + 1]), pack2(p[8 * t + 2], p[8 * t + 3]), pack2(p[8 * t + 4], p[8 * t + 5]), pack2(p[8 * t + 6], p[8 * t + 7]));
-    else
+    Part<T> w, rest;
+    if constexpr (sizeof(T) == 2) {
+      uint32_t x[4], y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float a = p[8 * t + 2 * i], b = p[8 * t + 2 * i + 1];
+        x[i] = pack2(a, b);
+        y[i] = FINE ? pack2(a - __uint_as_float(x[i] << 16), b - __uint_as_float(x[i] & 0xffff0000u)) : 0u;
+      }
+      w.v = make_uint4(x[0], x[1], x[2], x[3]);
+      rest.v = make_uint4(y[0], y[1], y[2], y[3]);
+    } else
 #pragma unroll
       for (int i = 0; i < 4; ++i) w.set(i, p[8 * t + 2 * i], p[8 * t + 2 * i + 1]);
 #pragma unroll
@@ -157,6 +166,7 @@ __device__ __forceinline__ void across_product(Lane at, Lane at8, int r0, const 
 #pragma unroll
         for (int i = 0; i < 4; ++i) f.set(i, x[2 * i], x[2 * i + 1]);
       }
+      if constexpr (FINE && sizeof(T) == 2) out[ob] = step_product<T>(f, rest, out[ob]);
       out[ob] = step_product<T>(f, w, out[ob]);
     }
   }
@@ -399,7 +409,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 :
     const unsigned to = (2 * stage + 1) * Tl::BYTES;
     const Lane across(across_tile + to), across8(across_tile8 + to);
 #pragma unroll
-    for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl>(across, across8, 32 * b, s[b], o);
+    for (int b = 0; b < Tl::NB; ++b) across_product<T, Tl, false>(across, across8, 32 * b, s[b], o);
   };
   if constexpr (SPLIT) {
     // one tile of each in LDS: the next one of k is under way from the scores on, the next one of v from their product on
@@ -460,7 +470,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 :
 
 // ---- backward: dq, and delta for the other kernel ---------------------------------------------------------------------
 // id: of the workgroups for queries, of which there are `all`.
-template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
+template <typename T, int DW, bool SPLIT, bool FINE> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
   using Tl = Tile<T, DW, SPLIT>;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
@@ -525,7 +535,7 @@ template <typename T, int DW, bool SPLIT> __device__ __forceinline__ void bwd_q(
         if (k0 + 8 * (v >> 2) + 4 * hi + (v & 3) > q) s[v] = 0.f;
     }
     const unsigned to = 2 * stage * Tl::BYTES;
-    across_product<T, Tl>(Lane(across_tile + to), Lane(across_tile8 + to), 32 * b, s, dq);
+    across_product<T, Tl, FINE>(Lane(across_tile + to), Lane(across_tile8 + to), 32 * b, s, dq);
   };
   if constexpr (SPLIT) {
     // v's tile is read first and given back first: the next one of it is under way while k's is in use, and k's under the next product with v
@@ -581,7 +591,7 @@ template <typename T, int DW, bool SPLIT>
 __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 96 ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
-  bwd_q<T, DW, SPLIT>(a, smem, blockIdx.x, gridDim.x, true);
+  bwd_q<T, DW, SPLIT, false>(a, smem, blockIdx.x, gridDim.x, true);
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------------------------
@@ -695,10 +705,10 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
 #pragma unroll
       for (int ks = 0; ks < Tl::STEPS; ++ks) s = step_product<T>(rows_frag<T, Tl>(rows, 0, ks), kf[ks], s);
       finish(s, dp, span.first + i % per_head * 32, 0, 0);
-      across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
+      across_product<T, Tl, OWN>(across, across8, Tl::OTHER, s, dv);
       wait_newest<63>();
       if (more) issue(i + 4, 0, true);
-      across_product<T, Tl>(across, across8, 0, dp, dk);
+      across_product<T, Tl, OWN>(across, across8, 0, dp, dk);
       wait_newest<63>();
       if (more) issue(i + 4, 0, false);
     }
@@ -726,8 +736,8 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
         }
         finish(s, dp, b0, b, stage);
         const Lane across(across_tile + to), across8(across_tile8 + to);
-        across_product<T, Tl>(across, across8, Tl::OTHER, s, dv);
-        across_product<T, Tl>(across, across8, 0, dp, dk);
+        across_product<T, Tl, OWN>(across, across8, Tl::OTHER, s, dv);
+        across_product<T, Tl, OWN>(across, across8, 0, dp, dk);
       }
     }
   }
@@ -760,11 +770,12 @@ __global__ __launch_bounds__(256, (sizeof(T) == 2 && (DW < 128 || !SPLIT)) || DW
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   bwd_kv<T, DW, SPLIT, false>(a, smem, blockIdx.x, shares);
 }
-// Both in one launch, for few rows: the workgroups past `queries` are those for keys.
+// Both in one launch, for few rows: the workgroups past `queries` are those for keys.  bf16: P and dS in two planes, as there is time for it (0.1 of 7.7 us, 128 tokens, 8 heads of 64; 0.9 of 16.6, 512 tokens):
+// with sums this short their rounding is half of what a gradient is off (2.5e-3 of its norm, 2.0e-3 so; 1.7e-3 are its own rounding).
 template <typename T, int DW> __global__ __launch_bounds__(256, 1) void packed_bwd_both_kernel(const PackedAttention a, const unsigned queries) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, true>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
-  if (blockIdx.x < queries) bwd_q<T, DW, true>(a, smem, blockIdx.x, queries, false);
+  if (blockIdx.x < queries) bwd_q<T, DW, true, true>(a, smem, blockIdx.x, queries, false);
   else bwd_kv<T, DW, true, true>(a, smem, blockIdx.x - queries, 1);
 }
 
