@@ -10,8 +10,8 @@
 // product, whose row operand is read from LDS across rows (bf16: transposing reads) in that same order.
 // SPLIT, for launches of few workgroups: all four wavefronts have the same 32 rows, each walks every fourth tile of the other side, filled by itself
 // into LDS of its own (no barrier), and they join their sums at the end.
-// Work is found on the device: sequence s takes offsets[s + 1] / ROWS - offsets[s] / ROWS + 1 workgroups per head, which is what it needs or one more, so
-// that workgroup t's sequence is the last with offsets[s] / ROWS + s <= t: no table, no launch ahead.
+// Work is found on the device (find_span): a sequence needs at most offsets[s + 1] / ROWS - offsets[s] / ROWS + 1 workgroups per head, which bounds the grid by
+// tokens / ROWS + sequences: no table, no launch ahead.
 // fp32: the same with every operand as three bf16 planes (Part), tiles of 32 rows instead of 64.
 #include "elem.h"
 #include "kernels.h"
@@ -234,23 +234,61 @@ __device__ __forceinline__ void tile_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Sum, or largest, of a wavefront's values (none below zero).
+template <bool LARGEST> __device__ __forceinline__ int of_wave(int x) {
+  auto with = [&](int y) { x = LARGEST ? max(x, y) : x + y; };
+  with(__builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false));   // neighbours, pairs, and the other halves of 8 and of 16 lanes
+  with(__builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false));
+  with(__builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false));
+  with(__builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, false));
+  const int a = __builtin_amdgcn_readlane(x, 0), b = __builtin_amdgcn_readlane(x, 16), c = __builtin_amdgcn_readlane(x, 32), d = __builtin_amdgcn_readlane(x, 48);
+  return LARGEST ? max(max(a, b), max(c, d)) : a + b + c + d;
+}
+
 struct Span { int begin, len, first; };  // rows of a sequence, and the workgroup's first row in it; len 0: nothing to do
+// The work of the workgroup that starts as the t-th of `all`, without a table.  Two to 63 sequences, one a lane: the longest work starts first, as the
+// launch lasts until it ends.  (A level is how many workgroups of its sequence have less to do; they start from the highest level on, those of one
+// level by sequence.  us, 8192 tokens in 24 sequences, 12 heads of 64 over 4, in their own order / so: forward 28.0 / 22.3, backward 90 / 76; 25 sequences
+// of 32 5.0 / 5.0.)  One has that order anyway; more take their workgroups in their own order, the longest of each first.
 // Offsets that are not as they should be give some span within the tensor.
-template <int OWN> __device__ __forceinline__ Span find_span(const PackedAttention& a, int t, int lane) {
+template <int OWN, bool KEYS> __device__ __forceinline__ Span find_span(const PackedAttention& a, int t, int all, int lane) {
   auto at = [&](int s) { return min(max(a.offsets[s], 0), a.tokens); };
+  Span s{0, 0, 0};
+  if (a.sequences > 1 && a.sequences < 64) {
+    const int begin = at(min(lane, a.sequences)), len = max(at(min(lane + 1, a.sequences)) - begin, 0), n = (len + OWN - 1) / OWN;
+    if (of_wave<false>(n) <= t) return s;
+    // the lowest level that has no more than t workgroups above it; `above`: how many
+    int low = 0, high = of_wave<true>(n), above = 0;
+    while (high - low > 1) {
+      const int middle = (low + high) >> 1, from = of_wave<false>(max(n - middle, 0));
+      if (from > t) low = middle;
+      else high = middle, above = from;
+    }
+    const uint64_t there = __ballot(n > low);
+    const bool mine = n > low && __builtin_amdgcn_mbcnt_hi((uint32_t)(there >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)there, 0)) == (unsigned)(t - above);
+    const int of = __ffsll((unsigned long long)__ballot(mine)) - 1;
+    s.begin = __builtin_amdgcn_readlane(begin, of);
+    s.len = __builtin_amdgcn_readlane(len, of);
+    s.first = (KEYS ? __builtin_amdgcn_readlane(n, of) - 1 - low : low) * OWN;
+    if (s.first < 0 || s.first >= s.len) s.len = 0;
+    return s;
+  }
+  // sequence s has its workgroups from offsets[s] / OWN + s on: the last one with that at or below `place`
+  const int place = KEYS ? t : all - 1 - t;
   int lo = 0, n = a.sequences;
   for (;;) {
-    const int step = (n + 63) >> 6;
-    const bool before = lane * step < n && at(lo + lane * step) / OWN + lo + lane * step <= t;
-    const int count = __popcll(__ballot(before));
-    lo += max(count - 1, 0) * step;
-    if (step == 1) break;
+    const int step = (n + 62) / 63, i = min(lo + lane * step, a.sequences), from = at(i);
+    const bool before = lane * step < n && from / OWN + i <= place;
+    const int count = max(__popcll(__ballot(before)), 1);
+    lo += (count - 1) * step;
+    if (step == 1) {
+      s.begin = __builtin_amdgcn_readlane(from, count - 1);
+      s.len = max(__builtin_amdgcn_readlane(from, count) - s.begin, 0);
+      break;
+    }
     n = min(step, a.sequences - lo);
   }
-  Span s;
-  s.begin = __builtin_amdgcn_readfirstlane(at(lo));
-  s.len = max(__builtin_amdgcn_readfirstlane(at(lo + 1)) - s.begin, 0);
-  s.first = (t - (s.begin / OWN + lo)) * OWN;
+  s.first = (place - (s.begin / OWN + lo)) * OWN;
   if (s.first < 0 || s.first >= s.len) s.len = 0;
   return s;
 }
@@ -337,7 +375,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 :
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
-  const Span span = find_span<Tl::OWN>(a, gridDim.x / a.heads - 1 - blockIdx.x / a.heads, lane);
+  const Span span = find_span<Tl::OWN, false>(a, blockIdx.x / a.heads, gridDim.x / a.heads, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -439,7 +477,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 :
         issue(i + 1, stage ^ 1, false);
         issue(i + 1, stage ^ 1, true);
       }
-      if (i * Tl::OTHER > last) continue;
+      if (i * Tl::OTHER > last || last - 31 >= span.len) continue;
       scores(i, stage);
       probabilities();
       values(stage);
@@ -475,7 +513,7 @@ template <typename T, int DW, bool SPLIT, bool FINE> __device__ __forceinline__ 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = id % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
-  const Span span = find_span<Tl::OWN>(a, all / a.heads - 1 - id / a.heads, lane);
+  const Span span = find_span<Tl::OWN, false>(a, id / a.heads, all / a.heads, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -569,7 +607,7 @@ template <typename T, int DW, bool SPLIT, bool FINE> __device__ __forceinline__ 
 #pragma unroll
       for (int b = 0; b < Tl::NB; ++b) {
         const int k0 = i * Tl::OTHER + 32 * b;
-        if (k0 > last) continue;
+        if (k0 > last || last - 31 >= span.len) continue;
         v16f_t s, dp;
         scores(s, b, stage);
         dprobabilities(dp, b, stage);
@@ -605,7 +643,7 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int share = wg % shares, kv = wg / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
-  const Span span = find_span<Tl::OWN>(a, wg / (shares * a.kv_heads), lane);
+  const Span span = find_span<Tl::OWN, true>(a, wg / (shares * a.kv_heads), 0, lane);
   if (span.len == 0) return;
   const unsigned row_bytes = (a.heads + 2 * a.kv_heads) * W * Tl::E, out_bytes = a.heads * W * Tl::E;
   const char* base = static_cast<const char*>(a.qkv) + (int64_t)span.begin * row_bytes;
@@ -725,7 +763,7 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
 #pragma unroll 1
       for (int b = 0; b < Tl::NB; ++b) {
         const int b0 = t0 + 32 * b;
-        if (b0 + 31 < first || b0 >= span.len) continue;
+        if (b0 + 31 < first || b0 >= span.len || first >= span.len) continue;
         v16f_t s = zero16(), dp = zero16();
         const unsigned to = 2 * stage * Tl::BYTES + 32 * b * Tl::CPR * 16;
         const Lane rows(rows_of_tile + to);
