@@ -425,6 +425,18 @@ def test_packed_attention(dtype, before, lengths, behind, heads, kv_heads, width
     near(dqkv[used.cuda()], res["dqkv"][used], tol["dqkv"][used], "dqkv")
 
 
+# enough workgroups that wavefronts do not share rows, in every width's kernels; 63 and 64 sequences, which are put in order in different ways
+CROWDED = [(0, [37] * 62 + [200], 5, 12, 4, 64), (3, [37, 0, 90, 1] * 16, 0, 12, 12, 32), (0, [300, 700, 129, 64, 500], 0, 32, 8, 128), (0, [511, 2, 640], 0, 64, 64, 96),
+           (0, [900, 800], 1, 56, 8, 80), (0, [129] * 40, 1, 16, 16, 16), (2, [1500], 0, 72, 24, 48)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("before,lengths,behind,heads,kv_heads,width", CROWDED, ids=lambda v: str(v) if not isinstance(v, list) or len(v) < 7 else "many")
+def test_packed_attention_of_many_workgroups(dtype, before, lengths, behind, heads, kv_heads, width):
+    for parts in (0, 8):
+        test_packed_attention(dtype, before, lengths, behind, heads, kv_heads, width, parts)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("size", [12.0, 1e-3])
 def test_packed_attention_of_large_and_small_scores(dtype, size):
@@ -468,6 +480,17 @@ def test_packed_attention_of_broken_offsets_stays_inside():
     _, qkv, dout = attention_case(0, [200], 0, 2, 1, 64, torch.bfloat16, 8)
     for at in ([0, 500], [-50, 100, 250], [150, 20, 200], [300, 400], [2 ** 31 - 1, -2 ** 31, 7], [-9, -5]):
         attention_call(BF16, qkv, at, 2, 1, 64, 0.125, dout, 2)
+
+
+@pytest.mark.parametrize("sequences", [2, 40, 63, 64, 300])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_packed_attention_of_many_broken_offsets_stays_inside(dtype, sequences):
+    for heads in (2, 24):
+        _, qkv, dout = attention_case(0, [700], 0, heads, 2, 64, TYPES[dtype], 8)
+        g = torch.Generator().manual_seed(sequences)
+        for low, high in ((-100, 1000), (0, 701), (-2 ** 31, 2 ** 31 - 1)):
+            at = torch.randint(low, high, (sequences + 1,), generator=g).tolist()
+            attention_call(dtype, qkv, at, heads, 2, 64, 0.125, dout, 2)
 
 
 def test_packed_attention_gradient_against_differences():
