@@ -857,27 +857,39 @@ int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int6
 //   792 345 / 345; 128: 264 408 / 271, 384 73 / 63, 528 463 / 531 (dq crosses at the same counts);
 //   backward by its kernel for keys, bf16 64: 528 204 / 185, 768 57.6 / 53.2, 896 93 / 98; 96: 528 255 / 255; 128: 192 115 / 106, 272 152 / 153, 384 60 / 73;
 //   fp32 64: 384 123 / 114, 528 889 / 927; 128: 264 1488 / 1441, 384 240 / 254.  Where query heads share a key head, 128 rows need their shares' fold too:
-//   bf16 128: 2048 tokens, 16 heads over 2 216 / 150, 4096 tokens, 16 over 4 329 / 455.
+//   bf16 128: 2048 tokens, 16 heads over 2 216 / 150, in 20 sequences 73 / 56, 4096 tokens, 16 over 4 329 / 455; 96: 4096 tokens, 16 over 2 335 / 231; fp32 64: 1211 / 806; and up to
+//   width 96 it costs more than the shorter way unless sequences are long: 8192 tokens in 24 sequences, 12 heads of 64 over 4 83 / 72, 32 of 96 over 8
+//   219 / 198, fp32 32 of 32 over 8 311 / 262, in one sequence bf16 16 of 64 over 8 515 / 535.
 template <typename T> bool split_wanted(const PackedAttention& a, bool kv) {
   int most;
+  const bool shared = a.heads > a.kv_heads;
   if (!kv) most = sizeof(T) == 2 ? (a.width <= 64 ? 500 : 330) : (a.width <= 64 ? 800 : 400);
-  else if (a.width > 96) most = a.heads > a.kv_heads ? 380 : 240;
-  else if (sizeof(T) == 2) most = a.width <= 64 ? 768 : 500;
-  else most = a.width <= 32 ? 800 : 450;
+  else if (a.width > 96 && shared && workgroups(a, 32, a.kv_heads) <= 300) return a.tokens > 64;
+  else if (a.width > 96) most = shared ? 380 : 240;
+  else if (shared && a.tokens <= 2048 * (int64_t)a.sequences) return a.tokens > 64;
+  else if (sizeof(T) == 2) most = a.width <= 64 ? 768 : shared ? 640 : 500;
+  else most = a.width <= 32 ? 800 : shared ? 640 : 450;
   return a.tokens > 64 && workgroups(a, 128, a.heads) <= most;  // (one tile of 64 rows has nothing to share)
 }
 // Workgroups that share a key tile's query heads: as few as make 1024 workgroups, two rounds of two per CU (a causal launch's workgroups differ in
 // length by as much as their tiles are many, and the longest, which start first, have to be short against the whole).  Not where sequences are
 // shorter than a tile on average: there is nothing to share.  us, backward in bf16, unshared / at 512 / 1024 / 2048: 8192 tokens, 32 heads of 128 over 8
 // 2150 / 2147 / 1785 / 1791; 4096 tokens, 16 heads of 64 over 4 215 / 215 / 175 / 178, in 16 sequences 65 / 65 / 57 / 62; 500 tokens in 60, 32 heads over 8
-// 20 / 25 / 29 / 29.
+// 20 / 25 / 29 / 29.  Where wavefronts share the keys' rows (own == 32) it goes by the rows that a workgroup has left on average: LONG or more, of sequences
+// that differ, 2048 workgroups for the longest one's sake (1024 / 2048: 16384 tokens in 20, 16 heads over 2, of 32 266 / 191, of 96 538 / 396), under
+// SHORT, a few tiles a wavefront, 512 (1024 / 512: 4096
+// tokens in 100, 12 heads of 64 over 4 44 / 29, fp32 16 of 96 over 2 199 / 166; in 40 of 32 over 2 72 / 89, 12 of 96 over 4 206 / 169).
 int shares_of(const PackedAttention& a, int own) {
+  constexpr int SHORT = 512, LONG = 3000;
   const int group = a.heads / a.kv_heads;
-  const int64_t have = workgroups(a, own, a.kv_heads);
+  const int64_t have = workgroups(a, own, a.kv_heads), mean = a.tokens / a.sequences;
   int shares = 1;
-  if (a.tokens / 32 < a.sequences) return shares;
-  for (int n = 2; n <= group && have * shares < 1024; ++n)
-    if (group % n == 0 && n <= a.max_parts) shares = n;
+  if (mean < 32) return shares;
+  for (int n = 2; n <= group && n <= a.max_parts; ++n) {
+    const int64_t rows = mean * (group / shares);
+    if (have * shares >= (own > 32 ? 1024 : rows < SHORT ? 512 : rows >= LONG && a.sequences > 1 ? 2048 : 1024)) break;
+    if (group % n == 0) shares = n;
+  }
   return shares;
 }
 
