@@ -94,8 +94,8 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
 /* ---- token models on packed batches ----------------------------------------------------------------------------
  * Rows are tokens.  Tensors are row-major and packed; nothing but what is said to be written is touched.  Outputs must not alias
  * inputs except where it is said.  Sizes of zero are CDP_EINVAL like negative ones, and so
- * are scales that are not finite.  The device of the pointers and of `stream` has to be
- * the current one.  Every call may be captured into a graph; calls that overlap in time need workspaces of their own.  The same inputs give
+ * are scales that are not finite, and sizes whose launch would have 2^32 threads (none of less than 2^22 rows, 2^29 words, 2^34
+ * elements of a table, 2^23 heads times tokens and sequences).  The device of the pointers and of `stream` has to be the current one.  Every call may be captured into a graph; calls that overlap in time need workspaces of their own.  The same inputs give
  * the same bits.
  *
  * Embedding: rows of table[vocab][C] (C <= 2^24) by ids[rows].  A token whose id is outside [0, vocab) (padding) has a row of zeros and no gradient.
@@ -133,6 +133,8 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const
  *   backward 0: out[tokens][heads * width] = softmax(scale * q k^T) v, lse[heads][tokens] (fp32) = log of the sum that the softmax divides
  *               by, sum exp(scale * q k^T)   (dout, dqkv, workspace unused)
  *   backward 1: dqkv from dout[tokens][heads * width] and the forward's out and lse
+ * Sums are fp32; between two products the element type rounds P and dS.  What is infinite or NaN in a row of k or v may reach every row of its
+ * sequence, earlier ones too (0 * NaN), and no other sequence.
  * Rows outside all sequences are neither read for another's sake nor written.  Offsets that are not as said give wrong results, within
  * the tensors.
  * workspace (backward): 4 * heads * tokens + 512 bytes (CDP_EINVAL if smaller).  Where it holds P times 8 * kv_heads * tokens * width

@@ -360,8 +360,10 @@ int attention_launches(bool backward, int B, int NT, int D, int heads, int dtype
 // T -> f32 copy (cdp_get_weights of a ring copy).
 hipError_t launch_to_f32(const void* src, float* dst, int64_t n, int dtype, hipStream_t stream);
 
+// Whether a launch of one-dimensional workgroups numbers its threads in 32 bits, as it has to.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups < (1ll << 32) && workgroups * threads <= 0xffffffffll; }
 // Operators of token models on packed batches (embedding_kernels.hip, residual_norm.hip, packed_attention.hip, grad_clip.hip): the entry points of
-// cdp_kernels.h after their checks.
+// cdp_kernels.h after their checks.  hipErrorInvalidConfiguration: more than a launch can number, and nothing has been launched.
 hipError_t launch_embedding_fwd(const void* table, const int32_t* ids, void* out, float scale, int rows, int vocab, int C, int dtype,
                                 hipStream_t stream);
 int64_t embedding_bwd_workspace_bytes(int rows, int C);

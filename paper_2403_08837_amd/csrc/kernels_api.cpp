@@ -194,6 +194,8 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
                               heads, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
 }
 
+static int launched(hipError_t e) { return e == hipSuccess ? CDP_OK : e == hipErrorInvalidConfiguration ? CDP_EINVAL : CDP_EHIP; }
+
 int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* ids, const void* dout, void* out, float scale,
                     void* workspace, size_t workspace_bytes, int rows, int vocab, int C, void* stream) {
   if (!ids || !out || rows <= 0 || vocab <= 0 || C <= 0 || C > (1 << 24) || !std::isfinite(scale) || backward < 0 || backward > 2 || (dtype != DT_F32 && dtype != DT_BF16)) return CDP_EINVAL;
@@ -202,13 +204,12 @@ int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* i
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (!backward) {
     if (!table || !aligned_to(table, eb)) return CDP_EINVAL;
-    return launch_embedding_fwd(table, ids, out, scale, rows, vocab, C, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+    return launched(launch_embedding_fwd(table, ids, out, scale, rows, vocab, C, dtype, st));
   }
   if (!dout || !aligned_to(dout, eb) || !workspace || !aligned_to(workspace, 16) ||
       workspace_bytes < (size_t)embedding_bwd_workspace_bytes(rows, C))
     return CDP_EINVAL;
-  return launch_embedding_bwd(ids, dout, static_cast<float*>(out), scale, workspace, backward == 2, rows, vocab, C, dtype, st) == hipSuccess
-             ? CDP_OK : CDP_EHIP;
+  return launched(launch_embedding_bwd(ids, dout, static_cast<float*>(out), scale, workspace, backward == 2, rows, vocab, C, dtype, st));
 }
 
 int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gate, const float* gamma_post, const float* gamma_pre,
@@ -223,7 +224,7 @@ int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gat
   memset(&a, 0, sizeof(a));
   a.x = x; a.h = h; a.gate = gate; a.gamma_post = gamma_post; a.gamma_pre = gamma_pre;
   a.r = r; a.y = y; a.rows = rows; a.C = C; a.scale = scale; a.eps = eps;
-  return launch_residual_norm_fwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;
+  return launched(launch_residual_norm_fwd(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
 int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const void* h, const void* gate, const float* gamma_post,
@@ -247,7 +248,7 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const
   a.dr = dr; a.dy = dy; a.dx = dx; a.dh = dh; a.dgate = dgate; a.dgamma_post = dgamma_post; a.dgamma_pre = dgamma_pre;
   a.part = static_cast<float*>(workspace);
   a.rows = rows; a.C = C; a.accumulate = accumulate != 0; a.scale = scale; a.eps = eps;
-  return launch_residual_norm_bwd(a, dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? CDP_OK : CDP_EHIP;
+  return launched(launch_residual_norm_bwd(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
 int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32_t* offsets, void* out, float* lse, const void* dout,
@@ -264,7 +265,7 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
   a.qkv = qkv; a.offsets = offsets; a.out = out; a.lse = lse;
   a.tokens = tokens; a.sequences = sequences; a.heads = heads; a.kv_heads = kv_heads; a.width = width; a.scale = scale;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  if (!backward) return launch_packed_attention_fwd(a, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+  if (!backward) return launched(launch_packed_attention_fwd(a, dtype, st));
   const size_t rows = (size_t)heads * tokens, need = 4 * rows + 512;
   if (!dout || !dqkv || !aligned_to(dout, 16) || !aligned_to(dqkv, 16) || !workspace || !aligned_to(workspace, 16) || workspace_bytes < need)
     return CDP_EINVAL;
@@ -272,7 +273,7 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
   a.delta = static_cast<float*>(workspace);
   a.parts = a.delta + (rows + 63) / 64 * 64;
   a.max_parts = (int64_t)((workspace_bytes - need) / (8 * (size_t)kv_heads * tokens * width));
-  return launch_packed_attention_bwd(a, dtype, st) == hipSuccess ? CDP_OK : CDP_EHIP;
+  return launched(launch_packed_attention_bwd(a, dtype, st));
 }
 
 int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm,
@@ -286,8 +287,7 @@ int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* cons
     total += counts[i];
     if (counts[i] && (!grads[i] || !aligned_to(grads[i], eb) || (outs && (!outs[i] || !aligned_to(outs[i], eb))))) return CDP_EINVAL;
   }
-  return launch_grad_clip(tensors, grads, outs, counts, max_norm, norm, workspace, dtype, static_cast<hipStream_t>(stream)) == hipSuccess
-             ? CDP_OK : CDP_EHIP;
+  return launched(launch_grad_clip(tensors, grads, outs, counts, max_norm, norm, workspace, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

