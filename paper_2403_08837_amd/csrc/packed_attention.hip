@@ -33,10 +33,12 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Tile of `OTHER` rows of one head, DW columns (the width rounded up, zeros behind it), in LDS.  16-byte chunk c of row r sits in slot c ^ swz(r) of the
+// Tile of `OTHER` rows of one head, DW columns (zeros past the width; products along a row take SW of them), in LDS.  16-byte chunk c of row r sits in slot c ^ swz(r) of the
 // row: 16 consecutive rows' chunk c are 16 different slots modulo 256 bytes, and so are the pieces that a read across rows takes.
-template <typename T, int DW, bool SPLIT> struct Tile {
-  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = DW / 16, CHUNKS = CPR / 2;  // products along a row; 16-byte reads of it by either lane half
+constexpr int columns(int sw) { return (sw + 31) / 32 * 32; }
+template <typename T, int SW, bool SPLIT> struct Tile {
+  static constexpr int DW = columns(SW);
+  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = SW / 16, CHUNKS = SW * E / 32;  // products along a row; 16-byte reads of it by either lane half
   static constexpr int OWN = SPLIT ? 32 : 128, OTHER = SPLIT || E == 4 ? 32 : 64, NB = OTHER / 32, OB = DW / 32;
   static constexpr int BYTES = OTHER * DW * E, FILLERS = SPLIT ? 1 : 4, LOADS = BYTES / 1024 / FILLERS;  // wavefronts that fill a tile, loads of each
   static_assert(LOADS * FILLERS * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
@@ -373,9 +375,10 @@ template <typename T, int DW> __device__ __forceinline__ void join_shares(T* row
 }
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
-  using Tl = Tile<T, DW, SPLIT>;
+template <typename T, int SW, bool SPLIT>
+__global__ __launch_bounds__(256, sizeof(T) == 4 && SW > (SPLIT ? 64 : 96) ? 1 : 2) void packed_fwd_kernel(const PackedAttention a) {
+  using Tl = Tile<T, SW, SPLIT>;
+  constexpr int DW = Tl::DW;
   __shared__ __attribute__((aligned(1024))) char memory[Tl::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
@@ -514,8 +517,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && DW > (SPLIT ? 64 : 96) ? 1 :
 
 // ---- backward: dq, and delta for the other kernel ---------------------------------------------------------------------
 // id: of the workgroups for queries, of which there are `all`.
-template <typename T, int DW, bool SPLIT, bool FINE> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
-  using Tl = Tile<T, DW, SPLIT>;
+template <typename T, int SW, bool SPLIT, bool FINE> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
+  using Tl = Tile<T, SW, SPLIT>;
+  constexpr int DW = Tl::DW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
   const int head = id % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
@@ -631,11 +635,11 @@ template <typename T, int DW, bool SPLIT, bool FINE> __device__ __forceinline__ 
     store_own<T, DW>(row, dq, a.scale, hi, W);
   }
 }
-template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 96 ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
-  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
+template <typename T, int SW, bool SPLIT>
+__global__ __launch_bounds__(256, sizeof(T) == 2 || SW <= 64 ? 2 : 1) void packed_bwd_q_kernel(const PackedAttention a) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, SW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
-  bwd_q<T, DW, SPLIT, false>(a, smem, blockIdx.x, gridDim.x, true);
+  bwd_q<T, SW, SPLIT, false>(a, smem, blockIdx.x, gridDim.x, true);
 }
 
 // ---- backward: dk and dv ------------------------------------------------------------------------------------------------
@@ -643,8 +647,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 || DW < 96 ? 2 : 1) void packed
 // the chip short of workgroups the heads are shared by `shares` of them, whose sums (fp32, in the workspace) packed_bwd_fold_kernel adds in a fixed order.
 // OWN: delta is not in memory yet; the workgroup makes that of all the rows it will meet first (up to OWN_ROWS of them: no span is longer than the tensor).
 constexpr int OWN_ROWS = 512;
-template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ void bwd_kv(const PackedAttention& a, unsigned smem, unsigned wg, int shares) {
-  using Tl = Tile<T, DW, SPLIT>;
+template <typename T, int SW, bool SPLIT, bool OWN> __device__ __forceinline__ void bwd_kv(const PackedAttention& a, unsigned smem, unsigned wg, int shares) {
+  using Tl = Tile<T, SW, SPLIT>;
+  constexpr int DW = Tl::DW;
   __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 2][2][64];  // per wavefront or stage: lse and delta of the tile's rows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
   const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
@@ -808,19 +813,19 @@ template <typename T, int DW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   else
     write(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W, (int64_t)a.kv_heads * W);
 }
-template <typename T, int DW, bool SPLIT>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 && (DW < 128 || !SPLIT)) || DW < 64 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
-  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, SPLIT>::LDS];
+template <typename T, int SW, bool SPLIT>
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && (SW <= 96 || !SPLIT)) || SW <= 32 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, SW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
-  bwd_kv<T, DW, SPLIT, false>(a, smem, blockIdx.x, shares);
+  bwd_kv<T, SW, SPLIT, false>(a, smem, blockIdx.x, shares);
 }
 // Both in one launch, for few rows: the workgroups past `queries` are those for keys.  bf16: P and dS in two planes, as there is time for it (0.1 of 7.7 us, 128 tokens, 8 heads of 64; 0.9 of 16.6, 512 tokens):
 // with sums this short their rounding is half of what a gradient is off (2.5e-3 of its norm, 2.0e-3 so; 1.7e-3 are its own rounding).
-template <typename T, int DW> __global__ __launch_bounds__(256, 1) void packed_bwd_both_kernel(const PackedAttention a, const unsigned queries) {
-  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, DW, true>::LDS];
+template <typename T, int SW> __global__ __launch_bounds__(256, 1) void packed_bwd_both_kernel(const PackedAttention a, const unsigned queries) {
+  __shared__ __attribute__((aligned(1024))) char memory[Tile<T, SW, true>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
-  if (blockIdx.x < queries) bwd_q<T, DW, true, true>(a, smem, blockIdx.x, queries, false);
-  else bwd_kv<T, DW, true, true>(a, smem, blockIdx.x - queries, 1);
+  if (blockIdx.x < queries) bwd_q<T, SW, true, true>(a, smem, blockIdx.x, queries, false);
+  else bwd_kv<T, SW, true, true>(a, smem, blockIdx.x - queries, 1);
 }
 
 // Sums of the shares: [share][dk, dv][tokens][kv_heads][width] -> the rows of dqkv that belong to a sequence, eight columns a thread.
@@ -845,12 +850,20 @@ template <typename T> __global__ __launch_bounds__(256) void packed_bwd_fold_ker
   for (int e = 0; e < 8 / Elem<T>::VEC; ++e) reinterpret_cast<uint4*>(out)[e] = c[e].v;
 }
 
+// Kernels for every 16 columns, as products along a row go, though across rows they go by 32 (us, forward and backward, at widths of whole 32 / so: fp32
+// 2500 tokens in 5 sequences, 8 heads of 80 39 and 118 / 37 and 112, 4096 in 2 of 16 43 and 126 / 38 and 108; bf16 8192 in 2 of 48 80 and 228 / 77 and 215).
 #define CDP_WIDTHS(CALL)                                     \
   do {                                                       \
-    if (a.width <= 32) { constexpr int DW = 32; CALL; }      \
-    else if (a.width <= 64) { constexpr int DW = 64; CALL; } \
-    else if (a.width <= 96) { constexpr int DW = 96; CALL; } \
-    else { constexpr int DW = 128; CALL; }                   \
+    switch ((a.width + 15) / 16) {                       \
+      case 1: { constexpr int SW = 16; CALL; } break;    \
+      case 2: { constexpr int SW = 32; CALL; } break;    \
+      case 3: { constexpr int SW = 48; CALL; } break;    \
+      case 4: { constexpr int SW = 64; CALL; } break;    \
+      case 5: { constexpr int SW = 80; CALL; } break;    \
+      case 6: { constexpr int SW = 96; CALL; } break;    \
+      case 7: { constexpr int SW = 112; CALL; } break;   \
+      default: { constexpr int SW = 128; CALL; }         \
+    }                                                    \
   } while (0)
 
 int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int64_t)a.tokens / own + a.sequences) * heads; }
@@ -901,18 +914,18 @@ int shares_of(const PackedAttention& a, int own) {
 
 template <typename T, bool SPLIT> hipError_t forward(const PackedAttention& a, hipStream_t stream) {
   const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.heads));
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_fwd_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_fwd_kernel<T, SW, SPLIT>), grid, dim3(256), 0, stream, a));
   return hipGetLastError();
 }
 template <typename T, bool SPLIT> hipError_t backward_q(const PackedAttention& a, hipStream_t stream) {
   const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.heads));
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_q_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_q_kernel<T, SW, SPLIT>), grid, dim3(256), 0, stream, a));
   return hipGetLastError();
 }
 template <typename T, bool SPLIT> hipError_t backward_kv(const PackedAttention& a, hipStream_t stream) {
   const int shares = shares_of(a, SPLIT ? 32 : 128);
   const dim3 grid((unsigned)workgroups(a, SPLIT ? 32 : 128, a.kv_heads) * shares);
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, DW, SPLIT>), grid, dim3(256), 0, stream, a, shares));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_kv_kernel<T, SW, SPLIT>), grid, dim3(256), 0, stream, a, shares));
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || shares == 1) return e;
   const int64_t n = (int64_t)a.tokens * a.kv_heads * a.width / 8;
@@ -928,7 +941,7 @@ bool both_wanted(const PackedAttention& a) {
 }
 template <typename T> hipError_t backward_both(const PackedAttention& a, hipStream_t stream) {
   const unsigned queries = (unsigned)workgroups(a, 32, a.heads), keys = (unsigned)workgroups(a, 32, a.kv_heads);
-  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_both_kernel<T, DW>), dim3(queries + keys), dim3(256), 0, stream, a, queries));
+  CDP_WIDTHS(hipLaunchKernelGGL((packed_bwd_both_kernel<T, SW>), dim3(queries + keys), dim3(256), 0, stream, a, queries));
   return hipGetLastError();
 }
 template <typename T> hipError_t backward(const PackedAttention& a, hipStream_t stream) {
