@@ -6,7 +6,7 @@
 // order: no third launch, no atomics.  The second pass goes through the units backwards: what the first read last is still cached.
 // fp32, 400 million elements in 300 tensors: 0.90 ms, 5.3 TB/s over the two reads and the write.
 // Sets of up to 64 pieces of 4 KB are one launch of one workgroup, whose wavefronts keep their pieces in registers between the two.
-// The tensors' addresses travel in the kernel arguments, 128 of them a launch; a wavefront finds the tensor of a unit by comparing all of them at once.
+// The tensors' addresses travel in the kernel arguments, 160 of them a launch (160 tensors of 100 elements 11.6 us, 161 20.0); a wavefront finds the tensor of a unit by comparing all of them at once.
 #include "elem.h"
 #include "kernels.h"
 
@@ -17,13 +17,13 @@ namespace cdp {
 
 namespace {
 
-constexpr int CLIP_TENSORS = 128, CLIP_GROUPS = 2048, UNIT_BYTES = 32768;
+constexpr int CLIP_TENSORS = 160, CLIP_GROUPS = 2048, UNIT_BYTES = 32768;
 constexpr int SOLE = 1024, SOLE_BYTES = 4096, SOLE_EACH = 4, SOLE_UNITS = SOLE / 64 * SOLE_EACH;  // one workgroup: threads, bytes of a piece, pieces of a wavefront, of all
 
 struct ClipTable {
   const void* g[CLIP_TENSORS];
   void* out[CLIP_TENSORS];
-  int64_t count[CLIP_TENSORS];
+  uint16_t last[CLIP_TENSORS];  // elements of its last unit
   int32_t units[CLIP_TENSORS];  // of the tensors before it; past the last tensor all units (2^31 of them are 64 TB)
   int32_t total;
 };
@@ -37,11 +37,14 @@ template <typename T, int BYTES = UNIT_BYTES> struct Unit {
   bool whole;   // 16-byte pieces
   __device__ __forceinline__ Unit(const ClipTable& t, int u, bool scaling) {
     const int lane = threadIdx.x & 63;
-    const int i = __popcll(__ballot(t.units[lane] <= u)) + __popcll(__ballot(t.units[lane + 64] <= u)) - 1;
+    int i = -1;
+#pragma unroll
+    for (int k = 0; k < CLIP_TENSORS; k += 64) i += __popcll(__ballot(k + lane < CLIP_TENSORS && t.units[min(k + lane, CLIP_TENSORS - 1)] <= u));
+    const int behind = i + 1 < CLIP_TENSORS ? t.units[i + 1] : t.total;
     const int64_t first = (int64_t)(u - t.units[i]) * SIZE;
     g = static_cast<const T*>(t.g[i]) + first;
     out = scaling ? static_cast<T*>(t.out[i]) + first : nullptr;
-    n = (int)min((int64_t)SIZE, t.count[i] - first);
+    n = u + 1 < behind ? SIZE : t.last[i];
     whole = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(out)) & 15) == 0;
   }
 };
@@ -130,19 +133,24 @@ template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(c
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Chunk16<T> c[SOLE_EACH][L];
   double s = 0;
+  // (a piece past the last: the last one, of nothing)
+  auto piece = [&](int k) {
+    const int u = wave + k * (SOLE / 64);
+    U w(t, min(u, max(t.total - 1, 0)), scaling);
+    if (u >= t.total) w.n = 0;
+    return w;
+  };
+  const U w[SOLE_EACH] = {piece(0), piece(1), piece(2), piece(3)};
+  static_assert(SOLE_EACH == 4, "pieces");
+  auto wholes = [&](int k) { return w[k].whole ? w[k].n / U::V : 0; };
+#pragma unroll
+  for (int k = 0; k < SOLE_EACH; ++k)
+    if (const int pieces = wholes(k))
+#pragma unroll
+      for (int l = 0; l < L; ++l) c[k][l].v = reinterpret_cast<const uint4*>(w[k].g)[min(lane + 64 * l, pieces - 1)];
 #pragma unroll
   for (int k = 0; k < SOLE_EACH; ++k) {
-    if (wave + k * (SOLE / 64) >= t.total) break;
-    const U w(t, wave + k * (SOLE / 64), scaling);
-    if (!w.whole || w.n < U::V) continue;
-#pragma unroll
-    for (int l = 0; l < L; ++l) c[k][l].v = reinterpret_cast<const uint4*>(w.g)[min(lane + 64 * l, w.n / U::V - 1)];
-  }
-#pragma unroll
-  for (int k = 0; k < SOLE_EACH; ++k) {
-    if (wave + k * (SOLE / 64) >= t.total) break;
-    const U w(t, wave + k * (SOLE / 64), scaling);
-    const int pieces = w.whole ? w.n / U::V : 0;
+    const int pieces = wholes(k);
 #pragma unroll
     for (int l = 0; l < L; ++l)
       if (lane + 64 * l < pieces)
@@ -151,8 +159,8 @@ template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(c
           const double v = Elem<T>::to_f32(c[k][l].e[e]);
           s += v * v;
         }
-    for (int e = pieces * U::V + lane; e < w.n; e += 64) {
-      const double v = Elem<T>::to_f32(w.g[e]);
+    for (int e = pieces * U::V + lane; e < w[k].n; e += 64) {
+      const double v = Elem<T>::to_f32(w[k].g[e]);
       s += v * v;
     }
   }
@@ -163,19 +171,17 @@ template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(c
   const float f = over ? (float)(max_norm / r) : 1.f;
 #pragma unroll
   for (int k = 0; k < SOLE_EACH; ++k) {
-    if (wave + k * (SOLE / 64) >= t.total) break;
-    const U w(t, wave + k * (SOLE / 64), true);
-    if (!over && w.out == w.g) continue;
-    const int pieces = w.whole ? w.n / U::V : 0;
+    if (!over && w[k].out == w[k].g) continue;
+    const int pieces = wholes(k);
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       if (lane + 64 * l >= pieces) continue;
       if (over)
 #pragma unroll
         for (int e = 0; e < U::V; ++e) c[k][l].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k][l].e[e]));
-      reinterpret_cast<uint4*>(w.out)[lane + 64 * l] = c[k][l].v;
+      reinterpret_cast<uint4*>(w[k].out)[lane + 64 * l] = c[k][l].v;
     }
-    for (int e = pieces * U::V + lane; e < w.n; e += 64) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
+    for (int e = pieces * U::V + lane; e < w[k].n; e += 64) w[k].out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w[k].g[e])) : w[k].g[e];
   }
 }
 
@@ -188,9 +194,9 @@ hipError_t clip(int tensors, const void* const* grads, void* const* outs, const 
       const bool there = i0 + i < tensors && counts[i0 + i] > 0;
       t.g[i] = there ? grads[i0 + i] : nullptr;
       t.out[i] = there && outs ? outs[i0 + i] : nullptr;
-      t.count[i] = there ? counts[i0 + i] : 0;
+      t.last[i] = there ? (uint16_t)((counts[i0 + i] - 1) % size + 1) : 0;
       t.units[i] = units;  // (of tensors with the same one, only the last has units)
-      if (there) units += (int32_t)((t.count[i] + size - 1) / size);
+      if (there) units += (int32_t)((counts[i0 + i] + size - 1) / size);
     }
     t.total = units;
     return t;

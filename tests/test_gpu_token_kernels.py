@@ -427,7 +427,7 @@ def test_packed_attention(dtype, before, lengths, behind, heads, kv_heads, width
 
 # enough workgroups that wavefronts do not share rows, in every width's kernels; 63 and 64 sequences, which are put in order in different ways
 CROWDED = [(0, [37] * 62 + [200], 5, 12, 4, 64), (3, [37, 0, 90, 1] * 16, 0, 12, 12, 32), (0, [300, 700, 129, 64, 500], 0, 32, 8, 128), (0, [511, 2, 640], 0, 64, 64, 96),
-           (0, [900, 800], 1, 56, 8, 80), (0, [129] * 40, 1, 16, 16, 16), (2, [1500], 0, 72, 24, 48)]
+           (0, [900, 800], 1, 56, 8, 80), (0, [640, 33], 3, 64, 16, 104), (0, [129] * 40, 1, 16, 16, 16), (2, [1500], 0, 72, 24, 48)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -542,6 +542,13 @@ def test_grad_clip(dtype, counts, max_norm):
     clip_call(dtype, grads, grads, max_norm)   # in place
     assert all(torch.equal(g, o) for g, o in zip(grads, outs))
     hold.check()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("counts", [[7] * 160, [1025] * 161, [0] * 100 + [50000] + [0] * 59, [0] * 200 + [5], [16384, 0, 8192, 16385, 8193] * 33, [1024] * 16 + [0] + [2048] * 16 + [3]],
+                         ids=lambda c: "%d of %d" % (len(c), sum(c)))
+def test_grad_clip_of_whole_tables_and_units(dtype, counts):
+    test_grad_clip(dtype, counts, 1.0)
 
 
 def test_grad_clip_of_what_is_not_finite_or_zero():
