@@ -107,7 +107,8 @@ int cdp_k_attention(int dtype, int backward, const void* qkv, void* P, const voi
 int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* ids, const void* dout, void* out, float scale,
                     void* workspace, size_t workspace_bytes, int rows, int vocab, int C, void* stream);
 
-/* The end of one block and the start of the next, over rows of C <= 16384 channels, norm(v) = v / sqrt(mean(v^2) + eps):
+/* The end of one block and the start of the next, over rows of C <= 16384 channels, norm(v) = v / sqrt(mean(v^2) + eps),
+ * for rows whose squares have a sum that fp32 holds (rms up to 1e17):
  *   u = norm(h) * gamma_post       h[rows][C]: what the block computed; gamma_post NULL: u = h
  *   r = x + scale * sigmoid(gate) * u       gate[rows][C]; NULL: no gate.  h NULL: r = x, and gate and gamma_post are NULL
  *   y = norm(r) * gamma_pre        gamma_pre NULL: no y

@@ -244,14 +244,15 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     }
     row_sums<LR>(s, lds[parity]);
     const float rho = a.gamma_pre ? rsqrtf(s[0] * inv + a.eps) : 0.f;
-    const float across = rho * rho * rho * (s[1] * inv);  // rho rho mean(a rhat): what a value of r takes from d
-    const float dot = a.gamma_post ? eta * eta * eta * inv * (s[2] + rho * s[3] - across * s[4]) : 0.f;
+    // mean(a rhat) and mean(b n), each factor next to the sum that it brings back to size: a reciprocal's square or cube would leave fp32 first
+    const float mean_a = rho * (s[1] * inv);
+    const float mean_b = a.gamma_post ? eta * (inv * (s[2] + rho * (s[3] - mean_a * (rho * s[4])))) : 0.f;
     float d[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float dy = w.dy[i];
-      d[i] = w.dr[i] + (rho * (dy * pre[i]) - across * r[i]);
-      sum_of(1, i) += dy * (r[i] * rho);
+      const float dy = w.dy[i], rhat = r[i] * rho;
+      d[i] = w.dr[i] + rho * (dy * pre[i] - rhat * mean_a);
+      sum_of(1, i) += dy * rhat;
     }
     store_row<T, Group, K>(a.dx, at, off, d);
     float dg[N];
@@ -260,7 +261,7 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
       const float h = w.h[i], du = a.scale * sig[i] * d[i], n = h * eta;
       sum_of(0, i) += du * n;
       dg[i] = du * (n * post[i]) * (1.f - sig[i]);
-      d[i] = eta * (du * post[i]) - dot * h;
+      d[i] = eta * (du * post[i] - n * mean_b);
     }
     store_row<T, Group, K>(a.dgate, at, off, dg);
     store_row<T, Group, K>(a.dh, at, off, d);

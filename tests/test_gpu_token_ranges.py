@@ -1,0 +1,62 @@
+"""Operators of token models over the ranges that they are offered for: far magnitudes, open gates, launches of many rows, every kernel of packed attention.
+
+Against their formulas in 64 bits, tolerances as in test_gpu_token_kernels.py: U = 2^-24 and half(t) are half a step of fp32 and of the element type."""
+import math
+
+import numpy as np
+import pytest
+
+from paper_2403_08837_amd import binding as b
+from test_gpu_token_kernels import (BF16, F32, TYPES, U, Held, attention_call, attention_case, attention_reference, clip_call, half, near, norm_case, norm_reference, norm_tolerance,
+                                    p, randn, workspace)
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+# ---- norms around a block ---------------------------------------------------------------------------------------------
+def norm_calls(v, dtype, scale, eps, shift=0):
+    """Both directions on tensors that begin `shift` elements past a 16-byte border: everything that is written, by name."""
+    rows, C = v["x"].shape
+    t, hold = TYPES[dtype], Held()
+    dev = {k: None if x is None else hold(x, x.dtype, shift) for k, x in v.items()}
+    made = lambda there: hold.out(t, rows, C, shift=shift) if there is not None else None  # noqa: E731
+    got = {"r": made(v["x"]), "y": made(v["pre"]), "dx": made(v["x"]), "dh": made(v["h"]), "dgate": made(v["gate"])}
+    for k in ("post", "pre"):
+        got["d" + k] = hold.out(torch.float32, C, shift=shift) if v[k] is not None else None
+    b.cdp_k_residual_norm(dtype, p(dev["x"]), p(dev["h"]), p(dev["gate"]), p(dev["post"]), p(dev["pre"]), p(got["r"]), p(got["y"]), scale, eps, rows, C)
+    need = 8 * C * min(rows, 512) + 256
+    b.cdp_k_residual_norm_backward(dtype, 0, p(dev["x"]) if v["pre"] is not None else 0, p(dev["h"]), p(dev["gate"]), p(dev["post"]), p(dev["pre"]), p(dev["dr"]), p(dev["dy"]),
+                                   p(got["dx"]), p(got["dh"]), p(got["dgate"]), p(got["dpost"]), p(got["dpre"]), scale, eps, p(workspace(need)), need, rows, C)
+    hold.check()
+    return {k: x for k, x in got.items() if x is not None}
+
+
+def norm_check(v, dtype, scale, eps, shift=0):
+    rows = v["x"].shape[0]
+    got = norm_calls(v, dtype, scale, eps, shift)
+    args = [None if v[k] is None else v[k].cuda().double() for k in ("x", "h", "gate", "post", "pre", "dr", "dy")]
+    res, size = norm_reference(*args, scale, float(np.float32(eps)))
+    for k, x in got.items():
+        near(x, res[k].cpu(), norm_tolerance(k, res, size, dtype, rows).cpu(), k)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("form", ["all", "no post", "norm alone", "end", "no dr"])
+@pytest.mark.parametrize("x_size,h_size", [(1e13, 1.0), (1e15, 1e-12), (1e17, 1e17), (1.0, 1e13), (1.0, 1e15), (1e-12, 1e17), (1e-12, 1e-12)])
+@pytest.mark.parametrize("C", [776, 250])
+def test_residual_norm_of_large_and_small_rows(dtype, form, x_size, h_size, C):
+    """Magnitudes whose squares fp32 holds (and whose cubes it does not)."""
+    v = norm_case(form, 21, C, TYPES[dtype], C)
+    for k, size in (("x", x_size), ("h", h_size)):
+        v[k] = None if v[k] is None else (v[k].double() * size).to(v[k].dtype)
+    norm_check(v, dtype, 0.75, 1e-5)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("eps", [1e-24, 1e-30])
+def test_residual_norm_of_zeros_with_a_small_eps(dtype, eps):
+    """Rows of zeros among others: their reciprocal roots are 1e12 and 1e15, what they make of dy is finite."""
+    v = norm_case("all", 12, 264, TYPES[dtype], 3)
+    v["x"][2], v["h"][2], v["h"][7] = 0, 0, 0
+    norm_check(v, dtype, 0.75, eps)
