@@ -260,7 +260,8 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     for (int i = 0; i < N; ++i) {
       const float h = w.h[i], du = a.scale * sig[i] * d[i], n = h * eta;
       sum_of(0, i) += du * n;
-      dg[i] = du * (n * post[i]) * (1.f - sig[i]);
+      // 1 - sigmoid(g), not as a difference: of an open gate that has no bits left (g = 10: 1e-3 off, from 17 on zero)
+      dg[i] = du * (n * post[i]) * sigmoid(-w.g[i]);
       d[i] = eta * (du * post[i] - n * mean_b);
     }
     store_row<T, Group, K>(a.dgate, at, off, dg);

@@ -60,3 +60,19 @@ def test_residual_norm_of_zeros_with_a_small_eps(dtype, eps):
     v = norm_case("all", 12, 264, TYPES[dtype], 3)
     v["x"][2], v["h"][2], v["h"][7] = 0, 0, 0
     norm_check(v, dtype, 0.75, eps)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_residual_norm_of_open_gates(dtype):
+    """dgate of gates that are nearly open or shut is as exact as its factor sig (1 - sig) is small.  exp(-|g|): the exponent in units of 2 is rounded
+    twice, 2 |g| U, and the power is 2 U off; one addition, a reciprocal of 2 U, their product, and four more products: (2 |g| + 16) U."""
+    t = TYPES[dtype]
+    gate = torch.tensor([[g * s for g in (0.5, 3.0, 5.0, 10.0, 12.0, 15.0, 17.0, 20.0, 40.0, 60.0, 0.0, 1.0) for s in (1, -1)]])
+    h, dr = randn(1, *gate.shape).to(t), randn(2, *gate.shape).to(t)
+    got = norm_calls({"x": h, "h": h, "gate": gate.to(t), "post": None, "pre": None, "dr": dr, "dy": None}, dtype, 0.75, 1e-5)
+    g = gate.to(t).double()
+    q, e = 1 / (1 + torch.exp(-g.abs())), torch.exp(-g.abs())
+    sig = torch.where(g < 0, e * q, q)
+    want = 0.75 * h.double() * dr.double() * e * q * q
+    near(got["dgate"], want, ((2 * g.abs() + 16) * U + half(dtype)) * want.abs(), "dgate")
+    near(got["dh"], 0.75 * sig * dr.double(), ((2 * g.abs() + 16) * U + half(dtype)) * (0.75 * sig * dr.double()).abs(), "dh")
