@@ -247,12 +247,18 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     // mean(a rhat) and mean(b n), each factor next to the sum that it brings back to size: a reciprocal's square or cube would leave fp32 first
     const float mean_a = rho * (s[1] * inv);
     const float mean_b = a.gamma_post ? eta * (inv * (s[2] + rho * (s[3] - mean_a * (rho * s[4])))) : 0.f;
+    // (branches, not factors of zero: without the norms what is infinite in h is not met)
     float d[N];
+    if (a.gamma_pre) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const float dy = w.dy[i], rhat = r[i] * rho;
-      d[i] = w.dr[i] + rho * (dy * pre[i] - rhat * mean_a);
-      sum_of(1, i) += dy * rhat;
+      for (int i = 0; i < N; ++i) {
+        const float dy = w.dy[i], rhat = r[i] * rho;
+        d[i] = w.dr[i] + rho * (dy * pre[i] - rhat * mean_a);
+        sum_of(1, i) += dy * rhat;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] = w.dr[i];
     }
     store_row<T, Group, K>(a.dx, at, off, d);
     float dg[N];
@@ -262,8 +268,11 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
       sum_of(0, i) += du * n;
       // 1 - sigmoid(g), not as a difference: of an open gate that has no bits left (g = 10: 1e-3 off, from 17 on zero)
       dg[i] = du * (n * post[i]) * sigmoid(-w.g[i]);
-      d[i] = eta * (du * post[i] - n * mean_b);
+      d[i] = eta * (du * post[i]);
     }
+    if (a.gamma_post)
+#pragma unroll
+      for (int i = 0; i < N; ++i) d[i] -= eta * (w.h[i] * eta * mean_b);
     store_row<T, Group, K>(a.dgate, at, off, dg);
     store_row<T, Group, K>(a.dh, at, off, d);
   };

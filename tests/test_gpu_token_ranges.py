@@ -76,3 +76,27 @@ def test_residual_norm_of_open_gates(dtype):
     want = 0.75 * h.double() * dr.double() * e * q * q
     near(got["dgate"], want, ((2 * g.abs() + 16) * U + half(dtype)) * want.abs(), "dgate")
     near(got["dh"], 0.75 * sig * dr.double(), ((2 * g.abs() + 16) * U + half(dtype)) * (0.75 * sig * dr.double()).abs(), "dh")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("gated", [False, True])
+def test_residual_of_what_is_not_finite(dtype, gated):
+    """Without norms nothing but its own place sees an infinite or missing value of h, and there only what the formula says does."""
+    t, rows, C = TYPES[dtype], 3, 16
+    v = norm_case("end", rows, C, t, 4)
+    v["post"] = None
+    if not gated:
+        v["gate"] = None
+    v["h"][1, 3], v["h"][2, 5] = float("inf"), float("nan")
+    got = norm_calls(v, dtype, 0.75, 1e-5)
+    sig = torch.sigmoid(v["gate"].double()) if gated else torch.ones(rows, C, dtype=torch.float64)
+    dr, h = v["dr"].double(), v["h"].double()
+    near(got["dx"], dr, 0.0, "dx")
+    near(got["dh"], 0.75 * sig * dr, (half(dtype) + 32 * U) * (0.75 * sig * dr).abs(), "dh")
+    want = v["x"].double() + 0.75 * sig * h
+    near(got["r"], want, torch.nan_to_num((half(dtype) + 32 * U) * (v["x"].double().abs() + (0.75 * sig * h).abs()), nan=0.0, posinf=0.0), "r")
+    if gated:
+        want = 0.75 * h * dr * sig * (1 - sig)
+        near(got["dgate"], want, torch.nan_to_num((half(dtype) + 32 * U) * want.abs(), nan=0.0, posinf=0.0), "dgate")
+    v["post"] = norm_case("end", rows, C, t, 4)["post"]  # (a row of h without a norm has no gradient; r has)
+    near(norm_calls(v, dtype, 0.75, 1e-5)["dx"], dr, 0.0, "dx, with a norm of h")
