@@ -149,7 +149,8 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
  *   outs[i][0 .. counts[i]) = norm > max_norm ? grads[i] * (max_norm / norm) : grads[i]   (elem type; outs[i] may be grads[i])
  * grads, outs, counts: HOST arrays of device pointers and element counts (0: nothing there; up
  * to 2^40 in all), read during the call.  outs NULL: the norm alone.
- * A norm that is NaN leaves the gradients as they are; one that is infinite scales by zero.
+ * A norm that is NaN leaves the gradients as they are; that of an infinite gradient scales by zero.  That of finite ones may be too large for norm[0],
+ * which reads infinite then; they are scaled by what it is.
  * workspace: CDP_CLIP_BYTES, 8-byte aligned; nothing in it has to be cleared. */
 #define CDP_CLIP_BYTES 65536u
 int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm,

@@ -91,8 +91,20 @@ template <typename T, int THREADS> __device__ __forceinline__ double unit_square
   }
   return s;
 }
-template <typename T, int THREADS> __device__ __forceinline__ void unit_scale(const Unit<T>& w, bool over, float f) {
-  if (!over && w.out == w.g) return;  // in place, nothing to do
+// What gradients are multiplied by.  Two factors, as one would be subnormal where gradients are large: 2^-100 or less, and what is left.
+struct Factor {
+  bool over;  // (a norm that is not a number: no)
+  float first, rest;
+  __device__ __forceinline__ Factor(double norm, float max_norm) {
+    const double f = max_norm / norm;
+    over = norm > max_norm;
+    first = f >= 0x1p-100 ? 1.f : f >= 0x1p-200 ? 0x1p-100f : 0x1p-140f;
+    rest = (float)(f * (f >= 0x1p-100 ? 1. : f >= 0x1p-200 ? 0x1p100 : 0x1p140));
+  }
+  template <typename T> __device__ __forceinline__ T operator()(T v) const { return Elem<T>::from_f32(rest * (first * Elem<T>::to_f32(v))); }
+};
+template <typename T, int THREADS> __device__ __forceinline__ void unit_scale(const Unit<T>& w, const Factor& f) {
+  if (!f.over && w.out == w.g) return;  // in place, nothing to do
   constexpr int L = UNIT_BYTES / 16 / THREADS;
   const int t = threadIdx.x, pieces = w.whole ? w.n / Unit<T>::V : 0;
   Chunk16<T> c[L];
@@ -103,13 +115,13 @@ template <typename T, int THREADS> __device__ __forceinline__ void unit_scale(co
 #pragma unroll
   for (int k = 0; k < L; ++k) {
     if (t + THREADS * k >= pieces) continue;
-    if (over)
+    if (f.over)
 #pragma unroll
-      for (int e = 0; e < Unit<T>::V; ++e) c[k].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k].e[e]));
+      for (int e = 0; e < Unit<T>::V; ++e) c[k].e[e] = f(c[k].e[e]);
     reinterpret_cast<Words*>(w.out)[t + THREADS * k] = __builtin_bit_cast(Words, c[k].v);
   }
-  if (pieces * Unit<T>::V + t < w.n) w.out[pieces * Unit<T>::V + t] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(behind)) : behind;
-  for (int e = pieces * Unit<T>::V + t + THREADS; e < w.n; e += THREADS) w.out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w.g[e])) : w.g[e];
+  if (pieces * Unit<T>::V + t < w.n) w.out[pieces * Unit<T>::V + t] = f.over ? f(behind) : behind;
+  for (int e = pieces * Unit<T>::V + t + THREADS; e < w.n; e += THREADS) w.out[e] = f.over ? f(w.g[e]) : w.g[e];
 }
 
 // Sum of squares of a workgroup's units, written to part[workgroup], or, past the first table, added to it.
@@ -132,9 +144,8 @@ template <typename T> __global__ __launch_bounds__(256) void grad_scale_kernel(c
   const double r = sqrt(group_sum<256>(s, lds));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)r;
   if (!scaling) return;
-  const bool over = r > max_norm;  // (not a number: no)
-  const float f = over ? (float)(max_norm / r) : 1.f;
-  for (int v = blockIdx.x; v < t.total; v += gridDim.x) unit_scale<T, 256>(Unit<T>(t, t.total - 1 - v, true), over, f);
+  const Factor f(r, max_norm);
+  for (int v = blockIdx.x; v < t.total; v += gridDim.x) unit_scale<T, 256>(Unit<T>(t, t.total - 1 - v, true), f);
 }
 // Both for a set of one table and few pieces; a wavefront has the pieces wave, wave + 16, ..
 template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(const ClipTable t, float* norm, float max_norm, int scaling) {
@@ -186,22 +197,21 @@ template <typename T> __global__ __launch_bounds__(SOLE) void grad_sole_kernel(c
   const double r = sqrt(group_sum<SOLE>(s, lds));
   if (threadIdx.x == 0) *norm = (float)r;
   if (!scaling) return;
-  const bool over = r > max_norm;
-  const float f = over ? (float)(max_norm / r) : 1.f;
+  const Factor f(r, max_norm);
 #pragma unroll
   for (int k = 0; k < SOLE_EACH; ++k) {
-    if (!over && w[k].out == w[k].g) continue;
+    if (!f.over && w[k].out == w[k].g) continue;
     const int pieces = wholes(k);
 #pragma unroll
     for (int l = 0; l < L; ++l) {
       if (lane + 64 * l >= pieces) continue;
-      if (over)
+      if (f.over)
 #pragma unroll
-        for (int e = 0; e < U::V; ++e) c[k][l].e[e] = Elem<T>::from_f32(f * Elem<T>::to_f32(c[k][l].e[e]));
+        for (int e = 0; e < U::V; ++e) c[k][l].e[e] = f(c[k][l].e[e]);
       reinterpret_cast<Words*>(w[k].out)[lane + 64 * l] = __builtin_bit_cast(Words, c[k][l].v);
     }
-    if (pieces * U::V + lane < w[k].n) w[k].out[pieces * U::V + lane] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(behind[k])) : behind[k];
-    for (int e = pieces * U::V + lane + 64; e < w[k].n; e += 64) w[k].out[e] = over ? Elem<T>::from_f32(f * Elem<T>::to_f32(w[k].g[e])) : w[k].g[e];
+    if (pieces * U::V + lane < w[k].n) w[k].out[pieces * U::V + lane] = f.over ? f(behind[k]) : behind[k];
+    for (int e = pieces * U::V + lane + 64; e < w[k].n; e += 64) w[k].out[e] = f.over ? f(w[k].g[e]) : w[k].g[e];
   }
 }
 

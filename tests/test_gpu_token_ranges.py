@@ -100,3 +100,20 @@ def test_residual_of_what_is_not_finite(dtype, gated):
         near(got["dgate"], want, torch.nan_to_num((half(dtype) + 32 * U) * want.abs(), nan=0.0, posinf=0.0), "dgate")
     v["post"] = norm_case("end", rows, C, t, 4)["post"]  # (a row of h without a norm has no gradient; r has)
     near(norm_calls(v, dtype, 0.75, 1e-5)["dx"], dr, 0.0, "dx, with a norm of h")
+
+
+# ---- gradient clipping -----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n", [5, 60001, 3000017])
+@pytest.mark.parametrize("max_norm", [1.0, 1e-6, 1e-20])
+def test_grad_clip_by_small_factors(dtype, n, max_norm):
+    """Factors that are subnormal or smaller in fp32: what is left of the gradients is not."""
+    t = TYPES[dtype]
+    v = (1 + randn(n, n).abs().clamp(max=2)).mul(1e38).to(t)
+    grads, outs = [v.cuda()], [torch.full((n,), float("nan"), dtype=t, device="cuda")]
+    norm = clip_call(dtype, grads, outs, max_norm)
+    want = math.sqrt(float((v.double() / 1e38).square().sum())) * 1e38
+    if want < 3.4e38:
+        near(norm, torch.tensor([want], dtype=torch.float64), 2 * U * want, "norm")
+    want = v.double() * (max_norm / want)
+    near(outs[0], want, (half(dtype) + 4 * U) * want.abs(), "out")
