@@ -102,6 +102,33 @@ def test_residual_of_what_is_not_finite(dtype, gated):
     near(norm_calls(v, dtype, 0.75, 1e-5)["dx"], dr, 0.0, "dx, with a norm of h")
 
 
+def test_packed_attention_products_of_fp32():
+    """A score of two products that all but cancel, a b - fl(a b), enlarged 2^20 times: one token per sequence, whose lse is that score.  A product is
+    that of three planes of 8 bits of either operand without the three smallest of nine: with 2^-7 and 2^-15 at most behind the first and the second plane, 2 x 2^-22 + 2^-30 of the
+    product.  The last of its sums, whose terms are as large, has U; what the five sums before it have is 2^-6 at most.  Then 8 U of lse itself."""
+    g = np.random.default_rng(5)
+    T, H, W = 200, 8, 8
+    a, c = ((1 + g.random((T, H))).astype(np.float32) for _ in range(2))
+    a[0], c[0] = 1 + 2.0 ** -7 - 2.0 ** -23, 1 + 2.0 ** -7 - 2.0 ** -23
+    a[1], c[1] = 1 + 2.0 ** -7 - 2.0 ** -15, 1 + 2.0 ** -6 - 2.0 ** -22
+    qkv = torch.zeros(T, 3, H, W)
+    qkv[:, 0, :, 0], qkv[:, 1, :, 0] = torch.from_numpy(a), torch.from_numpy(c)
+    qkv[:, 0, :, 1], qkv[:, 1, :, 1] = torch.from_numpy(-(a * c)), 1.0
+    out, lse, _ = attention_call(F32, qkv.reshape(T, 3 * H * W), list(range(T + 1)), H, H, W, 2.0 ** 20, None, 0)
+    product = a.astype(np.float64) * c
+    want = torch.from_numpy((product - (a * c)).T * 2.0 ** 20)
+    near(lse, want, 2.0 ** 20 * ((2.0 ** -21 + 2.0 ** -30 + U) * torch.from_numpy(product.T) + 5 * U * 2.0 ** -6) + 8 * U * want.abs(), "lse")
+
+
+def test_packed_attention_of_the_largest_values():
+    """Finite values that round to an infinite one in fewer bits are finite: one key, whose value is the result."""
+    big = torch.finfo(torch.float32).max
+    qkv = torch.zeros(2, 24)
+    qkv[0, 16:], qkv[1, 16:] = big, torch.tensor([big, -big, 2.0 ** 127, 3.39e38, 3.397e38, -3.4e38, 1.0, 0.0])
+    out, lse, _ = attention_call(F32, qkv, [0, 1, 2], 1, 1, 8, 1.0, None, 0)
+    assert torch.equal(out.cpu(), qkv[:, 16:]) and not lse.any()
+
+
 # ---- gradient clipping -----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n", [5, 60001, 3000017])
