@@ -136,8 +136,8 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const
  *   backward 1: dqkv from dout[tokens][heads * width] and the forward's out and lse
  * Sums are fp32; fp32 products leave out less than 2^-21 of themselves (2^-24.5 on average).  Between two products the
  * element type rounds P and dS.
- * What is infinite or NaN in a row of k or v may reach every row of its
- * sequence, earlier ones too (0 * NaN), and no other sequence.
+ * What is infinite or NaN in a row of qkv or dout may reach every row of its sequence, earlier and later ones (0 * NaN), as NaN in fp32, and no other
+ * sequence.
  * Rows outside all sequences are neither read for another's sake nor written.  Offsets that are not as said give wrong results, within
  * the tensors.
  * workspace (backward): 4 * heads * tokens + 512 bytes (CDP_EINVAL if smaller).  Where it holds P times 8 * kv_heads * tokens * width

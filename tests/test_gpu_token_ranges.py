@@ -120,6 +120,23 @@ def test_packed_attention_products_of_fp32():
     near(lse, want, 2.0 ** 20 * ((2.0 ** -21 + 2.0 ** -30 + U) * torch.from_numpy(product.T) + 5 * U * 2.0 ** -6) + 8 * U * want.abs(), "lse")
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("heads,kv_heads,width,lengths", [(2, 1, 16, [20, 33, 9]), (4, 4, 64, [40, 100, 31]), (4, 2, 72, [300, 321, 65]), (54, 54, 64, [130, 129, 140])])
+def test_packed_attention_of_what_is_not_finite_stays_in_its_sequence(dtype, heads, kv_heads, width, lengths):
+    """Rows of q, k, v and dout in the middle sequence, its first and last among them: the other two have the same bits as without."""
+    at, qkv, dout = attention_case(1, lengths, 2, heads, kv_heads, width, TYPES[dtype], 7)
+    clean = attention_call(dtype, qkv, at, heads, kv_heads, width, 0.2, dout, 0)
+    qkv, dout = qkv.clone(), dout.clone()
+    x = qkv.view(qkv.shape[0], heads + 2 * kv_heads, width)
+    for row, what in ((at[1], float("inf")), (at[1] + 3, float("nan")), (at[2] - 1, -float("inf"))):
+        x[row, ::2], dout[row, 5:] = what, what
+    got = attention_call(dtype, qkv, at, heads, kv_heads, width, 0.2, dout, 0)
+    for a, b_ in ((at[0], at[1]), (at[2], at[3])):
+        for i, (one, two) in enumerate(zip(clean, got)):
+            one, two = (v.T[a:b_] if i == 1 else v[a:b_] for v in (one, two))
+            assert torch.equal(one, two) and bool(torch.isfinite(one).all())
+
+
 def test_packed_attention_of_the_largest_values():
     """Finite values that round to an infinite one in fewer bits are finite: one key, whose value is the result."""
     big = torch.finfo(torch.float32).max
