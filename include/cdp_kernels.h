@@ -134,8 +134,9 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const
  *   backward 0: out[tokens][heads * width] = softmax(scale * q k^T) v, lse[heads][tokens] (fp32) = log of the sum that the softmax divides
  *               by, sum exp(scale * q k^T)   (dout, dqkv, workspace unused)
  *   backward 1: dqkv from dout[tokens][heads * width] and the forward's out and lse
- * Sums are fp32; fp32 products leave out less than 2^-21 of themselves (2^-24.5 on average).  Between two products the
- * element type rounds P and dS.
+ * Sums are fp32.  fp32 products leave out less than 2^-21 of themselves (2^-24.5 on average).  bf16: between two products P and dS are
+ * rounded to the element type, but held in two of it where one launch does the backward of few rows.  That and the order of sums go by
+ * all sizes of a call: what a sequence is packed with may change its results by their roundings.
  * What is infinite or NaN in a row of qkv or dout may reach every row of its sequence, earlier and later ones (0 * NaN), as NaN in fp32, and no other
  * sequence.
  * Rows outside all sequences are neither read for another's sake nor written.  Offsets that are not as said give wrong results, within
