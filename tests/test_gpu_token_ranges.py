@@ -102,6 +102,25 @@ def test_residual_of_what_is_not_finite(dtype, gated):
     near(norm_calls(v, dtype, 0.75, 1e-5)["dx"], dr, 0.0, "dx, with a norm of h")
 
 
+# more row groups than workgroups backward (512), so that every one has a second and third, of one wavefront's lanes or several, on aligned tensors and others
+MANY_ROWS = [(20000, 64), (6272, 192), (2100, 768), (1700, 1000), (1300, 2056), (1100, 4096), (1037, 8192), (515, 16384), (700, 1500)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,C", MANY_ROWS)
+@pytest.mark.parametrize("form,shift", [("all", 0), ("all", 1), ("norm alone", 0), ("no dr", 0)])
+def test_residual_norm_of_many_rows(dtype, rows, C, form, shift):
+    norm_check(norm_case(form, rows, C, TYPES[dtype], C), dtype, 0.75, 1e-5, shift)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows,C", [(2, 64), (64, 64), (34, 256), (600, 96), (4, 4096), (2, 8192), (4, 16384), (6, 768), (40, 1000), (1030, 520)])
+def test_residual_norm_of_aligned_rows(dtype, rows, C):
+    """Even numbers of rows on tensors of 16-byte borders."""
+    for form in ("all", "no post", "no gate", "h alone", "norm alone", "end", "no dr"):
+        norm_check(norm_case(form, rows, C, TYPES[dtype], C), dtype, 0.75, 1e-5)
+
+
 def test_packed_attention_products_of_fp32():
     """A score of two products that all but cancel, a b - fl(a b), enlarged 2^20 times: one token per sequence, whose lse is that score.  A product is
     that of three planes of 8 bits of either operand without the three smallest of nine: with 2^-7 and 2^-15 at most behind the first and the second plane, 2 x 2^-22 + 2^-30 of the
