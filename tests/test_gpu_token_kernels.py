@@ -425,7 +425,7 @@ def test_packed_attention(dtype, before, lengths, behind, heads, kv_heads, width
     near(dqkv[used.cuda()], res["dqkv"][used], tol["dqkv"][used], "dqkv")
 
 
-# enough workgroups that wavefronts do not share rows, in every width's kernels; 63 and 64 sequences, which are put in order in different ways
+# launches of many workgroups (test_gpu_token_ranges.py has a case for every kernel); 63 and 64 sequences, which are put in order in different ways
 CROWDED = [(0, [37] * 62 + [200], 5, 12, 4, 64), (3, [37, 0, 90, 1] * 16, 0, 12, 12, 32), (0, [300, 700, 129, 64, 500], 0, 32, 8, 128), (0, [511, 2, 640], 0, 64, 64, 96),
            (0, [900, 800], 1, 56, 8, 80), (0, [640, 33], 3, 64, 16, 104), (0, [129] * 40, 1, 16, 16, 16), (2, [1500], 0, 72, 24, 48)]
 

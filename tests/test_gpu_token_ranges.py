@@ -121,6 +121,40 @@ def test_residual_norm_of_aligned_rows(dtype, rows, C):
         norm_check(norm_case(form, rows, C, TYPES[dtype], C), dtype, 0.75, 1e-5)
 
 
+# ---- packed causal attention --------------------------------------------------------------------------------------------
+# Cases by which every kernel is compared, of every width: queries and keys, wavefronts that share 32 rows and those that have 32 each, equal heads and grouped
+# ones, and those whose query heads are shared by workgroups (with room for their sums in the workspace).
+PLACES = [(0, [2100], 2, 54, 6, 16), (0, [2090], 0, 54, 6, 32), (1, [2060], 0, 54, 6, 40), (0, [2100], 0, 54, 6, 64), (0, [2050], 0, 54, 6, 72), (0, [2077], 3, 45, 5, 96)]
+PLACES += [(0, [130, 131] * 4, 1, 54, 54, w) for w in (16, 32, 40, 64, 80, 88, 112, 128)]
+PLACES += [(0, [300, 290], 11, 2, 2, w) for w in (8, 32, 48, 64, 80, 96, 104, 128)]
+PLACES += [(2, [600, 95], 0, 4, 2, w) for w in (16, 24, 48, 64, 72, 96, 112, 120)]
+PLACES += [(0, [60, 39], 1, 2, 2, w) for w in (80, 104)] + [(0, [33, 60], 0, 4, 2, w) for w in (72, 112)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("before,lengths,behind,heads,kv_heads,width", PLACES, ids=str)
+def test_packed_attention_by_every_kernel(dtype, before, lengths, behind, heads, kv_heads, width):
+    t, scale = TYPES[dtype], 1.3 * width ** -0.5
+    at, qkv, dout = attention_case(before, lengths, behind, heads, kv_heads, width, t, width)
+    outside = torch.ones(qkv.shape[0], dtype=torch.bool)
+    outside[at[0]:at[-1]] = False
+    qkv[outside], dout[outside] = float("nan"), float("nan")
+    used = ~outside
+    scale32 = float(np.float32(scale))
+    with torch.device("cuda"):  # (the references' products of long sequences)
+        clean = lambda v: torch.where(outside.cuda()[:, None], 0.0, v.cuda().double())  # noqa: E731
+        res, tol, _ = attention_reference(clean(qkv), at, heads, kv_heads, width, scale32, dtype)
+    for parts in (0, 8) if heads > kv_heads else (0,):
+        out, lse, dqkv = attention_call(dtype, qkv, at, heads, kv_heads, width, scale, dout, parts)
+        near(out.cpu()[used], res["out"].cpu()[used], tol["out"].cpu()[used], "out")
+        near(lse.cpu()[:, used], res["lse"].cpu()[:, used], tol["lse"].cpu()[:, used], "lse")
+        with torch.device("cuda"):
+            back, back_tol, _ = attention_reference(clean(qkv), at, heads, kv_heads, width, scale32, dtype, clean(dout), clean(out), torch.where(outside.cuda(), 0.0, lse.double()))
+        near(dqkv.cpu()[used], back["dqkv"].cpu()[used], back_tol["dqkv"].cpu()[used], "dqkv, %d parts" % parts)
+        for v in (out, lse.T, dqkv):
+            assert bool(torch.isnan(v[outside.cuda()]).all())
+
+
 def test_packed_attention_products_of_fp32():
     """A score of two products that all but cancel, a b - fl(a b), enlarged 2^20 times: one token per sequence, whose lse is that score.  A product is
     that of three planes of 8 bits of either operand without the three smallest of nine: with 2^-7 and 2^-15 at most behind the first and the second plane, 2 x 2^-22 + 2^-30 of the
