@@ -226,14 +226,16 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     const int64_t at = group * Ly::SLOTS * C * (int)sizeof(T);
     unsigned off[K];
     offsets(group, off);
-    float e[1] = {0.f}, s[NS] = {}, sig[N], r[N];
+    float e[1] = {0.f}, s[NS] = {}, sig[N], away[Ly::HEAVY ? 1 : N], r[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) e[0] += w.h[i] * w.h[i];
     row_sums<LR>(e, lds_eta[parity]);
     const float eta = a.gamma_post ? rsqrtf(e[0] * inv + a.eps) : 1.f, f = a.scale * eta;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      sig[i] = a.gate ? sigmoid(w.g[i]) : 1.f;
+      const float x = __expf(-w.g[i]);
+      sig[i] = a.gate ? __builtin_amdgcn_rcpf(1.f + x) : 1.f;
+      if constexpr (!Ly::HEAVY) away[i] = x;
       const float hp = w.h[i] * post[i], ad = w.dy[i] * pre[i], sgh = a.scale * sig[i] * hp;
       r[i] = w.x[i] + f * hp * sig[i];
       s[0] += r[i] * r[i];
@@ -266,8 +268,12 @@ __global__ __launch_bounds__(LR > 256 ? LR : 256) void residual_norm_bwd_kernel(
     for (int i = 0; i < N; ++i) {
       const float h = w.h[i], du = a.scale * sig[i] * d[i], n = h * eta;
       sum_of(0, i) += du * n;
-      // 1 - sigmoid(g), not as a difference: of an open gate that has no bits left (g = 10: 1e-3 off, from 17 on zero)
-      dg[i] = du * (n * post[i]) * sigmoid(-w.g[i]);
+      // 1 - sigmoid(g), not as a difference: of an open gate that has no bits left (g = 10: 1e-3 off, from 17 on zero).  exp(-g) sigmoid(g), and 1 where that
+      // is inf * 0; where the register for it would be spilled sigmoid(-g) is faster (us, backward, 4096 x 12288 in bf16 448 / 373; 16384 x 4096 223 / 226)
+      float shut;
+      if constexpr (Ly::HEAVY) shut = sigmoid(-w.g[i]);
+      else shut = fminf(away[i] * sig[i], 1.f);
+      dg[i] = du * (n * post[i]) * shut;
       d[i] = eta * (du * post[i]);
     }
     if (a.gamma_post)
