@@ -214,3 +214,97 @@ def test_grad_clip_by_small_factors(dtype, n, max_norm):
         near(norm, torch.tensor([want], dtype=torch.float64), 2 * U * want, "norm")
     want = v.double() * (max_norm / want)
     near(outs[0], want, (half(dtype) + 4 * U) * want.abs(), "out")
+
+
+# ---- more than 32 bits --------------------------------------------------------------------------------------------------
+FAR = 540_000, 4096  # rows and columns: more than 2^31 elements, 4.4 GB in bf16
+
+
+def far_tensor(seed, rows, C):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn((rows, C), generator=g, device="cuda", dtype=torch.bfloat16)
+
+
+def test_embedding_of_rows_past_2_to_the_31():
+    """Lookup and gradient; words are taken in turn, so that a word's tokens lie everywhere."""
+    (rows, C), vocab = FAR, 1001
+    table, ids = far_tensor(1, vocab, C), (torch.arange(rows, device="cuda") % vocab).to(torch.int32)
+    out = torch.empty((rows, C), device="cuda", dtype=torch.bfloat16)
+    b.cdp_k_embedding(BF16, 0, p(table), p(ids), 0, p(out), 1.0, 0, 0, rows, vocab, C)
+    for at in range(0, rows, 50_000):
+        assert torch.equal(out[at:at + 50_000], table[ids[at:at + 50_000].long()])
+    need = 16 * rows + 8 * C * -(-rows // 32) + 512
+    dtable, ws = torch.empty((vocab, C), device="cuda"), torch.empty(need, dtype=torch.uint8, device="cuda")
+    b.cdp_k_embedding(BF16, 1, 0, p(ids), p(out), p(dtable), 1.0, p(ws), need, rows, vocab, C)
+    n = torch.bincount(ids, minlength=vocab).double()[:, None]
+    near(dtable, (n * table.double()).cpu(), ((n + 2) * U * n * table.double().abs()).cpu(), "dtable")
+
+
+@pytest.mark.parametrize("rows,vocab", [(5000, (1 << 20) - 1), (5000, 1 << 20), (5000, (1 << 20) + 5), (600_000, 4001), (530_000, 3)])
+def test_embedding_gradient_of_many_words_and_tokens(rows, vocab):
+    """Keys of 32 and of 64 bits over several runs; three rounds of merges."""
+    C = 4
+    ids = torch.randint(-1, vocab + 1, (rows,), generator=torch.Generator().manual_seed(rows))
+    ids[::7] = vocab - 1
+    dout, need = randn(2, rows, C).float(), 16 * rows + 8 * C * -(-rows // 32) + 512
+    got = torch.full((vocab, C), float("nan"), device="cuda")
+    ids_d, dout_d = ids.to(torch.int32).cuda(), dout.cuda()
+    b.cdp_k_embedding(F32, 1, 0, p(ids_d), p(dout_d), p(got), 1.0, p(workspace(need)), need, rows, vocab, C)
+    inside = (ids >= 0) & (ids < vocab)
+    at, d = torch.where(inside, ids, 0), dout.double() * inside[:, None]
+    grad, size, n = (torch.zeros((vocab, k), dtype=torch.float64).index_add_(0, at, v) for k, v in ((C, d), (C, d.abs()), (1, inside.double()[:, None])))
+    near(got, grad, (n + 2) * U * size, "dtable")
+
+
+def test_residual_norm_of_rows_past_2_to_the_31():
+    (rows, C), scale, eps = FAR, 0.75, 1e-5
+    v = {k: far_tensor(i, rows, C) for i, k in enumerate(("x", "h", "gate", "dr", "dy"))}
+    post, pre = ((1 + randn(i, C, scale=0.2)).float().cuda() for i in (8, 9))
+    got = {k: torch.full((rows, C), float("nan"), device="cuda", dtype=torch.bfloat16) for k in ("r", "y", "dx", "dh", "dgate")}
+    dpost, dpre, need = torch.empty(C, device="cuda"), torch.empty(C, device="cuda"), 8 * C * 512 + 256
+    b.cdp_k_residual_norm(BF16, p(v["x"]), p(v["h"]), p(v["gate"]), p(post), p(pre), p(got["r"]), p(got["y"]), scale, eps, rows, C)
+    b.cdp_k_residual_norm_backward(BF16, 0, p(v["x"]), p(v["h"]), p(v["gate"]), p(post), p(pre), p(v["dr"]), p(v["dy"]), p(got["dx"]), p(got["dh"]), p(got["dgate"]), p(dpost),
+                                   p(dpre), scale, eps, p(workspace(need)), need, rows, C)
+    at = torch.tensor([0, 1, 262_143, 262_144, 524_287, 524_288, 524_289, rows - 2, rows - 1], device="cuda")
+    args = [v[k][at].double() for k in ("x", "h", "gate")] + [post.double(), pre.double()] + [v[k][at].double() for k in ("dr", "dy")]
+    res, size = norm_reference(*args, scale, float(np.float32(eps)))
+    for k, x in got.items():
+        near(x[at], res[k].cpu(), norm_tolerance(k, res, size, BF16, rows).cpu(), k)
+        assert not any(bool(torch.isnan(x[i:i + 90_000]).any()) for i in range(0, rows, 90_000))
+    assert bool(torch.isfinite(dpost).all()) and bool(torch.isfinite(dpre).all())
+
+
+def test_packed_attention_past_4_gib():
+    """600 sequences of 1000 tokens, 30 heads over one: rows of 8 KB."""
+    n, S, H, K, W, scale = 1000, 600, 30, 1, 128, 0.1
+    T = n * S + 3
+    qkv, dout = far_tensor(1, T, (H + 2 * K) * W), far_tensor(2, T, H * W)
+    offsets = torch.arange(S + 1, device="cuda", dtype=torch.int32) * n
+    out, dqkv = (torch.full_like(v, float("nan")) for v in (dout, qkv))
+    lse, need = torch.full((H, T), float("nan"), device="cuda"), 4 * H * T + 512
+    b.cdp_k_attention_packed(BF16, 0, p(qkv), p(offsets), p(out), p(lse), 0, 0, 0, 0, T, S, H, K, W, scale)
+    b.cdp_k_attention_packed(BF16, 1, p(qkv), p(offsets), p(out), p(lse), p(dout), p(dqkv), p(workspace(need)), need, T, S, H, K, W, scale)
+    for s in (0, 261, 524, 525, S - 1):
+        rows = slice(n * s, n * (s + 1))
+        with torch.device("cuda"):
+            x, scale32 = qkv[rows].double(), float(np.float32(scale))
+            res, tol, _ = attention_reference(x, [0, n], H, K, W, scale32, BF16)
+            back, back_tol, _ = attention_reference(x, [0, n], H, K, W, scale32, BF16, dout[rows].double(), out[rows].double(), lse[:, rows].double())
+        for got, k in ((out[rows], "out"), (lse[:, rows], "lse")):
+            near(got, res[k].cpu(), tol[k].cpu(), k)
+        near(dqkv[rows], back["dqkv"].cpu(), back_tol["dqkv"].cpu(), "dqkv")
+    assert all(bool(torch.isnan(v[n * S:]).all()) for v in (out, lse.T, dqkv))
+
+
+def test_grad_clip_of_more_than_2_to_the_32_elements():
+    """Ones: the norm is the root of their number, whichever are lost is seen."""
+    n = (1 << 32) + 12345
+    g = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    g[-1] = 3.0
+    norm = clip_call(BF16, [g], [g], 64.0)
+    want = math.sqrt(n + 8)
+    near(norm, torch.tensor([want], dtype=torch.float64), 2 * U * want, "norm")
+    one = torch.tensor(64.0 / want, dtype=torch.float64)
+    near(g[:1], one.reshape(1), (2.0 ** -8 + 4 * U) * one, "first")
+    near(g[-1:], 3 * one.reshape(1), 3 * (2.0 ** -8 + 4 * U) * one, "last")
+    assert all(bool((g[i:min(i + (1 << 28), n - 1)] == g[0]).all()) for i in range(0, n - 1, 1 << 28))
