@@ -112,7 +112,8 @@ int cdp_k_embedding(int dtype, int backward, const void* table, const int32_t* i
  *   u = norm(h) * gamma_post       h[rows][C]: what the block computed; gamma_post NULL: u = h
  *   r = x + scale * sigmoid(gate) * u       gate[rows][C]; NULL: no gate.  h NULL: r = x, and gate and gamma_post are NULL
  *   y = norm(r) * gamma_pre        gamma_pre NULL: no y
- * x, h, gate, r, y in the element type, gamma_* fp32[C].  r may be NULL (not wanted) if y is not; r may be x. */
+ * x, h, gate, r, y in the element type, gamma_* fp32[C].  r may be NULL (not wanted) if y is not; r may be x, which the
+ * backward of y reads, however: not where that is to follow. */
 int cdp_k_residual_norm(int dtype, const void* x, const void* h, const void* gate, const float* gamma_post, const float* gamma_pre,
                         void* r, void* y, float scale, float eps, int rows, int C, void* stream);
 
@@ -137,6 +138,7 @@ int cdp_k_residual_norm_backward(int dtype, int accumulate, const void* x, const
  * Sums are fp32.  fp32 products leave out less than 2^-21 of themselves (2^-24.5 on average).  bf16: between two products P and dS are
  * rounded to the element type, but held in two of it where one launch does the backward of few rows.  That and the order of sums go by
  * all sizes of a call: what a sequence is packed with may change its results by their roundings.
+ * The backward makes probabilities from lse, with its rounding: |lse| * 2^-22 of themselves.
  * What is infinite or NaN in a row of qkv or dout may reach every row of its sequence, earlier and later ones (0 * NaN), as NaN in fp32, and no other
  * sequence.
  * Rows outside all sequences are neither read for another's sake nor written.  Offsets that are not as said give wrong results, within

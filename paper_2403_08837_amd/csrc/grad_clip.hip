@@ -6,7 +6,8 @@
 // order: no third launch, no atomics.  The second pass goes through the units backwards: what the first read last is still cached.
 // fp32, 400 million elements in 300 tensors: 0.88 ms, 5.5 TB/s over the two reads and the write.
 // Sets of up to 64 pieces of 4 KB are one launch of one workgroup, whose wavefronts keep their pieces in registers between the two.
-// The tensors' addresses travel in the kernel arguments, 160 of them a launch (160 tensors of 100 elements 9.3 us, 161 15.1); a wavefront finds the tensor of a unit by comparing all of them at once.
+// The tensors' addresses travel in the kernel arguments, 160 of them a launch (160 tensors of 100 elements 9.3 us, 161 15.1); a wavefront finds the
+// tensor of a unit by comparing all of them at once.
 #include "elem.h"
 #include "kernels.h"
 
@@ -18,7 +19,8 @@ namespace cdp {
 namespace {
 
 constexpr int CLIP_TENSORS = 160, CLIP_GROUPS = 2048, UNIT_BYTES = 32768;
-constexpr int SOLE = 1024, SOLE_BYTES = 4096, SOLE_EACH = 4, SOLE_UNITS = SOLE / 64 * SOLE_EACH;  // one workgroup: threads, bytes of a piece, pieces of a wavefront, of all
+// one workgroup: threads, bytes of a piece, pieces of a wavefront, of all
+constexpr int SOLE = 1024, SOLE_BYTES = 4096, SOLE_EACH = 4, SOLE_UNITS = SOLE / 64 * SOLE_EACH;
 
 struct ClipTable {
   const void* g[CLIP_TENSORS];

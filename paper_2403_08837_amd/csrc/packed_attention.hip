@@ -15,9 +15,10 @@
 // fp32: the same with every operand as three bf16 planes (Part), tiles of 32 rows instead of 64.
 //
 // Bound by the matrix cores for long sequences, with the exponentials and the LDS reads between the products: 8192 tokens, 32 heads of 128 over 8, bf16: forward
-// 525 us, 1050 TFLOP/s (a large matrix product: 1339), backward 1800 us, 765; fp32 4096 tokens, 16 heads of 128 over 4: 450 us, 153 TFLOP/s, and
-// 1640, 105.  For short ones by a workgroup's own way: its span, its rows, its tiles, one memory round trip after the other: 8192 tokens in 24
-// sequences, 12 heads of 64 over 4, bf16: 22 us and 65, of which bytes and products would be 7 and 14.
+// 530 us, 1040 TFLOP/s (a large matrix product: 1339), backward 1800 us, 765; fp32 4096 tokens, 16 heads of 128 over 4: 452 us, 153 TFLOP/s, and
+// 1655, 104 (its kernel for keys has all 512 registers of a lane and spills 40 more: k and v in planes are 192, the sums 128; at width 112 16; where
+// wavefronts share rows 67 and 43, in the launch for both 69 and 49).  For short ones by a workgroup's own way: its span, its rows, its tiles, one memory
+// round trip after the other: 8192 tokens in 24 sequences, 12 heads of 64 over 4, bf16: 22 us and 65, of which bytes and products would be 7 and 14.
 #include "elem.h"
 #include "kernels.h"
 
@@ -33,12 +34,13 @@ typedef __attribute__((address_space(3))) void* lds_ptr;
 
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
-// Tile of `OTHER` rows of one head, DW columns (zeros past the width; products along a row take SW of them), in LDS.  16-byte chunk c of row r sits in slot c ^ swz(r) of the
-// row: 16 consecutive rows' chunk c are 16 different slots modulo 256 bytes, and so are the pieces that a read across rows takes.
+// Tile of `OTHER` rows of one head, DW columns (zeros past the width; products along a row take SW of them), in LDS.  16-byte chunk c of row r sits in slot
+// c ^ swz(r) of the row: 16 consecutive rows' chunk c are 16 different slots modulo 256 bytes, and so are the pieces that a read across rows takes.
 constexpr int columns(int sw) { return (sw + 31) / 32 * 32; }
 template <typename T, int SW, bool SPLIT> struct Tile {
   static constexpr int DW = columns(SW);
-  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC, STEPS = SW / 16, CHUNKS = SW * E / 32;  // products along a row; 16-byte reads of it by either lane half
+  static constexpr int E = sizeof(T), VEC = 16 / E, CPR = DW / VEC;
+  static constexpr int STEPS = SW / 16, CHUNKS = SW * E / 32;  // products along a row; 16-byte reads of it by either lane half
   static constexpr int OWN = SPLIT ? 32 : 128, OTHER = SPLIT || E == 4 ? 32 : 64, NB = OTHER / 32, OB = DW / 32;
   static constexpr int BYTES = OTHER * DW * E, FILLERS = SPLIT ? 1 : 4, LOADS = BYTES / 1024 / FILLERS;  // wavefronts that fill a tile, loads of each
   static_assert(LOADS * FILLERS * 1024 == BYTES, "tiles are dealt to the wavefronts in 1 KB blocks");
@@ -137,9 +139,10 @@ template <typename Tl> __device__ __forceinline__ unsigned across_place(int lane
   }
 }
 // bf16: p is rounded to the operand's type, as the matrix instruction has no other: half a step of every term, in a sum of terms of either sign as
-// much again as the result's own rounding.  FINE: p in two planes, its rounding and what that leaves, a second product for each.  Errors of out and of dqkv, of their
-// norm, rounded / FINE (1.6e-3 is the rounding of the results themselves): 8192 tokens in 24 sequences, 12 heads of 64 over 4 2.0e-3 / 1.6e-3 and 2.4e-3 / 1.8e-3; us,
-// forward and backward: 22.6 / 27.1 and 66 / 75, one sequence, 32 heads of 128 over 8 533 / 691 and 1811 / 2371.  So it is for the launches that have the time.
+// much again as the result's own rounding.  FINE: p in two planes, its rounding and what that leaves, a second product for each.  Errors of out and of
+// dqkv, of their norm, rounded / FINE (1.6e-3 is the rounding of the results themselves): 8192 tokens in 24 sequences, 12 heads of 64 over 4 2.0e-3 /
+// 1.6e-3 and 2.4e-3 / 1.8e-3; us, forward and backward: 22.6 / 27.1 and 66 / 75, one sequence, 32 heads of 128 over 8 533 / 691 and 1811 / 2371.  So it is
+// for the launches that have the time.
 template <typename T, typename Tl, bool FINE, int OB>
 __device__ __forceinline__ void across_product(Lane at, Lane at8, int r0, const v16f_t& p, v16f_t (&out)[OB]) {
   constexpr int PITCH = Tl::CPR * 16;
@@ -386,7 +389,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && SW > (SPLIT ? 64 : 96) ? 1 :
   __shared__ __attribute__((aligned(1024))) char memory[Tl::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
-  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;
   const int head = blockIdx.x % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
   const Span span = find_span<Tl::OWN, false>(a, blockIdx.x / a.heads, gridDim.x / a.heads, lane);
   if (span.len == 0) return;
@@ -402,7 +406,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && SW > (SPLIT ? 64 : 96) ? 1 :
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-    auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
+  auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
     const int k0 = i * Tl::OTHER;
     loads.issue(lds + (2 * stage + v) * Tl::BYTES, filler, (v ? vbase : kbase) + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
@@ -521,11 +525,13 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 && SW > (SPLIT ? 64 : 96) ? 1 :
 
 // ---- backward: dq, and delta for the other kernel ---------------------------------------------------------------------
 // id: of the workgroups for queries, of which there are `all`.
-template <typename T, int SW, bool SPLIT, bool FINE> __device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
+template <typename T, int SW, bool SPLIT, bool FINE>
+__device__ __forceinline__ void bwd_q(const PackedAttention& a, unsigned smem, unsigned id, unsigned all, bool write_delta) {
   using Tl = Tile<T, SW, SPLIT>;
   constexpr int DW = Tl::DW;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
-  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;
   const int head = id % a.heads, kv = head / (a.heads / a.kv_heads), W = a.width;
   const Span span = find_span<Tl::OWN, false>(a, id / a.heads, all / a.heads, lane);
   if (span.len == 0) return;
@@ -558,7 +564,7 @@ template <typename T, int SW, bool SPLIT, bool FINE> __device__ __forceinline__ 
   loads.start(filler, lane, row_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-    auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
+  auto issue = [&](int i, int stage, bool v) {  // tiles of k, then of v
     const int k0 = i * Tl::OTHER;
     loads.issue(lds + (2 * stage + v) * Tl::BYTES, filler, (v ? vbase : kbase) + (int64_t)k0 * row_bytes, span.len - k0, row_bytes, W);
   };
@@ -656,7 +662,8 @@ template <typename T, int SW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   constexpr int DW = Tl::DW;
   __shared__ __attribute__((aligned(16))) float stats[SPLIT ? 4 : 2][2][64];  // per wavefront or stage: lse and delta of the tile's rows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l31 = lane & 31, hi = lane >> 5;
-  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  // which of the workgroup's 32-row groups is the wavefront's; its place among those that fill a tile
+  const int rows_of = SPLIT ? 0 : wave, filler = SPLIT ? 0 : wave;
   const int share = wg % shares, kv = wg / shares % a.kv_heads, group = a.heads / a.kv_heads, W = a.width;
   const Span span = find_span<Tl::OWN, true>(a, wg / (shares * a.kv_heads), 0, lane);
   if (span.len == 0) return;
@@ -674,7 +681,7 @@ template <typename T, int SW, bool SPLIT, bool OWN> __device__ __forceinline__ v
   oloads.start(filler, lane, out_bytes, W);
   const unsigned lds = smem + (SPLIT ? wave * (Tl::LDS / 4) : 0);
   const unsigned rows_of_tile = lds + rows_place<Tl>(l31, hi), across_tile = lds + across_place<Tl>(lane, 0), across_tile8 = lds + across_place<Tl>(lane, 8);
-    const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
+  const int per_head = (span.len - span.first + Tl::OTHER - 1) / Tl::OTHER, tiles = per_head * (group / shares);
   const int head0 = kv * group + share * (group / shares);
   __shared__ float own_memory[OWN ? OWN_ROWS : 1];  // [head of the group][query - first]
   const unsigned own = (unsigned)(uintptr_t)(lds_ptr)own_memory;
@@ -818,13 +825,14 @@ template <typename T, int SW, bool SPLIT, bool OWN> __device__ __forceinline__ v
     write(static_cast<T*>(a.dqkv) + (int64_t)(span.begin + key) * (a.heads + 2 * a.kv_heads) * W + (a.heads + kv) * W, (int64_t)a.kv_heads * W);
 }
 template <typename T, int SW, bool SPLIT>
-__global__ __launch_bounds__(256, (sizeof(T) == 2 && (SW <= 96 || !SPLIT)) || SW <= 32 ? 2 : 1) void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
+__global__ __launch_bounds__(256, (sizeof(T) == 2 && (SW <= 96 || !SPLIT)) || SW <= 32 ? 2 : 1)
+void packed_bwd_kv_kernel(const PackedAttention a, const int shares) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, SW, SPLIT>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
   bwd_kv<T, SW, SPLIT, false>(a, smem, blockIdx.x, shares);
 }
-// Both in one launch, for few rows: the workgroups past `queries` are those for keys.  bf16: P and dS in two planes, as there is time for it (0.1 of 7.7 us, 128 tokens, 8 heads of 64; 0.9 of 16.6, 512 tokens):
-// with sums this short their rounding is half of what a gradient is off (2.5e-3 of its norm, 2.0e-3 so; 1.7e-3 are its own rounding).
+// Both in one launch, for few rows: the workgroups past `queries` are those for keys.  bf16: P and dS in two planes, as there is time for it (0.1 of 7.7 us,
+// 128 tokens, 8 heads of 64; 0.9 of 16.6, 512 tokens): their rounding is half of what a gradient is off (2.5e-3 of its norm, 2.0e-3 so; 1.7e-3 are its own).
 template <typename T, int SW> __global__ __launch_bounds__(256, 1) void packed_bwd_both_kernel(const PackedAttention a, const unsigned queries) {
   __shared__ __attribute__((aligned(1024))) char memory[Tile<T, SW, true>::LDS];
   const unsigned smem = (unsigned)(uintptr_t)(lds_ptr)memory;
@@ -880,9 +888,12 @@ int64_t workgroups(const PackedAttention& a, int own, int heads) { return ((int6
 //   792 345 / 345; 128: 264 408 / 271, 384 73 / 63, 528 463 / 531 (dq crosses at the same counts);
 //   backward by its kernel for keys, bf16 64: 528 204 / 185, 768 57.6 / 53.2, 896 93 / 98; 96: 528 255 / 255; 128: 192 115 / 106, 272 152 / 153, 384 60 / 73;
 //   fp32 64: 384 123 / 114, 528 889 / 927; 128: 264 1488 / 1441, 384 240 / 254.  Where query heads share a key head, 128 rows need their shares' fold too:
-//   bf16 128: 2048 tokens, 16 heads over 2 216 / 150, in 20 sequences 73 / 56, 4096 tokens, 16 over 4 329 / 455; 96: 4096 tokens, 16 over 2 335 / 231; fp32 64: 1211 / 806; and up to
-//   width 96 it costs more than the shorter way unless sequences are long: 8192 tokens in 24 sequences, 12 heads of 64 over 4 83 / 72, 32 of 96 over 8
-//   219 / 198, fp32 32 of 32 over 8 311 / 262, in one sequence bf16 16 of 64 over 8 515 / 535.
+//   above width 96 that goes by the workgroups for keys of 32 rows: bf16 128, 16 heads over 2, 130 216 / 150, 168 (20 sequences) 73 / 56, 216 (30) 56 / 57, 258
+//   462 / 417, 302 549 / 556, 402 762 / 901; fp32 158 1429 / 1003, 258 2494 / 2490, 302 3140 / 3523.  Up to width 96 by those of 128 rows again: bf16 96,
+//   16 over 2, 528 337 / 234, 640 429 / 326, 80, 16 over 4, 640 301 / 304; fp32 64, 16 over 2, 528 1215 / 815, 640 1569 / 1239, 48, 16 over 4, 640
+//   1083 / 1093 (with eight query heads to a key head still so at 752, bf16 538 / 440, fp32 1993 / 1724), and there 128 rows cost more than
+//   the shorter way unless sequences are long: 8192 tokens in 24 sequences, 12 heads of 64 over 4 83 / 72, 32 of 96 over 8 219 / 198, fp32 32 of 32 over 8
+//   311 / 262, in one sequence bf16 16 of 64 over 8 515 / 535.
 template <typename T> bool split_wanted(const PackedAttention& a, bool kv) {
   int most;
   const bool shared = a.heads > a.kv_heads;

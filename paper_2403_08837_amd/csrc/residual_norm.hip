@@ -9,7 +9,9 @@
 // r is made again from x, in fp32 as the forward had it (from the rounded r the gradient of gamma_pre would be off by half a step of bf16), and
 // mean(b n) falls into sums that do not wait for rho,
 //   sum b h = sum sg dr h + rho sum sg a h - rho^2 mean(a rhat) sum sg r h,   sg = scale sig gamma_post.
-// us and TB/s, bf16, all tensors: 16384 x 4096 forward 125 and 5.4, backward 228 and 4.7; 6272 x 768 9.2 and 5.2, 26.7 and 2.9 (the fold is 4.4 of it).
+// us and TB/s, bf16, all tensors: 16384 x 4096 forward 124 and 5.4, backward 223 and 4.8; 6272 x 768 9.4 and 5.1, 26.4 and 2.9 (the fold is 4.4 of it); fp32
+// 8192 x 4096 118 and 5.7, 219 and 4.9.  Past 8192 channels a lane's 16 values of five tensors are more than the 128 registers of a workgroup of 1024:
+// backward 28 to 61 of them are spilled, 4096 x 12288 119 and 4.2, 356 and 2.3, fp32 2048 x 16384 119 and 5.6, 308 and 3.5.
 // Column sums stay in registers over a workgroup's rows; what the workgroups have is added up by residual_norm_fold_kernel in a fixed order.
 #include "elem.h"
 #include "kernels.h"
@@ -105,7 +107,8 @@ template <typename T, typename Group, int K> struct Values {
     return Elem<T>::to_f32(c.e[i % V]);
   }
 };
-template <typename T, typename Group, int K, int N> __device__ __forceinline__ void store_row(void* p, int64_t bytes, const unsigned (&off)[K], const float (&v)[N]) {
+template <typename T, typename Group, int K, int N>
+__device__ __forceinline__ void store_row(void* p, int64_t bytes, const unsigned (&off)[K], const float (&v)[N]) {
   constexpr int V = N / K;
   const __amdgpu_buffer_rsrc_t b = buffer_at(p, bytes);
 #pragma unroll
