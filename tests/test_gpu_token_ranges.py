@@ -7,7 +7,7 @@ import numpy as np
 import pytest
 
 from paper_2403_08837_amd import binding as b
-from test_gpu_token_kernels import (BF16, F32, TYPES, U, Held, attention_call, attention_case, attention_reference, clip_call, half, near, norm_case, norm_reference, norm_tolerance,
+from test_gpu_token_kernels import (BF16, F32, TYPES, U, Held, Step, attention_call, attention_case, attention_reference, clip_call, half, near, norm_case, norm_reference, norm_tolerance,
                                     p, randn, workspace)
 
 pytestmark = pytest.mark.gpu
@@ -308,3 +308,32 @@ def test_grad_clip_of_more_than_2_to_the_32_elements():
     near(g[:1], one.reshape(1), (2.0 ** -8 + 4 * U) * one, "first")
     near(g[-1:], 3 * one.reshape(1), 3 * (2.0 ** -8 + 4 * U) * one, "last")
     assert all(bool((g[i:min(i + (1 << 28), n - 1)] == g[0]).all()) for i in range(0, n - 1, 1 << 28))
+
+
+# ---- together -------------------------------------------------------------------------------------------------------------
+def test_steps_that_overlap_on_two_streams():
+    """Two training steps, each with workspaces of its own, under way at once, and one of them replayed from a graph beside the other's calls: the same bits."""
+    steps, streams = (Step([30, 1, 64, 0, 33], 40), Step([500, 90, 7], 41)), (torch.cuda.Stream(), torch.cuda.Stream())
+    want = []
+    for s in steps:
+        s.run()
+        torch.cuda.synchronize()
+        want.append([v.clone() for v in s.state()])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        steps[0].run(streams[0].cuda_stream)
+    for replayed in (False, True):
+        for s in steps:
+            for v in s.state():
+                v.fill_(float("nan"))
+        torch.cuda.synchronize()
+        for _ in range(10):
+            for i, (s, stream) in enumerate(zip(steps, streams)):
+                with torch.cuda.stream(stream):
+                    if replayed and i == 0:
+                        graph.replay()
+                    else:
+                        s.run(stream.cuda_stream)
+        torch.cuda.synchronize()
+        for s, values in zip(steps, want):
+            assert all(torch.equal(got, v) for got, v in zip(s.state(), values))
