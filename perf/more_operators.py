@@ -4,6 +4,7 @@ A case is a dict of plain values; ``kind`` says which operator it is about:
 
   rotary   ``cdp_k_head_norm_rotary``, ``cdp_k_head_norm_rotary_backward``: norms of each query and key head and the rotation by position, in one pass
   gated    ``cdp_k_gated_linear``, ``cdp_k_gated_linear_backward``: act(x wg^T) * (x wu^T), the first half of a gated feed-forward block
+  linear   ``cdp_k_linear``, ``cdp_k_linear_backward``: act(x w^T + bias) + residual, the projections around it
   logprob  ``cdp_k_token_logprob``, ``cdp_k_token_logprob_backward``: log probabilities of given tokens, entropy and the likeliest tokens of each row
 
 Where ``own`` is false, ``run`` is elementary torch operations in 32 bits (angles in 64), rounded once; ``exact`` is the same from the definitions in 64.
@@ -16,7 +17,7 @@ import torch
 own = False
 
 DTYPES = {"f32": (0, torch.float32, 4), "bf16": (1, torch.bfloat16, 2)}
-ACTS = {"silu": 0, "gelu": 1, "sigmoid": 2}
+ACTS = {"silu": 0, "gelu": 1, "sigmoid": 2, "none": 3}
 EPS = 1e-6
 
 
@@ -31,18 +32,18 @@ def listed():
         # Odd lengths and head width, pairs beside each other, half of each head rotated, fp32.
         dict(name="rotary_odd_f32", kind="rotary", dtype="f32", tokens=2501, sequences=7, split=3, far=1000, heads=8, kv_heads=8, width=80, rotary=40, interleaved=True,
              norm=True, backward=True),
-        # One micro-batch of the smallest width, fp32, forward and backward.
-        dict(name="gated_small_f32", kind="gated", dtype="f32", rows=8, inputs=64, hidden=256, act="silu", backward=True),
         # One new token of a large model: the weights are read once.
         dict(name="gated_token_bf16", kind="gated", dtype="bf16", rows=1, inputs=4096, hidden=12288, act="silu", backward=False),
         # 32 x 196 tokens of ViT-B's width, a training step.
         dict(name="gated_vit_bf16", kind="gated", dtype="bf16", rows=6272, inputs=768, hidden=2048, act="gelu", backward=True),
         # A long prompt of a large model, a training step.
         dict(name="gated_large_bf16", kind="gated", dtype="bf16", rows=8192, inputs=4096, hidden=12288, act="silu", backward=True),
+        # One micro-batch of the smallest width, fp32, forward and backward.
+        dict(name="linear_small_f32", kind="linear", dtype="f32", rows=8, inputs=64, outputs=64, act="silu", bias=True, residual=False, backward=True),
+        # A large model's projection back to its width, with the residual, a training step.
+        dict(name="linear_wide_bf16", kind="linear", dtype="bf16", rows=8192, inputs=4096, outputs=4096, act="none", bias=False, residual=True, backward=True),
         # Ragged sizes in fp32, a training step.
-        dict(name="gated_odd_f32", kind="gated", dtype="f32", rows=1999, inputs=520, hidden=1368, act="silu", backward=True),
-        # A toy vocabulary with five alternatives: launch costs.
-        dict(name="logprob_small_f32", kind="logprob", dtype="f32", rows=64, vocab=1000, pitch=1000, top=5, padding=0.0, masked=0.0, scale=1.0, backward=True),
+        dict(name="linear_odd_f32", kind="linear", dtype="f32", rows=1999, inputs=520, outputs=1368, act="gelu", bias=True, residual=True, backward=True),
         # The next token of 16 sequences from a large vocabulary, a tenth of it ruled out, with twenty alternatives.
         dict(name="logprob_sampling_bf16", kind="logprob", dtype="bf16", rows=16, vocab=128000, pitch=128000, top=20, padding=0.0, masked=0.1, scale=1.25, backward=False),
         # The loss of 4096 tokens over a large vocabulary, a quarter of them prompts that are not learnt; its gradient in both directions.
@@ -59,7 +60,7 @@ def _log(rng, lo, hi, step=1):
 
 
 def draw(rng):
-    kind = rng.choice(["rotary", "gated", "gated", "logprob"])
+    kind = rng.choice(["rotary", "gated", "linear", "logprob"])
     dtype = rng.choice(["bf16", "bf16", "f32"])
     e = DTYPES[dtype][2]
     if kind == "rotary":
@@ -70,11 +71,14 @@ def draw(rng):
         return dict(kind=kind, dtype=dtype, tokens=tokens, sequences=min(tokens, _log(rng, 1, 64)), split=rng.randint(0, 1000), far=rng.choice([0, 0, 4000, 1_000_000]),
                     heads=heads, kv_heads=kv_heads, width=width, rotary=rng.choice([width, width, width // 2, 2 * rng.randint(1, width // 2)]),
                     interleaved=rng.random() < 0.4, norm=rng.random() < 0.7, backward=rng.random() < 0.6)
-    if kind == "gated":
-        inputs, hidden = _log(rng, 32, 4096, 8), _log(rng, 32, 12288, 8)
-        most = (400_000_000_000 if dtype == "bf16" else 20_000_000_000) // (inputs * hidden)
+    if kind in ("gated", "linear"):
+        inputs, width = _log(rng, 32, 4096, 8), _log(rng, 32, 12288, 8)
+        most = (400_000_000_000 if dtype == "bf16" else 20_000_000_000) // (inputs * width)
         rows = _log(rng, 1, max(2, min(8192, most)))
-        return dict(kind=kind, dtype=dtype, rows=rows, inputs=inputs, hidden=hidden, act=rng.choice(["silu", "silu", "gelu", "sigmoid"]), backward=rng.random() < 0.6)
+        c = dict(kind=kind, dtype=dtype, rows=rows, inputs=inputs, backward=rng.random() < 0.6)
+        if kind == "gated":
+            return dict(c, hidden=width, act=rng.choice(["silu", "silu", "gelu", "sigmoid"]))
+        return dict(c, outputs=width, act=rng.choice(["none", "none", "silu", "gelu"]), bias=rng.random() < 0.5, residual=rng.random() < 0.5)
     vocab = _log(rng, 2, 128000)
     pitch = vocab + rng.choice([0, 0, 1, -vocab % 64])
     rows = _log(rng, 1, min(8192, 1_000_000_000 // e // pitch))
@@ -118,6 +122,15 @@ def prepare(case, seed):
             s.update(g=empty(R, H), u=empty(R, H), dh=normal(R, H).to(t), dx=empty(R, I), dwg=empty(H, I), dwu=empty(H, I))
             planes += (12 if e == 4 else 4) * R * H + 1024 + min(512 << 20, 32 * max(R, 2 * H) * I)  # and room for shared sums
         s["ws"] = torch.empty(planes, dtype=torch.uint8, device="cuda")
+    elif case["kind"] == "linear":
+        R, I, O = case["rows"], case["inputs"], case["outputs"]
+        s.update(x=normal(R, I).to(t), w=(normal(O, I) / math.sqrt(I)).to(t), bias=(0.1 * normal(O)).to(t) if case["bias"] else None,
+                 residual=normal(R, O).to(t) if case["residual"] else None, y=empty(R, O), z=None)
+        planes = 6 * (R * I + O * I) + 1024 if e == 4 else 0
+        if case["backward"]:
+            s.update(z=empty(R, O) if case["act"] != "none" else None, dy=normal(R, O).to(t), dx=empty(R, I), dw=empty(O, I), dbias=empty(O) if case["bias"] else None)
+            planes += (6 if e == 4 else 2) * R * O + 4 * O * min(R, 256) + 1024 + min(512 << 20, 32 * max(R, O) * I)  # and room for shared sums
+        s["ws"] = torch.empty(planes, dtype=torch.uint8, device="cuda")
     else:
         R, V, P = case["rows"], case["vocab"], case["pitch"]
         logits = 2.5 * normal(R, P)
@@ -137,8 +150,8 @@ def prepare(case, seed):
 
 def run(s):
     if own:
-        return {"rotary": _rotary_own, "gated": _gated_own, "logprob": _logprob_own}[s["case"]["kind"]](s)
-    return {"rotary": _rotary, "gated": _gated, "logprob": _logprob}[s["case"]["kind"]](s)
+        return {"rotary": _rotary_own, "gated": _gated_own, "linear": _linear_own, "logprob": _logprob_own}[s["case"]["kind"]](s)
+    return {"rotary": _rotary, "gated": _gated, "linear": _linear, "logprob": _logprob}[s["case"]["kind"]](s)
 
 
 # ---- plain forms ------------------------------------------------------------------------------------------------------
@@ -185,6 +198,8 @@ def _rotary(s):
 
 def _act(name, g):
     """An activation and its derivative."""
+    if name == "none":
+        return g, torch.ones_like(g)
     sig = 1 / (1 + torch.exp(-g))
     if name == "silu":
         return g * sig, sig * (1 + g * (1 - sig))
@@ -204,6 +219,24 @@ def _gated(s):
         dh = s["dh"].float()
         dg, du = dh * u * da, dh * a
         res.update(g=g.to(t), u=u.to(t), dx=(torch.matmul(dg, wg) + torch.matmul(du, wu)).to(t), dwg=torch.matmul(dg.t(), x).to(t), dwu=torch.matmul(du.t(), x).to(t))
+    return res
+
+
+def _linear(s):
+    c, t = s["case"], s["dtype"]
+    x, w = s["x"].float(), s["w"].float()
+    z = torch.matmul(x, w.t())
+    if c["bias"]:
+        z += s["bias"].float()
+    a, da = _act(c["act"], z)
+    res = {"y": (a + s["residual"].float() if c["residual"] else a).to(t)}
+    if c["backward"]:
+        dz = s["dy"].float() * da
+        if c["act"] != "none":
+            res["z"] = z.to(t)
+        res.update(dx=torch.matmul(dz, w).to(t), dw=torch.matmul(dz.t(), x).to(t))
+        if c["bias"]:
+            res["dbias"] = dz.sum(0).to(t)
     return res
 
 
@@ -271,6 +304,22 @@ def _gated_own(s):
     return res
 
 
+def _linear_own(s):
+    from paper_2403_08837_amd import binding as cdp
+    c = s["case"]
+    sizes = (_at(s["ws"]), s["ws"].numel(), c["rows"], c["inputs"], c["outputs"])
+    cdp.cdp_k_linear(s["code"], ACTS[c["act"]], _at(s["x"]), _at(s["w"]), _at(s["bias"]), _at(s["residual"]), _at(s["y"]), _at(s["z"]), *sizes)
+    res = {"y": s["y"]}
+    if c["backward"]:
+        cdp.cdp_k_linear_backward(s["code"], ACTS[c["act"]], _at(s["x"]), _at(s["w"]), _at(s["z"]), _at(s["dy"]), _at(s["dx"]), _at(s["dw"]), _at(s["dbias"]), *sizes)
+        if c["act"] != "none":
+            res["z"] = s["z"]
+        res.update(dx=s["dx"], dw=s["dw"])
+        if c["bias"]:
+            res["dbias"] = s["dbias"]
+    return res
+
+
 def _logprob_own(s):
     from paper_2403_08837_amd import binding as cdp
     c = s["case"]
@@ -299,6 +348,13 @@ def work(case):
         if case["backward"]:
             b += e * (2 * R * H + 2 * R * I + 4 * H * I + 3 * R * H)
         return {"bytes": b, "flops": (12 if case["backward"] else 4) * R * I * H}
+    if case["kind"] == "linear":
+        R, I, O = case["rows"], case["inputs"], case["outputs"]
+        z = int(case["act"] != "none")
+        b = e * (R * I + O * I + R * O * (1 + int(case["residual"])))
+        if case["backward"]:
+            b += e * (2 * R * I + 2 * O * I + R * O * (1 + 2 * z))
+        return {"bytes": b, "flops": (6 if case["backward"] else 2) * R * I * O}
     R, V = case["rows"], case["vocab"]
     used = round(R * (1 - case["padding"]))
     return {"bytes": e * used * V + 16 * R + 8 * R * case["top"] + (e * (used + R) * V if case["backward"] else 0), "flops": used * V * (6 + (8 if case["backward"] else 0))}
@@ -307,7 +363,7 @@ def work(case):
 # ---- the definitions in 64 bits ---------------------------------------------------------------------------------------
 def exact(case, seed):
     s = prepare(case, seed)
-    return {"rotary": _rotary_exact, "gated": _gated_exact, "logprob": _logprob_exact}[case["kind"]](s)
+    return {"rotary": _rotary_exact, "gated": _gated_exact, "linear": _linear_exact, "logprob": _logprob_exact}[case["kind"]](s)
 
 
 def _rotary_exact(s):
@@ -348,6 +404,24 @@ def _gated_exact(s):
     if c["backward"]:
         h.backward(s["dh"].double())
         res.update(g=g.detach(), u=u.detach(), dx=x.grad, dwg=wg.grad, dwu=wu.grad)
+    return res
+
+
+def _linear_exact(s):
+    c = s["case"]
+    x, w = (s[k].double().requires_grad_(c["backward"]) for k in ("x", "w"))
+    bias = s["bias"].double().requires_grad_(c["backward"]) if c["bias"] else None
+    z = torch.nn.functional.linear(x, w, bias)
+    act = {"silu": torch.nn.functional.silu, "gelu": torch.nn.functional.gelu, "none": lambda v: v}[c["act"]]
+    y = act(z)
+    res = {"y": (y + s["residual"].double() if c["residual"] else y).detach()}
+    if c["backward"]:
+        y.backward(s["dy"].double())
+        if c["act"] != "none":
+            res["z"] = z.detach()
+        res.update(dx=x.grad, dw=w.grad)
+        if c["bias"]:
+            res["dbias"] = bias.grad
     return res
 
 
