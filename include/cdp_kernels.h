@@ -161,6 +161,73 @@ int cdp_k_attention_packed(int dtype, int backward, const void* qkv, const int32
 int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm,
                     float* norm, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Norms of query and key heads and their rotation by position, over qkv[tokens][(heads + 2 * kv_heads) * width] as cdp_k_attention_packed takes it, and with its
+ * limits on sizes and alignment.  Of a head x of q or k, with norm(x) = x / sqrt(mean(x^2) + eps) (for heads whose squares have a sum that fp32 holds):
+ *   n = norm(x) * gamma_q (q), gamma_k (k)     gamma (fp32[width]) NULL: n = x
+ *   the pairs of the first `rotary` values (even; 0: no rotation, positions and freqs unused) are turned by the angle positions[token] * freqs[i]:
+ *   (a, b) -> (a cos - b sin, b cos + a sin); pair i is (n[i], n[i + rotary / 2]), with interleaved != 0 (n[2 i], n[2 i + 1]); the other values stay.
+ * positions: device int32[tokens], any; freqs: device fp32[rotary / 2], finite.  Angles are made in 64 bits: positions of 2^31 are as exact as small ones.
+ * out[tokens][(heads + 2 * kv_heads) * width]: v heads are copied.  out may be qkv (v is not touched then), which the backward reads, however, where there is a gamma.
+ * What is infinite or NaN in a head stays in that head. */
+int cdp_k_head_norm_rotary(int dtype, const void* qkv, const int32_t* positions, const float* freqs, const float* gamma_q, const float* gamma_k, void* out,
+                           float eps, int interleaved, int tokens, int heads, int kv_heads, int width, int rotary, void* stream);
+
+/* Its gradients from dout[tokens][(heads + 2 * kv_heads) * width]: dqkv (elem type, written; v heads copied), dgamma_q[width], dgamma_k[width] (fp32, with
+ * gamma_q and gamma_k): overwritten, with accumulate != 0 added to.  qkv: as the forward had it (NULL where there is no gamma).  dqkv may be dout.
+ * workspace (with a gamma): 8 * width * min(tokens, 1024) + 256 bytes (CDP_EINVAL if smaller). */
+int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, const int32_t* positions, const float* freqs, const float* gamma_q,
+                                    const float* gamma_k, const void* dout, void* dqkv, float* dgamma_q, float* dgamma_k, float eps, int interleaved,
+                                    void* workspace, size_t workspace_bytes, int tokens, int heads, int kv_heads, int width, int rotary, void* stream);
+
+/* The first half of a gated feed-forward block: h[rows][hidden] = act(g) * u, g = x wg^T, u = x wu^T, from x[rows][in], wg[hidden][in], wu[hidden][in].
+ *   act 0: SiLU g * sigmoid(g)    1: exact GELU g * Phi(g)    2: sigmoid(g)    3: g
+ * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20.  g and u (both or neither): written too, for the backward.
+ * Sums are fp32.  fp32: factors are taken as three bf16 numbers that add up to them (2^-27 of a factor is left out, and what is below 2^-133) and the three
+ * smallest products of those are left out (2^-26); up to 16 rows forward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
+ * workspace: fp32 6 * (rows + 2 * hidden) * in + 1024 bytes (CDP_EINVAL if smaller), bf16 none (may be NULL).  Where it holds more, P times 8 * rows * hidden
+ * bytes, products of few tiles share their reduction over up to P workgroups: faster, other roundings. */
+int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, size_t workspace_bytes,
+                       int rows, int in, int hidden, void* stream);
+
+/* Its gradients from dh[rows][hidden], x, wg, wu, and g, u as the forward wrote them:  dg = dh * u * act'(g) and du = dh * act(g), which bf16 rounds to the
+ * element type;  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
+ * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 6 * (rows + 2 * hidden) * in + 12 * rows * hidden + 2048 (CDP_EINVAL if smaller), and as above where it holds
+ * more: P times 4 * rows * in bytes for dx, P times 8 * hidden * in for dwg and dwu. */
+int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
+                                void* dwg, void* dwu, void* workspace, size_t workspace_bytes, int rows, int in, int hidden, void* stream);
+
+/* y[rows][out] = act(z) + residual[rows][out], z = x w^T + bias[out], from x[rows][in], w[out][in]; bias and residual NULL: none.  Types, alignment, sizes, acts, exactness
+ * as above.  z not NULL: written too, for the backward (which needs it unless act is 3).  y may be residual.
+ * workspace: fp32 6 * (rows + out) * in + 1024 bytes (CDP_EINVAL if smaller), bf16 none; where it holds P times 4 * rows * out bytes more, as above. */
+int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
+                 size_t workspace_bytes, int rows, int in, int out, void* stream);
+
+/* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products;  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
+ * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted), fp32 needs x and w for either product.  The gradient of the residual is dy.
+ * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 6 * (rows + out) * in + 6 * rows * out + 4 * out * min(rows, 256) + 2048
+ * (CDP_EINVAL if smaller), and as above where it holds more: P times 4 * rows * in bytes for dx, P times 4 * out * in for dw. */
+int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
+                          size_t workspace_bytes, int rows, int in, int out, void* stream);
+
+/* Of rows of logits, z = scale * logits[row * ld + 0 .. vocab) (scale > 0; ld >= vocab, up to 2^31; vocab up to 2^28), all fp32:
+ *   lse[row] = log sum exp z;  logprob[row] = z[targets[row]] - lse (with targets);  entropy[row] = - sum p log p, p = exp(z - lse) (may be NULL)
+ *   top_ids[row][top] (int32), top_logprobs[row][top]: the likeliest tokens in order and their z - lse; of equal logits the lowest id first.
+ *   top up to 64 and vocab (0: none)
+ * targets: device int32[rows], or NULL (no logprob).  A row whose target is outside [0, vocab) is not read: zeros, and -1 for ids.
+ * Logits of -infinity are tokens that cannot be: p = 0, log probability -infinity.  A row of nothing else has lse and logprob -infinity, entropy 0.  A row
+ * with NaN or +infinity in it is NaN; NaN ranks as -infinity.
+ * workspace: CDP_LOGPROB_BYTES, or NULL; with it few long rows are shared by several workgroups: faster, other roundings. */
+#define CDP_LOGPROB_BYTES (1u << 20)
+int cdp_k_token_logprob(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, float* logprob, float* entropy, float* lse,
+                        int32_t* top_ids, float* top_logprobs, int top, void* workspace, size_t workspace_bytes, int rows, int vocab, void* stream);
+
+/* The gradient of the logits from those of logprob (dlogprob[rows]; NULL: none) and entropy (dentropy[rows], with entropy as the forward wrote it; NULL:
+ * none) and the forward's lse:  dlogits[j] = scale * (dlogprob * ((j == target) - p[j]) - dentropy * p[j] * (log p[j] + entropy)), elem type, at the rows and
+ * columns of logits (ld; what is between rows stays).  dlogits may be logits.  Zeros for a row whose target is outside [0, vocab) and for one of -infinity alone.
+ * Probabilities are made from lse, with its rounding: |lse| * 2^-22 of themselves. */
+int cdp_k_token_logprob_backward(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, const float* lse, const float* entropy,
+                                 const float* dlogprob, const float* dentropy, void* dlogits, int rows, int vocab, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

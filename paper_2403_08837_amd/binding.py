@@ -24,7 +24,9 @@ EXPORTS = ["cdp_arena_bytes", "cdp_init", "cdp_set_weights", "cdp_param_count", 
            "cdp_drain", "cdp_get_weights", "cdp_get_losses", "cdp_get_trace", "cdp_get_live_counts",
            "cdp_get_live_bytes", "cdp_get_stats", "cdp_last_error", "cdp_destroy", "cdp_profile_gemm", "cdp_get_gemm_profile",
            "cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention",
-           "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip"]
+           "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip",
+           "cdp_k_head_norm_rotary", "cdp_k_head_norm_rotary_backward", "cdp_k_gated_linear",
+           "cdp_k_gated_linear_backward", "cdp_k_linear", "cdp_k_linear_backward", "cdp_k_token_logprob", "cdp_k_token_logprob_backward"]
 
 
 class cdp_layer_desc(C.Structure):
@@ -105,6 +107,14 @@ def lib() -> C.CDLL:
         L.cdp_k_residual_norm_backward.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, f32, f32, vp, sz, i32, i32, vp]
         L.cdp_k_attention_packed.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, i32, i32, f32, vp]
         L.cdp_k_grad_clip.argtypes = [i32, i32, vp, vp, vp, f32, vp, vp, sz, vp]
+        L.cdp_k_head_norm_rotary.argtypes = [i32, vp, vp, vp, vp, vp, vp, f32, i32, i32, i32, i32, i32, i32, vp]
+        L.cdp_k_head_norm_rotary_backward.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, f32, i32, vp, sz, i32, i32, i32, i32, i32, vp]
+        L.cdp_k_gated_linear.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, vp]
+        L.cdp_k_gated_linear_backward.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, vp]
+        L.cdp_k_linear.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, vp]
+        L.cdp_k_linear_backward.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, i32, i32, i32, vp]
+        L.cdp_k_token_logprob.argtypes = [i32, vp, C.c_int64, vp, f32, vp, vp, vp, vp, vp, i32, vp, sz, i32, i32, vp]
+        L.cdp_k_token_logprob_backward.argtypes = [i32, vp, C.c_int64, vp, f32, vp, vp, vp, vp, vp, i32, i32, vp]
         for name in EXPORTS:
             if name not in ("cdp_last_error", "cdp_destroy"):
                 getattr(L, name).restype = C.c_int
@@ -113,7 +123,9 @@ def lib() -> C.CDLL:
 
 
 _CALLS = ("cdp_k_gemm", "cdp_k_conv", "cdp_k_conv_wgrad_static", "cdp_k_layernorm", "cdp_k_gelu", "cdp_k_attention",
-          "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip")
+          "cdp_k_embedding", "cdp_k_residual_norm", "cdp_k_residual_norm_backward", "cdp_k_attention_packed", "cdp_k_grad_clip",
+          "cdp_k_head_norm_rotary", "cdp_k_head_norm_rotary_backward", "cdp_k_gated_linear",
+          "cdp_k_gated_linear_backward", "cdp_k_linear", "cdp_k_linear_backward", "cdp_k_token_logprob", "cdp_k_token_logprob_backward")
 
 
 def _calls():
@@ -139,7 +151,9 @@ def _entry(name: str):
 
 
 _cdp_k_gemm, _cdp_k_conv, _cdp_k_conv_wgrad_static, _cdp_k_layernorm, _cdp_k_gelu, _cdp_k_attention, \
-    _cdp_k_embedding, _cdp_k_residual_norm, _cdp_k_residual_norm_backward, _cdp_k_attention_packed, _cdp_k_grad_clip = map(_entry, _CALLS)
+    _cdp_k_embedding, _cdp_k_residual_norm, _cdp_k_residual_norm_backward, _cdp_k_attention_packed, _cdp_k_grad_clip, \
+    _cdp_k_head_norm_rotary, _cdp_k_head_norm_rotary_backward, _cdp_k_gated_linear, _cdp_k_gated_linear_backward, _cdp_k_linear, \
+    _cdp_k_linear_backward, _cdp_k_token_logprob, _cdp_k_token_logprob_backward = map(_entry, _CALLS)
 
 
 def _check(rc: int, ctx=None) -> None:
@@ -395,6 +409,94 @@ def cdp_k_grad_clip(dtype, tensors, grads_ptr, outs_ptr, counts_ptr, max_norm, n
         rc = lib().cdp_k_grad_clip(*args)
     if rc != CDP_OK:
         raise CdpError(rc, "cdp_k_grad_clip")
+
+
+def cdp_k_head_norm_rotary(dtype, qkv_ptr, positions_ptr, freqs_ptr, gamma_q_ptr, gamma_k_ptr, out_ptr, eps, interleaved, tokens, heads, kv_heads, width, rotary, stream=0) -> None:
+    """Norms of query and key heads (with gammas) and their rotation by position; v heads are copied."""
+    args = (dtype, qkv_ptr, positions_ptr or None, freqs_ptr or None, gamma_q_ptr or None, gamma_k_ptr or None, out_ptr, eps, interleaved, tokens, heads, kv_heads,
+            width, rotary, stream or None)
+    rc = _cdp_k_head_norm_rotary(*args)
+    if rc is None:
+        rc = lib().cdp_k_head_norm_rotary(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_head_norm_rotary")
+
+
+def cdp_k_head_norm_rotary_backward(dtype, accumulate, qkv_ptr, positions_ptr, freqs_ptr, gamma_q_ptr, gamma_k_ptr, dout_ptr, dqkv_ptr, dgamma_q_ptr, dgamma_k_ptr, eps,
+                                    interleaved, ws_ptr, ws_bytes, tokens, heads, kv_heads, width, rotary, stream=0) -> None:
+    """Gradients of cdp_k_head_norm_rotary."""
+    args = (dtype, accumulate, qkv_ptr or None, positions_ptr or None, freqs_ptr or None, gamma_q_ptr or None, gamma_k_ptr or None, dout_ptr, dqkv_ptr,
+            dgamma_q_ptr or None, dgamma_k_ptr or None, eps, interleaved, ws_ptr or None, ws_bytes, tokens, heads, kv_heads, width, rotary, stream or None)
+    rc = _cdp_k_head_norm_rotary_backward(*args)
+    if rc is None:
+        rc = lib().cdp_k_head_norm_rotary_backward(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_head_norm_rotary_backward")
+
+
+def cdp_k_gated_linear(dtype, act, x_ptr, wg_ptr, wu_ptr, h_ptr, g_ptr, u_ptr, ws_ptr, ws_bytes, rows, inputs, hidden, stream=0) -> None:
+    """h = act(x wg^T) * (x wu^T); act 0 SiLU, 1 GELU, 2 sigmoid, 3 none.  g_ptr, u_ptr: the two products, for the backward, or 0."""
+    args = (dtype, act, x_ptr, wg_ptr, wu_ptr, h_ptr, g_ptr or None, u_ptr or None, ws_ptr or None, ws_bytes, rows, inputs, hidden, stream or None)
+    rc = _cdp_k_gated_linear(*args)
+    if rc is None:
+        rc = lib().cdp_k_gated_linear(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_gated_linear")
+
+
+def cdp_k_gated_linear_backward(dtype, act, x_ptr, wg_ptr, wu_ptr, g_ptr, u_ptr, dh_ptr, dx_ptr, dwg_ptr, dwu_ptr, ws_ptr, ws_bytes, rows, inputs, hidden, stream=0) -> None:
+    """Gradients of cdp_k_gated_linear: dx, and dwg with dwu (0: not wanted)."""
+    args = (dtype, act, x_ptr, wg_ptr, wu_ptr, g_ptr, u_ptr, dh_ptr, dx_ptr or None, dwg_ptr or None, dwu_ptr or None, ws_ptr or None, ws_bytes, rows, inputs, hidden,
+            stream or None)
+    rc = _cdp_k_gated_linear_backward(*args)
+    if rc is None:
+        rc = lib().cdp_k_gated_linear_backward(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_gated_linear_backward")
+
+
+def cdp_k_linear(dtype, act, x_ptr, w_ptr, bias_ptr, residual_ptr, y_ptr, z_ptr, ws_ptr, ws_bytes, rows, inputs, outputs, stream=0) -> None:
+    """y = act(x w^T + bias) + residual; act 0 SiLU, 1 GELU, 2 sigmoid, 3 none.  z_ptr: the argument of act, for the backward, or 0."""
+    args = (dtype, act, x_ptr, w_ptr, bias_ptr or None, residual_ptr or None, y_ptr, z_ptr or None, ws_ptr or None, ws_bytes, rows, inputs, outputs, stream or None)
+    rc = _cdp_k_linear(*args)
+    if rc is None:
+        rc = lib().cdp_k_linear(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_linear")
+
+
+def cdp_k_linear_backward(dtype, act, x_ptr, w_ptr, z_ptr, dy_ptr, dx_ptr, dw_ptr, dbias_ptr, ws_ptr, ws_bytes, rows, inputs, outputs, stream=0) -> None:
+    """Gradients of cdp_k_linear: dx, dw and dbias (0: not wanted); that of the residual is dy."""
+    args = (dtype, act, x_ptr or None, w_ptr or None, z_ptr or None, dy_ptr, dx_ptr or None, dw_ptr or None, dbias_ptr or None, ws_ptr or None, ws_bytes, rows, inputs,
+            outputs, stream or None)
+    rc = _cdp_k_linear_backward(*args)
+    if rc is None:
+        rc = lib().cdp_k_linear_backward(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_linear_backward")
+
+
+def cdp_k_token_logprob(dtype, logits_ptr, ld, targets_ptr, scale, logprob_ptr, entropy_ptr, lse_ptr, top_ids_ptr, top_logprobs_ptr, top, ws_ptr, ws_bytes, rows, vocab,
+                        stream=0) -> None:
+    """Log probabilities of the targets, entropy, log sum of exponentials and the `top` likeliest tokens of each row of scale * logits."""
+    args = (dtype, logits_ptr, ld, targets_ptr or None, scale, logprob_ptr or None, entropy_ptr or None, lse_ptr, top_ids_ptr or None, top_logprobs_ptr or None, top,
+            ws_ptr or None, ws_bytes, rows, vocab, stream or None)
+    rc = _cdp_k_token_logprob(*args)
+    if rc is None:
+        rc = lib().cdp_k_token_logprob(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_token_logprob")
+
+
+def cdp_k_token_logprob_backward(dtype, logits_ptr, ld, targets_ptr, scale, lse_ptr, entropy_ptr, dlogprob_ptr, dentropy_ptr, dlogits_ptr, rows, vocab, stream=0) -> None:
+    """dlogits from the gradients of logprob and entropy."""
+    args = (dtype, logits_ptr, ld, targets_ptr or None, scale, lse_ptr, entropy_ptr or None, dlogprob_ptr or None, dentropy_ptr or None, dlogits_ptr, rows, vocab,
+            stream or None)
+    rc = _cdp_k_token_logprob_backward(*args)
+    if rc is None:
+        rc = lib().cdp_k_token_logprob_backward(*args)
+    if rc != CDP_OK:
+        raise CdpError(rc, "cdp_k_token_logprob_backward")
 
 
 # ---- convenience wrapper used by tests and bench -------------------------------------------

@@ -400,5 +400,63 @@ hipError_t launch_packed_attention_fwd(const PackedAttention& a, int dtype, hipS
 hipError_t launch_packed_attention_bwd(const PackedAttention& a, int dtype, hipStream_t stream);
 hipError_t launch_grad_clip(int tensors, const void* const* grads, void* const* outs, const int64_t* counts, float max_norm, float* norm,
                             void* workspace, int dtype, hipStream_t stream);
+// (head_rotary.hip, token_linear.hip, token_logprob.hip, likewise)
+struct HeadRotary {
+  const void* qkv;
+  const int32_t* positions;
+  const float *freqs, *gamma_q, *gamma_k;
+  void* out;                           // forward: written
+  const void* dout;                    // backward
+  void* dqkv;
+  float *dgamma_q, *dgamma_k, *part;
+  int tokens, heads, kv_heads, width, rotary, interleaved, accumulate;
+  int in_place;                        // the result is where the input was: v heads stay
+  float eps;
+};
+constexpr int HEAD_ROTARY_MAX_PARTS = 1024;
+int64_t head_rotary_bwd_workspace_bytes(int tokens, int width);
+hipError_t launch_head_rotary(const HeadRotary& a, bool backward, int dtype, hipStream_t stream);
+enum { TOKEN_SILU = 0, TOKEN_GELU = 1, TOKEN_SIGMOID = 2, TOKEN_NONE = 3 };
+struct GatedLinear {
+  const void *x, *wg, *wu;
+  void *h, *g, *u;                     // forward: written (g, u: or null); backward: g, u read
+  const void* dh;                      // backward
+  void *dx, *dwg, *dwu;
+  void* workspace;
+  int64_t workspace_bytes;
+  int rows, in, hidden, act;
+};
+struct TokenLinear {
+  const void *x, *w, *bias, *residual;
+  void *y, *z;                         // forward: written (z: or null); backward: z read
+  const void* dy;                      // backward
+  void *dx, *dw, *dbias;
+  void* workspace;
+  int64_t workspace_bytes;
+  int rows, in, out, act;
+};
+constexpr int LINEAR_MAX_WIDTH = 1 << 20, LINEAR_MAX_PARTS = 256;
+int64_t token_linear_workspace_bytes(bool backward, int rows, int in, int out, int dtype);
+hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream);
+hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream);
+int64_t gated_linear_workspace_bytes(bool backward, int rows, int in, int hidden, int dtype);
+hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stream);
+hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream);
+struct TokenLogprob {
+  const void* logits;
+  int64_t ld;
+  const int32_t* targets;
+  float *logprob, *entropy, *lse;      // forward: written; backward: lse, entropy read
+  int32_t* top_ids;
+  float* top_logprobs;
+  const float *dlogprob, *dentropy;    // backward
+  void* dlogits;
+  float4* part_sums;                   // forward: of LOGPROB_MAX_PARTS parts of rows, or null
+  unsigned long long* part_keys;
+  int rows, vocab, top, parts;
+  float scale;
+};
+constexpr int LOGPROB_MAX_TOP = 64, LOGPROB_MAX_SPLIT = 32, LOGPROB_MAX_PARTS = 1024, LOGPROB_MAX_VOCAB = 1 << 28;
+hipError_t launch_token_logprob(const TokenLogprob& a, bool backward, int dtype, hipStream_t stream);
 
 }  // namespace cdp

@@ -30,6 +30,30 @@ static_assert((int64_t)CDP_CONV_SHARE_BYTES == CONV_SPLIT_WS_BYTES + CONV_SPLIT_
 
 static bool aligned_to(const void* p, uintptr_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+// What the head norms' two entry points check alike.
+static bool head_rotary(HeadRotary& a, int dtype, const void* qkv, const int32_t* positions, const float* freqs, const float* gamma_q, const float* gamma_k,
+                        float eps, int interleaved, int tokens, int heads, int kv_heads, int width, int rotary) {
+  if (tokens <= 0 || heads <= 0 || kv_heads <= 0 || heads > 4096 || (int64_t)heads + 2ll * kv_heads > 4096 || width <= 0 || width % 8 || width > 128 || rotary < 0 ||
+      rotary % 2 || rotary > width || !(eps > 0.f) || (dtype != DT_F32 && dtype != DT_BF16))
+    return false;
+  if ((rotary && (!positions || !freqs)) || (!rotary && !gamma_q && !gamma_k)) return false;
+  if (!aligned_to(qkv, 16)) return false;
+  for (const void* p : {(const void*)positions, (const void*)freqs, (const void*)gamma_q, (const void*)gamma_k})
+    if (!aligned_to(p, 4)) return false;
+  memset(&a, 0, sizeof(a));
+  a.qkv = qkv; a.positions = positions; a.freqs = freqs; a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.eps = eps; a.interleaved = interleaved != 0;
+  a.tokens = tokens; a.heads = heads; a.kv_heads = kv_heads; a.width = width; a.rotary = rotary;
+  return true;
+}
+static bool linear_sizes(int dtype, int act, int rows, int in, int hidden) {
+  return rows > 0 && in > 0 && hidden > 0 && in % 8 == 0 && hidden % 8 == 0 && in <= LINEAR_MAX_WIDTH && hidden <= LINEAR_MAX_WIDTH && act >= TOKEN_SILU &&
+         act <= TOKEN_NONE && (dtype == DT_F32 || dtype == DT_BF16);
+}
+static bool logprob_sizes(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, int rows, int vocab) {
+  return (dtype == DT_F32 || dtype == DT_BF16) && logits && aligned_to(logits, dtype == DT_BF16 ? 2 : 4) && aligned_to(targets, 4) && rows > 0 && vocab > 0 &&
+         vocab <= LOGPROB_MAX_VOCAB && ld >= vocab && ld <= (1ll << 31) && scale > 0.f && std::isfinite(scale);
+}
+
 extern "C" {
 
 int cdp_k_gemm(int dtype, int tile_shape, int a_kmajor, int b_kmajor, const void* A, const void* B, float* C, int M, int N,
@@ -288,6 +312,125 @@ int cdp_k_grad_clip(int dtype, int tensors, const void* const* grads, void* cons
     if (counts[i] && (!grads[i] || !aligned_to(grads[i], eb) || (outs && (!outs[i] || !aligned_to(outs[i], eb))))) return CDP_EINVAL;
   }
   return launched(launch_grad_clip(tensors, grads, outs, counts, max_norm, norm, workspace, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_head_norm_rotary(int dtype, const void* qkv, const int32_t* positions, const float* freqs, const float* gamma_q, const float* gamma_k, void* out,
+                           float eps, int interleaved, int tokens, int heads, int kv_heads, int width, int rotary, void* stream) {
+  if (!out) return CDP_EINVAL;
+  HeadRotary a;
+  if (!head_rotary(a, dtype, qkv, positions, freqs, gamma_q, gamma_k, eps, interleaved, tokens, heads, kv_heads, width, rotary) || !qkv || !aligned_to(out, 16))
+    return CDP_EINVAL;
+  a.out = out;
+  a.in_place = out == qkv;
+  return launched(launch_head_rotary(a, false, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, const int32_t* positions, const float* freqs, const float* gamma_q,
+                                    const float* gamma_k, const void* dout, void* dqkv, float* dgamma_q, float* dgamma_k, float eps, int interleaved,
+                                    void* workspace, size_t workspace_bytes, int tokens, int heads, int kv_heads, int width, int rotary, void* stream) {
+  HeadRotary a;
+  if (!head_rotary(a, dtype, qkv, positions, freqs, gamma_q, gamma_k, eps, interleaved, tokens, heads, kv_heads, width, rotary)) return CDP_EINVAL;
+  if (!dout || !dqkv || !aligned_to(dout, 16) || !aligned_to(dqkv, 16) || !gamma_q != !dgamma_q || !gamma_k != !dgamma_k || !aligned_to(dgamma_q, 4) ||
+      !aligned_to(dgamma_k, 4))
+    return CDP_EINVAL;
+  if ((gamma_q || gamma_k) && (!qkv || !workspace || !aligned_to(workspace, 16) || workspace_bytes < (size_t)head_rotary_bwd_workspace_bytes(tokens, width)))
+    return CDP_EINVAL;
+  a.dout = dout; a.dqkv = dqkv; a.dgamma_q = dgamma_q; a.dgamma_k = dgamma_k;
+  a.part = static_cast<float*>(workspace);
+  a.accumulate = accumulate != 0;
+  a.in_place = dout == dqkv;
+  return launched(launch_head_rotary(a, true, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, size_t workspace_bytes,
+                       int rows, int in, int hidden, void* stream) {
+  if (!linear_sizes(dtype, act, rows, in, hidden) || !x || !wg || !wu || !h || !g != !u) return CDP_EINVAL;
+  for (const void* p : {x, wg, wu, (const void*)h, (const void*)g, (const void*)u, (const void*)workspace})
+    if (!aligned_to(p, 16)) return CDP_EINVAL;
+  const int64_t need = gated_linear_workspace_bytes(false, rows, in, hidden, dtype);
+  if (need && (!workspace || workspace_bytes < (size_t)need)) return CDP_EINVAL;
+  GatedLinear a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.wg = wg; a.wu = wu; a.h = h; a.g = g; a.u = u;
+  a.workspace = workspace; a.workspace_bytes = workspace ? (int64_t)std::min<size_t>(workspace_bytes, INT64_MAX / 2) : 0;
+  a.rows = rows; a.in = in; a.hidden = hidden; a.act = act;
+  return launched(launch_gated_linear(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
+                                void* dwg, void* dwu, void* workspace, size_t workspace_bytes, int rows, int in, int hidden, void* stream) {
+  if (!linear_sizes(dtype, act, rows, in, hidden) || !x || !wg || !wu || !g || !u || !dh || !dwg != !dwu || (!dx && !dwg)) return CDP_EINVAL;
+  for (const void* p : {x, wg, wu, g, u, dh, (const void*)dx, (const void*)dwg, (const void*)dwu, (const void*)workspace})
+    if (!aligned_to(p, 16)) return CDP_EINVAL;
+  if (!workspace || workspace_bytes < (size_t)gated_linear_workspace_bytes(true, rows, in, hidden, dtype)) return CDP_EINVAL;
+  GatedLinear a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.wg = wg; a.wu = wu; a.g = const_cast<void*>(g); a.u = const_cast<void*>(u); a.dh = dh; a.dx = dx; a.dwg = dwg; a.dwu = dwu;
+  a.workspace = workspace; a.workspace_bytes = (int64_t)std::min<size_t>(workspace_bytes, INT64_MAX / 2);
+  a.rows = rows; a.in = in; a.hidden = hidden; a.act = act;
+  return launched(launch_gated_linear_bwd(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
+                 size_t workspace_bytes, int rows, int in, int out, void* stream) {
+  if (!linear_sizes(dtype, act, rows, in, out) || !x || !w || !y) return CDP_EINVAL;
+  for (const void* p : {x, w, bias, residual, (const void*)y, (const void*)z, (const void*)workspace})
+    if (!aligned_to(p, 16)) return CDP_EINVAL;
+  const int64_t need = token_linear_workspace_bytes(false, rows, in, out, dtype);
+  if (need && (!workspace || workspace_bytes < (size_t)need)) return CDP_EINVAL;
+  TokenLinear a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.w = w; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
+  a.workspace = workspace; a.workspace_bytes = workspace ? (int64_t)std::min<size_t>(workspace_bytes, INT64_MAX / 2) : 0;
+  a.rows = rows; a.in = in; a.out = out; a.act = act;
+  return launched(launch_token_linear(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
+                          size_t workspace_bytes, int rows, int in, int out, void* stream) {
+  if (!linear_sizes(dtype, act, rows, in, out) || !dy || (!z && act != TOKEN_NONE) || (!dx && !dw && !dbias)) return CDP_EINVAL;
+  if ((dx && !w) || (dw && !x) || (dtype == DT_F32 && (dx || dw) && (!x || !w))) return CDP_EINVAL;
+  for (const void* p : {x, w, z, dy, (const void*)dx, (const void*)dw, (const void*)dbias, (const void*)workspace})
+    if (!aligned_to(p, 16)) return CDP_EINVAL;
+  if (!workspace || workspace_bytes < (size_t)token_linear_workspace_bytes(true, rows, in, out, dtype)) return CDP_EINVAL;
+  TokenLinear a;
+  memset(&a, 0, sizeof(a));
+  a.x = x; a.w = w; a.z = const_cast<void*>(z); a.dy = dy; a.dx = dx; a.dw = dw; a.dbias = dbias;
+  a.workspace = workspace; a.workspace_bytes = (int64_t)std::min<size_t>(workspace_bytes, INT64_MAX / 2);
+  a.rows = rows; a.in = in; a.out = out; a.act = act;
+  return launched(launch_token_linear_bwd(a, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_token_logprob(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, float* logprob, float* entropy, float* lse,
+                        int32_t* top_ids, float* top_logprobs, int top, void* workspace, size_t workspace_bytes, int rows, int vocab, void* stream) {
+  if (!logprob_sizes(dtype, logits, ld, targets, scale, rows, vocab) || !lse || (logprob && !targets)) return CDP_EINVAL;
+  if (top < 0 || top > LOGPROB_MAX_TOP || top > vocab || (top && (!top_ids || !top_logprobs))) return CDP_EINVAL;
+  for (const void* p : {(const void*)logprob, (const void*)entropy, (const void*)lse, (const void*)top_ids, (const void*)top_logprobs})
+    if (!aligned_to(p, 4)) return CDP_EINVAL;
+  if (workspace && (!aligned_to(workspace, 16) || workspace_bytes < CDP_LOGPROB_BYTES)) return CDP_EINVAL;
+  static_assert(CDP_LOGPROB_BYTES >= LOGPROB_MAX_PARTS * (sizeof(float4) + LOGPROB_MAX_TOP * 8), "sums and keys of every part");
+  TokenLogprob a;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits; a.ld = ld; a.targets = targets; a.logprob = logprob; a.entropy = entropy; a.lse = lse;
+  a.top_ids = top_ids; a.top_logprobs = top_logprobs;
+  a.part_sums = static_cast<float4*>(workspace);
+  a.part_keys = reinterpret_cast<unsigned long long*>(a.part_sums + LOGPROB_MAX_PARTS);
+  a.rows = rows; a.vocab = vocab; a.top = top; a.scale = scale;
+  return launched(launch_token_logprob(a, false, dtype, static_cast<hipStream_t>(stream)));
+}
+
+int cdp_k_token_logprob_backward(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, const float* lse, const float* entropy,
+                                 const float* dlogprob, const float* dentropy, void* dlogits, int rows, int vocab, void* stream) {
+  if (!logprob_sizes(dtype, logits, ld, targets, scale, rows, vocab) || !lse || !dlogits || !aligned_to(dlogits, dtype == DT_BF16 ? 2 : 4)) return CDP_EINVAL;
+  if ((dlogprob && !targets) || (dentropy && !entropy) || (!dlogprob && !dentropy)) return CDP_EINVAL;
+  for (const float* p : {lse, entropy, dlogprob, dentropy})
+    if (!aligned_to(p, 4)) return CDP_EINVAL;
+  TokenLogprob a;
+  memset(&a, 0, sizeof(a));
+  a.logits = logits; a.ld = ld; a.targets = targets; a.lse = const_cast<float*>(lse); a.entropy = const_cast<float*>(entropy);
+  a.dlogprob = dlogprob; a.dentropy = dentropy; a.dlogits = dlogits;
+  a.rows = rows; a.vocab = vocab; a.scale = scale;
+  return launched(launch_token_logprob(a, true, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -57,7 +57,8 @@ template <typename... A> PyObject* checked(int (*f)(A...), PyObject* const* args
   return call(f, args, std::index_sequence_for<A...>{});
 }
 
-enum Entry { GEMM, CONV, CONV_WGRAD_STATIC, LAYERNORM, GELU, ATTENTION, EMBEDDING, RESIDUAL_NORM, RESIDUAL_NORM_BACKWARD, ATTENTION_PACKED, GRAD_CLIP, ENTRIES };
+enum Entry { GEMM, CONV, CONV_WGRAD_STATIC, LAYERNORM, GELU, ATTENTION, EMBEDDING, RESIDUAL_NORM, RESIDUAL_NORM_BACKWARD, ATTENTION_PACKED, GRAD_CLIP, HEAD_NORM_ROTARY,
+             HEAD_NORM_ROTARY_BACKWARD, GATED_LINEAR, GATED_LINEAR_BACKWARD, LINEAR, LINEAR_BACKWARD, TOKEN_LOGPROB, TOKEN_LOGPROB_BACKWARD, ENTRIES };
 void* address[ENTRIES];  // null: not told yet
 
 template <int E, typename F> PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -88,6 +89,14 @@ PyMethodDef methods[] = {method("cdp_k_gemm", &entry<GEMM, decltype(&cdp_k_gemm)
                          method("cdp_k_residual_norm_backward", &entry<RESIDUAL_NORM_BACKWARD, decltype(&cdp_k_residual_norm_backward)>),
                          method("cdp_k_attention_packed", &entry<ATTENTION_PACKED, decltype(&cdp_k_attention_packed)>),
                          method("cdp_k_grad_clip", &entry<GRAD_CLIP, decltype(&cdp_k_grad_clip)>),
+                         method("cdp_k_head_norm_rotary", &entry<HEAD_NORM_ROTARY, decltype(&cdp_k_head_norm_rotary)>),
+                         method("cdp_k_head_norm_rotary_backward", &entry<HEAD_NORM_ROTARY_BACKWARD, decltype(&cdp_k_head_norm_rotary_backward)>),
+                         method("cdp_k_gated_linear", &entry<GATED_LINEAR, decltype(&cdp_k_gated_linear)>),
+                         method("cdp_k_gated_linear_backward", &entry<GATED_LINEAR_BACKWARD, decltype(&cdp_k_gated_linear_backward)>),
+                         method("cdp_k_linear", &entry<LINEAR, decltype(&cdp_k_linear)>),
+                         method("cdp_k_linear_backward", &entry<LINEAR_BACKWARD, decltype(&cdp_k_linear_backward)>),
+                         method("cdp_k_token_logprob", &entry<TOKEN_LOGPROB, decltype(&cdp_k_token_logprob)>),
+                         method("cdp_k_token_logprob_backward", &entry<TOKEN_LOGPROB_BACKWARD, decltype(&cdp_k_token_logprob_backward)>),
                          method("use", &use),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

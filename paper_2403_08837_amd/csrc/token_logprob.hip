@@ -1,0 +1,415 @@
+// Log probabilities of given tokens, the entropy and the likeliest tokens of rows of logits, and the gradient.  With z = scale * logits, of a row:
+//   lse = log sum exp z,  p = exp(z - lse),  logprob = z[target] - lse,  entropy = lse - sum p z;
+//   dlogits[j] = scale * (dlogprob * ((j == target) - p[j]) - dentropy * p[j] * (log p[j] + entropy)).
+//
+// Bound by memory: a row is read once forward, read and written once backward.  A lane keeps the maximum m of what it has seen with s = sum 2^y and
+// t = sum 2^y y, y = (logit - m) scale log2(e): a new maximum multiplies s by f = 2^d and makes t = f (t + d s).  That maximum is raised once for eight values at most.
+// entropy = log s - (t / s) log 2 over the row.
+//
+// The likeliest tokens come from the same pass: the k-th largest of the lanes' maxima (ordered by value, then by place) is a lower border, since k lanes hold
+// something at least as good, and only the lanes at or above it (k of them) can hold anything better.  Their share of the row, k of 256 parts of it,
+// is read again, and what is not below the border, little more than k tokens, is ranked.
+#include "elem.h"
+#include "kernels.h"
+#include "lane_sums.h"
+
+#include <algorithm>
+
+namespace cdp {
+
+namespace {
+
+constexpr int THREADS = 256, WAVES = THREADS / 64, UNROLL = 4;
+constexpr int MAX_FOUND = 1024;  // tokens not below the border that LDS holds at once; where there are more (it takes ordered rows) the border is raised
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.69314718055994531f;
+typedef unsigned long long u64;
+
+// A row as 16-byte pieces of aligned memory: piece k has the elements k * V - lead .. k * V - lead + V - 1, the first and the last of them perhaps not all.
+template <typename T> struct Row {
+  static constexpr int V = Elem<T>::VEC;
+  const T* at;     // of element 0
+  int lead, size;  // elements that piece 0 lacks; elements
+  __device__ __forceinline__ Row(const T* p, int n) : at(p), lead((int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T))), size(n) {}
+  __device__ __forceinline__ int pieces() const { return (int)(((unsigned)size + lead + V - 1) / V); }
+  __device__ __forceinline__ bool whole(int k) const { return (k > 0 || !lead) && (int64_t)(k + 1) * V - lead <= size; }
+  __device__ __forceinline__ uint4 get(int k) const { return *reinterpret_cast<const uint4*>(at + ((int64_t)k * V - lead)); }
+  // elements outside the row read as `none`
+  __device__ __forceinline__ void values(int k, float none, float (&v)[V]) const {
+    Chunk16<T> c;
+    if (whole(k)) {
+      c.v = get(k);
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = Elem<T>::to_f32(c.e[i]);
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const int64_t j = (int64_t)k * V - lead + i;
+      v[i] = j >= 0 && j < size ? Elem<T>::to_f32(at[j]) : none;
+    }
+  }
+};
+
+// 32 bits that order floats (-0 as 0, NaN as the lowest), and with a place 64 bits: larger values first, then lower places.  0: nothing.
+__device__ __forceinline__ unsigned ordered(float v) {
+  v = v != v ? -INFINITY : v + 0.f;
+  const unsigned u = __float_as_uint(v);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(unsigned o) { return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o); }
+__device__ __forceinline__ u64 key_of(float v, unsigned place) { return (u64)ordered(v) << 32 | (0xffffffffu - place); }
+__device__ __forceinline__ int place_of(u64 key) { return (int)(0xffffffffu - (unsigned)key); }
+
+struct Sums {
+  float m = -INFINITY, s = 0.f, t = 0.f;
+  static __device__ __forceinline__ Sums of(float4 q) {
+    Sums w;
+    w.m = q.x;
+    w.s = q.y;
+    w.t = q.z;
+    return w;
+  }
+  __device__ __forceinline__ float4 all() const { return make_float4(m, s, t, 0.f); }
+  // the values so far relative to another maximum, not below m
+  __device__ __forceinline__ void raise(float to, float c) {
+    const float d = (m - to) * c, f = __builtin_amdgcn_exp2f(d);
+    const bool some = m > -INFINITY;  // (else s and t are zero, or NaN)
+    t = some ? f * (t + d * s) : t;
+    s = some ? f * s : s;
+    m = to;
+  }
+  __device__ __forceinline__ void join(Sums b, float c) {
+    const float to = fmaxf(m, b.m);
+    if (m != to) raise(to, c);
+    if (b.m != to) b.raise(to, c);
+    s += b.s;
+    t += b.t;
+  }
+  template <int V> __device__ __forceinline__ void add(const float (&v)[V], float c) {
+    const float from = m > -INFINITY ? m * c : 0.f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float y = fmaf(v[i], c, -from), e = __builtin_amdgcn_exp2f(y);
+      s += e;
+      t += e * fmaxf(y, -256.f);  // (a value of -infinity has e = 0; one that is NaN is in s)
+    }
+  }
+};
+__device__ __forceinline__ float lane_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
+
+struct Found {
+  float4 sums[WAVES];
+  u64 best[THREADS], found[MAX_FOUND];
+  int lanes[THREADS];
+  u64 border;
+  int count, chosen;
+};
+
+// The `top` largest of keys[0 .. n) in order, by their ranks; out(rank, key).
+template <typename F> __device__ __forceinline__ void ranked(const u64* keys, int n, int top, F&& out) {
+  for (int i = threadIdx.x; i < n; i += THREADS) {
+    const u64 key = keys[i];
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; ++j) rank += keys[j] > key;
+    if (rank < top) out(rank, key);
+  }
+}
+
+// What a row is, from its sums.
+__device__ __forceinline__ void write_row(const TokenLogprob& a, int64_t row, const Sums& w, const void* logits, int target, bool bf16) {
+  const bool none = w.m == -INFINITY && w.s == 0.f;  // everything masked
+  const float ls = logf(w.s), lse = none ? -INFINITY : fmaf(a.scale, w.m, ls);
+  a.lse[row] = lse;
+  if (a.entropy) a.entropy[row] = none ? 0.f : ls - LN2 * (w.t / w.s);
+  if (a.logprob) {
+    const float l = bf16 ? bf16_to_f32(static_cast<const uint16_t*>(logits)[target]) : static_cast<const float*>(logits)[target];
+    a.logprob[row] = none || l == -INFINITY ? (w.s != w.s ? w.s : -INFINITY) : fmaf(a.scale, l - w.m, -ls);
+  }
+}
+__device__ __forceinline__ float top_logprob(const TokenLogprob& a, const Sums& w, float l) {
+  if (w.m == -INFINITY && w.s == 0.f) return -INFINITY;
+  return l == -INFINITY && w.s == w.s ? -INFINITY : fmaf(a.scale, l - w.m, -logf(w.s));
+}
+// A row that is not wanted: nothing of it is read.
+__device__ __forceinline__ void write_none(const TokenLogprob& a, int64_t row) {
+  if (threadIdx.x == 0) {
+    a.lse[row] = 0.f;
+    if (a.entropy) a.entropy[row] = 0.f;
+    if (a.logprob) a.logprob[row] = 0.f;
+  }
+  for (int i = threadIdx.x; i < a.top; i += THREADS) {
+    a.top_ids[row * a.top + i] = -1;
+    a.top_logprobs[row * a.top + i] = 0.f;
+  }
+}
+
+// Part blockIdx.x % parts of row blockIdx.x / parts: with parts > 1 its sums and its `top` largest go to the workspace.
+template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token_logprob_kernel(const TokenLogprob a) {
+  constexpr int V = Elem<T>::VEC;
+  __shared__ Found f;
+  const int64_t row = (int64_t)(blockIdx.x / (unsigned)a.parts);
+  const int part = blockIdx.x % (unsigned)a.parts, tid = threadIdx.x;
+  const int target = a.targets ? a.targets[row] : 0;
+  if (target < 0 || target >= a.vocab) {
+    if (part == 0) write_none(a, row);
+    return;
+  }
+  const T* const logits = static_cast<const T*>(a.logits) + row * a.ld;
+  const Row<T> r(logits, a.vocab);
+  const float c = a.scale * LOG2E;
+  const int all = r.pieces(), share = (all + a.parts - 1) / a.parts;
+  const int begin = min(part * share, all), end = min(begin + share, all);
+  int inner = begin, whole_end = end;  // the pieces that are whole
+  if (begin < end) {
+    if (!r.whole(begin)) ++inner;
+    if (end - 1 >= inner && !r.whole(end - 1)) --whole_end;
+  }
+  Sums w;
+  int best_piece = begin + tid;  // that of the lane's maximum, the first of several
+  auto take = [&](const float (&v)[V], int k) {
+    float most = fmaxf(v[0], v[1]);
+#pragma unroll
+    for (int i = 2; i < V; ++i) most = fmaxf(most, v[i]);
+    if (most > w.m) {
+      w.raise(most, c);
+      best_piece = k;
+    }
+    w.add<V>(v, c);
+  };
+  // lane l takes the pieces begin + l, begin + l + THREADS, ..
+  int k = begin + tid;
+  if (k < inner && k < end) {
+    float v[V];
+    r.values(k, -INFINITY, v);
+    take(v, k);
+    k += THREADS;
+  }
+  for (; k + (UNROLL - 1) * THREADS < whole_end; k += UNROLL * THREADS) {
+    Chunk16<T> q[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) q[u].v = r.get(k + u * THREADS);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      float v[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = Elem<T>::to_f32(q[u].e[i]);
+      take(v, k + u * THREADS);
+    }
+  }
+  for (; k < end; k += THREADS) {
+    float v[V];
+    r.values(k, -INFINITY, v);
+    take(v, k);
+  }
+  if constexpr (TOP) f.best[tid] = begin + tid < end ? (u64)ordered(w.m) << 32 | (0xffffffffu - (unsigned)best_piece) : 0;
+#pragma unroll
+  for (int mask = 1; mask < 64; mask *= 2) {
+    Sums b;
+    b.m = lane_xor(w.m, mask);
+    b.s = lane_xor(w.s, mask);
+    b.t = lane_xor(w.t, mask);
+    w.join(b, c);
+  }
+  if ((tid & 63) == 0) f.sums[tid >> 6] = w.all();
+  if (tid == 0) f.count = f.chosen = 0, f.border = 0;
+  __syncthreads();
+  w = Sums::of(f.sums[0]);
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) w.join(Sums::of(f.sums[i]), c);
+  if (tid == 0) {
+    if (a.parts == 1) write_row(a, row, w, logits, target, sizeof(T) == 2);
+    else a.part_sums[blockIdx.x] = w.all();
+  }
+  if constexpr (TOP) {
+    {
+      const u64 key = f.best[tid];
+      int rank = 0;
+#pragma unroll 8
+      for (int j = 0; j < THREADS; ++j) rank += f.best[j] > key;
+      if (key && rank < a.top) {
+        f.lanes[atomicAdd(&f.chosen, 1)] = tid;
+        // (anything in that piece or in one before it)
+        if (rank == a.top - 1) f.border = (key >> 32) << 32 | (0xffffffffu - (unsigned)((int64_t)(place_of(key) + 1) * V - 1 - r.lead));
+      }
+    }
+    __syncthreads();
+    const int steps = (share + THREADS - 1) / THREADS, chosen = f.chosen;
+    int n;
+    for (;;) {
+      const u64 border = f.border;
+      for (int i = tid; i < chosen * steps; i += THREADS) {
+        const int piece = begin + f.lanes[i / steps] + i % steps * THREADS;
+        if (piece >= end) continue;
+        float v[V];
+        r.values(piece, 0.f, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int64_t j = (int64_t)piece * V - r.lead + e;
+          if (j < 0 || j >= a.vocab) continue;
+          const u64 key = key_of(v[e], (unsigned)j);
+          if (key >= border) {
+            const int at = atomicAdd(&f.count, 1);
+            if (at < MAX_FOUND) f.found[at] = key;
+          }
+        }
+      }
+      __syncthreads();
+      n = f.count;
+      if (n <= MAX_FOUND) break;
+      // the border of those that were kept; what is below it is not among the `top` largest of all
+      __syncthreads();
+      if (tid == 0) f.count = 0;
+      ranked(f.found, MAX_FOUND, a.top, [&](int rank, u64 key) {
+        if (rank == a.top - 1) f.border = key;
+      });
+      __syncthreads();
+    }
+    if (a.parts == 1) {
+      ranked(f.found, n, a.top, [&](int rank, u64 key) {
+        a.top_ids[row * a.top + rank] = place_of(key);
+        a.top_logprobs[row * a.top + rank] = top_logprob(a, w, value_of((unsigned)(key >> 32)));
+      });
+    } else {
+      u64* const to = a.part_keys + (int64_t)blockIdx.x * a.top;
+      ranked(f.found, n, a.top, [&](int rank, u64 key) { to[rank] = key; });
+      for (int i = n + tid; i < a.top; i += THREADS) to[i] = 0;
+    }
+  }
+}
+
+// Joins the parts of a row.
+template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_join_kernel(const TokenLogprob a) {
+  __shared__ u64 found[LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP];
+  __shared__ u64 least[LOGPROB_MAX_SPLIT];
+  __shared__ int count;
+  const int64_t row = blockIdx.x;
+  const int target = a.targets ? a.targets[row] : 0, tid = threadIdx.x;
+  if (target < 0 || target >= a.vocab) return;
+  const float c = a.scale * LOG2E;
+  Sums w;
+  for (int i = 0; i < a.parts; ++i) w.join(Sums::of(a.part_sums[row * a.parts + i]), c);
+  if (tid == 0) write_row(a, row, w, static_cast<const T*>(a.logits) + row * a.ld, target, sizeof(T) == 2);
+  if (!a.top) return;
+  // each part's list is in order: the least of their each's-th keys is not above the `top`-th of all
+  const u64* const keys = a.part_keys + row * a.parts * a.top;
+  const int each = (a.top + a.parts - 1) / a.parts;
+  if (tid == 0) count = 0;
+  if (tid < a.parts) least[tid] = keys[tid * a.top + each - 1];
+  __syncthreads();
+  u64 border = least[0];
+  for (int i = 1; i < a.parts; ++i) border = border < least[i] ? border : least[i];
+  for (int i = tid; i < a.parts * a.top; i += THREADS) {
+    const u64 key = keys[i];
+    if (key && key >= border) found[atomicAdd(&count, 1)] = key;
+  }
+  __syncthreads();
+  ranked(found, count, a.top, [&](int rank, u64 key) {
+    a.top_ids[row * a.top + rank] = place_of(key);
+    a.top_logprobs[row * a.top + rank] = top_logprob(a, w, value_of((unsigned)(key >> 32)));
+  });
+}
+
+// Pieces blockIdx.y * share .. of row blockIdx.x.
+template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_bwd_kernel(const TokenLogprob a, int share) {
+  constexpr int V = Elem<T>::VEC;
+  const int64_t row = blockIdx.x;
+  const int target = a.targets ? a.targets[row] : 0;
+  const Row<T> r(static_cast<const T*>(a.logits) + row * a.ld, a.vocab);
+  T* const out = static_cast<T*>(a.dlogits) + row * a.ld;
+  const bool alike = (reinterpret_cast<uintptr_t>(out) & 15) == (reinterpret_cast<uintptr_t>(r.at) & 15);
+  const int begin = (int)min((int64_t)blockIdx.y * share, (int64_t)r.pieces()), end = min(begin + share, r.pieces());
+  const bool wanted = target >= 0 && target < a.vocab;
+  float c = 0.f, from = 0.f, A = 0.f, B = 0.f, at_target = 0.f;
+  bool some = wanted;
+  if (wanted) {
+    const float lse = a.lse[row], dl = a.dlogprob ? a.dlogprob[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
+    some = lse != -INFINITY;  // (a row with everything masked has no gradient)
+    c = a.scale * LOG2E;
+    from = lse * LOG2E;
+    A = a.scale * (dl + (a.dentropy ? dh * a.entropy[row] : 0.f));
+    if (lse != lse) A = lse;
+    B = a.scale * dh * LN2;
+    at_target = a.scale * dl;
+  }
+  auto store = [&](int k, const float (&v)[V]) {
+    const int64_t j = (int64_t)k * V - r.lead;
+    if (alike && r.whole(k)) {
+      Chunk16<T> q;
+#pragma unroll
+      for (int i = 0; i < V; ++i) q.e[i] = Elem<T>::from_f32(v[i]);
+      *reinterpret_cast<uint4*>(out + j) = q.v;
+      return;
+    }
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (j + i >= 0 && j + i < r.size) out[j + i] = Elem<T>::from_f32(v[i]);
+  };
+  auto gradient = [&](int k, float (&v)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const float y = fmaxf(fmaf(v[i], c, -from), -256.f);  // (where it is NaN, A is)
+      v[i] = -(__builtin_amdgcn_exp2f(y) * fmaf(B, y, A));
+    }
+    const int64_t at = (int64_t)target - ((int64_t)k * V - r.lead);
+    if (at >= 0 && at < V && a.targets)
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] += i == (int)at ? at_target : 0.f;
+  };
+  int k = begin + threadIdx.x;
+  if (!some) {
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = 0.f;
+    for (; k < end; k += THREADS) store(k, v);
+    return;
+  }
+  for (; k + (UNROLL - 1) * THREADS < end; k += UNROLL * THREADS) {
+    float v[UNROLL][V];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) r.values(k + u * THREADS, 0.f, v[u]);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      gradient(k + u * THREADS, v[u]);
+      store(k + u * THREADS, v[u]);
+    }
+  }
+  for (; k < end; k += THREADS) {
+    float v[V];
+    r.values(k, 0.f, v);
+    gradient(k, v);
+    store(k, v);
+  }
+}
+
+template <typename T> hipError_t forward(TokenLogprob a, hipStream_t stream) {
+  // parts of a row where there are few: 1024 workgroups at most and at least 16 KB each
+  const int64_t bytes = (int64_t)a.vocab * (int)sizeof(T);
+  a.parts = a.part_sums ? (int)std::max<int64_t>(1, std::min<int64_t>({LOGPROB_MAX_SPLIT, LOGPROB_MAX_PARTS / a.rows, bytes >> 14})) : 1;
+  const int64_t groups = (int64_t)a.rows * a.parts;
+  if (!launchable(groups, THREADS)) return hipErrorInvalidConfiguration;
+  if (a.top) hipLaunchKernelGGL((token_logprob_kernel<T, true>), dim3((unsigned)groups), dim3(THREADS), 0, stream, a);
+  else hipLaunchKernelGGL((token_logprob_kernel<T, false>), dim3((unsigned)groups), dim3(THREADS), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.parts == 1) return e;
+  hipLaunchKernelGGL((token_logprob_join_kernel<T>), dim3(a.rows), dim3(THREADS), 0, stream, a);
+  return hipGetLastError();
+}
+template <typename T> hipError_t backward(const TokenLogprob& a, hipStream_t stream) {
+  constexpr int V = Elem<T>::VEC;
+  const int64_t pieces = ((int64_t)a.vocab + V - 1) / V + 1;
+  const int share = 4 * UNROLL * THREADS;  // 64 KB of a row
+  const int64_t segments = (pieces + share - 1) / share;
+  if (!launchable(a.rows * segments, THREADS)) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((token_logprob_bwd_kernel<T>), dim3(a.rows, (unsigned)segments), dim3(THREADS), 0, stream, a, share);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_token_logprob(const TokenLogprob& a, bool backward_, int dtype, hipStream_t stream) {
+  if (backward_) return dtype == DT_BF16 ? backward<uint16_t>(a, stream) : backward<float>(a, stream);
+  return dtype == DT_BF16 ? forward<uint16_t>(a, stream) : forward<float>(a, stream);
+}
+
+}  // namespace cdp
