@@ -41,13 +41,6 @@ template <typename T> __device__ __forceinline__ float sigmoid_of(float g, float
   away = fminf(away * s, 1.f);  // 1 - s, not as a difference (1 where that is inf * 0)
   return s;
 }
-template <typename T> __device__ __forceinline__ float act_of(int act, float g) {
-  float away;
-  if (act == TOKEN_NONE) return g;
-  if (act == TOKEN_SILU) return g * sigmoid_of<T>(g, away);
-  if (act == TOKEN_GELU) return gelu_f<T>(g);
-  return sigmoid_of<T>(g, away);
-}
 template <typename T> __device__ __forceinline__ void act_both(int act, float g, float& a, float& da) {
   float away;
   if (act == TOKEN_SILU) {
@@ -65,6 +58,21 @@ template <typename T> __device__ __forceinline__ void act_both(int act, float g,
   } else {
     a = sigmoid_of<T>(g, away);
     da = a * away;
+  }
+}
+
+// (one branch for all values)
+template <typename T, int N> __device__ __forceinline__ void act_all(int act, float (&v)[N]) {
+  float away;
+  if (act == TOKEN_SILU) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] *= sigmoid_of<T>(v[k], away);
+  } else if (act == TOKEN_GELU) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = gelu_f<T>(v[k]);
+  } else if (act == TOKEN_SIGMOID) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = sigmoid_of<T>(v[k], away);
   }
 }
 
@@ -227,7 +235,7 @@ struct Product {
   void *out, *out2, *out3;      // GATED: h, g, u (g, u may be null); LINEAR: y, z (or null); pair: dwg, dwu; else the result
   const void *bias, *residual;  // LINEAR: or null
   float* part;                  // splits > 1: sums [splits][results of all][M][N]
-  int f32, act, pair;
+  int act, pair;
 };
 enum { GATED, LINEAR, DGRAD, WGRAD };
 
@@ -236,25 +244,25 @@ template <int TILE, int NWAVE, int BK, bool SLOW> struct Slabs {
   static constexpr int ROW = SLOW ? TILE * 2 : BK * 2, CPR = ROW / 16, RPB = 1024 / ROW;  // bytes and 16-byte chunks of a tile row, rows per 1 KB block
   static constexpr int BYTES = TILE * BK * 2, LP = BYTES / 1024 / NWAVE;                    // loads of a wavefront per slab
   static_assert(LP * 1024 * NWAVE == BYTES && CPR <= 64 && TILE >= 64, "tile rows are dealt to the wavefronts in 1 KB blocks");
-  unsigned off[LP];
+  unsigned off[LP];  // byte offsets from the tile's first element in this slab, ~0: outside
+  int chunk[2];      // !SLOW: first reduction index, in the slab, of the chunk of even and odd loads
   // chunk c of tile row r sits in slot c ^ swz(r)
-  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : BK == 64 ? (r >> 1) & 7 : (r >> 2) & 3; }
+  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : (r >> 1) & 7; }
   static __device__ __forceinline__ int piece(int r) { return TILE >= 128 ? r & 3 : (r >> 1) & 1; }  // SLOW: 64-byte pieces of four rows on banks of their own
-  // place of lane's chunk of load i: tile row, chunk in it
-  static __device__ __forceinline__ void where(int i, int wave, int lane, int& r, int& c) {
-    r = (wave * LP + i) * RPB + lane / CPR;
-    c = (lane % CPR) ^ swz(r);
-  }
-  // byte offsets from the tile's first element; `left`: reduction indices in this slab.  row_of: tile row -> row of the matrix, from the tile's first
-  template <typename F> __device__ __forceinline__ void start(int wave, int lane, int left, int first, int size, int ld, F&& row_of) {
+  // row_of: tile row -> row of the matrix, from the tile's first; `first` of `size` rows (SLOW: columns)
+  template <typename F> __device__ __forceinline__ void start(int wave, int lane, int first, int size, int ld, F&& row_of) {
 #pragma unroll
     for (int i = 0; i < LP; ++i) {
-      int r, c;
-      where(i, wave, lane, r, c);
-      if (SLOW) off[i] = r < left && first + c * 8 < size ? 2u * ((unsigned)r * (unsigned)ld + c * 8) : ~0u;
-      else off[i] = c * 8 < left ? 2u * ((unsigned)min(row_of(r), size - 1 - first) * (unsigned)ld + c * 8) : ~0u;  // rows past the last repeat it
+      const int r = (wave * LP + i) * RPB + lane / CPR, c = (lane % CPR) ^ swz(r);
+      if (SLOW) off[i] = first + c * 8 < size ? 2u * ((unsigned)r * (unsigned)ld + c * 8) : ~0u;
+      else off[i] = 2u * ((unsigned)min(row_of(r), size - 1 - first) * (unsigned)ld + c * 8);  // rows past the last repeat it
+      if (!SLOW && i < 2) chunk[i] = c * 8;
     }
+    static_assert(SLOW || (BK == 64 && LP % 2 == 0), "loads two apart have the same chunks");
   }
+  // `left` reduction indices in the slab: what is past them reads as zero.  SLOW: they are rows, and the buffer ends there.
+  __device__ __forceinline__ unsigned place(int i, int left) const { return SLOW || chunk[i & 1] < left ? off[i] : ~0u; }
+  static __device__ __forceinline__ unsigned records(int left, int ld) { return SLOW ? 2u * (unsigned)left * (unsigned)ld : left > 0 ? 0xfffffff0u : 0u; }
 };
 __device__ __forceinline__ void load_lds(unsigned lds, unsigned off, const void* base, unsigned records) {
   typedef unsigned v4u __attribute__((ext_vector_type(4)));
@@ -286,38 +294,35 @@ __device__ __forceinline__ uint4 eight(const float* v) {
   const auto y = __builtin_amdgcn_permlane32_swap(two(v[2], v[3]), two(v[6], v[7]), false, false);
   return make_uint4(x[0], y[0], x[1], y[1]);
 }
-// A 32 x 32 block of results: row m, columns n ..; v[8 q + 4 .. + e] are the columns 8 q + 4 hi + e of it (q < 4, e < 4).
-__device__ __forceinline__ void store_block(void* out, bool f32, int64_t m, int n, int M, int N, int hi, const float (&v)[16]) {
-  if (f32) {
-    if (m >= M) return;
+// A 32 x 32 block of results: row m, columns n ..; v[4 q + e] is column 8 q + 4 hi + e of it (q < 4, e < 4).
+__device__ __forceinline__ void store_block(float* out, int64_t m, int n, int M, int N, int hi, const float (&v)[16]) {
+  if (m >= M) return;
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      if (n + 8 * q + 4 * hi < N)
-        *reinterpret_cast<float4*>(static_cast<float*>(out) + m * N + n + 8 * q + 4 * hi) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
-    return;
-  }
+  for (int q = 0; q < 4; ++q)
+    if (n + 8 * q + 4 * hi < N) *reinterpret_cast<float4*>(out + m * N + n + 8 * q + 4 * hi) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+}
+__device__ __forceinline__ void store_block(uint16_t* out, int64_t m, int n, int M, int N, int hi, const float (&v)[16]) {
 #pragma unroll
   for (int q = 0; q < 2; ++q) {
     const uint4 w = eight(v + 8 * q);
-    if (m < M && n + 16 * q + 8 * hi < N) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + m * N + n + 16 * q + 8 * hi) = w;
+    if (m < M && n + 16 * q + 8 * hi < N) *reinterpret_cast<uint4*>(out + m * N + n + 16 * q + 8 * hi) = w;
   }
 }
-
 // Adds row m of a matrix to a block.
-__device__ __forceinline__ void add_block(const void* from, bool f32, int64_t m, int n, int M, int N, int hi, float (&v)[16]) {
+template <typename T> __device__ __forceinline__ void add_block(const T* from, int64_t m, int n, int M, int N, int hi, float (&v)[16]) {
   if (m >= M) return;
 #pragma unroll
   for (int q = 0; q < 4; ++q) {
     const int c = n + 8 * q + 4 * hi;
     if (c >= N) continue;
-    if (f32) {
-      const float4 w = *reinterpret_cast<const float4*>(static_cast<const float*>(from) + m * N + c);
+    if constexpr (sizeof(T) == 4) {
+      const float4 w = *reinterpret_cast<const float4*>(from + m * N + c);
       v[4 * q] += w.x;
       v[4 * q + 1] += w.y;
       v[4 * q + 2] += w.z;
       v[4 * q + 3] += w.w;
     } else {
-      const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(from) + m * N + c);
+      const uint2 w = *reinterpret_cast<const uint2*>(from + m * N + c);
       v[4 * q] += __uint_as_float(w.x << 16);
       v[4 * q + 1] += __uint_as_float(w.x & 0xffff0000u);
       v[4 * q + 2] += __uint_as_float(w.y << 16);
@@ -326,7 +331,7 @@ __device__ __forceinline__ void add_block(const void* from, bool f32, int64_t m,
   }
 }
 
-template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int BK, int STAGES, int WPS>
+template <int WHAT, typename T, int BM, int BN, int WAVES_M, int WAVES_N, int BK, int STAGES, int WPS>
 __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_kernel(const Product P) {
   constexpr int NWAVE = WAVES_M * WAVES_N, WTM = BM / WAVES_M, WTN = BN / WAVES_N, MI = WTM / 32, NI = WTN / 32, KK = BK / 16;
   constexpr bool DUAL = WHAT == GATED, ASLOW = WHAT == WGRAD, BSLOW = WHAT == DGRAD || WHAT == WGRAD;
@@ -352,7 +357,7 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
   SB sb;
   const char *pa, *pb, *pb2;
   int seg = first_slab / per_segment, slab = first_slab - seg * per_segment, left = todo;
-  unsigned records = todo > 0 ? 0xfffffff0u : 0u;
+  int in_slab = min(BK, P.K - slab * BK);  // reduction indices in the next slab; 0 behind the last, and the loads that the counted waits expect read nothing
   auto b_row = [](int r) { return DUAL ? (r >> 6) * 32 + (r & 31) : r; };  // DUAL: 32 columns of B, 32 of B2, ..
   auto bases = [&] {
     const uint16_t* const a = (WHAT == WGRAD && second ? P.other[seg] : P.A[seg]);
@@ -361,24 +366,18 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
     pb = reinterpret_cast<const char*>(BSLOW ? b + (int64_t)slab * BK * P.ldb + col0 : b + (int64_t)col0 * P.ldb + slab * BK);
     if (DUAL) pb2 = reinterpret_cast<const char*>(P.other[seg] + (int64_t)col0 * P.ldb + slab * BK);
   };
-  auto offsets = [&] {
-    const int in_slab = min(BK, P.K - slab * BK);
-    sa.start(wave, lane, in_slab, row0, P.M, P.lda, [](int r) { return r; });
-    sb.start(wave, lane, in_slab, col0, P.N, P.ldb, b_row);
-  };
-  if (todo > 0) {
-    bases();
-    offsets();
-  }
+  bases();
+  sa.start(wave, lane, row0, P.M, P.lda, [](int r) { return r; });
+  sb.start(wave, lane, col0, P.N, P.ldb, b_row);
   auto issue = [&](unsigned at, int e) {
-    if (e < SA::LP) return load_lds(at + (wave * SA::LP + e) * 1024, sa.off[e], pa, records);
+    if (e < SA::LP) return load_lds(at + (wave * SA::LP + e) * 1024, sa.place(e, in_slab), pa, SA::records(in_slab, P.lda));
     const int i = e - SA::LP;
     const bool two = DUAL && (((wave * SB::LP + i) * SB::RPB >> 5) & 1);
-    load_lds(at + SA::BYTES + (wave * SB::LP + i) * 1024, sb.off[i], two ? pb2 : pb, records);
+    load_lds(at + SA::BYTES + (wave * SB::LP + i) * 1024, sb.place(i, in_slab), two ? pb2 : pb, SB::records(in_slab, P.ldb));
   };
   auto advance = [&] {
     if (--left <= 0) {
-      records = 0;  // loads past the last slab, which the counted waits expect, read nothing
+      in_slab = 0;
       return;
     }
     pa += ASLOW ? 2ll * BK * P.lda : 2ll * BK;
@@ -388,10 +387,8 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
       slab = 0;
       ++seg;
       bases();
-      if (P.K % BK) offsets();
-    } else if (slab == per_segment - 1 && P.K % BK) {
-      offsets();
     }
+    in_slab = min(BK, P.K - slab * BK);
   };
 #pragma unroll
   for (int q = 0; q < STAGES; ++q) {
@@ -471,19 +468,12 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
     }
     advance();
   };
-  for (int t = todo;;) {
+  // whole rounds of the stages: slabs past the last are zeros, and one way out of the loop leaves the accumulators where they are
+  for (int t = todo; t > 0; t -= STAGES) {
     step(std::integral_constant<int, 0>{});
-    if (--t <= 0) break;
     step(std::integral_constant<int, 1>{});
-    if (--t <= 0) break;
-    if constexpr (STAGES > 2) {
-      step(std::integral_constant<int, 2>{});
-      if (--t <= 0) break;
-    }
-    if constexpr (STAGES > 3) {
-      step(std::integral_constant<int, 3>{});
-      if (--t <= 0) break;
-    }
+    if constexpr (STAGES > 2) step(std::integral_constant<int, 2>{});
+    if constexpr (STAGES > 3) step(std::integral_constant<int, 3>{});
   }
   wait_newest<0>();  // no load is left that writes LDS when this workgroup gives it back
   const int64_t MN = (int64_t)P.M * P.N;
@@ -491,51 +481,41 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int64_t m = row0 + wm * WTM + i * 32 + l31;
-    if constexpr (DUAL) {
 #pragma unroll
-      for (int j = 0; j < NI; j += 2) {
-        const int n = col0 + (wn * NI + j) / 2 * 32;
-        float g[16], u[16];
+    for (int j = 0; j < NI; j += DUAL ? 2 : 1) {
+      const int n = DUAL ? col0 + (wn * NI + j) / 2 * 32 : col0 + wn * WTN + j * 32;
+      float v[16];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-          g[v] = acc[i][j][v];
-          u[v] = acc[i][j + 1][v];
+      for (int k = 0; k < 16; ++k) v[k] = acc[i][j][k];
+      if (P.splits > 1) {
+        store_block(part + (second ? MN : 0), m, n, P.M, P.N, hi, v);
+        if constexpr (DUAL) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = acc[i][j + 1][k];
+          store_block(part + MN, m, n, P.M, P.N, hi, v);
         }
-        if (P.splits > 1) {
-          store_block(part, true, m, n, P.M, P.N, hi, g);
-          store_block(part + MN, true, m, n, P.M, P.N, hi, u);
-          continue;
-        }
+      } else if constexpr (DUAL) {
         if (P.out2) {
-          store_block(P.out2, P.f32, m, n, P.M, P.N, hi, g);
-          store_block(P.out3, P.f32, m, n, P.M, P.N, hi, u);
-        }
+          float u[16];
 #pragma unroll
-        for (int v = 0; v < 16; ++v) g[v] = (P.f32 ? act_of<float>(P.act, g[v]) : act_of<uint16_t>(P.act, g[v])) * u[v];
-        store_block(P.out, P.f32, m, n, P.M, P.N, hi, g);
+          for (int k = 0; k < 16; ++k) u[k] = acc[i][j + 1][k];
+          store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
+          store_block(static_cast<T*>(P.out3), m, n, P.M, P.N, hi, u);
+        }
+        act_all<T>(P.act, v);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] *= acc[i][j + 1][k];
+        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
+      } else if constexpr (WHAT == LINEAR) {
+        if (P.bias) add_block(static_cast<const T*>(P.bias), 0, n, 1, P.N, hi, v);
+        if (P.out2) store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
+        act_all<T>(P.act, v);
+        if (P.residual) add_block(static_cast<const T*>(P.residual), m, n, P.M, P.N, hi, v);
+        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
+      } else {
+        store_block(static_cast<T*>(second ? P.out2 : P.out), m, n, P.M, P.N, hi, v);
       }
-    } else {
-#pragma unroll
-      for (int j = 0; j < NI; ++j) {
-        float v[16];
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = acc[i][j][k];
-        const int n = col0 + wn * WTN + j * 32;
-        if (P.splits > 1) {
-          store_block(part + (second ? MN : 0), true, m, n, P.M, P.N, hi, v);
-          continue;
-        }
-        if constexpr (WHAT == LINEAR) {
-          if (P.bias) add_block(P.bias, P.f32, 0, n, 1, P.N, hi, v);
-          if (P.out2) store_block(P.out2, P.f32, m, n, P.M, P.N, hi, v);
-#pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = P.f32 ? act_of<float>(P.act, v[k]) : act_of<uint16_t>(P.act, v[k]);
-          if (P.residual) add_block(P.residual, P.f32, m, n, P.M, P.N, hi, v);
-          store_block(P.out, P.f32, m, n, P.M, P.N, hi, v);
-          continue;
-        }
-        store_block(second ? P.out2 : P.out, P.f32, m, n, P.M, P.N, hi, v);
-      }
+      __builtin_amdgcn_sched_barrier(0);  // one block's values and addresses at a time
     }
   }
 }
@@ -573,8 +553,7 @@ template <typename T> __global__ __launch_bounds__(256) void token_join_kernel(c
   if (what == LINEAR) {
     if (P.bias) add(P.bias, i % P.N, v);  // (N is a multiple of 8)
     if (P.out2) store(P.out2, i, v);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_of<T>(P.act, v[e]);
+    act_all<T>(P.act, v);
     if (P.residual) add(P.residual, i, v);
     store(P.out, i, v);
   } else if (what == GATED) {
@@ -584,8 +563,9 @@ template <typename T> __global__ __launch_bounds__(256) void token_join_kernel(c
       store(P.out2, i, v);
       store(P.out3, i, u);
     }
+    act_all<T>(P.act, v);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = act_of<T>(P.act, v[e]) * u[e];
+    for (int e = 0; e < 8; ++e) v[e] *= u[e];
     store(P.out, i, v);
   } else if (i < MN) {
     store(P.out, i, v);
@@ -672,20 +652,20 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
   if constexpr (DUAL) {
     if (a.out2) store(lane < 32 ? a.out2 : a.out3);
     if (lane >= 32) return;
+    act_all<T>(a.act, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_of<T>(a.act, v[e]) * u[e];
+    for (int e = 0; e < 4; ++e) v[e] *= u[e];
   } else {
     if (a.bias) add(a.bias, col);
     if (a.out2) store(a.out2);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = act_of<T>(a.act, v[e]);
+    act_all<T>(a.act, v);
     if (a.residual) add(a.residual, at);
   }
   store(a.out);
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
-template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int WPS> hipError_t launch_tiles(Product& p, int64_t room, hipStream_t stream) {
+template <int WHAT, typename T, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int WPS> hipError_t launch_tiles(Product& p, int64_t room, hipStream_t stream) {
   constexpr int BK = 64, COLS = WHAT == GATED ? BN / 2 : BN;
   p.tiles_m = (p.M + BM - 1) / BM;
   p.tiles_n = (p.N + COLS - 1) / COLS;
@@ -697,19 +677,22 @@ template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int WP
   int64_t splits = std::max<int64_t>(1, std::min({resident / tiles, slabs / 8, room / (4 * MN)}));
   p.slabs_per = (int)((slabs + splits - 1) / splits);
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
-  hipLaunchKernelGGL((token_product_kernel<WHAT, BM, BN, WAVES_M, WAVES_N, BK, STAGES, WPS>), dim3((unsigned)(tiles * p.splits)), dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
+  hipLaunchKernelGGL((token_product_kernel<WHAT, T, BM, BN, WAVES_M, WAVES_N, BK, STAGES, WPS>), dim3((unsigned)(tiles * p.splits)), dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   const dim3 grid((unsigned)(((WHAT == GATED ? MN / 2 : MN) / 8 + 255) / 256));
-  if (p.f32) hipLaunchKernelGGL((token_join_kernel<float>), grid, dim3(256), 0, stream, p, (int)WHAT);
-  else hipLaunchKernelGGL((token_join_kernel<uint16_t>), grid, dim3(256), 0, stream, p, (int)WHAT);
+  hipLaunchKernelGGL((token_join_kernel<T>), grid, dim3(256), 0, stream, p, (int)WHAT);
   return hipGetLastError();
 }
-template <int WHAT> hipError_t launch_product(Product& p, int64_t room, hipStream_t stream) {
+template <int WHAT, typename T> hipError_t launch_tiled(Product& p, int64_t room, hipStream_t stream) {
   const int64_t cols = WHAT == GATED ? 2ll * p.N : p.N, pair = p.pair ? 2 : 1;
-  if (((p.M + 255) / 256) * ((cols + 255) / 256) * pair >= 256) return launch_tiles<WHAT, 256, 256, 2, 4, 2, 2>(p, room, stream);
-  if (p.M <= 64) return launch_tiles<WHAT, 64, 128, 2, 2, 3, 2>(p, room, stream);
-  return launch_tiles<WHAT, 128, 128, 2, 2, 2, 2>(p, room, stream);
+  if (((p.M + 255) / 256) * ((cols + 255) / 256) * pair >= 256) return launch_tiles<WHAT, T, 256, 256, 2, 4, 2, 2>(p, room, stream);
+  if (p.M <= 64) return launch_tiles<WHAT, T, 64, 128, 2, 2, 3, 2>(p, room, stream);
+  return launch_tiles<WHAT, T, 128, 128, 2, 2, 2, 2>(p, room, stream);
+}
+
+template <int WHAT> hipError_t launch_product(Product& p, int64_t room, bool f32, hipStream_t stream) {
+  return f32 ? launch_tiled<WHAT, float>(p, room, stream) : launch_tiled<WHAT, uint16_t>(p, room, stream);
 }
 
 // The six products of planes, the smallest first.
@@ -772,11 +755,12 @@ hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stre
   memset(&p, 0, sizeof(p));
   p.K = a.in; p.M = a.rows; p.N = a.hidden; p.lda = p.ldb = a.in;
   p.out = a.h; p.out2 = a.g; p.out3 = a.u;
-  p.f32 = dtype == DT_F32; p.act = a.act;
+  p.act = a.act;
+  const bool f32 = dtype == DT_F32;
   char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
   const int64_t xn = (int64_t)a.rows * a.in, wn = (int64_t)a.hidden * a.in;
   const uint16_t *x = static_cast<const uint16_t*>(a.x), *wg = static_cast<const uint16_t*>(a.wg), *wu = static_cast<const uint16_t*>(a.wu);
-  if (p.f32) {
+  if (f32) {
     uint16_t* planes[3];
     const hipError_t e = cut({a.x, a.wg, a.wu}, {xn, wn, wn}, at, planes, stream);
     if (e != hipSuccess) return e;
@@ -784,7 +768,7 @@ hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stre
     wg = planes[1];
     wu = planes[2];
   }
-  const Segments of(p.f32);
+  const Segments of(f32);
   p.segments = of.count;
   for (int s = 0; s < of.count; ++s) {
     p.A[s] = x + of.a[s] * xn;
@@ -792,7 +776,7 @@ hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stre
     p.other[s] = wu + of.b[s] * wn;
   }
   p.part = reinterpret_cast<float*>(at);
-  return launch_product<GATED>(p, std::max<int64_t>(0, end - at), stream);
+  return launch_product<GATED>(p, std::max<int64_t>(0, end - at), f32, stream);
 }
 
 hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream) {
@@ -835,8 +819,8 @@ hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t 
       p.B[2 * s] = wg + of.b[s] * wn;
       p.B[2 * s + 1] = wu + of.b[s] * wn;
     }
-    p.out = a.dx; p.f32 = f32; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), stream);
+    p.out = a.dx; p.part = reinterpret_cast<float*>(at);
+    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
     if (e != hipSuccess) return e;
   }
   if (a.dwg) {
@@ -848,8 +832,8 @@ hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t 
       p.other[s] = du + of.a[s] * n;
       p.B[s] = x + of.b[s] * xn;
     }
-    p.out = a.dwg; p.out2 = a.dwu; p.f32 = f32; p.pair = 1; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), stream);
+    p.out = a.dwg; p.out2 = a.dwu; p.pair = 1; p.part = reinterpret_cast<float*>(at);
+    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
   }
   return e;
 }
@@ -860,25 +844,26 @@ hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stre
   memset(&p, 0, sizeof(p));
   p.K = a.in; p.M = a.rows; p.N = a.out; p.lda = p.ldb = a.in;
   p.out = a.y; p.out2 = a.z; p.bias = a.bias; p.residual = a.residual;
-  p.f32 = dtype == DT_F32; p.act = a.act;
+  p.act = a.act;
+  const bool f32 = dtype == DT_F32;
   char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
   const int64_t xn = (int64_t)a.rows * a.in, wn = (int64_t)a.out * a.in;
   const uint16_t *x = static_cast<const uint16_t*>(a.x), *w = static_cast<const uint16_t*>(a.w);
-  if (p.f32) {
+  if (f32) {
     uint16_t* planes[3];
     const hipError_t e = cut({a.x, a.w, nullptr}, {xn, wn, 0}, at, planes, stream);
     if (e != hipSuccess) return e;
     x = planes[0];
     w = planes[1];
   }
-  const Segments of(p.f32);
+  const Segments of(f32);
   p.segments = of.count;
   for (int s = 0; s < of.count; ++s) {
     p.A[s] = x + of.a[s] * xn;
     p.B[s] = w + of.b[s] * wn;
   }
   p.part = reinterpret_cast<float*>(at);
-  return launch_product<LINEAR>(p, std::max<int64_t>(0, end - at), stream);
+  return launch_product<LINEAR>(p, std::max<int64_t>(0, end - at), f32, stream);
 }
 
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream) {
@@ -935,8 +920,8 @@ hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t 
       p.A[s] = dz + of.a[s] * n;
       p.B[s] = w + of.b[s] * wn;
     }
-    p.out = a.dx; p.f32 = f32; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), stream);
+    p.out = a.dx; p.part = reinterpret_cast<float*>(at);
+    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
     if (e != hipSuccess) return e;
   }
   if (a.dw) {
@@ -947,8 +932,8 @@ hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t 
       p.A[s] = dz + of.a[s] * n;
       p.B[s] = x + of.b[s] * xn;
     }
-    p.out = a.dw; p.f32 = f32; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), stream);
+    p.out = a.dw; p.part = reinterpret_cast<float*>(at);
+    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
   }
   return e;
 }
