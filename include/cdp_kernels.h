@@ -184,28 +184,28 @@ int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, 
  * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20.  g and u (both or neither): written too, for the backward.
  * Sums are fp32.  fp32: factors are taken as three bf16 numbers that add up to them (2^-27 of a factor is left out, and what is below 2^-133) and the three
  * smallest products of those are left out (2^-26); up to 16 rows forward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
- * workspace: fp32 6 * (rows + 2 * hidden) * in + 1024 bytes (CDP_EINVAL if smaller), bf16 none (may be NULL).  Where it holds more, P times 8 * rows * hidden
- * bytes, products of few tiles share their reduction over up to P workgroups: faster, other roundings. */
+ * workspace: none needed (may be NULL).  Where there is one (16-byte aligned), of P times 8 * rows * hidden bytes, few tiles of long sums share their sums over up
+ * to P workgroups: faster, other roundings. */
 int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, size_t workspace_bytes,
                        int rows, int in, int hidden, void* stream);
 
 /* Its gradients from dh[rows][hidden], x, wg, wu, and g, u as the forward wrote them:  dg = dh * u * act'(g) and du = dh * act(g), which bf16 rounds to the
  * element type;  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
- * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 6 * (rows + 2 * hidden) * in + 12 * rows * hidden + 2048 (CDP_EINVAL if smaller), and as above where it holds
- * more: P times 4 * rows * in bytes for dx, P times 8 * hidden * in for dwg and dwu. */
+ * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 8 * rows * hidden + 1024 (CDP_EINVAL if smaller), and as above where it holds more: P times
+ * 8 * hidden * in bytes for dwg and dwu, then P times 4 * rows * in for dx. */
 int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
                                 void* dwg, void* dwu, void* workspace, size_t workspace_bytes, int rows, int in, int hidden, void* stream);
 
 /* y[rows][out] = act(z) + residual[rows][out], z = x w^T + bias[out], from x[rows][in], w[out][in]; bias and residual NULL: none.  Types, alignment, sizes, acts, exactness
  * as above.  z not NULL: written too, for the backward (which needs it unless act is 3).  y may be residual.
- * workspace: fp32 6 * (rows + out) * in + 1024 bytes (CDP_EINVAL if smaller), bf16 none; where it holds P times 4 * rows * out bytes more, as above. */
+ * workspace: none needed; where there is one of P times 4 * rows * out bytes, as above. */
 int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
                  size_t workspace_bytes, int rows, int in, int out, void* stream);
 
 /* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products;  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
- * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted), fp32 needs x and w for either product.  The gradient of the residual is dy.
- * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 6 * (rows + out) * in + 6 * rows * out + 4 * out * min(rows, 256) + 2048
- * (CDP_EINVAL if smaller), and as above where it holds more: P times 4 * rows * in bytes for dx, P times 4 * out * in for dw. */
+ * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted).  The gradient of the residual is dy.
+ * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 4 * rows * out + 4 * out * min(rows, 256) + 1024 (CDP_EINVAL if smaller), and as
+ * above where it holds more: P times 4 * out * in bytes for dw, then P times 4 * rows * in for dx. */
 int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
                           size_t workspace_bytes, int rows, int in, int out, void* stream);
 

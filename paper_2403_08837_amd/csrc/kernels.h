@@ -436,10 +436,10 @@ struct TokenLinear {
   int rows, in, out, act;
 };
 constexpr int LINEAR_MAX_WIDTH = 1 << 20, LINEAR_MAX_PARTS = 256;
-int64_t token_linear_workspace_bytes(bool backward, int rows, int in, int out, int dtype);
+int64_t token_linear_bwd_workspace_bytes(int rows, int out, int dtype);
 hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream);
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream);
-int64_t gated_linear_workspace_bytes(bool backward, int rows, int in, int hidden, int dtype);
+int64_t gated_linear_bwd_workspace_bytes(int rows, int hidden, int dtype);
 hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stream);
 hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream);
 struct TokenLogprob {

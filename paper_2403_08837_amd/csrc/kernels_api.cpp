@@ -347,8 +347,6 @@ int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const 
   if (!linear_sizes(dtype, act, rows, in, hidden) || !x || !wg || !wu || !h || !g != !u) return CDP_EINVAL;
   for (const void* p : {x, wg, wu, (const void*)h, (const void*)g, (const void*)u, (const void*)workspace})
     if (!aligned_to(p, 16)) return CDP_EINVAL;
-  const int64_t need = gated_linear_workspace_bytes(false, rows, in, hidden, dtype);
-  if (need && (!workspace || workspace_bytes < (size_t)need)) return CDP_EINVAL;
   GatedLinear a;
   memset(&a, 0, sizeof(a));
   a.x = x; a.wg = wg; a.wu = wu; a.h = h; a.g = g; a.u = u;
@@ -362,7 +360,7 @@ int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* w
   if (!linear_sizes(dtype, act, rows, in, hidden) || !x || !wg || !wu || !g || !u || !dh || !dwg != !dwu || (!dx && !dwg)) return CDP_EINVAL;
   for (const void* p : {x, wg, wu, g, u, dh, (const void*)dx, (const void*)dwg, (const void*)dwu, (const void*)workspace})
     if (!aligned_to(p, 16)) return CDP_EINVAL;
-  if (!workspace || workspace_bytes < (size_t)gated_linear_workspace_bytes(true, rows, in, hidden, dtype)) return CDP_EINVAL;
+  if (!workspace || workspace_bytes < (size_t)gated_linear_bwd_workspace_bytes(rows, hidden, dtype)) return CDP_EINVAL;
   GatedLinear a;
   memset(&a, 0, sizeof(a));
   a.x = x; a.wg = wg; a.wu = wu; a.g = const_cast<void*>(g); a.u = const_cast<void*>(u); a.dh = dh; a.dx = dx; a.dwg = dwg; a.dwu = dwu;
@@ -376,8 +374,6 @@ int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* b
   if (!linear_sizes(dtype, act, rows, in, out) || !x || !w || !y) return CDP_EINVAL;
   for (const void* p : {x, w, bias, residual, (const void*)y, (const void*)z, (const void*)workspace})
     if (!aligned_to(p, 16)) return CDP_EINVAL;
-  const int64_t need = token_linear_workspace_bytes(false, rows, in, out, dtype);
-  if (need && (!workspace || workspace_bytes < (size_t)need)) return CDP_EINVAL;
   TokenLinear a;
   memset(&a, 0, sizeof(a));
   a.x = x; a.w = w; a.bias = bias; a.residual = residual; a.y = y; a.z = z;
@@ -389,10 +385,10 @@ int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* b
 int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
                           size_t workspace_bytes, int rows, int in, int out, void* stream) {
   if (!linear_sizes(dtype, act, rows, in, out) || !dy || (!z && act != TOKEN_NONE) || (!dx && !dw && !dbias)) return CDP_EINVAL;
-  if ((dx && !w) || (dw && !x) || (dtype == DT_F32 && (dx || dw) && (!x || !w))) return CDP_EINVAL;
+  if ((dx && !w) || (dw && !x)) return CDP_EINVAL;
   for (const void* p : {x, w, z, dy, (const void*)dx, (const void*)dw, (const void*)dbias, (const void*)workspace})
     if (!aligned_to(p, 16)) return CDP_EINVAL;
-  if (!workspace || workspace_bytes < (size_t)token_linear_workspace_bytes(true, rows, in, out, dtype)) return CDP_EINVAL;
+  if (!workspace || workspace_bytes < (size_t)token_linear_bwd_workspace_bytes(rows, out, dtype)) return CDP_EINVAL;
   TokenLinear a;
   memset(&a, 0, sizeof(a));
   a.x = x; a.w = w; a.z = const_cast<void*>(z); a.dy = dy; a.dx = dx; a.dw = dw; a.dbias = dbias;

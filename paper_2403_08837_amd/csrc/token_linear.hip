@@ -8,8 +8,8 @@
 // index, read by the transposing LDS loads: nothing is transposed in memory.  Both lie swizzled, so that a fragment read meets every bank once.
 // Of a gated map a workgroup has as many columns of wg as of wu, dealt so that a wavefront holds both of the same columns, and the activation and the product
 // happen in registers; g and u (z) are written beside h (y) where the backward is to follow.
-//   fp32: an operand is cut into three bf16 planes (rounded: 2^-9, 2^-18 and 2^-27 of it are left), and the six products of planes of which more than 2^-26
-// comes are segments of one reduction.
+//   fp32 (exact_body): operands pass through registers, where each is cut into three bf16 planes (rounded: 2^-9, 2^-18 and 2^-27 of it are left), which lie in LDS as
+// the bf16 operands do; the six products of planes of which more than 2^-26 comes are added up, the smallest first.
 //   few tiles: the reduction is shared by `splits` workgroups, whose sums (fp32, in the workspace) are joined in order.
 // Forward of up to 16 rows (single tokens): bound by reading the weights once (token_few_kernel).
 #include "elem.h"
@@ -17,6 +17,7 @@
 #include "kernels.h"
 
 #include <algorithm>
+#include <climits>
 #include <cstring>
 
 namespace cdp {
@@ -77,122 +78,64 @@ template <typename T, int N> __device__ __forceinline__ void act_all(int act, fl
 }
 
 // ---- elementwise passes -----------------------------------------------------------------------------------------------
-// Three bf16 planes of a float.
-__device__ __forceinline__ void planes_of(float v, uint16_t (&p)[3]) {
-  uint16_t h = f32_to_bf16(v);
-  if ((h & 0x7fff) == 0x7f80 && fabsf(v) <= 3.402823466e38f) --h;  // rounded up to infinity
-  p[0] = h;
-  v -= bf16_to_f32(h);
-  p[1] = f32_to_bf16(v);
-  v -= bf16_to_f32(p[1]);
-  p[2] = f32_to_bf16(v);
-}
-// Planes of up to three tensors, each [3][n]; n a multiple of 8.
-struct Cut {
-  const float* from[3];
-  uint16_t* to[3];
-  int64_t n[3];
-  int64_t first[4];  // 8-element pieces of the tensors before
-};
-__global__ __launch_bounds__(256) void token_cut_kernel(const Cut c) {
-  const int64_t piece = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (piece >= c.first[3]) return;
-  const int t = (piece >= c.first[1]) + (piece >= c.first[2]);
-  const int64_t i = (piece - c.first[t]) * 8;
-  Chunk16<float> q[2];
-  q[0].v = *reinterpret_cast<const uint4*>(c.from[t] + i);
-  q[1].v = *reinterpret_cast<const uint4*>(c.from[t] + i + 4);
-  Chunk16<uint16_t> o[3];
+// Eight neighbours.
+template <typename T> struct Eight {
+  static constexpr int V = Elem<T>::VEC, Q = 8 / V;
+  Chunk16<T> q[Q];
+  __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    uint16_t p[3];
-    planes_of(q[e / 4].e[e % 4], p);
-#pragma unroll
-    for (int k = 0; k < 3; ++k) o[k].e[e] = p[k];
+    for (int k = 0; k < Q; ++k) q[k].v = *reinterpret_cast<const uint4*>(p + k * V);
   }
+  __device__ __forceinline__ void store(T* p) const {
 #pragma unroll
-  for (int k = 0; k < 3; ++k) *reinterpret_cast<uint4*>(c.to[t] + k * c.n[t] + i) = o[k].v;
-}
-// dg and du from g, u and dh.  bf16: rounded, as the operands of the products that follow; fp32: as planes.
-template <typename T>
-__global__ __launch_bounds__(256) void gated_grad_kernel(const T* g, const T* u, const T* dh, uint16_t* dg, uint16_t* du, int64_t n, int act) {
+    for (int k = 0; k < Q; ++k) *reinterpret_cast<uint4*>(p + k * V) = q[k].v;
+  }
+  __device__ __forceinline__ float operator[](int e) const { return Elem<T>::to_f32(q[e / V].e[e % V]); }
+  __device__ __forceinline__ void set(int e, float v) { q[e / V].e[e % V] = Elem<T>::from_f32(v); }
+};
+// dg and du from g, u and dh; bf16: rounded, as the operands of the products that follow.
+template <typename T> __global__ __launch_bounds__(256) void gated_grad_kernel(const T* g, const T* u, const T* dh, T* dg, T* du, int64_t n, int act) {
   const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (i >= n) return;
-  constexpr int Q = 8 / Elem<T>::VEC;
-  Chunk16<T> a[Q], b[Q], d[Q];
-#pragma unroll
-  for (int q = 0; q < Q; ++q) {
-    a[q].v = *reinterpret_cast<const uint4*>(g + i + q * Elem<T>::VEC);
-    b[q].v = *reinterpret_cast<const uint4*>(u + i + q * Elem<T>::VEC);
-    d[q].v = *reinterpret_cast<const uint4*>(dh + i + q * Elem<T>::VEC);
-  }
-  Chunk16<uint16_t> og[sizeof(T) == 2 ? 1 : 3], ou[sizeof(T) == 2 ? 1 : 3];
+  Eight<T> a, b, d;
+  a.load(g + i);
+  b.load(u + i);
+  d.load(dh + i);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    constexpr int V = Elem<T>::VEC;
-    const float gv = Elem<T>::to_f32(a[e / V].e[e % V]), uv = Elem<T>::to_f32(b[e / V].e[e % V]), dv = Elem<T>::to_f32(d[e / V].e[e % V]);
     float f, df;
-    act_both<T>(act, gv, f, df);
-    const float x = dv * uv * df, y = dv * f;
-    if constexpr (sizeof(T) == 2) {
-      og[0].e[e] = f32_to_bf16(x);
-      ou[0].e[e] = f32_to_bf16(y);
-    } else {
-      uint16_t p[3];
-      planes_of(x, p);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) og[k].e[e] = p[k];
-      planes_of(y, p);
-#pragma unroll
-      for (int k = 0; k < 3; ++k) ou[k].e[e] = p[k];
-    }
+    act_both<T>(act, a[e], f, df);
+    const float x = d[e] * b[e] * df, y = d[e] * f;
+    a.set(e, x);
+    b.set(e, y);
   }
-#pragma unroll
-  for (int k = 0; k < (sizeof(T) == 2 ? 1 : 3); ++k) {
-    *reinterpret_cast<uint4*>(dg + k * n + i) = og[k].v;
-    *reinterpret_cast<uint4*>(du + k * n + i) = ou[k].v;
-  }
+  a.store(dg + i);
+  b.store(du + i);
 }
-
-// dz from dy and z (act none: dy; dz null then in bf16), and its column sums: 256 columns of the rows blockIdx.y * share .. a workgroup, whose sums of dz as it
+// dz from dy and z (null: not wanted, or it is dy), and its column sums: 256 columns of the rows blockIdx.y * share .. a workgroup, whose sums of dz as it
 // is before it is rounded go to part[blockIdx.y][out] (null: not wanted), or, where there is one part, to dbias.
 template <typename T>
-__global__ __launch_bounds__(256) void linear_grad_kernel(const T* z, const T* dy, uint16_t* dz, float* part, T* dbias, int rows, int out, int share, int act) {
-  constexpr int V = Elem<T>::VEC, Q = 8 / V;
+__global__ __launch_bounds__(256) void linear_grad_kernel(const T* z, const T* dy, T* dz, float* part, T* dbias, int rows, int out, int share, int act) {
   __shared__ float sums[8][256 + 8];
   const int lane = threadIdx.x & 31, strip = threadIdx.x >> 5, col = (blockIdx.x * 32 + lane) * 8;
   const int row0 = blockIdx.y * share, row1 = min(row0 + share, rows);
-  const int64_t n = (int64_t)rows * out;
   float s[8] = {};
   if (col < out)
-#pragma unroll 2
+#pragma unroll 4
     for (int r = row0 + strip; r < row1; r += 8) {
       const int64_t i = (int64_t)r * out + col;
-      Chunk16<T> a[Q], d[Q];
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        d[q].v = *reinterpret_cast<const uint4*>(dy + i + q * V);
-        a[q].v = act == TOKEN_NONE ? d[q].v : *reinterpret_cast<const uint4*>(z + i + q * V);
-      }
-      Chunk16<uint16_t> o[sizeof(T) == 2 ? 1 : 3];
+      Eight<T> a, d;
+      d.load(dy + i);
+      if (act != TOKEN_NONE) a.load(z + i);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        float f, df, v = Elem<T>::to_f32(d[e / V].e[e % V]);
-        act_both<T>(act, Elem<T>::to_f32(a[e / V].e[e % V]), f, df);
-        v *= df;
+        float f, df = 1.f;
+        if (act != TOKEN_NONE) act_both<T>(act, a[e], f, df);
+        const float v = d[e] * df;
         s[e] += v;
-        if constexpr (sizeof(T) == 2) {
-          o[0].e[e] = f32_to_bf16(v);
-        } else {
-          uint16_t p[3];
-          planes_of(v, p);
-#pragma unroll
-          for (int k = 0; k < 3; ++k) o[k].e[e] = p[k];
-        }
+        d.set(e, v);
       }
-      if (dz)
-#pragma unroll
-        for (int k = 0; k < (sizeof(T) == 2 ? 1 : 3); ++k) *reinterpret_cast<uint4*>(dz + k * n + i) = o[k].v;
+      if (dz) d.store(dz + i);
     }
   if (!part && !dbias) return;
 #pragma unroll
@@ -206,29 +149,35 @@ __global__ __launch_bounds__(256) void linear_grad_kernel(const T* z, const T* d
   if (dbias) dbias[at] = Elem<T>::from_f32(v);
   else part[(int64_t)blockIdx.y * out + at] = v;
 }
-// 8 columns a workgroup, 32 lanes share the parts of a column.
-template <typename T> __global__ __launch_bounds__(256) void linear_bias_kernel(const float* part, T* dbias, int parts, int out) {
-  __shared__ float shares[32][8];
-  const int c = threadIdx.x & 7, share = threadIdx.x >> 3, col = blockIdx.x * 8 + c;
+// Sums of the parts of dbias: THREADS / 32 columns a workgroup, 32 lanes share the parts of a column.
+struct BiasParts {
+  const float* part;
+  void* dbias;
+  int parts, out;
+};
+template <typename T, int THREADS> __device__ __forceinline__ void bias_body(const BiasParts& a, int block, unsigned char* smem) {
+  constexpr int C = THREADS / 32;
+  float* const shares = reinterpret_cast<float*>(smem);
+  const int c = threadIdx.x % C, share = threadIdx.x / C, col = block * C + c;
   float s = 0.f;
+  if (col < a.out)
 #pragma unroll 8
-  for (int k = share; k < parts; k += 32) s += part[(int64_t)k * out + col];
-  shares[share][c] = s;
+    for (int k = share; k < a.parts; k += 32) s += a.part[(int64_t)k * a.out + col];
+  shares[share * C + c] = s;
   __syncthreads();
-  if (share) return;
+  if (share || col >= a.out) return;
   s = 0.f;
 #pragma unroll
-  for (int k = 0; k < 32; ++k) s += shares[k][c];
-  dbias[col] = Elem<T>::from_f32(s);
+  for (int k = 0; k < 32; ++k) s += shares[k * C + c];
+  static_cast<T*>(a.dbias)[col] = Elem<T>::from_f32(s);
 }
 
 // ---- the products -----------------------------------------------------------------------------------------------------
-constexpr int MAX_SEGMENTS = 12;
-// out[M][N] = sum over segments of A_s B_s, each over K.  A_s[m][k] at A[m * lda + k] (or A[k * lda + m]), B_s[n][k] likewise.
-// GATED: the columns of B come from two matrices, B and B2, and the results are h (and g, u).  LINEAR: y (and z).  WGRAD with pair: two such products (dwg, dwu),
-// the second of A2.
+// out[M][N] = sum over segments of A_s B_s, each over K.  A_s[m][k] at A[m * lda + k] (WGRAD: A[k * lda + m]), B_s[n][k] likewise (DGRAD, WGRAD: B[k * ldb + n]).
+// GATED: the columns of B come from two matrices, B and `other`, and the results are h (and g, u).  LINEAR: y (and z).  WGRAD with pair: two such products (dwg,
+// dwu), the second of `other` for A.
 struct Product {
-  const uint16_t *A[MAX_SEGMENTS], *B[MAX_SEGMENTS], *other[MAX_SEGMENTS / 2];  // other: B2 (GATED) or A2 (pair)
+  const void *A[2], *B[2], *other;
   int segments, K, M, N, lda, ldb;
   int tiles_m, tiles_n, tiles;  // of one product; of all
   int splits, slabs_per;        // parts of the reduction, slabs of each
@@ -236,6 +185,7 @@ struct Product {
   const void *bias, *residual;  // LINEAR: or null
   float* part;                  // splits > 1: sums [splits][results of all][M][N]
   int act, pair;
+  int workgroups() const { return tiles * splits; }
 };
 enum { GATED, LINEAR, DGRAD, WGRAD };
 
@@ -245,9 +195,10 @@ template <int TILE, int NWAVE, int BK, bool SLOW> struct Slabs {
   static constexpr int BYTES = TILE * BK * 2, LP = BYTES / 1024 / NWAVE;                    // loads of a wavefront per slab
   static_assert(LP * 1024 * NWAVE == BYTES && CPR <= 64 && TILE >= 64, "tile rows are dealt to the wavefronts in 1 KB blocks");
   unsigned off[LP];  // byte offsets from the tile's first element in this slab, ~0: outside
-  int chunk[2];      // !SLOW: first reduction index, in the slab, of the chunk of even and odd loads
+  static constexpr int KINDS = BK == 64 ? 2 : 4;
+  int chunk[KINDS];  // !SLOW: first reduction index, in the slab, of the chunk of load i: the same for loads KINDS apart
   // chunk c of tile row r sits in slot c ^ swz(r)
-  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : (r >> 1) & 7; }
+  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : BK == 64 ? (r >> 1) & 7 : r & 15; }
   static __device__ __forceinline__ int piece(int r) { return TILE >= 128 ? r & 3 : (r >> 1) & 1; }  // SLOW: 64-byte pieces of four rows on banks of their own
   // row_of: tile row -> row of the matrix, from the tile's first; `first` of `size` rows (SLOW: columns)
   template <typename F> __device__ __forceinline__ void start(int wave, int lane, int first, int size, int ld, F&& row_of) {
@@ -256,12 +207,12 @@ template <int TILE, int NWAVE, int BK, bool SLOW> struct Slabs {
       const int r = (wave * LP + i) * RPB + lane / CPR, c = (lane % CPR) ^ swz(r);
       if (SLOW) off[i] = first + c * 8 < size ? 2u * ((unsigned)r * (unsigned)ld + c * 8) : ~0u;
       else off[i] = 2u * ((unsigned)min(row_of(r), size - 1 - first) * (unsigned)ld + c * 8);  // rows past the last repeat it
-      if (!SLOW && i < 2) chunk[i] = c * 8;
+      if (!SLOW && i < KINDS) chunk[i] = c * 8;
     }
-    static_assert(SLOW || (BK == 64 && LP % 2 == 0), "loads two apart have the same chunks");
+    static_assert(SLOW || ((BK == 64 || BK == 128) && LP % KINDS == 0), "rows of a load and of the one KINDS on swizzle alike");
   }
   // `left` reduction indices in the slab: what is past them reads as zero.  SLOW: they are rows, and the buffer ends there.
-  __device__ __forceinline__ unsigned place(int i, int left) const { return SLOW || chunk[i & 1] < left ? off[i] : ~0u; }
+  __device__ __forceinline__ unsigned place(int i, int left) const { return SLOW || chunk[i & (KINDS - 1)] < left ? off[i] : ~0u; }
   static __device__ __forceinline__ unsigned records(int left, int ld) { return SLOW ? 2u * (unsigned)left * (unsigned)ld : left > 0 ? 0xfffffff0u : 0u; }
 };
 __device__ __forceinline__ void load_lds(unsigned lds, unsigned off, const void* base, unsigned records) {
@@ -331,49 +282,117 @@ template <typename T> __device__ __forceinline__ void add_block(const T* from, i
   }
 }
 
-template <int WHAT, typename T, int BM, int BN, int WAVES_M, int WAVES_N, int BK, int STAGES, int WPS>
-__global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_kernel(const Product P) {
+// What a workgroup makes of a product: its tile, its part of the reduction.
+template <int WHAT, int BM, int BN, int BK> struct Share {
+  int row0, col0, split, todo;  // slabs of BK to do
+  bool second;                  // of a pair
+  int seg, slab, per_segment;   // the first of them
+  __device__ __forceinline__ Share(const Product& P, int block) {
+    constexpr int COLS = WHAT == GATED ? BN / 2 : BN;
+    split = block / P.tiles;
+    // tiles in panels of eight columns, row by row inside a panel; 32 neighbours in that order go to one XCD
+    int tile = xcd_block_cyclic(block - split * P.tiles, P.tiles, 32);
+    const int one = P.tiles_m * P.tiles_n;
+    second = WHAT == WGRAD && tile >= one;
+    if (second) tile -= one;
+    const int panel = tile / (P.tiles_m * 8), in = tile - panel * P.tiles_m * 8, pw = min(8, P.tiles_n - panel * 8), tm = in / pw;
+    row0 = tm * BM;
+    col0 = (panel * 8 + in - tm * pw) * COLS;
+    per_segment = (int)(((unsigned)P.K + BK - 1) / BK);
+    const int first = split * P.slabs_per;
+    todo = min(P.slabs_per, per_segment * P.segments - first);
+    seg = first / per_segment;
+    slab = first - seg * per_segment;
+  }
+};
+// A barrier for what is in LDS: loads into registers stay on their way (__syncthreads waits for them).
+__device__ __forceinline__ void lds_barrier() {
+  wait_newest<63>();
+  slab_barrier();
+}
+// From the accumulators: block (i, j) of a wavefront, transposed (a lane has neighbouring columns of one row), of rows m0 + 32 i and columns n0 + 32 j; GATED: the
+// columns n0 + 16 j of both, at j and j + 1.
+template <int WHAT, typename T, int MI, int NI>
+__device__ __forceinline__ void leave(const Product& P, const v16f_t (&acc)[MI][NI], int m0, int n0, int split, bool second, int lane) {
+  constexpr bool DUAL = WHAT == GATED;
+  const int l31 = lane & 31, hi = lane >> 5;
+  const int64_t MN = (int64_t)P.M * P.N;
+  float* const part = P.part + (int64_t)split * (DUAL || P.pair ? 2 : 1) * MN;
+#pragma unroll
+  for (int i = 0; i < MI; ++i) {
+    const int64_t m = m0 + i * 32 + l31;
+#pragma unroll
+    for (int j = 0; j < NI; j += DUAL ? 2 : 1) {
+      const int n = n0 + j * (DUAL ? 16 : 32);
+      float v[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) v[k] = acc[i][j][k];
+      if (P.splits > 1) {
+        store_block(part + (second ? MN : 0), m, n, P.M, P.N, hi, v);
+        if constexpr (DUAL) {
+#pragma unroll
+          for (int k = 0; k < 16; ++k) v[k] = acc[i][j + 1][k];
+          store_block(part + MN, m, n, P.M, P.N, hi, v);
+        }
+      } else if constexpr (DUAL) {
+        if (P.out2) {
+          float u[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) u[k] = acc[i][j + 1][k];
+          store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
+          store_block(static_cast<T*>(P.out3), m, n, P.M, P.N, hi, u);
+        }
+        act_all<T>(P.act, v);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] *= acc[i][j + 1][k];
+        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
+      } else if constexpr (WHAT == LINEAR) {
+        if (P.bias) add_block(static_cast<const T*>(P.bias), 0, n, 1, P.N, hi, v);
+        if (P.out2) store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
+        act_all<T>(P.act, v);
+        if (P.residual) add_block(static_cast<const T*>(P.residual), m, n, P.M, P.N, hi, v);
+        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
+      } else {
+        store_block(static_cast<T*>(second ? P.out2 : P.out), m, n, P.M, P.N, hi, v);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // one block's values and addresses at a time
+    }
+  }
+}
+
+template <int WHAT, typename T, int BM, int BN, int WAVES_M, int WAVES_N, int BK, int STAGES>
+__device__ __forceinline__ void product_body(const Product& P, int block, unsigned char* smem) {
   constexpr int NWAVE = WAVES_M * WAVES_N, WTM = BM / WAVES_M, WTN = BN / WAVES_N, MI = WTM / 32, NI = WTN / 32, KK = BK / 16;
   constexpr bool DUAL = WHAT == GATED, ASLOW = WHAT == WGRAD, BSLOW = WHAT == DGRAD || WHAT == WGRAD;
   using SA = Slabs<BM, NWAVE, BK, ASLOW>;
   using SB = Slabs<BN, NWAVE, BK, BSLOW>;
-  constexpr int STAGE_BYTES = SA::BYTES + SB::BYTES, LP = SA::LP + SB::LP, COLS = DUAL ? BN / 2 : BN;
+  constexpr int STAGE_BYTES = SA::BYTES + SB::BYTES, LP = SA::LP + SB::LP;
   static_assert(!DUAL || NI % 2 == 0, "a wavefront has both of its columns");
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[STAGES * STAGE_BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WAVES_N, wn = wave % WAVES_N;
   const unsigned lds = (unsigned)(uintptr_t)(lds_ptr)smem;
-  // tiles in panels of eight columns, row by row inside a panel; 32 neighbours in that order go to one XCD
-  const int split = blockIdx.x / (unsigned)P.tiles;
-  int tile = xcd_block_cyclic((int)(blockIdx.x - (unsigned)split * P.tiles), P.tiles, 32);
-  const int one = P.tiles_m * P.tiles_n, second = WHAT == WGRAD && tile >= one;  // (of a pair)
-  if (second) tile -= one;
-  const int panel = tile / (P.tiles_m * 8), in = tile - panel * P.tiles_m * 8, pw = min(8, P.tiles_n - panel * 8), tm = in / pw;
-  const int row0 = tm * BM, col0 = (panel * 8 + in - tm * pw) * COLS;
-
-  // the slabs of this workgroup: `todo` from slab `split * slabs_per` of segment, slab order
-  const int per_segment = (P.K + BK - 1) / BK, total = per_segment * P.segments;
-  const int first_slab = split * P.slabs_per, todo = min(P.slabs_per, total - first_slab);
+  const Share<WHAT, BM, BN, BK> at(P, block);
+  const int row0 = at.row0, col0 = at.col0, per_segment = at.per_segment;
   SA sa;
   SB sb;
   const char *pa, *pb, *pb2;
-  int seg = first_slab / per_segment, slab = first_slab - seg * per_segment, left = todo;
+  int seg = at.seg, slab = at.slab, left = at.todo;
   int in_slab = min(BK, P.K - slab * BK);  // reduction indices in the next slab; 0 behind the last, and the loads that the counted waits expect read nothing
   auto b_row = [](int r) { return DUAL ? (r >> 6) * 32 + (r & 31) : r; };  // DUAL: 32 columns of B, 32 of B2, ..
   auto bases = [&] {
-    const uint16_t* const a = (WHAT == WGRAD && second ? P.other[seg] : P.A[seg]);
+    const uint16_t* const a = static_cast<const uint16_t*>(at.second ? P.other : P.A[seg]);
     pa = reinterpret_cast<const char*>(ASLOW ? a + (int64_t)slab * BK * P.lda + row0 : a + (int64_t)row0 * P.lda + slab * BK);
-    const uint16_t* const b = P.B[seg];
+    const uint16_t* const b = static_cast<const uint16_t*>(P.B[seg]);
     pb = reinterpret_cast<const char*>(BSLOW ? b + (int64_t)slab * BK * P.ldb + col0 : b + (int64_t)col0 * P.ldb + slab * BK);
-    if (DUAL) pb2 = reinterpret_cast<const char*>(P.other[seg] + (int64_t)col0 * P.ldb + slab * BK);
+    if (DUAL) pb2 = reinterpret_cast<const char*>(static_cast<const uint16_t*>(P.other) + (int64_t)col0 * P.ldb + slab * BK);
   };
   bases();
   sa.start(wave, lane, row0, P.M, P.lda, [](int r) { return r; });
   sb.start(wave, lane, col0, P.N, P.ldb, b_row);
-  auto issue = [&](unsigned at, int e) {
-    if (e < SA::LP) return load_lds(at + (wave * SA::LP + e) * 1024, sa.place(e, in_slab), pa, SA::records(in_slab, P.lda));
+  auto issue = [&](unsigned to, int e) {
+    if (e < SA::LP) return load_lds(to + (wave * SA::LP + e) * 1024, sa.place(e, in_slab), pa, SA::records(in_slab, P.lda));
     const int i = e - SA::LP;
     const bool two = DUAL && (((wave * SB::LP + i) * SB::RPB >> 5) & 1);
-    load_lds(at + SA::BYTES + (wave * SB::LP + i) * 1024, sb.place(i, in_slab), two ? pb2 : pb, SB::records(in_slab, P.ldb));
+    load_lds(to + SA::BYTES + (wave * SB::LP + i) * 1024, sb.place(i, in_slab), two ? pb2 : pb, SB::records(in_slab, P.ldb));
   };
   auto advance = [&] {
     if (--left <= 0) {
@@ -423,10 +442,10 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
     xb[0] = SA::BYTES + (wn * WTN + l31) * SB::ROW;
   }
   uint4 fa[2][MI], fb[2][NI];
-  auto slow = [&](unsigned at, int row_bytes) {
+  auto slow = [&](unsigned from, int row_bytes) {
     union { v4s h[2]; uint4 u; } r;
-    r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(smem + at));
-    r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(smem + at + 4 * row_bytes));
+    r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(smem + from));
+    r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(smem + from + 4 * row_bytes));
     return r.u;
   };
   auto frag = [&](int q, int kk, int buf, int e) {
@@ -468,64 +487,203 @@ __global__ __launch_bounds__(WAVES_M * WAVES_N * 64, WPS) void token_product_ker
     }
     advance();
   };
-  // whole rounds of the stages: slabs past the last are zeros, and one way out of the loop leaves the accumulators where they are
-  for (int t = todo; t > 0; t -= STAGES) {
+  // Large tiles: whole rounds of the stages, slabs past the last are zeros; one way out of the loop leaves the accumulators where they are (with a way out
+  // behind every step they are copied, and spilled: 8192 x 4096 x 4096 1080 us instead of 216).
+  constexpr bool ROUNDS = MI * NI > 2;
+  for (int t = at.todo; t > 0; t -= STAGES) {
     step(std::integral_constant<int, 0>{});
+    if (!ROUNDS && t == 1) break;
     step(std::integral_constant<int, 1>{});
-    if constexpr (STAGES > 2) step(std::integral_constant<int, 2>{});
-    if constexpr (STAGES > 3) step(std::integral_constant<int, 3>{});
-  }
-  wait_newest<0>();  // no load is left that writes LDS when this workgroup gives it back
-  const int64_t MN = (int64_t)P.M * P.N;
-  float* const part = P.part + (int64_t)split * (DUAL || P.pair ? 2 : 1) * MN;
-#pragma unroll
-  for (int i = 0; i < MI; ++i) {
-    const int64_t m = row0 + wm * WTM + i * 32 + l31;
-#pragma unroll
-    for (int j = 0; j < NI; j += DUAL ? 2 : 1) {
-      const int n = DUAL ? col0 + (wn * NI + j) / 2 * 32 : col0 + wn * WTN + j * 32;
-      float v[16];
-#pragma unroll
-      for (int k = 0; k < 16; ++k) v[k] = acc[i][j][k];
-      if (P.splits > 1) {
-        store_block(part + (second ? MN : 0), m, n, P.M, P.N, hi, v);
-        if constexpr (DUAL) {
-#pragma unroll
-          for (int k = 0; k < 16; ++k) v[k] = acc[i][j + 1][k];
-          store_block(part + MN, m, n, P.M, P.N, hi, v);
-        }
-      } else if constexpr (DUAL) {
-        if (P.out2) {
-          float u[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) u[k] = acc[i][j + 1][k];
-          store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
-          store_block(static_cast<T*>(P.out3), m, n, P.M, P.N, hi, u);
-        }
-        act_all<T>(P.act, v);
-#pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] *= acc[i][j + 1][k];
-        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
-      } else if constexpr (WHAT == LINEAR) {
-        if (P.bias) add_block(static_cast<const T*>(P.bias), 0, n, 1, P.N, hi, v);
-        if (P.out2) store_block(static_cast<T*>(P.out2), m, n, P.M, P.N, hi, v);
-        act_all<T>(P.act, v);
-        if (P.residual) add_block(static_cast<const T*>(P.residual), m, n, P.M, P.N, hi, v);
-        store_block(static_cast<T*>(P.out), m, n, P.M, P.N, hi, v);
-      } else {
-        store_block(static_cast<T*>(second ? P.out2 : P.out), m, n, P.M, P.N, hi, v);
-      }
-      __builtin_amdgcn_sched_barrier(0);  // one block's values and addresses at a time
+    if constexpr (STAGES > 2) {
+      if (!ROUNDS && t == 2) break;
+      step(std::integral_constant<int, 2>{});
     }
   }
+  wait_newest<0>();  // no load is left that writes LDS when this workgroup gives it back
+  leave<WHAT, T>(P, acc, at.row0 + wm * WTM, at.col0 + wn * (DUAL ? WTN / 2 : WTN), at.split, at.second, lane);
+}
+// ---- fp32 -------------------------------------------------------------------------------------------------------------
+// An fp32 operand's slab of 32 on its way into three planes of bf16 in LDS.  Loads are in flight while the slab before is contracted.
+template <int TILE, bool SLOW> struct Planes {
+  static constexpr int BK = 32, LP = TILE * BK / 4 / 256, PER_ROW = SLOW ? TILE / 4 : BK / 4;  // 16-byte loads of a thread; of a tile row
+  static constexpr int ROW = SLOW ? TILE * 2 : BK * 2, BYTES = TILE * BK * 2;                    // of a plane
+  unsigned off[LP];
+  int k0;  // !SLOW: first reduction index, in the slab, of every load
+  struct Held { uint4 v[LP]; };
+  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : (r >> 2) & 3; }
+  static __device__ __forceinline__ int piece(int r) { return TILE >= 128 ? r & 3 : (r >> 1) & 1; }
+  template <typename F> __device__ __forceinline__ void start(int first, int size, int ld, F&& row_of) {
+#pragma unroll
+    for (int i = 0; i < LP; ++i) {
+      const int id = i * 256 + threadIdx.x, r = id / PER_ROW, c = id % PER_ROW;
+      if (SLOW) off[i] = first + c * 4 < size ? 4u * ((unsigned)r * (unsigned)ld + c * 4) : ~0u;
+      else off[i] = 4u * ((unsigned)min(row_of(r), size - 1 - first) * (unsigned)ld + c * 4);
+    }
+    k0 = threadIdx.x % PER_ROW * 4;
+  }
+  // `left` reduction indices in the slab, what is past them reads as zero; b2: for the odd groups of 32 tile rows, or null
+  __device__ __forceinline__ void load(Held& held, const char* base, const char* b2, int left, int ld) const {
+    typedef __attribute__((ext_vector_type(4))) unsigned v4u;
+#pragma unroll
+    for (int i = 0; i < LP; ++i) {
+      const bool two = b2 && ((i * 256 / PER_ROW + (int)__builtin_amdgcn_readfirstlane(threadIdx.x / PER_ROW)) >> 5 & 1);  // (uniform: a wavefront has 8 rows)
+      const __amdgpu_buffer_rsrc_t b = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(two ? b2 : base), 0, SLOW ? 4u * (unsigned)left * (unsigned)ld : 0xfffffff0u, 0x00020000);
+      held.v[i] = __builtin_bit_cast(uint4, (v4u)__builtin_amdgcn_raw_buffer_load_b128(b, SLOW || k0 < left ? off[i] : ~0u, 0, 0));
+    }
+  }
+  // A float is the sum of its planes to 2^-27 of it; the largest finite ones, which would round up to infinity, through the largest bf16.
+  __device__ __forceinline__ void cut(const Held& held, unsigned char* planes) const {
+    auto two = [](float a, float b) { return (unsigned)f32_to_bf16(a) | (unsigned)f32_to_bf16(b) << 16; };
+    auto low = [](unsigned p) { return __uint_as_float(p << 16); };
+    auto high = [](unsigned p) { return __uint_as_float(p & 0xffff0000u); };
+    constexpr float MOST = 3.3895313892515355e38f;
+#pragma unroll
+    for (int i = 0; i < LP; ++i) {
+      const int id = i * 256 + threadIdx.x, r = id / PER_ROW, c = id % PER_ROW;
+      unsigned char* const to = planes + r * ROW + (((c >> 1) ^ swz(r)) << 4) + (c & 1) * 8;
+      float v[4] = {__uint_as_float(held.v[i].x), __uint_as_float(held.v[i].y), __uint_as_float(held.v[i].z), __uint_as_float(held.v[i].w)};
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        uint2 w;
+        if (p == 0) w = make_uint2(two(__builtin_amdgcn_fmed3f(v[0], -MOST, MOST), __builtin_amdgcn_fmed3f(v[1], -MOST, MOST)),
+                                   two(__builtin_amdgcn_fmed3f(v[2], -MOST, MOST), __builtin_amdgcn_fmed3f(v[3], -MOST, MOST)));
+        else w = make_uint2(two(v[0], v[1]), two(v[2], v[3]));
+        *reinterpret_cast<uint2*>(to + p * BYTES) = w;
+        v[0] -= low(w.x);
+        v[1] -= high(w.x);
+        v[2] -= low(w.y);
+        v[3] -= high(w.y);
+      }
+    }
+  }
+};
+// AHEAD slabs are on their way in registers; BUFFERS of planes.
+template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int AHEAD, int BUFFERS>
+__device__ __forceinline__ void exact_body(const Product& P, int block, unsigned char* smem) {
+  constexpr int BK = 32, WTM = BM / WAVES_M, WTN = BN / WAVES_N, MI = WTM / 32, NI = WTN / 32;
+  constexpr bool DUAL = WHAT == GATED, ASLOW = WHAT == WGRAD, BSLOW = WHAT == DGRAD || WHAT == WGRAD;
+  using PA = Planes<BM, ASLOW>;
+  using PB = Planes<BN, BSLOW>;
+  static_assert(WAVES_M * WAVES_N == 4 && (!DUAL || NI % 2 == 0), "");
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WAVES_N, wn = wave % WAVES_N;
+  const Share<WHAT, BM, BN, BK> at(P, block);
+  constexpr int BUFFER = 3 * (PA::BYTES + PB::BYTES);
+  PA sa;
+  PB sb;
+  sa.start(at.row0, P.M, P.lda, [](int r) { return r; });
+  sb.start(at.col0, P.N, P.ldb, [](int r) { return DUAL ? (r >> 6) * 32 + (r & 31) : r; });
+  int seg = at.seg, slab = at.slab, left_to_ask = at.todo;
+  typename PA::Held ha[AHEAD];
+  typename PB::Held hb[AHEAD];
+  auto request = [&](auto w) {
+    if (left_to_ask-- <= 0) return;
+    constexpr int h = decltype(w)::value;
+    const float* const a = static_cast<const float*>(at.second ? P.other : P.A[seg]);
+    const float* const b = static_cast<const float*>(P.B[seg]);
+    const int left = min(BK, P.K - slab * BK);
+    sa.load(ha[h], reinterpret_cast<const char*>(ASLOW ? a + (int64_t)slab * BK * P.lda + at.row0 : a + (int64_t)at.row0 * P.lda + slab * BK), nullptr, left, P.lda);
+    sb.load(hb[h], reinterpret_cast<const char*>(BSLOW ? b + (int64_t)slab * BK * P.ldb + at.col0 : b + (int64_t)at.col0 * P.ldb + slab * BK),
+            DUAL ? reinterpret_cast<const char*>(static_cast<const float*>(P.other) + (int64_t)at.col0 * P.ldb + slab * BK) : nullptr, left, P.ldb);
+    if (++slab == at.per_segment) {
+      slab = 0;
+      ++seg;
+    }
+  };
+  static_for<AHEAD>(request);
+  v16f_t acc[MI][NI];
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int j = 0; j < NI; ++j)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[i][j][v] = 0.f;
+  const int l31 = lane & 31, hi = lane >> 5, rho = lane & 15;
+  auto fragment = [&](const unsigned char* plane, int block, int kk, auto side) {
+    using S = decltype(side);
+    if constexpr (S::ROW == 64) {
+      return *reinterpret_cast<const uint4*>(plane + (block * 32 + l31) * 64 + (((kk * 2 + hi) ^ S::swz(l31)) << 4));
+    } else {
+      const unsigned char* const q = plane + (kk * 16 + 8 * hi + (rho >> 2)) * S::ROW + (4 * (block ^ S::piece(rho >> 2)) + 2 * ((lane >> 4) & 1) + ((rho & 3) >> 1)) * 16 + 8 * (rho & 1);
+      union { v4s h[2]; uint4 u; } r;
+      r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(q));
+      r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s)(q + 4 * S::ROW));
+      return r.u;
+    }
+  };
+  auto contract = [&](const unsigned char* la) {
+    const unsigned char* const lb = la + 3 * PA::BYTES;
+#pragma unroll
+    for (int kk = 0; kk < BK / 16; ++kk) {
+      uint4 fa[3][MI], fb[3][NI];
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[p][i] = fragment(la + p * PA::BYTES, wm * MI + i, kk, PA{});
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fb[p][j] = fragment(lb + p * PB::BYTES, wn * NI + j, kk, PB{});
+      }
+      constexpr int OF_A[6] = {2, 0, 1, 1, 0, 0}, OF_B[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+      for (int s = 0; s < 6; ++s)
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = mfma_bf16(fb[OF_B[s]][j], fa[OF_A[s]][i], acc[i][j]);
+    }
+  };
+  static_assert(AHEAD % BUFFERS == 0, "");
+  for (int t = at.todo; t > 0; t -= AHEAD) {
+    static_for<AHEAD>([&](auto w) {
+      constexpr int h = decltype(w)::value;
+      if (h > 0 && t <= h) return;
+      unsigned char* const la = smem + h % BUFFERS * BUFFER;
+      if (BUFFERS == 1) lds_barrier();  // the slab before has been read (of two buffers: the barrier behind the cut since then)
+      sa.cut(ha[h], la);
+      sb.cut(hb[h], la + 3 * PA::BYTES);
+      request(w);
+      lds_barrier();
+      contract(la);
+    });
+  }
+  leave<WHAT, float>(P, acc, at.row0 + wm * WTM, at.col0 + wn * (DUAL ? WTN / 2 : WTN), at.split, at.second, lane);
+}
+
+// ---- kernels ----------------------------------------------------------------------------------------------------------
+// Tiles by size: 0 64 x 64 in slabs of 128, 1 64 x 128, 2 128 x 128, all with two workgroups a CU, 3 256 x 256, one a CU.  A gated map's wavefronts have 64 columns or more.
+template <int WHAT, typename T, int SIZE> struct Tile {
+  static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED;
+  static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 || (SIZE == 0 && EXACT && DUAL) ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
+  static constexpr int WAVES_M = SIZE == 0 && EXACT && DUAL ? 4 : 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
+  static constexpr int BK = EXACT ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 1 ? 3 : 2;
+  static constexpr int AHEAD = SIZE < 2 ? 2 : 1, BUFFERS = AHEAD;  // EXACT
+  static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * BUFFERS : (BM + BN) * BK * 2 * STAGES;
+  static __device__ __forceinline__ void body(const Product& P, int block, unsigned char* smem) {
+    if constexpr (EXACT) exact_body<WHAT, BM, BN, WAVES_M, WAVES_N, AHEAD, BUFFERS>(P, block, smem);
+    else product_body<WHAT, T, BM, BN, WAVES_M, WAVES_N, BK, STAGES>(P, block, smem);
+  }
+};
+template <int WHAT, typename T, int SIZE>
+__global__ __launch_bounds__((Tile<WHAT, T, SIZE>::THREADS), (Tile<WHAT, T, SIZE>::THREADS) / 128 > 2 ? 2 : (Tile<WHAT, T, SIZE>::THREADS) / 128) void token_product_kernel(const Product P) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[Tile<WHAT, T, SIZE>::LDS];
+  Tile<WHAT, T, SIZE>::body(P, blockIdx.x, smem);
+}
+// Both products of a backward pass and the last sums of dbias, in the order dw, dx, dbias of workgroups (the first two of no tiles: not wanted).
+template <typename T, int SIZE>
+__global__ __launch_bounds__((Tile<WGRAD, T, SIZE>::THREADS), 2) void token_backward_kernel(const Product dw, const Product dx, const BiasParts bias) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[Tile<WGRAD, T, SIZE>::LDS];
+  const int weights = dw.tiles * dw.splits, all = weights + dx.tiles * dx.splits, block = blockIdx.x;
+  if (block < weights) Tile<WGRAD, T, SIZE>::body(dw, block, smem);
+  else if (block < all) Tile<DGRAD, T, SIZE>::body(dx, block - weights, smem);
+  else bias_body<T, Tile<WGRAD, T, SIZE>::THREADS>(bias, block - all, smem);
 }
 // Joins the sums of a shared reduction: eight neighbours a thread.
-template <typename T> __global__ __launch_bounds__(256) void token_join_kernel(const Product P, int what) {
-  const int64_t MN = (int64_t)P.M * P.N, stride = (what == GATED || P.pair ? 2 : 1) * MN, i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+template <typename T> __device__ __forceinline__ void join_body(const Product& P, int what, int64_t block) {
+  const int64_t MN = (int64_t)P.M * P.N, stride = (what == GATED || P.pair ? 2 : 1) * MN, i = (block * 256 + threadIdx.x) * 8;
   if (i >= (what == GATED ? MN : stride)) return;
   auto sum = [&](int64_t at, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll 4
     for (int s = 0; s < P.splits; ++s) {
       Chunk16<float> q[2];
       q[0].v = *reinterpret_cast<const uint4*>(P.part + s * stride + at);
@@ -572,6 +730,12 @@ template <typename T> __global__ __launch_bounds__(256) void token_join_kernel(c
   } else {
     store(P.out2, i - MN, v);
   }
+}
+template <typename T> __global__ __launch_bounds__(256) void token_join_kernel(const Product P, int what) { join_body<T>(P, what, blockIdx.x); }
+// Workgroups dw_groups are those of dw.
+template <typename T> __global__ __launch_bounds__(256) void token_backward_join_kernel(const Product dw, const Product dx, int dw_groups) {
+  if ((int)blockIdx.x < dw_groups) join_body<T>(dw, WGRAD, blockIdx.x);
+  else join_body<T>(dx, DGRAD, blockIdx.x - dw_groups);
 }
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
@@ -665,57 +829,110 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
-template <int WHAT, typename T, int BM, int BN, int WAVES_M, int WAVES_N, int STAGES, int WPS> hipError_t launch_tiles(Product& p, int64_t room, hipStream_t stream) {
-  constexpr int BK = 64, COLS = WHAT == GATED ? BN / 2 : BN;
-  p.tiles_m = (p.M + BM - 1) / BM;
-  p.tiles_n = (p.N + COLS - 1) / COLS;
-  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * (p.pair ? 2 : 1), slabs = (int64_t)(p.K + BK - 1) / BK * p.segments;
-  if (!launchable(tiles, WAVES_M * WAVES_N * 64) || slabs > INT32_MAX) return hipErrorInvalidConfiguration;
+constexpr int SIZES = 4, SLAB_OF[SIZES] = {128, 64, 64, 64}, SLAB_OF_F32 = 32;
+// Tiles of a product by size; workgroups that run at once.
+int64_t tiles_of(const Product& p, int what, int size, bool f32) {
+  const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
+  return (((int64_t)p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * (p.pair ? 2 : 1);
+}
+int resident(int size) { return size == 3 ? 256 : 512; }
+// The smallest tiles that all run at once, else 128 x 128, or 256 x 256 where they are a CU's worth or more.
+template <int N> int size_for(const Product* const (&p)[N], const int (&what)[N], bool f32) {
+  auto all = [&](int size) {
+    int64_t n = 0;
+    for (int i = 0; i < N; ++i) n += p[i]->K ? tiles_of(*p[i], what[i], size, f32) : 0;
+    return n;
+  };
+  if (!f32 && all(3) >= 256) return 3;
+  for (int size = 0; size < 2; ++size)
+    if (all(size) <= resident(size)) return size;
+  return 2;
+}
+// Tiles and parts of a product; `slabs_each`: slabs that a workgroup should have at least.
+bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t room) {
+  const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
+  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size];
+  p.tiles_m = (int)(((int64_t)p.M + bm - 1) / bm);
+  p.tiles_n = (p.N + bn - 1) / bn;
+  const int64_t tiles = tiles_of(p, what, size, f32), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
+  if (!launchable(tiles, 512) || slabs > INT32_MAX) return false;
   p.tiles = (int)tiles;
-  // parts of at least 8 slabs while they all run at once
-  const int64_t resident = 256 * (BM * BN >= 256 * 256 ? 1 : 2), MN = (int64_t)p.M * p.N * (WHAT == GATED || p.pair ? 2 : 1);
-  int64_t splits = std::max<int64_t>(1, std::min({resident / tiles, slabs / 8, room / (4 * MN)}));
+  const int64_t splits = std::max<int64_t>(1, std::min(slabs / slabs_each, room / (4 * results)));
   p.slabs_per = (int)((slabs + splits - 1) / splits);
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
-  hipLaunchKernelGGL((token_product_kernel<WHAT, T, BM, BN, WAVES_M, WAVES_N, BK, STAGES, WPS>), dim3((unsigned)(tiles * p.splits)), dim3(WAVES_M * WAVES_N * 64), 0, stream, p);
-  const hipError_t e = hipGetLastError();
+  return launchable((int64_t)p.tiles * p.splits, 512);
+}
+// Slabs that a workgroup should have for all to run at once; not shared where that saves less than joining costs (4 us, about 1000 reduction indices).
+template <int N> int64_t slabs_each(const Product* const (&p)[N], const int (&what)[N], int size, bool f32) {
+  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size];
+  int64_t work = 0, most = 1;
+  for (int i = 0; i < N; ++i) {
+    if (!p[i]->K) continue;
+    const int64_t slabs = ((int64_t)p[i]->K + bk - 1) / bk * p[i]->segments;
+    work += tiles_of(*p[i], what[i], size, f32) * slabs;
+    most = std::max(most, slabs);
+  }
+  const int64_t each = std::max<int64_t>((work + resident(size) - 1) / resident(size), 512 / bk);
+  return (most - each) * bk < 1024 ? INT32_MAX : each;
+}
+int64_t join_groups(const Product& p, int what) {
+  return p.splits > 1 ? ((int64_t)p.M * p.N * (what != GATED && p.pair ? 2 : 1) / 8 + 255) / 256 : 0;
+}
+
+template <int WHAT, typename T, int SIZE> void start_product(const Product& p, hipStream_t stream) {
+  hipLaunchKernelGGL((token_product_kernel<WHAT, T, SIZE>), dim3(p.workgroups()), dim3(Tile<WHAT, T, SIZE>::THREADS), 0, stream, p);
+}
+// A forward product.
+template <int WHAT, typename T> hipError_t launch_forward(Product& p, int64_t room, hipStream_t stream) {
+  constexpr bool F32 = sizeof(T) == 4;
+  const Product* const all[1] = {&p};
+  const int what[1] = {WHAT}, size = size_for(all, what, F32);
+  if (!plan(p, WHAT, size, F32, slabs_each(all, what, size, F32), room)) return hipErrorInvalidConfiguration;
+  if (size == 0) start_product<WHAT, T, 0>(p, stream);
+  else if (size == 1) start_product<WHAT, T, 1>(p, stream);
+  else if (size == 2) start_product<WHAT, T, 2>(p, stream);
+  else if constexpr (!F32) start_product<WHAT, T, 3>(p, stream);
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  const dim3 grid((unsigned)(((WHAT == GATED ? MN / 2 : MN) / 8 + 255) / 256));
-  hipLaunchKernelGGL((token_join_kernel<T>), grid, dim3(256), 0, stream, p, (int)WHAT);
+  hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)join_groups(p, WHAT)), dim3(256), 0, stream, p, (int)WHAT);
   return hipGetLastError();
 }
-template <int WHAT, typename T> hipError_t launch_tiled(Product& p, int64_t room, hipStream_t stream) {
-  const int64_t cols = WHAT == GATED ? 2ll * p.N : p.N, pair = p.pair ? 2 : 1;
-  if (((p.M + 255) / 256) * ((cols + 255) / 256) * pair >= 256) return launch_tiles<WHAT, T, 256, 256, 2, 4, 2, 2>(p, room, stream);
-  if (p.M <= 64) return launch_tiles<WHAT, T, 64, 128, 2, 2, 3, 2>(p, room, stream);
-  return launch_tiles<WHAT, T, 128, 128, 2, 2, 2, 2>(p, room, stream);
+template <typename T, int SIZE> void start_backward(const Product& dw, const Product& dx, const BiasParts& bias, hipStream_t stream) {
+  constexpr int THREADS = Tile<WGRAD, T, SIZE>::THREADS, C = THREADS / 32;
+  const int groups = dw.workgroups() + dx.workgroups() + (bias.dbias ? (bias.out + C - 1) / C : 0);
+  hipLaunchKernelGGL((token_backward_kernel<T, SIZE>), dim3(groups), dim3(THREADS), 0, stream, dw, dx, bias);
 }
-
-template <int WHAT> hipError_t launch_product(Product& p, int64_t room, bool f32, hipStream_t stream) {
-  return f32 ? launch_tiled<WHAT, float>(p, room, stream) : launch_tiled<WHAT, uint16_t>(p, room, stream);
+// The products of a backward pass (K 0: not wanted) in one launch, with the last sums of dbias: planned, so that what is refused is refused before anything runs ..
+template <typename T> int plan_backward(Product& dw, Product& dx, const BiasParts& bias, char* at, int64_t room) {  // their size of tiles, or -1
+  constexpr bool F32 = sizeof(T) == 4;
+  const Product* const all[2] = {&dw, &dx};
+  const int what[2] = {WGRAD, DGRAD}, size = size_for(all, what, F32);
+  const int64_t each = slabs_each(all, what, size, F32);
+  dw.part = reinterpret_cast<float*>(at);
+  if (dw.K) {
+    if (!plan(dw, WGRAD, size, F32, each, room)) return -1;
+    const int64_t used = dw.splits > 1 ? 4ll * dw.splits * dw.M * dw.N * (dw.pair ? 2 : 1) : 0;
+    at += used;
+    room -= used;
+  }
+  dx.part = reinterpret_cast<float*>(at);
+  if (dx.K && !plan(dx, DGRAD, size, F32, each, room)) return -1;
+  return launchable((int64_t)dw.workgroups() + dx.workgroups() + bias.out, 512) ? size : -1;
 }
-
-// The six products of planes, the smallest first.
-constexpr int PLANE_A[6] = {2, 0, 1, 1, 0, 0}, PLANE_B[6] = {0, 2, 1, 0, 1, 0};
+// .. and launched.
+template <typename T> hipError_t launch_backward(const Product& dw, const Product& dx, const BiasParts& bias, int size, hipStream_t stream) {
+  if (size == 0) start_backward<T, 0>(dw, dx, bias, stream);
+  else if (size == 1) start_backward<T, 1>(dw, dx, bias, stream);
+  else if (size == 2) start_backward<T, 2>(dw, dx, bias, stream);
+  else if constexpr (sizeof(T) == 2) start_backward<T, 3>(dw, dx, bias, stream);
+  const hipError_t e = hipGetLastError();
+  const int64_t first = join_groups(dw, WGRAD), groups = first + join_groups(dx, DGRAD);
+  if (e != hipSuccess || !groups) return e;
+  hipLaunchKernelGGL((token_backward_join_kernel<T>), dim3((unsigned)groups), dim3(256), 0, stream, dw, dx, (int)first);
+  return hipGetLastError();
+}
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-
-// Tensors of n[i] floats in planes at `at`, and where what follows begins.
-hipError_t cut(const void* const (&from)[3], const int64_t (&n)[3], char*& at, uint16_t* (&planes)[3], hipStream_t stream) {
-  Cut c;
-  c.first[0] = 0;
-  for (int i = 0; i < 3; ++i) {
-    c.from[i] = static_cast<const float*>(from[i]);
-    c.to[i] = planes[i] = reinterpret_cast<uint16_t*>(at);
-    c.n[i] = n[i];
-    c.first[i + 1] = c.first[i] + n[i] / 8;
-    at += rounded(6 * n[i]);
-  }
-  const int64_t groups = (c.first[3] + 255) / 256;
-  if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(token_cut_kernel, dim3((unsigned)groups), dim3(256), 0, stream, c);
-  return hipGetLastError();
-}
 template <bool DUAL> hipError_t launch_few(const Few& a, int dtype, hipStream_t stream) {
   const dim3 grid((a.cols + (DUAL ? 7 : 15)) / (DUAL ? 8 : 16));
   if (dtype == DT_BF16) hipLaunchKernelGGL((token_few_kernel<uint16_t, DUAL>), grid, dim3(256), 0, stream, a);
@@ -723,219 +940,110 @@ template <bool DUAL> hipError_t launch_few(const Few& a, int dtype, hipStream_t 
   return hipGetLastError();
 }
 constexpr int FEW_ROWS = 16;
-// The segments of a product of planes: `n` elements of A and B a plane; in bf16 the one of A and B.
-struct Segments {
-  int count;
-  int a[6], b[6];
-  explicit Segments(bool f32) : count(f32 ? 6 : 1) {
-    for (int s = 0; s < count; ++s) {
-      a[s] = f32 ? PLANE_A[s] : 0;
-      b[s] = f32 ? PLANE_B[s] : 0;
-    }
+
+template <typename T> hipError_t gated_backward(const GatedLinear& a, hipStream_t stream) {
+  char* at = static_cast<char*>(a.workspace);
+  const int64_t n = (int64_t)a.rows * a.hidden, groups = (n / 8 + 255) / 256;
+  if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
+  T *const dg = reinterpret_cast<T*>(at), *const du = reinterpret_cast<T*>(at + rounded((int)sizeof(T) * n));
+  at += 2 * rounded((int)sizeof(T) * n);
+  Product dw, dx;
+  memset(&dw, 0, sizeof(dw));
+  memset(&dx, 0, sizeof(dx));
+  if (a.dwg) {
+    dw.segments = 1;
+    dw.K = a.rows; dw.M = a.hidden; dw.N = a.in; dw.lda = a.hidden; dw.ldb = a.in;
+    dw.A[0] = dg; dw.other = du; dw.B[0] = a.x;
+    dw.out = a.dwg; dw.out2 = a.dwu; dw.pair = 1;
   }
-};
+  if (a.dx) {
+    dx.segments = 2;
+    dx.K = a.hidden; dx.M = a.rows; dx.N = a.in; dx.lda = a.hidden; dx.ldb = a.in;
+    dx.A[0] = dg; dx.A[1] = du; dx.B[0] = a.wg; dx.B[1] = a.wu;
+    dx.out = a.dx;
+  }
+  const BiasParts none = {nullptr, nullptr, 0, 0};
+  const int size = plan_backward<T>(dw, dx, none, at, static_cast<char*>(a.workspace) + a.workspace_bytes - at);
+  if (size < 0) return hipErrorInvalidConfiguration;
+  hipLaunchKernelGGL((gated_grad_kernel<T>), dim3((unsigned)groups), dim3(256), 0, stream, static_cast<const T*>(a.g), static_cast<const T*>(a.u),
+                     static_cast<const T*>(a.dh), dg, du, n, a.act);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  return launch_backward<T>(dw, dx, none, size, stream);
+}
+template <typename T> hipError_t linear_backward(const TokenLinear& a, hipStream_t stream) {
+  char* at = static_cast<char*>(a.workspace);
+  const int64_t n = (int64_t)a.rows * a.out;
+  // places in the workspace, whatever is wanted: a result does not depend on which others are
+  T* const to = (a.dx || a.dw) && a.act != TOKEN_NONE ? reinterpret_cast<T*>(at) : nullptr;  // dz, where it is not dy
+  at += rounded((int)sizeof(T) * n);
+  float* const sums = reinterpret_cast<float*>(at);
+  at += rounded(4ll * a.out * std::min(a.rows, LINEAR_MAX_PARTS));
+  const int share = (int)(((int64_t)a.rows + 8 * LINEAR_MAX_PARTS - 1) / (8 * LINEAR_MAX_PARTS) * 8), parts = (int)(((int64_t)a.rows + share - 1) / share);  // strips of whole eights of rows
+  BiasParts bias = {nullptr, nullptr, 0, 0};
+  if (a.dbias && parts > 1) bias = {sums, a.dbias, parts, a.out};
+  Product dw, dx;
+  memset(&dw, 0, sizeof(dw));
+  memset(&dx, 0, sizeof(dx));
+  const void* const dz = to ? to : a.dy;
+  if (a.dw) {
+    dw.segments = 1;
+    dw.K = a.rows; dw.M = a.out; dw.N = a.in; dw.lda = a.out; dw.ldb = a.in;
+    dw.A[0] = dz; dw.B[0] = a.x; dw.out = a.dw;
+  }
+  if (a.dx) {
+    dx.segments = 1;
+    dx.K = a.out; dx.M = a.rows; dx.N = a.in; dx.lda = a.out; dx.ldb = a.in;
+    dx.A[0] = dz; dx.B[0] = a.w; dx.out = a.dx;
+  }
+  const int size = plan_backward<T>(dw, dx, bias, at, static_cast<char*>(a.workspace) + a.workspace_bytes - at);
+  if (size < 0) return hipErrorInvalidConfiguration;
+  if (to || a.dbias) {
+    hipLaunchKernelGGL((linear_grad_kernel<T>), dim3((a.out + 255) / 256, parts), dim3(256), 0, stream, static_cast<const T*>(a.z), static_cast<const T*>(a.dy), to,
+                       bias.dbias ? sums : nullptr, bias.dbias ? nullptr : static_cast<T*>(a.dbias), a.rows, a.out, share, a.act);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || (!a.dx && !a.dw && !bias.dbias)) return e;
+  }
+  return launch_backward<T>(dw, dx, bias, size, stream);
+}
 
 }  // namespace
 
 // Bytes that the calls cannot do without.
-int64_t gated_linear_workspace_bytes(bool backward, int rows, int in, int hidden, int dtype) {
-  const int64_t planes = dtype == DT_F32 ? 6 * ((int64_t)rows * in + 2ll * hidden * in) + 1024 : 0;
-  if (!backward) return planes;
-  return planes + (dtype == DT_F32 ? 12 : 4) * (int64_t)rows * hidden + 1024;
-}
-int64_t token_linear_workspace_bytes(bool backward, int rows, int in, int out, int dtype) {
-  const int64_t planes = dtype == DT_F32 ? 6 * ((int64_t)rows * in + (int64_t)out * in) + 1024 : 0;
-  if (!backward) return planes;
-  return planes + (dtype == DT_F32 ? 6 : 2) * (int64_t)rows * out + 4ll * out * std::min(rows, LINEAR_MAX_PARTS) + 1024;
+int64_t gated_linear_bwd_workspace_bytes(int rows, int hidden, int dtype) { return (dtype == DT_F32 ? 8 : 4) * (int64_t)rows * hidden + 1024; }
+int64_t token_linear_bwd_workspace_bytes(int rows, int out, int dtype) {
+  return (dtype == DT_F32 ? 4 : 2) * (int64_t)rows * out + 4ll * out * std::min(rows, LINEAR_MAX_PARTS) + 1024;
 }
 
 hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stream) {
   if (a.rows <= FEW_ROWS) return launch_few<true>({a.x, a.wg, a.wu, a.h, a.g, a.u, nullptr, nullptr, a.rows, a.in, a.hidden, a.act}, dtype, stream);
   Product p;
   memset(&p, 0, sizeof(p));
+  p.segments = 1;
   p.K = a.in; p.M = a.rows; p.N = a.hidden; p.lda = p.ldb = a.in;
+  p.A[0] = a.x; p.B[0] = a.wg; p.other = a.wu;
   p.out = a.h; p.out2 = a.g; p.out3 = a.u;
   p.act = a.act;
-  const bool f32 = dtype == DT_F32;
-  char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
-  const int64_t xn = (int64_t)a.rows * a.in, wn = (int64_t)a.hidden * a.in;
-  const uint16_t *x = static_cast<const uint16_t*>(a.x), *wg = static_cast<const uint16_t*>(a.wg), *wu = static_cast<const uint16_t*>(a.wu);
-  if (f32) {
-    uint16_t* planes[3];
-    const hipError_t e = cut({a.x, a.wg, a.wu}, {xn, wn, wn}, at, planes, stream);
-    if (e != hipSuccess) return e;
-    x = planes[0];
-    wg = planes[1];
-    wu = planes[2];
-  }
-  const Segments of(f32);
-  p.segments = of.count;
-  for (int s = 0; s < of.count; ++s) {
-    p.A[s] = x + of.a[s] * xn;
-    p.B[s] = wg + of.b[s] * wn;
-    p.other[s] = wu + of.b[s] * wn;
-  }
-  p.part = reinterpret_cast<float*>(at);
-  return launch_product<GATED>(p, std::max<int64_t>(0, end - at), f32, stream);
+  p.part = static_cast<float*>(a.workspace);
+  return dtype == DT_BF16 ? launch_forward<GATED, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<GATED, float>(p, a.workspace_bytes, stream);
 }
-
 hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream) {
-  char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
-  const int64_t n = (int64_t)a.rows * a.hidden, groups = (n / 8 + 255) / 256, xn = (int64_t)a.rows * a.in, wn = (int64_t)a.hidden * a.in;
-  if (!launchable(groups, 256)) return hipErrorInvalidConfiguration;
-  const bool f32 = dtype == DT_F32;
-  const uint16_t *x = static_cast<const uint16_t*>(a.x), *wg = static_cast<const uint16_t*>(a.wg), *wu = static_cast<const uint16_t*>(a.wu);
-  hipError_t e;
-  if (f32) {
-    uint16_t* planes[3];
-    e = cut({a.x, a.wg, a.wu}, {xn, wn, wn}, at, planes, stream);
-    if (e != hipSuccess) return e;
-    x = planes[0];
-    wg = planes[1];
-    wu = planes[2];
-  }
-  uint16_t* const dg = reinterpret_cast<uint16_t*>(at);
-  at += rounded((f32 ? 6 : 2) * n);
-  uint16_t* const du = reinterpret_cast<uint16_t*>(at);
-  at += rounded((f32 ? 6 : 2) * n);
-  if (f32) {
-    hipLaunchKernelGGL((gated_grad_kernel<float>), dim3((unsigned)groups), dim3(256), 0, stream, static_cast<const float*>(a.g), static_cast<const float*>(a.u),
-                       static_cast<const float*>(a.dh), dg, du, n, a.act);
-  } else {
-    hipLaunchKernelGGL((gated_grad_kernel<uint16_t>), dim3((unsigned)groups), dim3(256), 0, stream, static_cast<const uint16_t*>(a.g),
-                       static_cast<const uint16_t*>(a.u), static_cast<const uint16_t*>(a.dh), dg, du, n, a.act);
-  }
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const Segments of(f32);
-  Product p;
-  if (a.dx) {
-    memset(&p, 0, sizeof(p));
-    p.segments = 2 * of.count;
-    p.K = a.hidden; p.M = a.rows; p.N = a.in; p.lda = a.hidden; p.ldb = a.in;
-    for (int s = 0; s < of.count; ++s) {
-      p.A[2 * s] = dg + of.a[s] * n;
-      p.A[2 * s + 1] = du + of.a[s] * n;
-      p.B[2 * s] = wg + of.b[s] * wn;
-      p.B[2 * s + 1] = wu + of.b[s] * wn;
-    }
-    p.out = a.dx; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
-    if (e != hipSuccess) return e;
-  }
-  if (a.dwg) {
-    memset(&p, 0, sizeof(p));
-    p.segments = of.count;
-    p.K = a.rows; p.M = a.hidden; p.N = a.in; p.lda = a.hidden; p.ldb = a.in;
-    for (int s = 0; s < of.count; ++s) {
-      p.A[s] = dg + of.a[s] * n;
-      p.other[s] = du + of.a[s] * n;
-      p.B[s] = x + of.b[s] * xn;
-    }
-    p.out = a.dwg; p.out2 = a.dwu; p.pair = 1; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
-  }
-  return e;
+  return dtype == DT_BF16 ? gated_backward<uint16_t>(a, stream) : gated_backward<float>(a, stream);
 }
-
 hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream) {
   if (a.rows <= FEW_ROWS) return launch_few<false>({a.x, a.w, nullptr, a.y, a.z, nullptr, a.bias, a.residual, a.rows, a.in, a.out, a.act}, dtype, stream);
   Product p;
   memset(&p, 0, sizeof(p));
+  p.segments = 1;
   p.K = a.in; p.M = a.rows; p.N = a.out; p.lda = p.ldb = a.in;
+  p.A[0] = a.x; p.B[0] = a.w;
   p.out = a.y; p.out2 = a.z; p.bias = a.bias; p.residual = a.residual;
   p.act = a.act;
-  const bool f32 = dtype == DT_F32;
-  char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
-  const int64_t xn = (int64_t)a.rows * a.in, wn = (int64_t)a.out * a.in;
-  const uint16_t *x = static_cast<const uint16_t*>(a.x), *w = static_cast<const uint16_t*>(a.w);
-  if (f32) {
-    uint16_t* planes[3];
-    const hipError_t e = cut({a.x, a.w, nullptr}, {xn, wn, 0}, at, planes, stream);
-    if (e != hipSuccess) return e;
-    x = planes[0];
-    w = planes[1];
-  }
-  const Segments of(f32);
-  p.segments = of.count;
-  for (int s = 0; s < of.count; ++s) {
-    p.A[s] = x + of.a[s] * xn;
-    p.B[s] = w + of.b[s] * wn;
-  }
-  p.part = reinterpret_cast<float*>(at);
-  return launch_product<LINEAR>(p, std::max<int64_t>(0, end - at), f32, stream);
+  p.part = static_cast<float*>(a.workspace);
+  return dtype == DT_BF16 ? launch_forward<LINEAR, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<LINEAR, float>(p, a.workspace_bytes, stream);
 }
-
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream) {
-  char *at = static_cast<char*>(a.workspace), *const end = at + a.workspace_bytes;
-  const int64_t n = (int64_t)a.rows * a.out, xn = (int64_t)a.rows * a.in, wn = (int64_t)a.out * a.in;
-  const bool f32 = dtype == DT_F32;
-  const uint16_t *x = static_cast<const uint16_t*>(a.x), *w = static_cast<const uint16_t*>(a.w), *dz = static_cast<const uint16_t*>(a.dy);
-  hipError_t e = hipSuccess;
-  const bool products = a.dx || a.dw;
-  if (f32 && products) {
-    uint16_t* planes[3];
-    e = cut({a.x, a.w, nullptr}, {xn, wn, 0}, at, planes, stream);
-    if (e != hipSuccess) return e;
-    x = planes[0];
-    w = planes[1];
-  }
-  // places in the workspace, whatever is wanted: a result does not depend on which others are
-  at = static_cast<char*>(a.workspace) + (f32 ? rounded(6 * xn) + rounded(6 * wn) : 0);
-  uint16_t* to = nullptr;  // dz, where it is not dy
-  if (products && (f32 || a.act != TOKEN_NONE)) dz = to = reinterpret_cast<uint16_t*>(at);
-  at += rounded((f32 ? 6 : 2) * n);
-  float* const sums = reinterpret_cast<float*>(at);
-  at += rounded(4ll * a.out * std::min(a.rows, LINEAR_MAX_PARTS));
-  if (to || a.dbias) {
-    // strips of 32 rows at least, for as many workgroups as run at once
-    const int columns = (a.out + 255) / 256;
-    int share = std::max({32, (a.rows + LINEAR_MAX_PARTS - 1) / LINEAR_MAX_PARTS});
-    const int parts = (a.rows + share - 1) / share;
-    float* const part = a.dbias && parts > 1 ? sums : nullptr;
-    const dim3 grid(columns, parts);
-    if (f32) {
-      hipLaunchKernelGGL((linear_grad_kernel<float>), grid, dim3(256), 0, stream, static_cast<const float*>(a.z), static_cast<const float*>(a.dy), to, part,
-                         part ? nullptr : static_cast<float*>(a.dbias), a.rows, a.out, share, a.act);
-    } else {
-      hipLaunchKernelGGL((linear_grad_kernel<uint16_t>), grid, dim3(256), 0, stream, static_cast<const uint16_t*>(a.z), static_cast<const uint16_t*>(a.dy), to,
-                         part, part ? nullptr : static_cast<uint16_t*>(a.dbias), a.rows, a.out, share, a.act);
-    }
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (part) {
-      if (f32) hipLaunchKernelGGL((linear_bias_kernel<float>), dim3(a.out / 8), dim3(256), 0, stream, part, static_cast<float*>(a.dbias), parts, a.out);
-      else hipLaunchKernelGGL((linear_bias_kernel<uint16_t>), dim3(a.out / 8), dim3(256), 0, stream, part, static_cast<uint16_t*>(a.dbias), parts, a.out);
-      e = hipGetLastError();
-      if (e != hipSuccess) return e;
-    }
-  }
-  const Segments of(f32);
-  Product p;
-  if (a.dx) {
-    memset(&p, 0, sizeof(p));
-    p.segments = of.count;
-    p.K = a.out; p.M = a.rows; p.N = a.in; p.lda = a.out; p.ldb = a.in;
-    for (int s = 0; s < of.count; ++s) {
-      p.A[s] = dz + of.a[s] * n;
-      p.B[s] = w + of.b[s] * wn;
-    }
-    p.out = a.dx; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<DGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
-    if (e != hipSuccess) return e;
-  }
-  if (a.dw) {
-    memset(&p, 0, sizeof(p));
-    p.segments = of.count;
-    p.K = a.rows; p.M = a.out; p.N = a.in; p.lda = a.out; p.ldb = a.in;
-    for (int s = 0; s < of.count; ++s) {
-      p.A[s] = dz + of.a[s] * n;
-      p.B[s] = x + of.b[s] * xn;
-    }
-    p.out = a.dw; p.part = reinterpret_cast<float*>(at);
-    e = launch_product<WGRAD>(p, std::max<int64_t>(0, end - at), f32, stream);
-  }
-  return e;
+  return dtype == DT_BF16 ? linear_backward<uint16_t>(a, stream) : linear_backward<float>(a, stream);
 }
 
 }  // namespace cdp

@@ -201,8 +201,7 @@ def planes(dtype):
 
 
 def gated_workspace(dtype, backward, R, I, H):
-    n = 6 * (R + 2 * H) * I + 1024 if dtype == F32 else 0
-    return n + (12 if dtype == F32 else 4) * R * H + 1024 if backward else n
+    return (8 if dtype == F32 else 4) * R * H + 1024 if backward else 0
 
 
 @pytest.mark.parametrize("shared", [0, 3])
@@ -240,15 +239,15 @@ def test_gated_linear(R, I, H, act, dtype, shared):
     sg, su = ((mid * v.abs() + 64 * U * (gd.abs() + 1) * s) for v, s in ((dg, (dhd * ud).abs()), (du, dhd.abs())))
     wantx = dg @ wgd + du @ wud
     sizex = (dg.abs() + sg) @ wgd.abs() + (du.abs() + su) @ wud.abs()
-    near(dx, wantx, half(dtype) * wantx.abs() + sg @ wgd.abs() + su @ wud.abs() + ((4 * H + 8) * U + planes(dtype)) * sizex, "dx")
-    for got, v, s, what in ((dwg, dg, sg, "dwg"), (dwu, du, su, "dwu")):
-        want = v.t() @ xd
-        near(got, want, half(dtype) * want.abs() + s.t() @ xd.abs() + ((2 * R + 8) * U + planes(dtype)) * ((v.abs() + s).t() @ xd.abs()), what)
-    # one of the two alone
+    # both, and one of the two alone
     dx2, dwg2, dwu2 = hold.out(t, R, I), hold.out(t, H, I), hold.out(t, H, I)
     b.cdp_k_gated_linear_backward(dtype, act, *map(p, dev), p(g), p(u), p(dhc), p(dx2), 0, 0, p(ws), need, R, I, H)
     b.cdp_k_gated_linear_backward(dtype, act, *map(p, dev), p(g), p(u), p(dhc), 0, p(dwg2), p(dwu2), p(ws), need, R, I, H)
-    assert torch.equal(dx, dx2) and torch.equal(dwg, dwg2) and torch.equal(dwu, dwu2)
+    for got in (dx, dx2):
+        near(got, wantx, half(dtype) * wantx.abs() + sg @ wgd.abs() + su @ wud.abs() + ((4 * H + 8) * U + planes(dtype)) * sizex, "dx")
+    for got, v, s, what in ((dwg, dg, sg, "dwg"), (dwu, du, su, "dwu"), (dwg2, dg, sg, "dwg"), (dwu2, du, su, "dwu")):
+        want = v.t() @ xd
+        near(got, want, half(dtype) * want.abs() + s.t() @ xd.abs() + ((2 * R + 8) * U + planes(dtype)) * ((v.abs() + s).t() @ xd.abs()), what)
     hold.check()
 
 
@@ -271,7 +270,7 @@ def test_linear(R, I, O, act, extra, dtype, shared):
     xd, wd, dyd = (work(v.double()) for v in (x, w, dy))
     dev = [hold(v, t) for v in (x, w)] + [hold(v, t) if v is not None else None for v in (bias, residual)]
     y, z, y2 = (hold.out(t, R, O) for _ in range(3))
-    need = (6 * (R + O) * I + 1024 if dtype == F32 else 0) + shared * 4 * R * O
+    need = shared * 4 * R * O
     ws = hold.workspace(need) if need else None
     b.cdp_k_linear(dtype, act, *map(p, dev), p(y), p(z), p(ws), need, R, I, O)
     if residual is not None:
@@ -290,7 +289,7 @@ def test_linear(R, I, O, act, extra, dtype, shared):
     near(y, (a + rd).cpu(), (half(dtype) * (a + rd).abs() + slope * e + 32 * U * (want.abs() + 1) + 2 * U * rd.abs()).cpu(), "y")
 
     dx, dw, dbias = hold.out(t, R, I), hold.out(t, O, I), hold.out(t, O)
-    need = (6 * (R + O) * I + 1024 + 6 * R * O if dtype == F32 else 2 * R * O) + 4 * O * min(R, 256) + 1024 + shared * 4 * max(R, O) * I
+    need = (4 if dtype == F32 else 2) * R * O + 4 * O * min(R, 256) + 1024 + shared * 4 * max(R, O) * I
     ws, dyc = hold.workspace(need), hold(dy, t)
     zin = p(z) if act != 3 else 0
     b.cdp_k_linear_backward(dtype, act, p(dev[0]), p(dev[1]), zin, p(dyc), p(dx), p(dw), p(dbias), p(ws), need, R, I, O)
@@ -299,15 +298,16 @@ def test_linear(R, I, O, act, extra, dtype, shared):
     dz = dyd * da
     close = (64 * U * (zd.abs() + 1) * dyd.abs()) if act != 3 else 0 * dyd
     s = (2.0 ** -8 if dtype == BF16 and act != 3 else 0.0) * dz.abs() + close
-    for got, v, sv, o, n, what in ((dx, dz, s, wd, O, "dx"), (dw, dz.t(), s.t(), xd, R, "dw")):
+    alone = [hold.out(t, *v.shape) for v in (dx, dw, dbias)]
+    for one in range(3):
+        b.cdp_k_linear_backward(dtype, act, p(dev[0]) if one == 1 else 0, p(dev[1]) if one == 0 else 0, zin, p(dyc), *(p(v) if k == one else 0 for k, v in enumerate(alone)),
+                                p(ws), need, R, I, O)
+    for got, v, sv, o, n, what in ((dx, dz, s, wd, O, "dx"), (dw, dz.t(), s.t(), xd, R, "dw"), (alone[0], dz, s, wd, O, "dx alone"), (alone[1], dz.t(), s.t(), xd, R, "dw alone")):
         want = v @ o
         near(got, want.cpu(), (half(dtype) * want.abs() + sv @ o.abs() + ((2 * n + 8) * U + planes(dtype)) * ((v.abs() + sv) @ o.abs())).cpu(), what)
     want = dz.sum(0)
-    near(dbias, want.cpu(), (half(dtype) * want.abs() + close.sum(0) + R * U * dz.abs().sum(0)).cpu(), "dbias")
-    for one in range(3):
-        outs = [hold.out(t, *v.shape) for v in (dx, dw, dbias)]
-        b.cdp_k_linear_backward(dtype, act, p(dev[0]), p(dev[1]), zin, p(dyc), *(p(v) if k == one else 0 for k, v in enumerate(outs)), p(ws), need, R, I, O)
-        assert torch.equal(outs[one], (dx, dw, dbias)[one])
+    for got in (dbias, alone[2]):
+        near(got, want.cpu(), (half(dtype) * want.abs() + close.sum(0) + R * U * dz.abs().sum(0)).cpu(), "dbias")
     hold.check()
 
 
