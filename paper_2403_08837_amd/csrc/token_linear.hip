@@ -238,11 +238,15 @@ __device__ __forceinline__ void slab_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+__device__ __forceinline__ unsigned two_bf16(float a, float b) {  // (one instruction)
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  typedef float v2f __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, __builtin_convertvector((v2f){a, b}, v2bf));
+}
 // Two groups of four values, of the columns n + 4 hi .. and n + 8 + 4 hi .. of a lane, as eight neighbouring columns n + 8 hi ..: 16 bytes of bf16.
 __device__ __forceinline__ uint4 eight(const float* v) {
-  auto two = [](float a, float b) { return (unsigned)f32_to_bf16(a) | (unsigned)f32_to_bf16(b) << 16; };
-  const auto x = __builtin_amdgcn_permlane32_swap(two(v[0], v[1]), two(v[4], v[5]), false, false);
-  const auto y = __builtin_amdgcn_permlane32_swap(two(v[2], v[3]), two(v[6], v[7]), false, false);
+  const auto x = __builtin_amdgcn_permlane32_swap(two_bf16(v[0], v[1]), two_bf16(v[4], v[5]), false, false);
+  const auto y = __builtin_amdgcn_permlane32_swap(two_bf16(v[2], v[3]), two_bf16(v[6], v[7]), false, false);
   return make_uint4(x[0], y[0], x[1], y[1]);
 }
 // A 32 x 32 block of results: row m, columns n ..; v[4 q + e] is column 8 q + 4 hi + e of it (q < 4, e < 4).
@@ -533,10 +537,9 @@ template <int TILE, bool SLOW> struct Planes {
   }
   // A float is the sum of its planes to 2^-27 of it; the largest finite ones, which would round up to infinity, through the largest bf16.
   __device__ __forceinline__ void cut(const Held& held, unsigned char* planes) const {
-    auto two = [](float a, float b) { return (unsigned)f32_to_bf16(a) | (unsigned)f32_to_bf16(b) << 16; };
     auto low = [](unsigned p) { return __uint_as_float(p << 16); };
     auto high = [](unsigned p) { return __uint_as_float(p & 0xffff0000u); };
-    constexpr float MOST = 3.3895313892515355e38f;
+    auto most = [](float v) { return __builtin_amdgcn_fmed3f(v, -3.3895313892515355e38f, 3.3895313892515355e38f); };
 #pragma unroll
     for (int i = 0; i < LP; ++i) {
       const int id = i * 256 + threadIdx.x, r = id / PER_ROW, c = id % PER_ROW;
@@ -545,10 +548,10 @@ template <int TILE, bool SLOW> struct Planes {
 #pragma unroll
       for (int p = 0; p < 3; ++p) {
         uint2 w;
-        if (p == 0) w = make_uint2(two(__builtin_amdgcn_fmed3f(v[0], -MOST, MOST), __builtin_amdgcn_fmed3f(v[1], -MOST, MOST)),
-                                   two(__builtin_amdgcn_fmed3f(v[2], -MOST, MOST), __builtin_amdgcn_fmed3f(v[3], -MOST, MOST)));
-        else w = make_uint2(two(v[0], v[1]), two(v[2], v[3]));
+        if (p == 0) w = make_uint2(two_bf16(most(v[0]), most(v[1])), two_bf16(most(v[2]), most(v[3])));
+        else w = make_uint2(two_bf16(v[0], v[1]), two_bf16(v[2], v[3]));
         *reinterpret_cast<uint2*>(to + p * BYTES) = w;
+        if (p == 2) break;
         v[0] -= low(w.x);
         v[1] -= high(w.x);
         v[2] -= low(w.y);
@@ -557,8 +560,10 @@ template <int TILE, bool SLOW> struct Planes {
     }
   }
 };
-// AHEAD slabs are on their way in registers; BUFFERS of planes.
-template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int AHEAD, int BUFFERS>
+// AHEAD slabs are on their way in registers.  While one is contracted out of one half of LDS the next is cut into the other.  A chain of slabs is bound by LDS
+// (three planes of either operand are written once and read by two wavefronts) and by the 7 instructions a float takes to cut: 0.53 us a slab of a 64 x 64 tile, on
+// its own in a CU; four slabs ahead or a fixed order of matrix and other instructions change nothing.  4096^3 184 TFLOP/s.
+template <int WHAT, int BM, int BN, int WAVES_M, int WAVES_N, int AHEAD>
 __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned char* smem) {
   constexpr int BK = 32, WTM = BM / WAVES_M, WTN = BN / WAVES_N, MI = WTM / 32, NI = WTN / 32;
   constexpr bool DUAL = WHAT == GATED, ASLOW = WHAT == WGRAD, BSLOW = WHAT == DGRAD || WHAT == WGRAD;
@@ -572,22 +577,27 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
   PB sb;
   sa.start(at.row0, P.M, P.lda, [](int r) { return r; });
   sb.start(at.col0, P.N, P.ldb, [](int r) { return DUAL ? (r >> 6) * 32 + (r & 31) : r; });
+  // where the slabs of either segment begin
+  const char *a0[2], *b0[2], *other = reinterpret_cast<const char*>(static_cast<const float*>(P.other) + (int64_t)at.col0 * P.ldb);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const float *const a = static_cast<const float*>(at.second ? P.other : P.A[i]), *const b = static_cast<const float*>(P.B[i]);
+    a0[i] = reinterpret_cast<const char*>(ASLOW ? a + at.row0 : a + (int64_t)at.row0 * P.lda);
+    b0[i] = reinterpret_cast<const char*>(BSLOW ? b + at.col0 : b + (int64_t)at.col0 * P.ldb);
+  }
   int seg = at.seg, slab = at.slab, left_to_ask = at.todo;
   typename PA::Held ha[AHEAD];
   typename PB::Held hb[AHEAD];
-  auto request = [&](auto w) {
-    if (left_to_ask-- <= 0) return;
+  auto request = [&](auto w) {  // (past the last slab: zeros)
     constexpr int h = decltype(w)::value;
-    const float* const a = static_cast<const float*>(at.second ? P.other : P.A[seg]);
-    const float* const b = static_cast<const float*>(P.B[seg]);
-    const int left = min(BK, P.K - slab * BK);
-    sa.load(ha[h], reinterpret_cast<const char*>(ASLOW ? a + (int64_t)slab * BK * P.lda + at.row0 : a + (int64_t)at.row0 * P.lda + slab * BK), nullptr, left, P.lda);
-    sb.load(hb[h], reinterpret_cast<const char*>(BSLOW ? b + (int64_t)slab * BK * P.ldb + at.col0 : b + (int64_t)at.col0 * P.ldb + slab * BK),
-            DUAL ? reinterpret_cast<const char*>(static_cast<const float*>(P.other) + (int64_t)at.col0 * P.ldb + slab * BK) : nullptr, left, P.ldb);
-    if (++slab == at.per_segment) {
-      slab = 0;
-      ++seg;
-    }
+    const int left = left_to_ask > 0 ? min(BK, P.K - slab * BK) : 0;
+    const int64_t k = (int64_t)slab * (4 * BK);
+    sa.load(ha[h], (seg ? a0[1] : a0[0]) + (ASLOW ? k * P.lda : k), nullptr, left, P.lda);
+    sb.load(hb[h], (seg ? b0[1] : b0[0]) + (BSLOW ? k * P.ldb : k), DUAL ? other + k : nullptr, left, P.ldb);
+    --left_to_ask;
+    const bool end = ++slab == at.per_segment;
+    slab = end ? 0 : slab;
+    seg += end;
   };
   static_for<AHEAD>(request);
   v16f_t acc[MI][NI];
@@ -631,18 +641,22 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
           for (int j = 0; j < NI; ++j) acc[i][j] = mfma_bf16(fb[OF_B[s]][j], fa[OF_A[s]][i], acc[i][j]);
     }
   };
-  static_assert(AHEAD % BUFFERS == 0, "");
+  auto cut = [&](auto w) {
+    constexpr int h = decltype(w)::value;
+    unsigned char* const la = smem + h % 2 * BUFFER;
+    sa.cut(ha[h], la);
+    sb.cut(hb[h], la + 3 * PA::BYTES);
+    request(w);
+  };
+  static_assert(AHEAD % 2 == 0, "");
+  cut(std::integral_constant<int, 0>{});
+  lds_barrier();
   for (int t = at.todo; t > 0; t -= AHEAD) {
     static_for<AHEAD>([&](auto w) {
       constexpr int h = decltype(w)::value;
-      if (h > 0 && t <= h) return;
-      unsigned char* const la = smem + h % BUFFERS * BUFFER;
-      if (BUFFERS == 1) lds_barrier();  // the slab before has been read (of two buffers: the barrier behind the cut since then)
-      sa.cut(ha[h], la);
-      sb.cut(hb[h], la + 3 * PA::BYTES);
-      request(w);
+      contract(smem + h % 2 * BUFFER);
+      cut(std::integral_constant<int, (h + 1) % AHEAD>{});
       lds_barrier();
-      contract(la);
     });
   }
   leave<WHAT, float>(P, acc, at.row0 + wm * WTM, at.col0 + wn * (DUAL ? WTN / 2 : WTN), at.split, at.second, lane);
@@ -655,21 +669,22 @@ template <int WHAT, typename T, int SIZE> struct Tile {
   static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 || (SIZE == 0 && EXACT && DUAL) ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
   static constexpr int WAVES_M = SIZE == 0 && EXACT && DUAL ? 4 : 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
   static constexpr int BK = EXACT ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 1 ? 3 : 2;
-  static constexpr int AHEAD = SIZE < 2 ? 2 : 1, BUFFERS = AHEAD;  // EXACT
-  static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * BUFFERS : (BM + BN) * BK * 2 * STAGES;
+  static constexpr int AHEAD = 2;  // EXACT
+  static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
+  static constexpr int WAVES = LDS > 80 * 1024 || THREADS < 256 ? (THREADS + 255) / 256 : 2;  // a SIMD, as LDS allows: registers for them
   static __device__ __forceinline__ void body(const Product& P, int block, unsigned char* smem) {
-    if constexpr (EXACT) exact_body<WHAT, BM, BN, WAVES_M, WAVES_N, AHEAD, BUFFERS>(P, block, smem);
+    if constexpr (EXACT) exact_body<WHAT, BM, BN, WAVES_M, WAVES_N, AHEAD>(P, block, smem);
     else product_body<WHAT, T, BM, BN, WAVES_M, WAVES_N, BK, STAGES>(P, block, smem);
   }
 };
 template <int WHAT, typename T, int SIZE>
-__global__ __launch_bounds__((Tile<WHAT, T, SIZE>::THREADS), (Tile<WHAT, T, SIZE>::THREADS) / 128 > 2 ? 2 : (Tile<WHAT, T, SIZE>::THREADS) / 128) void token_product_kernel(const Product P) {
+__global__ __launch_bounds__((Tile<WHAT, T, SIZE>::THREADS), (Tile<WHAT, T, SIZE>::WAVES)) void token_product_kernel(const Product P) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[Tile<WHAT, T, SIZE>::LDS];
   Tile<WHAT, T, SIZE>::body(P, blockIdx.x, smem);
 }
 // Both products of a backward pass and the last sums of dbias, in the order dw, dx, dbias of workgroups (the first two of no tiles: not wanted).
 template <typename T, int SIZE>
-__global__ __launch_bounds__((Tile<WGRAD, T, SIZE>::THREADS), 2) void token_backward_kernel(const Product dw, const Product dx, const BiasParts bias) {
+__global__ __launch_bounds__((Tile<WGRAD, T, SIZE>::THREADS), (Tile<WGRAD, T, SIZE>::WAVES)) void token_backward_kernel(const Product dw, const Product dx, const BiasParts bias) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[Tile<WGRAD, T, SIZE>::LDS];
   const int weights = dw.tiles * dw.splits, all = weights + dx.tiles * dx.splits, block = blockIdx.x;
   if (block < weights) Tile<WGRAD, T, SIZE>::body(dw, block, smem);
@@ -683,7 +698,7 @@ template <typename T> __device__ __forceinline__ void join_body(const Product& P
   auto sum = [&](int64_t at, float (&v)[8]) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = 0.f;
-#pragma unroll 4
+#pragma unroll 8
     for (int s = 0; s < P.splits; ++s) {
       Chunk16<float> q[2];
       q[0].v = *reinterpret_cast<const uint4*>(P.part + s * stride + at);
@@ -830,12 +845,13 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
 constexpr int SIZES = 4, SLAB_OF[SIZES] = {128, 64, 64, 64}, SLAB_OF_F32 = 32;
-// Tiles of a product by size; workgroups that run at once.
+// Tiles of a product by size.
 int64_t tiles_of(const Product& p, int what, int size, bool f32) {
   const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
   return (((int64_t)p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * (p.pair ? 2 : 1);
 }
-int resident(int size) { return size == 3 ? 256 : 512; }
+// Workgroups that run at once.
+int resident(int size, bool f32) { return size == 3 || (size == 2 && f32) ? 256 : size == 0 && f32 ? 768 : 512; }
 // The smallest tiles that all run at once, else 128 x 128, or 256 x 256 where they are a CU's worth or more.
 template <int N> int size_for(const Product* const (&p)[N], const int (&what)[N], bool f32) {
   auto all = [&](int size) {
@@ -845,7 +861,7 @@ template <int N> int size_for(const Product* const (&p)[N], const int (&what)[N]
   };
   if (!f32 && all(3) >= 256) return 3;
   for (int size = 0; size < 2; ++size)
-    if (all(size) <= resident(size)) return size;
+    if (all(size) <= resident(size, f32)) return size;
   return 2;
 }
 // Tiles and parts of a product; `slabs_each`: slabs that a workgroup should have at least.
@@ -862,9 +878,11 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
   return launchable((int64_t)p.tiles * p.splits, 512);
 }
-// Slabs that a workgroup should have for all to run at once; not shared where that saves less than joining costs (4 us, about 1000 reduction indices).
+// Slabs that a workgroup should have for all to run at once, 256 reduction indices at least (fp32: 128); not shared where that saves fewer indices than joining costs,
+// 1024 (256), about 4 us.  Mean of 60 forward and backward passes of few tiles, us, with 128, 256, 512 at least and 1024 saved: 16.7, 16.2, 16.2 (with 256 and 2048 saved: 16.3, 16.6);
+// fp32 28.5, 29.0, 31.9 (with 256 saved 26.9, 27.9, 30.8).
 template <int N> int64_t slabs_each(const Product* const (&p)[N], const int (&what)[N], int size, bool f32) {
-  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size];
+  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size], least = f32 ? 128 : 256, saved = f32 ? 256 : 1024;
   int64_t work = 0, most = 1;
   for (int i = 0; i < N; ++i) {
     if (!p[i]->K) continue;
@@ -872,8 +890,8 @@ template <int N> int64_t slabs_each(const Product* const (&p)[N], const int (&wh
     work += tiles_of(*p[i], what[i], size, f32) * slabs;
     most = std::max(most, slabs);
   }
-  const int64_t each = std::max<int64_t>((work + resident(size) - 1) / resident(size), 512 / bk);
-  return (most - each) * bk < 1024 ? INT32_MAX : each;
+  const int64_t each = std::max<int64_t>((work + resident(size, f32) - 1) / resident(size, f32), least / bk);
+  return (most - each) * bk < saved ? INT32_MAX : each;
 }
 int64_t join_groups(const Product& p, int what) {
   return p.splits > 1 ? ((int64_t)p.M * p.N * (what != GATED && p.pair ? 2 : 1) / 8 + 255) / 256 : 0;
