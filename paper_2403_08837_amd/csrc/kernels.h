@@ -451,12 +451,13 @@ struct TokenLogprob {
   float* top_logprobs;
   const float *dlogprob, *dentropy;    // backward
   void* dlogits;
-  float4* part_sums;                   // forward: of LOGPROB_MAX_PARTS parts of rows, or null
+  float4* part_sums;                   // of the parts of rows, in the workspace
   unsigned long long* part_keys;
   int rows, vocab, top, parts;
   float scale;
 };
-constexpr int LOGPROB_MAX_TOP = 64, LOGPROB_MAX_SPLIT = 32, LOGPROB_MAX_PARTS = 1024, LOGPROB_MAX_VOCAB = 1 << 28;
-hipError_t launch_token_logprob(const TokenLogprob& a, bool backward, int dtype, hipStream_t stream);
+constexpr int LOGPROB_MAX_TOP = 64, LOGPROB_MAX_SPLIT = 32, LOGPROB_MAX_VOCAB = 1 << 28, LOGPROB_BYTES = 1 << 20;
+hipError_t launch_token_logprob(const TokenLogprob& a, void* workspace, int dtype, hipStream_t stream);
+hipError_t launch_token_logprob_bwd(const TokenLogprob& a, int dtype, hipStream_t stream);
 
 }  // namespace cdp

@@ -404,15 +404,13 @@ int cdp_k_token_logprob(int dtype, const void* logits, int64_t ld, const int32_t
   for (const void* p : {(const void*)logprob, (const void*)entropy, (const void*)lse, (const void*)top_ids, (const void*)top_logprobs})
     if (!aligned_to(p, 4)) return CDP_EINVAL;
   if (workspace && (!aligned_to(workspace, 16) || workspace_bytes < CDP_LOGPROB_BYTES)) return CDP_EINVAL;
-  static_assert(CDP_LOGPROB_BYTES >= LOGPROB_MAX_PARTS * (sizeof(float4) + LOGPROB_MAX_TOP * 8), "sums and keys of every part");
+  static_assert(CDP_LOGPROB_BYTES == LOGPROB_BYTES, "");
   TokenLogprob a;
   memset(&a, 0, sizeof(a));
   a.logits = logits; a.ld = ld; a.targets = targets; a.logprob = logprob; a.entropy = entropy; a.lse = lse;
   a.top_ids = top_ids; a.top_logprobs = top_logprobs;
-  a.part_sums = static_cast<float4*>(workspace);
-  a.part_keys = reinterpret_cast<unsigned long long*>(a.part_sums + LOGPROB_MAX_PARTS);
   a.rows = rows; a.vocab = vocab; a.top = top; a.scale = scale;
-  return launched(launch_token_logprob(a, false, dtype, static_cast<hipStream_t>(stream)));
+  return launched(launch_token_logprob(a, workspace, dtype, static_cast<hipStream_t>(stream)));
 }
 
 int cdp_k_token_logprob_backward(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, const float* lse, const float* entropy,
@@ -426,7 +424,7 @@ int cdp_k_token_logprob_backward(int dtype, const void* logits, int64_t ld, cons
   a.logits = logits; a.ld = ld; a.targets = targets; a.lse = const_cast<float*>(lse); a.entropy = const_cast<float*>(entropy);
   a.dlogprob = dlogprob; a.dentropy = dentropy; a.dlogits = dlogits;
   a.rows = rows; a.vocab = vocab; a.scale = scale;
-  return launched(launch_token_logprob(a, true, dtype, static_cast<hipStream_t>(stream)));
+  return launched(launch_token_logprob_bwd(a, dtype, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -6,14 +6,15 @@
 // t = sum 2^y y, y = (logit - m) scale log2(e): a new maximum multiplies s by f = 2^d and makes t = f (t + d s).  That maximum is raised once for eight values at most.
 // entropy = log s - (t / s) log 2 over the row.
 //
-// The likeliest tokens come from the same pass: the k-th largest of the lanes' maxima (ordered by value, then by place) is a lower border, since k lanes hold
-// something at least as good, and only the lanes at or above it (k of them) can hold anything better.  Their share of the row, k of 256 parts of it,
-// is read again, and what is not below the border, little more than k tokens, is ranked.
+// The likeliest tokens come from the same pass: a border that k of the lanes' maxima (ordered by value, then by place) are not below is one that the k-th token is
+// not below either, and only lanes whose maximum is not below it, little more than k of 256, can hold better ones.  Their share of the row is read again, and
+// what is not below the border, little more than k tokens, is ranked.
 #include "elem.h"
 #include "kernels.h"
 #include "lane_sums.h"
 
 #include <algorithm>
+#include <climits>
 
 namespace cdp {
 
@@ -60,6 +61,12 @@ __device__ __forceinline__ float value_of(unsigned o) { return __uint_as_float(o
 __device__ __forceinline__ u64 key_of(float v, unsigned place) { return (u64)ordered(v) << 32 | (0xffffffffu - place); }
 __device__ __forceinline__ int place_of(u64 key) { return (int)(0xffffffffu - (unsigned)key); }
 
+// (fmaxf of values that come out of shifts and masks makes each canonical first: an instruction more for every one)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float v;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(v) : "v"(a), "v"(b), "v"(c));
+  return v;
+}
 struct Sums {
   float m = -INFINITY, s = 0.f, t = 0.f;
   static __device__ __forceinline__ Sums of(float4 q) {
@@ -95,13 +102,49 @@ struct Sums {
     }
   }
 };
-__device__ __forceinline__ float lane_xor(float v, int mask) { return __shfl_xor(v, mask, 64); }
+// The sums of a wavefront's lanes, in every lane: their maximum first, then one exponential each.
+__device__ __forceinline__ void join_lanes(Sums& w, float c) {
+  const float to = lanes_max<64>(w.m);
+  if (w.m != to) w.raise(to, c);
+  w.s = lanes_sum<64>(w.s);
+  w.t = lanes_sum<64>(w.t);
+}
+
+// The key of the wanted-th largest of a wavefront's lanes by value, then by place; 0 where there are fewer.
+__device__ __forceinline__ u64 border_of(float v, int place, bool there, int wanted) {
+  if (v != v) v = -INFINITY;
+  unsigned long long left = __builtin_amdgcn_ballot_w64(there);
+  const int lane = threadIdx.x & 63;
+  while (left) {
+    const bool mine = left >> lane & 1;
+    const float most = lanes_max<64>(mine ? v : -INFINITY);
+    const unsigned long long ties = __builtin_amdgcn_ballot_w64(mine && v == most);
+    const int n = __builtin_popcountll(ties);
+    if (n < wanted) {
+      wanted -= n;
+      left &= ~ties;
+      continue;
+    }
+    // of those of one value the wanted-th by place
+    unsigned long long equal = ties;
+    int at = 0;
+    for (; wanted > 0; --wanted) {
+      int first = equal >> lane & 1 ? place : INT_MAX;
+#pragma unroll
+      for (int mask = 1; mask < 64; mask *= 2) first = min(first, __shfl_xor(first, mask, 64));
+      at = first;
+      equal &= ~__builtin_amdgcn_ballot_w64((equal >> lane & 1) && place == first);
+    }
+    return key_of(most, (unsigned)at);
+  }
+  return 0;
+}
 
 struct Found {
   float4 sums[WAVES];
-  u64 best[THREADS], found[MAX_FOUND];
+  u64 found[MAX_FOUND];
   int lanes[THREADS];
-  u64 border;
+  u64 border, borders[WAVES];
   int count, chosen;
 };
 
@@ -117,13 +160,12 @@ template <typename F> __device__ __forceinline__ void ranked(const u64* keys, in
 }
 
 // What a row is, from its sums.
-__device__ __forceinline__ void write_row(const TokenLogprob& a, int64_t row, const Sums& w, const void* logits, int target, bool bf16) {
+__device__ __forceinline__ void write_row(const TokenLogprob& a, int64_t row, const Sums& w, float l) {  // l: the target's logit
   const bool none = w.m == -INFINITY && w.s == 0.f;  // everything masked
   const float ls = logf(w.s), lse = none ? -INFINITY : fmaf(a.scale, w.m, ls);
   a.lse[row] = lse;
   if (a.entropy) a.entropy[row] = none ? 0.f : ls - LN2 * (w.t / w.s);
   if (a.logprob) {
-    const float l = bf16 ? bf16_to_f32(static_cast<const uint16_t*>(logits)[target]) : static_cast<const float*>(logits)[target];
     a.logprob[row] = none || l == -INFINITY ? (w.s != w.s ? w.s : -INFINITY) : fmaf(a.scale, l - w.m, -ls);
   }
 }
@@ -157,7 +199,7 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
   }
   const T* const logits = static_cast<const T*>(a.logits) + row * a.ld;
   const Row<T> r(logits, a.vocab);
-  const float c = a.scale * LOG2E;
+  const float c = a.scale * LOG2E, l_target = Elem<T>::to_f32(logits[target]);
   const int all = r.pieces(), share = (all + a.parts - 1) / a.parts;
   const int begin = min(part * share, all), end = min(begin + share, all);
   int inner = begin, whole_end = end;  // the pieces that are whole
@@ -168,9 +210,9 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
   Sums w;
   int best_piece = begin + tid;  // that of the lane's maximum, the first of several
   auto take = [&](const float (&v)[V], int k) {
-    float most = fmaxf(v[0], v[1]);
+    float most = max3(v[0], v[1], v[2]);
 #pragma unroll
-    for (int i = 2; i < V; ++i) most = fmaxf(most, v[i]);
+    for (int i = 3; i < V; i += 2) most = max3(most, v[i], v[i + 1 < V ? i + 1 : i]);
     if (most > w.m) {
       w.raise(most, c);
       best_piece = k;
@@ -185,10 +227,13 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
     take(v, k);
     k += THREADS;
   }
+  const uint4* from = reinterpret_cast<const uint4*>(r.at - r.lead) + k;
   for (; k + (UNROLL - 1) * THREADS < whole_end; k += UNROLL * THREADS) {
     Chunk16<T> q[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) q[u].v = r.get(k + u * THREADS);
+    for (int u = 0; u < UNROLL; ++u) q[u].v = from[u * THREADS];
+    from += UNROLL * THREADS;
+    __builtin_amdgcn_sched_barrier(0);  // all of them before the first is waited for
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
       float v[V];
@@ -202,55 +247,47 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
     r.values(k, -INFINITY, v);
     take(v, k);
   }
-  if constexpr (TOP) f.best[tid] = begin + tid < end ? (u64)ordered(w.m) << 32 | (0xffffffffu - (unsigned)best_piece) : 0;
-#pragma unroll
-  for (int mask = 1; mask < 64; mask *= 2) {
-    Sums b;
-    b.m = lane_xor(w.m, mask);
-    b.s = lane_xor(w.s, mask);
-    b.t = lane_xor(w.t, mask);
-    w.join(b, c);
+  const float best = w.m;
+  if constexpr (TOP) {
+    const u64 border = border_of(best, best_piece, begin + tid < end, (a.top + WAVES - 1) / WAVES);
+    if ((tid & 63) == 0) f.borders[tid >> 6] = border;
   }
+  join_lanes(w, c);
   if ((tid & 63) == 0) f.sums[tid >> 6] = w.all();
-  if (tid == 0) f.count = f.chosen = 0, f.border = 0;
+  if (tid == 0) f.count = f.chosen = 0;
   __syncthreads();
   w = Sums::of(f.sums[0]);
 #pragma unroll
   for (int i = 1; i < WAVES; ++i) w.join(Sums::of(f.sums[i]), c);
   if (tid == 0) {
-    if (a.parts == 1) write_row(a, row, w, logits, target, sizeof(T) == 2);
+    if (a.parts == 1) write_row(a, row, w, l_target);
     else a.part_sums[blockIdx.x] = w.all();
   }
   if constexpr (TOP) {
-    {
-      const u64 key = f.best[tid];
-      int rank = 0;
-#pragma unroll 8
-      for (int j = 0; j < THREADS; ++j) rank += f.best[j] > key;
-      if (key && rank < a.top) {
-        f.lanes[atomicAdd(&f.chosen, 1)] = tid;
-        // (anything in that piece or in one before it)
-        if (rank == a.top - 1) f.border = (key >> 32) << 32 | (0xffffffffu - (unsigned)((int64_t)(place_of(key) + 1) * V - 1 - r.lead));
-      }
-    }
+    // as many lanes as `top` are not below the least of the wavefronts' borders
+    u64 border = f.borders[0];
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) border = f.borders[i] < border ? f.borders[i] : border;
+    if (begin + tid < end && key_of(best, (unsigned)best_piece) >= border) f.lanes[atomicAdd(&f.chosen, 1)] = tid;
+    // (of places of pieces one of places of elements: anything in that piece)
+    if (tid == 0) f.border = border ? (border >> 32) << 32 | (0xffffffffu - (unsigned)((int64_t)(place_of(border) + 1) * V - 1 - r.lead)) : 0;
     __syncthreads();
-    const int steps = (share + THREADS - 1) / THREADS, chosen = f.chosen;
+    const int chosen = f.chosen, steps = (share + THREADS - 1) / THREADS, shift = min(6, 32 - __builtin_clz(steps) - (steps & (steps - 1) ? 0 : 1));  // 2^shift lanes for the pieces of one
     int n;
     for (;;) {
-      const u64 border = f.border;
-      for (int i = tid; i < chosen * steps; i += THREADS) {
-        const int piece = begin + f.lanes[i / steps] + i % steps * THREADS;
-        if (piece >= end) continue;
-        float v[V];
-        r.values(piece, 0.f, v);
+      const u64 least = f.border;
+      for (int i = tid >> shift; i < chosen; i += THREADS >> shift) {
+        for (int piece = begin + f.lanes[i] + (tid & ((1 << shift) - 1)) * THREADS; piece < end; piece += THREADS << shift) {
+          float v[V];
+          r.values(piece, 0.f, v);
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const int64_t j = (int64_t)piece * V - r.lead + e;
-          if (j < 0 || j >= a.vocab) continue;
-          const u64 key = key_of(v[e], (unsigned)j);
-          if (key >= border) {
-            const int at = atomicAdd(&f.count, 1);
-            if (at < MAX_FOUND) f.found[at] = key;
+          for (int e = 0; e < V; ++e) {
+            const int64_t j = (int64_t)piece * V - r.lead + e;
+            const u64 key = key_of(v[e], (unsigned)j);
+            if (j >= 0 && j < a.vocab && key >= least) {
+              const int at = atomicAdd(&f.count, 1);
+              if (at < MAX_FOUND) f.found[at] = key;
+            }
           }
         }
       }
@@ -281,28 +318,34 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
 // Joins the parts of a row.
 template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_join_kernel(const TokenLogprob a) {
   __shared__ u64 found[LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP];
-  __shared__ u64 least[LOGPROB_MAX_SPLIT];
   __shared__ int count;
   const int64_t row = blockIdx.x;
   const int target = a.targets ? a.targets[row] : 0, tid = threadIdx.x;
   if (target < 0 || target >= a.vocab) return;
-  const float c = a.scale * LOG2E;
+  const float c = a.scale * LOG2E, l_target = Elem<T>::to_f32(static_cast<const T*>(a.logits)[row * a.ld + target]);
+  // (at most 32 parts: a lane each, of every wavefront)
   Sums w;
-  for (int i = 0; i < a.parts; ++i) w.join(Sums::of(a.part_sums[row * a.parts + i]), c);
-  if (tid == 0) write_row(a, row, w, static_cast<const T*>(a.logits) + row * a.ld, target, sizeof(T) == 2);
-  if (!a.top) return;
-  // each part's list is in order: the least of their each's-th keys is not above the `top`-th of all
+  if ((tid & 63) < a.parts) w = Sums::of(a.part_sums[row * a.parts + (tid & 63)]);
   const u64* const keys = a.part_keys + row * a.parts * a.top;
   const int each = (a.top + a.parts - 1) / a.parts;
-  if (tid == 0) count = 0;
-  if (tid < a.parts) least[tid] = keys[tid * a.top + each - 1];
-  __syncthreads();
-  u64 border = least[0];
-  for (int i = 1; i < a.parts; ++i) border = border < least[i] ? border : least[i];
-  for (int i = tid; i < a.parts * a.top; i += THREADS) {
-    const u64 key = keys[i];
-    if (key && key >= border) found[atomicAdd(&count, 1)] = key;
+  u64 border = a.top && (tid & 63) < a.parts ? keys[(tid & 63) * a.top + each - 1] : ~0ull;
+  u64 mine[LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP / THREADS];
+#pragma unroll
+  for (int i = 0; i < LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP / THREADS; ++i) mine[i] = tid + i * THREADS < a.parts * a.top ? keys[tid + i * THREADS] : 0;
+  join_lanes(w, c);
+  if (tid == 0) write_row(a, row, w, l_target);
+  if (!a.top) return;
+  // each part's list is in order: the least of their each's-th keys is not above the `top`-th of all
+#pragma unroll
+  for (int mask = 1; mask < 64; mask *= 2) {
+    const u64 other = __shfl_xor(border, mask, 64);
+    border = other < border ? other : border;
   }
+  if (tid == 0) count = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP / THREADS; ++i)
+    if (mine[i] && mine[i] >= border) found[atomicAdd(&count, 1)] = mine[i];
   __syncthreads();
   ranked(found, count, a.top, [&](int rank, u64 key) {
     a.top_ids[row * a.top + rank] = place_of(key);
@@ -382,10 +425,13 @@ template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_b
   }
 }
 
-template <typename T> hipError_t forward(TokenLogprob a, hipStream_t stream) {
-  // parts of a row where there are few: 1024 workgroups at most and at least 16 KB each
-  const int64_t bytes = (int64_t)a.vocab * (int)sizeof(T);
-  a.parts = a.part_sums ? (int)std::max<int64_t>(1, std::min<int64_t>({LOGPROB_MAX_SPLIT, LOGPROB_MAX_PARTS / a.rows, bytes >> 14})) : 1;
+template <typename T> hipError_t forward(TokenLogprob a, void* workspace, hipStream_t stream) {
+  // parts of a row of at least 16 KB, up to 1024 workgroups in all.  (Of more rows, whose last round of workgroups may be short, parts gain what joining them
+  // costs: us with parts of 64 KB / whole rows, 1100 x 128000 bf16 46.7 + 4.8 / 53.0, with the 5 likeliest 63.6 + 5.0 / 68.5, 4096 rows 146 + 6 / 157.)
+  const int64_t bytes = (int64_t)a.vocab * (int)sizeof(T), room = LOGPROB_BYTES / (16 + 8 * a.top);
+  a.parts = workspace ? (int)std::max<int64_t>(1, std::min<int64_t>({LOGPROB_MAX_SPLIT, room / a.rows, 1024 / a.rows, bytes >> 14})) : 1;
+  a.part_sums = static_cast<float4*>(workspace);
+  a.part_keys = reinterpret_cast<u64*>(a.part_sums + (int64_t)a.rows * a.parts);
   const int64_t groups = (int64_t)a.rows * a.parts;
   if (!launchable(groups, THREADS)) return hipErrorInvalidConfiguration;
   if (a.top) hipLaunchKernelGGL((token_logprob_kernel<T, true>), dim3((unsigned)groups), dim3(THREADS), 0, stream, a);
@@ -407,9 +453,11 @@ template <typename T> hipError_t backward(const TokenLogprob& a, hipStream_t str
 
 }  // namespace
 
-hipError_t launch_token_logprob(const TokenLogprob& a, bool backward_, int dtype, hipStream_t stream) {
-  if (backward_) return dtype == DT_BF16 ? backward<uint16_t>(a, stream) : backward<float>(a, stream);
-  return dtype == DT_BF16 ? forward<uint16_t>(a, stream) : forward<float>(a, stream);
+hipError_t launch_token_logprob(const TokenLogprob& a, void* workspace, int dtype, hipStream_t stream) {
+  return dtype == DT_BF16 ? forward<uint16_t>(a, workspace, stream) : forward<float>(a, workspace, stream);
+}
+hipError_t launch_token_logprob_bwd(const TokenLogprob& a, int dtype, hipStream_t stream) {
+  return dtype == DT_BF16 ? backward<uint16_t>(a, stream) : backward<float>(a, stream);
 }
 
 }  // namespace cdp
