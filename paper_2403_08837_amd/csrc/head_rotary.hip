@@ -1,6 +1,7 @@
 // Norms of query and key heads and the rotation of their pairs by position, in one pass over qkv[tokens][heads + 2 kv_heads][width], with the gradients:
 //   n = x rho gamma, rho = 1 / sqrt(mean x^2 + eps);  a pair (p, q) of n becomes (p cos - q sin, q cos + p sin), angle = position * freq;  v heads are copied.
-// Backward: the pairs of dout turned back are dn;  a = dn gamma, hat = x rho:  dx = rho (a - hat mean(a hat)),  dgamma = sum dn hat.
+// Backward: the pairs of dout turned back are dn;  a = dn gamma, hat = x rho:  dx = rho (a - hat mean(a hat)),  dgamma = sum dn hat.  Without norms that is the forward,
+// turned the other way.
 //
 // Bound by memory: a head is read and written once (backward: x and dout read, dx written).  A lane holds V pairs of a head, as two vectors of V neighbouring
 // values (16 bytes each where the sizes allow), so that a pair never crosses lanes and the norm is one sum over the G lanes of a head, backward two at once.  The
@@ -17,7 +18,7 @@ namespace cdp {
 
 namespace {
 
-constexpr int THREADS = 256, MAX_TOKENS = 8, MAX_PAIRS = 64;
+constexpr int THREADS = 256, MAX_TOKENS = 16, MAX_PAIRS = 64;
 
 template <typename T, int V> struct alignas(V * sizeof(T)) Vec { T e[V]; };
 
@@ -51,63 +52,81 @@ template <int V, bool INTER> constexpr int second_of(int j) { return INTER ? 2 *
 template <typename T, int V, bool INTER, int G, bool BACKWARD>
 __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a, int per) {
   using Values = Vec<T, V>;
-  constexpr int SLOTS = THREADS / G;
-  __shared__ __attribute__((aligned(16))) float2 turn[MAX_TOKENS * MAX_PAIRS];
+  constexpr int SLOTS = THREADS / G, AT_ONCE = BACKWARD ? 2 : 1;  // heads of a lane that are on their way together
+  __shared__ __attribute__((aligned(16))) float2 turns[BACKWARD ? 2 : 1][MAX_TOKENS * MAX_PAIRS];
   const int W = a.width, R = a.rotary, pairs = W / 2, c = threadIdx.x % G, slot = threadIdx.x / G;
   const int normed = a.heads + a.kv_heads, all = normed + a.kv_heads;
   const bool has = c * V < pairs;
   const Place at = place<V, INTER>(has ? c : 0, W, R);
   const float inv = 1.f / W;
-  float gq[2 * V], gk[2 * V], sq[BACKWARD ? 2 * V : 1], sk[BACKWARD ? 2 * V : 1];
-#pragma unroll
-  for (int i = 0; i < 2 * V; ++i) {
-    const int o = i < V ? at.o0 + i : at.o1 + i - V;
-    gq[i] = a.gamma_q ? a.gamma_q[o] : 1.f;
-    gk[i] = a.gamma_k ? a.gamma_k[o] : 1.f;
-    if constexpr (BACKWARD) sq[i] = sk[i] = 0.f;
+  __shared__ __attribute__((aligned(16))) float gammas[2][2 * MAX_PAIRS];  // of q and k heads; ones where there is none
+  if ((int)threadIdx.x < W) {
+    gammas[0][threadIdx.x] = a.gamma_q ? a.gamma_q[threadIdx.x] : 1.f;
+    gammas[1][threadIdx.x] = a.gamma_k ? a.gamma_k[threadIdx.x] : 1.f;
   }
+  float sq[BACKWARD ? 2 * V : 1], sk[BACKWARD ? 2 * V : 1];
+  if constexpr (BACKWARD)
+#pragma unroll
+    for (int i = 0; i < 2 * V; ++i) sq[i] = sk[i] = 0.f;
   const int64_t groups = ((int64_t)a.tokens + per - 1) / per;
+  // backward the next group's angles are made ahead of this one's heads, into the other half
+  auto angles_of = [&](int64_t group, float2* turn) {
+    const int64_t token0 = group * per;
+    const int n = (int)min((int64_t)per, a.tokens - token0) * pairs;
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+      const int t = i / pairs, p = i - t * pairs;
+      float2 w = 2 * p < R ? turned(a.positions[token0 + t], a.freqs[p]) : make_float2(1.f, 0.f);
+      if (a.back) w.y = -w.y;
+      turn[t * MAX_PAIRS + p] = w;
+    }
+  };
+  int half = 0;
+  angles_of(blockIdx.x, turns[0]);
   for (int64_t group = blockIdx.x; group < groups; group += gridDim.x) {
     const int64_t token0 = group * per;
     const int tokens = (int)min((int64_t)per, a.tokens - token0);
-    if (BACKWARD && group != blockIdx.x) __syncthreads();  // the angles before have been used
-    for (int i = threadIdx.x; i < tokens * pairs; i += THREADS) {
-      const int t = i / pairs, p = i - t * pairs;
-      turn[t * MAX_PAIRS + p] = 2 * p < R ? turned(a.positions[token0 + t], a.freqs[p]) : make_float2(1.f, 0.f);
-    }
     __syncthreads();
-    int t = slot / all, h = slot - t * all;
-    for (; t < tokens; h += SLOTS) {
-      while (h >= all) {
-        h -= all;
-        ++t;
-      }
-      if (t >= tokens) break;
-      if (a.in_place && h >= normed) continue;  // (heads go to lanes alike in place or not, and sums have one order)
-      const int64_t base = ((token0 + t) * all + h) * W;
+    const float2* const turn = turns[half];
+    if (BACKWARD) {
+      half ^= 1;
+      if (group + gridDim.x < groups) angles_of(group + gridDim.x, turns[half]);
+    }
+    struct Item {
+      int t, h;
+      Values lo, hi, x_lo, x_hi;
+    };
+    auto request = [&](Item& w) {
+      if (!has || w.t >= tokens || (a.in_place && w.h >= normed)) return;
+      const int64_t base = ((token0 + w.t) * all + w.h) * W;
       const T* const from = static_cast<const T*>(BACKWARD ? a.dout : a.qkv) + base;
-      T* const to = static_cast<T*>(BACKWARD ? a.dqkv : a.out) + base;
-      Values lo, hi;
-      if (has) {
-        lo = *reinterpret_cast<const Values*>(from + at.o0);
-        hi = *reinterpret_cast<const Values*>(from + at.o1);
+      w.lo = *reinterpret_cast<const Values*>(from + at.o0);
+      w.hi = *reinterpret_cast<const Values*>(from + at.o1);
+      if (BACKWARD && w.h < normed) {  // (both at once: one round trip)
+        const T* const was = static_cast<const T*>(a.qkv) + base;
+        w.x_lo = *reinterpret_cast<const Values*>(was + at.o0);
+        w.x_hi = *reinterpret_cast<const Values*>(was + at.o1);
       }
+    };
+    auto finish = [&](Item& w) {
+      const int t = w.t, h = w.h;
+      if (t >= tokens || (a.in_place && h >= normed)) return;  // (heads go to lanes alike in place or not, and sums have one order)
+      T* const to = static_cast<T*>(BACKWARD ? a.dqkv : a.out) + ((token0 + t) * all + h) * W;
+      Values &lo = w.lo, &hi = w.hi, &x_lo = w.x_lo, &x_hi = w.x_hi;
       if (h >= normed) {
         if (has) {
           *reinterpret_cast<Values*>(to + at.o0) = lo;
           *reinterpret_cast<Values*>(to + at.o1) = hi;
         }
-        continue;
+        return;
       }
       const bool is_q = h < a.heads, norm = is_q ? a.gamma_q != nullptr : a.gamma_k != nullptr;
-      float v[2 * V], x[BACKWARD ? 2 * V : 1], cs[V], sn[V];
+      const float* const gamma = gammas[is_q ? 0 : 1];
+      const float2* const angles = turn + t * MAX_PAIRS + (has ? c : 0) * V;
+      float v[2 * V];
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         v[i] = has ? Elem<T>::to_f32(lo.e[i]) : 0.f;
         v[V + i] = has ? Elem<T>::to_f32(hi.e[i]) : 0.f;
-        const float2 w = turn[t * MAX_PAIRS + (has ? c : 0) * V + i];
-        cs[i] = w.x;
-        sn[i] = w.y;
       }
       if constexpr (!BACKWARD) {
         if (norm) {
@@ -116,33 +135,30 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
           for (int i = 0; i < 2 * V; ++i) s += v[i] * v[i];
           const float rho = rsqrtf(lanes_sum<G>(s) * inv + a.eps);
 #pragma unroll
-          for (int i = 0; i < 2 * V; ++i) v[i] = v[i] * rho * (is_q ? gq[i] : gk[i]);
+          for (int i = 0; i < 2 * V; ++i) v[i] = v[i] * rho * gamma[i < V ? at.o0 + i : at.o1 + i - V];
         }
 #pragma unroll
         for (int j = 0; j < V; ++j) {
+          const float2 w = angles[j];
           const float p = v[first_of<V, INTER>(j)], q = v[second_of<V, INTER>(j)];
-          v[first_of<V, INTER>(j)] = p * cs[j] - q * sn[j];
-          v[second_of<V, INTER>(j)] = q * cs[j] + p * sn[j];
+          v[first_of<V, INTER>(j)] = p * w.x - q * w.y;
+          v[second_of<V, INTER>(j)] = q * w.x + p * w.y;
         }
       } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
+          const float2 w = angles[j];
           const float p = v[first_of<V, INTER>(j)], q = v[second_of<V, INTER>(j)];
-          v[first_of<V, INTER>(j)] = p * cs[j] + q * sn[j];
-          v[second_of<V, INTER>(j)] = q * cs[j] - p * sn[j];
+          v[first_of<V, INTER>(j)] = p * w.x - q * w.y;
+          v[second_of<V, INTER>(j)] = q * w.x + p * w.y;
         }
         if (norm) {
-          if (has) {
-            const T* const was = static_cast<const T*>(a.qkv) + base;
-            lo = *reinterpret_cast<const Values*>(was + at.o0);
-            hi = *reinterpret_cast<const Values*>(was + at.o1);
-          }
-          float ss = 0.f, sa = 0.f;
+          float x[2 * V], ss = 0.f, sa = 0.f;
 #pragma unroll
           for (int i = 0; i < 2 * V; ++i) {
-            x[i] = has ? Elem<T>::to_f32(i < V ? lo.e[i] : hi.e[i - V]) : 0.f;
+            x[i] = has ? Elem<T>::to_f32(i < V ? x_lo.e[i] : x_hi.e[i - V]) : 0.f;
             ss += x[i] * x[i];
-            sa += v[i] * (is_q ? gq[i] : gk[i]) * x[i];
+            sa += v[i] * gamma[i < V ? at.o0 + i : at.o1 + i - V] * x[i];
           }
           const float rho = rsqrtf(lanes_sum<G>(ss) * inv + a.eps), mean = rho * (lanes_sum<G>(sa) * inv);
 #pragma unroll
@@ -150,7 +166,7 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
             const float hat = x[i] * rho, g = v[i] * hat;
             if (is_q) sq[i] += g;
             else sk[i] += g;
-            v[i] = rho * (v[i] * (is_q ? gq[i] : gk[i]) - hat * mean);
+            v[i] = rho * (v[i] * gamma[i < V ? at.o0 + i : at.o1 + i - V] - hat * mean);
           }
         }
       }
@@ -163,10 +179,21 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
         *reinterpret_cast<Values*>(to + at.o0) = lo;
         *reinterpret_cast<Values*>(to + at.o1) = hi;
       }
+    };
+    Item w[AT_ONCE];
+    for (int t = slot / all, h = slot - t * all; t < tokens;) {
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        w[u].t = t;
+        w[u].h = h;
+        request(w[u]);
+        for (h += SLOTS; h >= all; h -= all) ++t;
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) finish(w[u]);
     }
   }
   if constexpr (BACKWARD) {
-    if (!a.dgamma_q && !a.dgamma_k) return;
     // the heads that a wavefront has at once between its lanes, its four wavefronts through LDS
     __shared__ float join[4][2 * MAX_PAIRS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -214,7 +241,7 @@ template <typename T, int V, bool INTER, int G> hipError_t launch(const HeadRota
   constexpr int SLOTS = THREADS / G;
   // tokens at once: enough heads to fill a workgroup a few times, fewer where that leaves less than two workgroups a CU
   const int heads = a.heads + 2 * a.kv_heads;
-  int per = std::max(1, std::min(MAX_TOKENS, 4 * SLOTS / heads));
+  int per = std::max(1, std::min(MAX_TOKENS, (backward ? 8 : 4) * SLOTS / heads));
   while (per > 1 && (a.tokens + per - 1) / per < 512) per /= 2;
   const int64_t groups = ((int64_t)a.tokens + per - 1) / per;
   if (!backward) {
@@ -222,20 +249,22 @@ template <typename T, int V, bool INTER, int G> hipError_t launch(const HeadRota
     hipLaunchKernelGGL((head_rotary_kernel<T, V, INTER, G, false>), dim3((unsigned)groups), dim3(THREADS), 0, stream, a, per);
     return hipGetLastError();
   }
-  const bool sums = a.dgamma_q || a.dgamma_k;
-  // a few groups are one workgroup's: a second launch for the sums costs more than it saves
-  const int parts = sums && groups <= 4 ? 1 : (int)std::min<int64_t>(groups, HEAD_ROTARY_MAX_PARTS);
-  hipLaunchKernelGGL((head_rotary_kernel<T, V, INTER, G, true>), dim3(parts), dim3(THREADS), 0, stream, a, per);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || parts == 1 || !sums) return e;
-  hipLaunchKernelGGL(head_rotary_fold_kernel, dim3(a.width / 8, 2), dim3(THREADS), 0, stream, a, parts);
-  return hipGetLastError();
+  if constexpr (V == 8) return hipErrorInvalidValue;  // (`any` takes fewer values at once: 131 us instead of 114 for 16384 tokens of 48 x 128, for want of registers)
+  else {
+    // a few groups are one workgroup's: a second launch for the sums costs more than it saves
+    const int parts = groups <= 4 ? 1 : (int)std::min<int64_t>(groups, HEAD_ROTARY_MAX_PARTS);
+    hipLaunchKernelGGL((head_rotary_kernel<T, V, INTER, G, true>), dim3(parts), dim3(THREADS), 0, stream, a, per);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || parts == 1) return e;
+    hipLaunchKernelGGL(head_rotary_fold_kernel, dim3(a.width / 8, 2), dim3(THREADS), 0, stream, a, parts);
+    return hipGetLastError();
+  }
 }
 template <typename T> hipError_t any(const HeadRotary& a, bool backward, hipStream_t stream) {
   const int W = a.width, both = a.rotary / 2 | (W - a.rotary) / 2;  // vectors begin at multiples of what divides both
   if (a.interleaved) return W <= 64 ? launch<T, 4, true, 8>(a, backward, stream) : launch<T, 4, true, 16>(a, backward, stream);
   if constexpr (sizeof(T) == 2)
-    if (both % 8 == 0) return W <= 64 ? launch<T, 8, false, 4>(a, backward, stream) : launch<T, 8, false, 8>(a, backward, stream);
+    if (both % 8 == 0 && !backward) return W <= 64 ? launch<T, 8, false, 4>(a, backward, stream) : launch<T, 8, false, 8>(a, backward, stream);
   if (both % 4 == 0) return W <= 64 ? launch<T, 4, false, 8>(a, backward, stream) : launch<T, 4, false, 16>(a, backward, stream);
   if (both % 2 == 0) return launch<T, 2, false, 32>(a, backward, stream);
   return launch<T, 1, false, 64>(a, backward, stream);
@@ -245,7 +274,14 @@ template <typename T> hipError_t any(const HeadRotary& a, bool backward, hipStre
 
 int64_t head_rotary_bwd_workspace_bytes(int tokens, int width) { return 8ll * width * std::min(tokens, HEAD_ROTARY_MAX_PARTS) + 256; }
 
-hipError_t launch_head_rotary(const HeadRotary& a, bool backward, int dtype, hipStream_t stream) {
+hipError_t launch_head_rotary(const HeadRotary& given, bool backward, int dtype, hipStream_t stream) {
+  HeadRotary a = given;
+  a.back = backward;
+  if (backward && !a.dgamma_q && !a.dgamma_k) {  // without norms: forward, turned the other way
+    a.qkv = a.dout;
+    a.out = a.dqkv;
+    backward = false;
+  }
   return dtype == DT_BF16 ? any<uint16_t>(a, backward, stream) : any<float>(a, backward, stream);
 }
 

@@ -411,6 +411,7 @@ struct HeadRotary {
   float *dgamma_q, *dgamma_k, *part;
   int tokens, heads, kv_heads, width, rotary, interleaved, accumulate;
   int in_place;                        // the result is where the input was: v heads stay
+  int back;                            // pairs are turned back
   float eps;
 };
 constexpr int HEAD_ROTARY_MAX_PARTS = 1024;
