@@ -195,10 +195,10 @@ template <int TILE, int NWAVE, int BK, bool SLOW> struct Slabs {
   static constexpr int BYTES = TILE * BK * 2, LP = BYTES / 1024 / NWAVE;                    // loads of a wavefront per slab
   static_assert(LP * 1024 * NWAVE == BYTES && CPR <= 64 && TILE >= 64, "tile rows are dealt to the wavefronts in 1 KB blocks");
   unsigned off[LP];  // byte offsets from the tile's first element in this slab, ~0: outside
-  static constexpr int KINDS = BK == 64 ? 2 : 4;
+  static constexpr int KINDS = BK == 32 ? 1 : BK == 64 ? 2 : 4;
   int chunk[KINDS];  // !SLOW: first reduction index, in the slab, of the chunk of load i: the same for loads KINDS apart
   // chunk c of tile row r sits in slot c ^ swz(r)
-  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : BK == 64 ? (r >> 1) & 7 : r & 15; }
+  static __device__ __forceinline__ int swz(int r) { return SLOW ? 4 * piece(r) : BK == 32 ? (r >> 2) & 3 : BK == 64 ? (r >> 1) & 7 : r & 15; }
   static __device__ __forceinline__ int piece(int r) { return TILE >= 128 ? r & 3 : (r >> 1) & 1; }  // SLOW: 64-byte pieces of four rows on banks of their own
   // row_of: tile row -> row of the matrix, from the tile's first; `first` of `size` rows (SLOW: columns)
   template <typename F> __device__ __forceinline__ void start(int wave, int lane, int first, int size, int ld, F&& row_of) {
@@ -209,7 +209,7 @@ template <int TILE, int NWAVE, int BK, bool SLOW> struct Slabs {
       else off[i] = 2u * ((unsigned)min(row_of(r), size - 1 - first) * (unsigned)ld + c * 8);  // rows past the last repeat it
       if (!SLOW && i < KINDS) chunk[i] = c * 8;
     }
-    static_assert(SLOW || ((BK == 64 || BK == 128) && LP % KINDS == 0), "rows of a load and of the one KINDS on swizzle alike");
+    static_assert(SLOW || ((BK == 32 || BK == 64 || BK == 128) && LP % KINDS == 0), "rows of a load and of the one KINDS on swizzle alike");
   }
   // `left` reduction indices in the slab: what is past them reads as zero.  SLOW: they are rows, and the buffer ends there.
   __device__ __forceinline__ unsigned place(int i, int left) const { return SLOW || chunk[i & (KINDS - 1)] < left ? off[i] : ~0u; }
@@ -502,6 +502,10 @@ __device__ __forceinline__ void product_body(const Product& P, int block, unsign
       if (!ROUNDS && t == 2) break;
       step(std::integral_constant<int, 2>{});
     }
+    if constexpr (STAGES > 3) {
+      if (!ROUNDS && t == 3) break;
+      step(std::integral_constant<int, 3>{});
+    }
   }
   wait_newest<0>();  // no load is left that writes LDS when this workgroup gives it back
   leave<WHAT, T>(P, acc, at.row0 + wm * WTM, at.col0 + wn * (DUAL ? WTN / 2 : WTN), at.split, at.second, lane);
@@ -664,11 +668,13 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
 
 // ---- kernels ----------------------------------------------------------------------------------------------------------
 // Tiles by size: 0 64 x 64 in slabs of 128, 1 64 x 128, 2 128 x 128, all with two workgroups a CU, 3 256 x 256, one a CU.  A gated map's wavefronts have 64 columns or more.
+// us, products of 8192 x 4096 x 12288: 256 x 256 with two slabs of 64 / four of 32, gated forward 1357 / 1420, both backward 2563 / 2504; with four wavefronts of 128 x 128
+// instead of eight of 128 x 64 1418 / 2664 (and they spill).
 template <int WHAT, typename T, int SIZE> struct Tile {
-  static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED;
+  static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED, BACK = WHAT == DGRAD || WHAT == WGRAD;
   static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 || (SIZE == 0 && EXACT && DUAL) ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
   static constexpr int WAVES_M = SIZE == 0 && EXACT && DUAL ? 4 : 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
-  static constexpr int BK = EXACT ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 1 ? 3 : 2;
+  static constexpr int BK = EXACT || (SIZE == 3 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 3 && BACK ? 4 : SIZE == 1 ? 3 : 2;
   static constexpr int AHEAD = 2;  // EXACT
   static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
   static constexpr int WAVES = LDS > 80 * 1024 || THREADS < 256 ? (THREADS + 255) / 256 : 2;  // a SIMD, as LDS allows: registers for them
@@ -844,7 +850,7 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
-constexpr int SIZES = 4, SLAB_OF[SIZES] = {128, 64, 64, 64}, SLAB_OF_F32 = 32;
+int slab_of(int what, int size, bool f32) { return f32 || (size == 3 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
 // Tiles of a product by size.
 int64_t tiles_of(const Product& p, int what, int size, bool f32) {
   const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
@@ -867,7 +873,7 @@ template <int N> int size_for(const Product* const (&p)[N], const int (&what)[N]
 // Tiles and parts of a product; `slabs_each`: slabs that a workgroup should have at least.
 bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t room) {
   const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
-  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size];
+  const int bk = slab_of(what, size, f32);
   p.tiles_m = (int)(((int64_t)p.M + bm - 1) / bm);
   p.tiles_n = (p.N + bn - 1) / bn;
   const int64_t tiles = tiles_of(p, what, size, f32), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
@@ -882,7 +888,7 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
 // 1024 (256), about 4 us.  Mean of 60 forward and backward passes of few tiles, us, with 128, 256, 512 at least and 1024 saved: 16.7, 16.2, 16.2 (with 256 and 2048 saved: 16.3, 16.6);
 // fp32 28.5, 29.0, 31.9 (with 256 saved 26.9, 27.9, 30.8).
 template <int N> int64_t slabs_each(const Product* const (&p)[N], const int (&what)[N], int size, bool f32) {
-  const int bk = f32 ? SLAB_OF_F32 : SLAB_OF[size], least = f32 ? 128 : 256, saved = f32 ? 256 : 1024;
+  const int bk = slab_of(what[0], size, f32), least = f32 ? 128 : 256, saved = f32 ? 256 : 1024;
   int64_t work = 0, most = 1;
   for (int i = 0; i < N; ++i) {
     if (!p[i]->K) continue;
