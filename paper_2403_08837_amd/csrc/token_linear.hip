@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <climits>
+#include <cmath>
 #include <cstring>
 
 namespace cdp {
@@ -672,8 +673,8 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
 // instead of eight of 128 x 64 1418 / 2664 (and they spill).
 template <int WHAT, typename T, int SIZE> struct Tile {
   static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED, BACK = WHAT == DGRAD || WHAT == WGRAD;
-  static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 || (SIZE == 0 && EXACT && DUAL) ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
-  static constexpr int WAVES_M = SIZE == 0 && EXACT && DUAL ? 4 : 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
+  static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
+  static constexpr int WAVES_M = 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
   static constexpr int BK = EXACT || (SIZE == 3 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 3 && BACK ? 4 : SIZE == 1 ? 3 : 2;
   static constexpr int AHEAD = 2;  // EXACT
   static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
@@ -852,31 +853,17 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 // ---- launches ---------------------------------------------------------------------------------------------------------
 int slab_of(int what, int size, bool f32) { return f32 || (size == 3 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
 // Tiles of a product by size.
-int64_t tiles_of(const Product& p, int what, int size, bool f32) {
-  const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
+int64_t tiles_of(const Product& p, int what, int size) {
+  const int bm = size == 3 ? 256 : size == 2 ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
   return (((int64_t)p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * (p.pair ? 2 : 1);
-}
-// Workgroups that run at once.
-int resident(int size, bool f32) { return size == 3 || (size == 2 && f32) ? 256 : size == 0 && f32 ? 768 : 512; }
-// The smallest tiles that all run at once, else 128 x 128, or 256 x 256 where they are a CU's worth or more.
-template <int N> int size_for(const Product* const (&p)[N], const int (&what)[N], bool f32) {
-  auto all = [&](int size) {
-    int64_t n = 0;
-    for (int i = 0; i < N; ++i) n += p[i]->K ? tiles_of(*p[i], what[i], size, f32) : 0;
-    return n;
-  };
-  if (!f32 && all(3) >= 256) return 3;
-  for (int size = 0; size < 2; ++size)
-    if (all(size) <= resident(size, f32)) return size;
-  return 2;
 }
 // Tiles and parts of a product; `slabs_each`: slabs that a workgroup should have at least.
 bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t room) {
-  const int bm = size == 3 ? 256 : size == 2 || (size == 0 && f32 && what == GATED) ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
+  const int bm = size == 3 ? 256 : size == 2 ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
   const int bk = slab_of(what, size, f32);
   p.tiles_m = (int)(((int64_t)p.M + bm - 1) / bm);
   p.tiles_n = (p.N + bn - 1) / bn;
-  const int64_t tiles = tiles_of(p, what, size, f32), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
+  const int64_t tiles = tiles_of(p, what, size), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
   if (!launchable(tiles, 512) || slabs > INT32_MAX) return false;
   p.tiles = (int)tiles;
   const int64_t splits = std::max<int64_t>(1, std::min(slabs / slabs_each, room / (4 * results)));
@@ -884,20 +871,55 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
   return launchable((int64_t)p.tiles * p.splits, 512);
 }
-// Slabs that a workgroup should have for all to run at once, 256 reduction indices at least (fp32: 128); not shared where that saves fewer indices than joining costs,
-// 1024 (256), about 4 us.  Mean of 60 forward and backward passes of few tiles, us, with 128, 256, 512 at least and 1024 saved: 16.7, 16.2, 16.2 (with 256 and 2048 saved: 16.3, 16.6);
-// fp32 28.5, 29.0, 31.9 (with 256 saved 26.9, 27.9, 30.8).
-template <int N> int64_t slabs_each(const Product* const (&p)[N], const int (&what)[N], int size, bool f32) {
-  const int bk = slab_of(what[0], size, f32), least = f32 ? 128 : 256, saved = f32 ? 256 : 1024;
-  int64_t work = 0, most = 1;
-  for (int i = 0; i < N; ++i) {
-    if (!p[i]->K) continue;
-    const int64_t slabs = ((int64_t)p[i]->K + bk - 1) / bk * p[i]->segments;
-    work += tiles_of(*p[i], what[i], size, f32) * slabs;
-    most = std::max(most, slabs);
+// Tiles and slabs a workgroup for products of one launch: the least of the times that the following gives.  A CU takes `slab` us for a slab of a tile, and `tile` us for
+// what else there is to one (for those that it has at a time); all CUs as long as the one with the most.  Joining costs a launch and its memory.  The figures are fitted to
+// products of 14 shapes at every size; over 80 passes of the range each, the mean time is 0.95 of that with the smallest tiles that all run at once (fp32), 1.0 (bf16).
+struct Choice {
+  int size;
+  int64_t each;
+};
+template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room) {
+  struct Cost { double slab, tile; int resident; };
+  static constexpr Cost BF16[4] = {{0.40, 1.0, 512}, {0.30, 1.6, 512}, {0.49, 2.0, 512}, {1.60, 5.0, 256}}, F32[3] = {{0.45, 1.5, 768}, {0.78, 2.0, 512}, {1.47, 7.0, 256}};
+  Choice best = {0, INT32_MAX};
+  double least = 1e30;
+  for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 4); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
+    const Cost cost = f32 ? F32[size] : BF16[size];
+    int64_t tiles[N], slabs[N], most = 1;
+    double unit[N];  // of a slab
+    for (int i = 0; i < N; ++i) {
+      const int bk = slab_of(what[i], size, f32);
+      tiles[i] = p[i]->K ? tiles_of(*p[i], what[i], size) : 0;
+      slabs[i] = p[i]->K ? ((int64_t)p[i]->K + bk - 1) / bk * p[i]->segments : 0;
+      // (of 64 x 64 tiles whose reduction is the slow index of both operands the time a slab is twice that: 136 x 680 x 5273 0.8 us)
+      unit[i] = cost.slab * bk / slab_of(LINEAR, size, f32) * (what[i] == WGRAD && size == 0 && !f32 ? 2 : 1);
+      most = std::max(most, slabs[i]);
+    }
+    for (int64_t parts = 1; parts <= 32; parts += parts < 4 ? 1 : parts / 2) {
+      const int64_t each = (most + parts - 1) / parts;
+      if (parts > 1 && each * slab_of(what[0], size, f32) < (f32 ? 128 : 256)) break;
+      double work = 0, longest = 0, join = 0, groups = 0, left = (double)room;
+      for (int i = 0; i < N; ++i) {
+        if (!tiles[i]) continue;
+        const double results = (double)p[i]->M * p[i]->N * (what[i] == GATED || p[i]->pair ? 2 : 1);
+        const double splits = std::max(1.0, std::min<double>(parts > 1 ? (double)(slabs[i] / each) : 1.0, std::floor(left / (4 * results))));
+        if (splits > 1) {
+          join = std::max(join, 4.0) + 8e-6 / 4.5 * results * splits;
+          left -= 4 * results * splits;
+        }
+        work += (double)tiles[i] * slabs[i] * unit[i];
+        longest = std::max(longest, slabs[i] / splits * unit[i]);
+        groups += tiles[i] * splits;
+      }
+      const double rounds = std::ceil(groups / 256);
+      const double time = std::max(rounds * work / groups, longest) + std::ceil(groups / cost.resident) * cost.tile + join;
+      if (time < least) {
+        least = time;
+        best = {size, parts > 1 ? each : (int64_t)INT32_MAX};
+      }
+    }
   }
-  const int64_t each = std::max<int64_t>((work + resident(size, f32) - 1) / resident(size, f32), least / bk);
-  return (most - each) * bk < saved ? INT32_MAX : each;
+  return best;
 }
 int64_t join_groups(const Product& p, int what) {
   return p.splits > 1 ? ((int64_t)p.M * p.N * (what != GATED && p.pair ? 2 : 1) / 8 + 255) / 256 : 0;
@@ -910,12 +932,16 @@ template <int WHAT, typename T, int SIZE> void start_product(const Product& p, h
 template <int WHAT, typename T> hipError_t launch_forward(Product& p, int64_t room, hipStream_t stream) {
   constexpr bool F32 = sizeof(T) == 4;
   const Product* const all[1] = {&p};
-  const int what[1] = {WHAT}, size = size_for(all, what, F32);
-  if (!plan(p, WHAT, size, F32, slabs_each(all, what, size, F32), room)) return hipErrorInvalidConfiguration;
-  if (size == 0) start_product<WHAT, T, 0>(p, stream);
-  else if (size == 1) start_product<WHAT, T, 1>(p, stream);
+  const int what[1] = {WHAT};
+  const Choice of = choose(all, what, F32, room);
+  const int size = of.size;
+  if (!plan(p, WHAT, size, F32, of.each, room)) return hipErrorInvalidConfiguration;
+  if (size == 1) start_product<WHAT, T, 1>(p, stream);
   else if (size == 2) start_product<WHAT, T, 2>(p, stream);
-  else if constexpr (!F32) start_product<WHAT, T, 3>(p, stream);
+  else if constexpr (!F32 || WHAT != GATED)
+    if (size == 0) start_product<WHAT, T, 0>(p, stream);
+  if constexpr (!F32)
+    if (size == 3) start_product<WHAT, T, 3>(p, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)join_groups(p, WHAT)), dim3(256), 0, stream, p, (int)WHAT);
@@ -930,8 +956,10 @@ template <typename T, int SIZE> void start_backward(const Product& dw, const Pro
 template <typename T> int plan_backward(Product& dw, Product& dx, const BiasParts& bias, char* at, int64_t room) {  // their size of tiles, or -1
   constexpr bool F32 = sizeof(T) == 4;
   const Product* const all[2] = {&dw, &dx};
-  const int what[2] = {WGRAD, DGRAD}, size = size_for(all, what, F32);
-  const int64_t each = slabs_each(all, what, size, F32);
+  const int what[2] = {WGRAD, DGRAD};
+  const Choice of = choose(all, what, F32, room);
+  const int size = of.size;
+  const int64_t each = of.each;
   dw.part = reinterpret_cast<float*>(at);
   if (dw.K) {
     if (!plan(dw, WGRAD, size, F32, each, room)) return -1;
