@@ -148,15 +148,36 @@ struct Found {
   int count, chosen;
 };
 
-// The `top` largest of keys[0 .. n) in order, by their ranks; out(rank, key).
-template <typename F> __device__ __forceinline__ void ranked(const u64* keys, int n, int top, F&& out) {
-  for (int i = threadIdx.x; i < n; i += THREADS) {
-    const u64 key = keys[i];
-    int rank = 0;
+// The `top` largest of keys[0 .. n) in order, out(rank, key); by all of a workgroup, for which the keys have been written, with room for a power of two of them.  A few by
+// their ranks, more sorted (us, by ranks / sorted: 400 keys 10 / 14, 906 48 / 18).
+template <typename F> __device__ __forceinline__ void ranked(u64* keys, int n, int top, F&& out) {
+  if (n <= 512) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+      const u64 key = keys[i];
+      int rank = 0;
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) rank += keys[j] > key;
-    if (rank < top) out(rank, key);
+      for (int j = 0; j < n; ++j) rank += keys[j] > key;
+      if (rank < top) out(rank, key);
+    }
+    return;
   }
+  int all = 256;
+  while (all < n) all *= 2;
+  for (int i = n + threadIdx.x; i < all; i += THREADS) keys[i] = 0;
+  for (int size = 2; size <= all; size *= 2)
+    for (int apart = size / 2; apart > 0; apart /= 2) {
+      __syncthreads();
+      for (int t = threadIdx.x; t < all / 2; t += THREADS) {
+        const int i = 2 * t - (t & (apart - 1)), j = i + apart;
+        const u64 x = keys[i], y = keys[j];
+        if ((x < y) == ((i & size) == 0)) {
+          keys[i] = y;
+          keys[j] = x;
+        }
+      }
+    }
+  __syncthreads();
+  for (int i = threadIdx.x; i < min(n, top); i += THREADS) out(i, keys[i]);
 }
 
 // What a row is, from its sums.
@@ -249,7 +270,12 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
   }
   const float best = w.m;
   if constexpr (TOP) {
-    const u64 border = border_of(best, best_piece, begin + tid < end, (a.top + WAVES - 1) / WAVES);
+    // the first `of` wavefronts have a share of the border each: those that have the lanes for it, and half of theirs at least (the best of a few lanes is no border)
+    int of = WAVES;
+    while (of > 1 && end - begin - 64 * (of - 1) < 32) --of;
+    if (end - begin < (a.top + of - 1) / of) of = 0;
+    u64 border = of ? ~0ull : 0;
+    if (tid >> 6 < of) border = border_of(best, best_piece, begin + tid < end, (a.top + of - 1) / of);
     if ((tid & 63) == 0) f.borders[tid >> 6] = border;
   }
   join_lanes(w, c);
@@ -264,7 +290,7 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
     else a.part_sums[blockIdx.x] = w.all();
   }
   if constexpr (TOP) {
-    // as many lanes as `top` are not below the least of the wavefronts' borders
+    // as many lanes as `top` are not below the least of the wavefronts' borders (~0: no say)
     u64 border = f.borders[0];
 #pragma unroll
     for (int i = 1; i < WAVES; ++i) border = f.borders[i] < border ? f.borders[i] : border;
@@ -444,7 +470,9 @@ template <typename T> hipError_t forward(TokenLogprob a, void* workspace, hipStr
 template <typename T> hipError_t backward(const TokenLogprob& a, hipStream_t stream) {
   constexpr int V = Elem<T>::VEC;
   const int64_t pieces = ((int64_t)a.vocab + V - 1) / V + 1;
-  const int share = 4 * UNROLL * THREADS;  // 64 KB of a row
+  // 64 KB of a row a workgroup, down to 4 KB where that leaves fewer than four a CU (us so / with 64 KB, 20 x 20803 bf16 3.8 / 8.9)
+  int share = 4 * UNROLL * THREADS;
+  while (share > THREADS && a.rows * ((pieces + share - 1) / share) < 1024) share /= 2;
   const int64_t segments = (pieces + share - 1) / share;
   if (!launchable(a.rows * segments, THREADS)) return hipErrorInvalidConfiguration;
   hipLaunchKernelGGL((token_logprob_bwd_kernel<T>), dim3(a.rows, (unsigned)segments), dim3(THREADS), 0, stream, a, share);
