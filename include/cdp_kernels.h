@@ -181,7 +181,7 @@ int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, 
 
 /* The first half of a gated feed-forward block: h[rows][hidden] = act(g) * u, g = x wg^T, u = x wu^T, from x[rows][in], wg[hidden][in], wu[hidden][in].
  *   act 0: SiLU g * sigmoid(g)    1: exact GELU g * Phi(g)    2: sigmoid(g)    3: g
- * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20.  g and u (both or neither): written too, for the backward.
+ * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20, rows up to 2^30.  g and u (both or neither): written too, for the backward.
  * Sums are fp32.  fp32: factors are taken as three bf16 numbers that add up to them (2^-27 of a factor is left out, and what is below 2^-133) and the three
  * smallest products of those are left out (2^-26); up to 16 rows forward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
  * workspace: none needed (may be NULL).  Where there is one (16-byte aligned), of P times 8 * rows * hidden bytes, few tiles of long sums share their sums over up
@@ -209,7 +209,7 @@ int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* b
 int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
                           size_t workspace_bytes, int rows, int in, int out, void* stream);
 
-/* Of rows of logits, z = scale * logits[row * ld + 0 .. vocab) (scale > 0; ld >= vocab, up to 2^31; vocab up to 2^28), all fp32:
+/* Of rows of logits, z = scale * logits[row * ld + 0 .. vocab) (scale > 0; ld >= vocab, up to 2^31; vocab up to 2^28; |z| within fp32), all fp32:
  *   lse[row] = log sum exp z;  logprob[row] = z[targets[row]] - lse (with targets);  entropy[row] = - sum p log p, p = exp(z - lse) (may be NULL)
  *   top_ids[row][top] (int32), top_logprobs[row][top]: the likeliest tokens in order and their z - lse; of equal logits the lowest id first.
  *   top up to 64 and vocab (0: none)

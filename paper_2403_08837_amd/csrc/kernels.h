@@ -436,7 +436,7 @@ struct TokenLinear {
   int64_t workspace_bytes;
   int rows, in, out, act;
 };
-constexpr int LINEAR_MAX_WIDTH = 1 << 20, LINEAR_MAX_PARTS = 256;
+constexpr int LINEAR_MAX_WIDTH = 1 << 20, LINEAR_MAX_ROWS = 1 << 30, LINEAR_MAX_PARTS = 256;
 int64_t token_linear_bwd_workspace_bytes(int rows, int out, int dtype);
 hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream);
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream);

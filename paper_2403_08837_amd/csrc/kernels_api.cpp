@@ -46,7 +46,7 @@ static bool head_rotary(HeadRotary& a, int dtype, const void* qkv, const int32_t
   return true;
 }
 static bool linear_sizes(int dtype, int act, int rows, int in, int hidden) {
-  return rows > 0 && in > 0 && hidden > 0 && in % 8 == 0 && hidden % 8 == 0 && in <= LINEAR_MAX_WIDTH && hidden <= LINEAR_MAX_WIDTH && act >= TOKEN_SILU &&
+  return rows > 0 && rows <= LINEAR_MAX_ROWS && in > 0 && hidden > 0 && in % 8 == 0 && hidden % 8 == 0 && in <= LINEAR_MAX_WIDTH && hidden <= LINEAR_MAX_WIDTH && act >= TOKEN_SILU &&
          act <= TOKEN_NONE && (dtype == DT_F32 || dtype == DT_BF16);
 }
 static bool logprob_sizes(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, int rows, int vocab) {

@@ -79,7 +79,7 @@ struct Sums {
   __device__ __forceinline__ float4 all() const { return make_float4(m, s, t, 0.f); }
   // the values so far relative to another maximum, not below m
   __device__ __forceinline__ void raise(float to, float c) {
-    const float d = (m - to) * c, f = __builtin_amdgcn_exp2f(d);
+    const float d = fmaxf((m - to) * c, -256.f), f = __builtin_amdgcn_exp2f(d);  // (0 from there on)
     const bool some = m > -INFINITY;  // (else s and t are zero, or NaN)
     t = some ? f * (t + d * s) : t;
     s = some ? f * s : s;
@@ -93,10 +93,11 @@ struct Sums {
     t += b.t;
   }
   template <int V> __device__ __forceinline__ void add(const float (&v)[V], float c) {
-    const float from = m > -INFINITY ? m * c : 0.f;
+    const float from = m > -INFINITY ? m : 0.f;
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float y = fmaf(v[i], c, -from), e = __builtin_amdgcn_exp2f(y);
+      // (the difference first: the product's rounding would be an exponent for logits of 1e9 and more)
+      const float y = (v[i] - from) * c, e = __builtin_amdgcn_exp2f(y);
       s += e;
       t += e * fmaxf(y, -256.f);  // (a value of -infinity has e = 0; one that is NaN is in s)
     }
@@ -389,13 +390,12 @@ template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_b
   const bool alike = (reinterpret_cast<uintptr_t>(out) & 15) == (reinterpret_cast<uintptr_t>(r.at) & 15);
   const int begin = (int)min((int64_t)blockIdx.y * share, (int64_t)r.pieces()), end = min(begin + share, r.pieces());
   const bool wanted = target >= 0 && target < a.vocab;
-  float c = 0.f, from = 0.f, A = 0.f, B = 0.f, at_target = 0.f;
+  float lse = 0.f, A = 0.f, B = 0.f, at_target = 0.f;
   bool some = wanted;
   if (wanted) {
-    const float lse = a.lse[row], dl = a.dlogprob ? a.dlogprob[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
+    lse = a.lse[row];
+    const float dl = a.dlogprob ? a.dlogprob[row] : 0.f, dh = a.dentropy ? a.dentropy[row] : 0.f;
     some = lse != -INFINITY;  // (a row with everything masked has no gradient)
-    c = a.scale * LOG2E;
-    from = lse * LOG2E;
     A = a.scale * (dl + (a.dentropy ? dh * a.entropy[row] : 0.f));
     if (lse != lse) A = lse;
     B = a.scale * dh * LN2;
@@ -417,7 +417,8 @@ template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_b
   auto gradient = [&](int k, float (&v)[V]) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      const float y = fmaxf(fmaf(v[i], c, -from), -256.f);  // (where it is NaN, A is)
+      // a product rounded as lse was, so that the largest of far apart logits has p = 1; not over 1 by lse's rounding; where it is NaN, A is
+      const float z = a.scale * v[i], y = __builtin_amdgcn_fmed3f((z - lse) * LOG2E, -256.f, 0.f);
       v[i] = -(__builtin_amdgcn_exp2f(y) * fmaf(B, y, A));
     }
     const int64_t at = (int64_t)target - ((int64_t)k * V - r.lead);

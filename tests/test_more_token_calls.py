@@ -29,7 +29,7 @@ REFUSED += [("cdp_k_head_norm_rotary_backward", ROT_B, w) for w in (
     dict(dtype=2), dict(qkv=0), dict(dout=0), dict(dqkv=0), dict(gq=0), dict(dgq=0), dict(gk=0), dict(dgk=0), dict(ws=0), dict(ws=P + 8), dict(ws_bytes=8 * 16 * 8 + 255), dict(dout=P + 8),
     dict(dqkv=P + 8), dict(dgq=P + 2), dict(dgk=P + 2), dict(eps=0.0), dict(rotary=3), dict(width=20), dict(tokens=0), dict(gq=0, dgq=0, gk=0, dgk=0, rotary=0), dict(positions=0))]
 REFUSED += [("cdp_k_gated_linear", GATED, w) for w in (
-    dict(dtype=2), dict(act=-1), dict(act=4), dict(x=0), dict(wg=0), dict(wu=0), dict(h=0), dict(g=0), dict(u=0), dict(rows=0), dict(rows=-4), dict(inputs=0),
+    dict(dtype=2), dict(act=-1), dict(act=4), dict(x=0), dict(wg=0), dict(wu=0), dict(h=0), dict(g=0), dict(u=0), dict(rows=0), dict(rows=-4), dict(rows=(1 << 30) + 1), dict(inputs=0),
     dict(inputs=12), dict(hidden=20), dict(hidden=0), dict(inputs=(1 << 20) + 8, ws_bytes=BIG), dict(hidden=(1 << 20) + 8, ws_bytes=BIG), dict(x=P + 8), dict(wg=P + 2), dict(wu=P + 4), dict(h=P + 8), dict(g=P + 8), dict(u=P + 8), dict(ws=P + 8))]
 REFUSED += [("cdp_k_gated_linear_backward", GATED_B, w) for w in (
     dict(dtype=3), dict(act=5), dict(x=0), dict(wg=0), dict(wu=0), dict(g=0), dict(u=0), dict(dh=0), dict(dwg=0), dict(dwu=0), dict(dx=0, dwg=0, dwu=0), dict(ws=0), dict(ws_bytes=4 * 8 * 24 + 1023), dict(dtype=0),
