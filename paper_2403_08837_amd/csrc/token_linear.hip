@@ -675,7 +675,7 @@ template <int WHAT, typename T, int SIZE> struct Tile {
   static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED, BACK = WHAT == DGRAD || WHAT == WGRAD;
   static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
   static constexpr int WAVES_M = 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
-  static constexpr int BK = EXACT || (SIZE == 3 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 3 && BACK ? 4 : SIZE == 1 ? 3 : 2;
+  static constexpr int BK = EXACT || (SIZE >= 2 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE >= 2 && BACK ? 4 : SIZE == 1 ? 3 : 2;
   static constexpr int AHEAD = 2;  // EXACT
   static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
   static constexpr int WAVES = LDS > 80 * 1024 || THREADS < 256 ? (THREADS + 255) / 256 : 2;  // a SIMD, as LDS allows: registers for them
@@ -851,7 +851,7 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
-int slab_of(int what, int size, bool f32) { return f32 || (size == 3 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
+int slab_of(int what, int size, bool f32) { return f32 || (size >= 2 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
 // Tiles of a product by size.
 int64_t tiles_of(const Product& p, int what, int size) {
   const int bm = size == 3 ? 256 : size == 2 ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
@@ -871,7 +871,7 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
   return launchable((int64_t)p.tiles * p.splits, 512);
 }
-// Tiles and slabs a workgroup for products of one launch: the least of the times that the following gives.  A CU takes `slab` us for a slab of a tile, and `tile` us for
+// Tiles and slabs a workgroup for products of one launch: the least of the times that the following gives.  A CU takes `slab` us for a slab of a tile (`alone`: where it has one), and `tile` us for
 // what else there is to one (for those that it has at a time); all CUs as long as the one with the most.  Joining costs a launch and its memory.  The figures are fitted to
 // products of 14 shapes at every size; over 80 passes of the range each, the mean time is 0.95 of that with the smallest tiles that all run at once (fp32), 1.0 (bf16).
 struct Choice {
@@ -879,12 +879,15 @@ struct Choice {
   int64_t each;
 };
 template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room) {
-  struct Cost { double slab, tile; int resident; };
-  static constexpr Cost BF16[4] = {{0.40, 1.0, 512}, {0.30, 1.6, 512}, {0.49, 2.0, 512}, {1.60, 5.0, 256}}, F32[3] = {{0.45, 1.5, 768}, {0.78, 2.0, 512}, {1.47, 7.0, 256}};
+  struct Cost { double slab, alone, tile; int resident; };
+  static constexpr Cost BF16[4] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}},
+                        F32[3] = {{0.45, 0.53, 1.5, 768}, {0.78, 0.85, 2.0, 512}, {1.47, 1.47, 7.0, 256}};
   Choice best = {0, INT32_MAX};
   double least = 1e30;
+  const bool back = what[0] == DGRAD || what[0] == WGRAD;
   for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 4); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
-    const Cost cost = f32 ? F32[size] : BF16[size];
+    Cost cost = f32 ? F32[size] : BF16[size];
+    if (back && size == 2 && !f32) cost.alone = cost.slab;  // (four slabs on their way)
     int64_t tiles[N], slabs[N], most = 1;
     double unit[N];  // of a slab
     for (int i = 0; i < N; ++i) {
@@ -908,7 +911,7 @@ template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N
           left -= 4 * results * splits;
         }
         work += (double)tiles[i] * slabs[i] * unit[i];
-        longest = std::max(longest, slabs[i] / splits * unit[i]);
+        longest = std::max(longest, slabs[i] / splits * unit[i] * cost.alone / cost.slab);
         groups += tiles[i] * splits;
       }
       const double rounds = std::ceil(groups / 256);
