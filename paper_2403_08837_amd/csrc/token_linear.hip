@@ -668,14 +668,16 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
 }
 
 // ---- kernels ----------------------------------------------------------------------------------------------------------
-// Tiles by size: 0 64 x 64 in slabs of 128, 1 64 x 128, 2 128 x 128, all with two workgroups a CU, 3 256 x 256, one a CU.  A gated map's wavefronts have 64 columns or more.
+// Tiles by size: 0 64 x 64 in slabs of 128, 1 64 x 128, 2 128 x 128, 4 the same in slabs of 32, four of them on their way, for tiles that have a CU to themselves, all with two
+// workgroups a CU, 3 256 x 256, one a CU.  A gated map's wavefronts have 64 columns or more.
+// us, size 2 / 4: fewer tiles than CUs, forward 512 x 4096 x 4096 41 / 33, backward 1500 x 1536 x 6144 129 / 114; more, backward of 6272 x 768 x 2048, gated, 85 / 92.
 // us, products of 8192 x 4096 x 12288: 256 x 256 with two slabs of 64 / four of 32, gated forward 1357 / 1420, both backward 2563 / 2504; with four wavefronts of 128 x 128
 // instead of eight of 128 x 64 1418 / 2664 (and they spill).
 template <int WHAT, typename T, int SIZE> struct Tile {
   static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED, BACK = WHAT == DGRAD || WHAT == WGRAD;
-  static constexpr int BM = SIZE == 3 ? 256 : SIZE == 2 ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
+  static constexpr int BM = SIZE == 3 ? 256 : SIZE >= 2 ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
   static constexpr int WAVES_M = 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
-  static constexpr int BK = EXACT || (SIZE >= 2 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE >= 2 && BACK ? 4 : SIZE == 1 ? 3 : 2;
+  static constexpr int BK = EXACT || SIZE == 4 || (SIZE == 3 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 4 || (SIZE == 3 && BACK) ? 4 : SIZE == 1 ? 3 : 2;
   static constexpr int AHEAD = 2;  // EXACT
   static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
   static constexpr int WAVES = LDS > 80 * 1024 || THREADS < 256 ? (THREADS + 255) / 256 : 2;  // a SIMD, as LDS allows: registers for them
@@ -851,16 +853,17 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
 }
 
 // ---- launches ---------------------------------------------------------------------------------------------------------
-int slab_of(int what, int size, bool f32) { return f32 || (size >= 2 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
+int slab_of(int what, int size, bool f32) { return f32 || size == 4 || (size == 3 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
+int rows_of(int size) { return size == 3 ? 256 : size >= 2 ? 128 : 64; }
+int columns_of(int what, int size) { return (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1); }
 // Tiles of a product by size.
 int64_t tiles_of(const Product& p, int what, int size) {
-  const int bm = size == 3 ? 256 : size == 2 ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
+  const int bm = rows_of(size), bn = columns_of(what, size);
   return (((int64_t)p.M + bm - 1) / bm) * ((p.N + bn - 1) / bn) * (p.pair ? 2 : 1);
 }
 // Tiles and parts of a product; `slabs_each`: slabs that a workgroup should have at least.
 bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t room) {
-  const int bm = size == 3 ? 256 : size == 2 ? 128 : 64, bn = (size == 3 ? 256 : size >= 1 ? 128 : 64) / (what == GATED ? 2 : 1);
-  const int bk = slab_of(what, size, f32);
+  const int bm = rows_of(size), bn = columns_of(what, size), bk = slab_of(what, size, f32);
   p.tiles_m = (int)(((int64_t)p.M + bm - 1) / bm);
   p.tiles_n = (p.N + bn - 1) / bn;
   const int64_t tiles = tiles_of(p, what, size), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
@@ -880,14 +883,12 @@ struct Choice {
 };
 template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room) {
   struct Cost { double slab, alone, tile; int resident; };
-  static constexpr Cost BF16[4] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}},
+  static constexpr Cost BF16[5] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}, {0.57, 0.46, 2.0, 512}},
                         F32[3] = {{0.45, 0.53, 1.5, 768}, {0.78, 0.85, 2.0, 512}, {1.47, 1.47, 7.0, 256}};
   Choice best = {0, INT32_MAX};
   double least = 1e30;
-  const bool back = what[0] == DGRAD || what[0] == WGRAD;
-  for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 4); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
-    Cost cost = f32 ? F32[size] : BF16[size];
-    if (back && size == 2 && !f32) cost.alone = cost.slab;  // (four slabs on their way)
+  for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 5); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
+    const Cost& cost = f32 ? F32[size] : BF16[size];
     int64_t tiles[N], slabs[N], most = 1;
     double unit[N];  // of a slab
     for (int i = 0; i < N; ++i) {
@@ -895,7 +896,7 @@ template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N
       tiles[i] = p[i]->K ? tiles_of(*p[i], what[i], size) : 0;
       slabs[i] = p[i]->K ? ((int64_t)p[i]->K + bk - 1) / bk * p[i]->segments : 0;
       // (of 64 x 64 tiles whose reduction is the slow index of both operands the time a slab is twice that: 136 x 680 x 5273 0.8 us)
-      unit[i] = cost.slab * bk / slab_of(LINEAR, size, f32) * (what[i] == WGRAD && size == 0 && !f32 ? 2 : 1);
+      unit[i] = cost.slab * bk / (f32 ? 32 : size ? 64 : 128) * (what[i] == WGRAD && size == 0 && !f32 ? 2 : 1);
       most = std::max(most, slabs[i]);
     }
     for (int64_t parts = 1; parts <= 32; parts += parts < 4 ? 1 : parts / 2) {
@@ -944,7 +945,7 @@ template <int WHAT, typename T> hipError_t launch_forward(Product& p, int64_t ro
   else if constexpr (!F32 || WHAT != GATED)
     if (size == 0) start_product<WHAT, T, 0>(p, stream);
   if constexpr (!F32)
-    if (size == 3) start_product<WHAT, T, 3>(p, stream);
+    if (size >= 3) size == 3 ? start_product<WHAT, T, 3>(p, stream) : start_product<WHAT, T, 4>(p, stream);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL((token_join_kernel<T>), dim3((unsigned)join_groups(p, WHAT)), dim3(256), 0, stream, p, (int)WHAT);
@@ -979,7 +980,7 @@ template <typename T> hipError_t launch_backward(const Product& dw, const Produc
   if (size == 0) start_backward<T, 0>(dw, dx, bias, stream);
   else if (size == 1) start_backward<T, 1>(dw, dx, bias, stream);
   else if (size == 2) start_backward<T, 2>(dw, dx, bias, stream);
-  else if constexpr (sizeof(T) == 2) start_backward<T, 3>(dw, dx, bias, stream);
+  else if constexpr (sizeof(T) == 2) size == 3 ? start_backward<T, 3>(dw, dx, bias, stream) : start_backward<T, 4>(dw, dx, bias, stream);
   const hipError_t e = hipGetLastError();
   const int64_t first = join_groups(dw, WGRAD), groups = first + join_groups(dx, DGRAD);
   if (e != hipSuccess || !groups) return e;

@@ -74,7 +74,7 @@ def check_gated(R, I, H, act, dtype, room):
 
 
 # enough for 256 x 256 tiles in bf16 and 128 x 128 in fp32, ragged and whole; long sums of few results; wide and narrow
-LARGE = [(4096, 1024, 4096), (4100, 1032, 3080), (2000, 776, 2056), (8200, 64, 1024), (64, 8192, 128), (9000, 40, 48), (300, 4104, 1000), (1500, 3000, 704)]
+LARGE = [(4096, 1024, 4096), (4100, 1032, 3080), (2000, 776, 2056), (8200, 64, 1024), (64, 8192, 128), (9000, 40, 48), (300, 4104, 1000), (1500, 3000, 704), (4090, 4104, 2048)]
 
 
 @pytest.mark.parametrize("room", [0, 64 << 20])
@@ -86,7 +86,7 @@ def test_linear_of_large_sizes(R, I, O, dtype, room):
 
 @pytest.mark.parametrize("room", [0, 64 << 20])
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("R,I,H", [(4096, 1024, 2048), (4100, 1032, 2056), (2000, 776, 1032), (8200, 64, 512), (64, 8192, 72), (9000, 40, 24), (300, 4104, 1000)])
+@pytest.mark.parametrize("R,I,H", [(4096, 1024, 2048), (4100, 1032, 2056), (2000, 776, 1032), (8200, 64, 512), (64, 8192, 72), (9000, 40, 24), (300, 4104, 1000), (4090, 4104, 1024)])
 def test_gated_linear_of_large_sizes(R, I, H, dtype, room):
     check_gated(R, I, H, 0, dtype, room)
 
