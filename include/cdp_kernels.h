@@ -183,14 +183,14 @@ int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, 
  *   act 0: SiLU g * sigmoid(g)    1: exact GELU g * Phi(g)    2: sigmoid(g)    3: g
  * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20, rows up to 2^30.  g and u (both or neither): written too, for the backward.
  * Sums are fp32.  fp32: factors are taken as three bf16 numbers that add up to them (2^-27 of a factor is left out, and what is below 2^-133) and the three
- * smallest products of those are left out (2^-26); up to 16 rows forward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
+ * smallest products of those are left out (2^-26); up to 16 rows, forward and of few outputs backward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
  * workspace: none needed (may be NULL).  Where there is one (16-byte aligned), of P times 8 * rows * hidden bytes, few tiles of long sums share their sums over up
  * to P workgroups: faster, other roundings. */
 int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, size_t workspace_bytes,
                        int rows, int in, int hidden, void* stream);
 
 /* Its gradients from dh[rows][hidden], x, wg, wu, and g, u as the forward wrote them:  dg = dh * u * act'(g) and du = dh * act(g), which bf16 rounds to the
- * element type;  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
+ * element type (not always of up to 16 rows);  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
  * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 8 * rows * hidden + 1024 (CDP_EINVAL if smaller), and as above where it holds more: P times
  * 8 * hidden * in bytes for dwg and dwu, then P times 4 * rows * in for dx. */
 int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
@@ -202,7 +202,8 @@ int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* w
 int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
                  size_t workspace_bytes, int rows, int in, int out, void* stream);
 
-/* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products;  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
+/* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products (not always of up
+ * to 16 rows);  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
  * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted).  The gradient of the residual is dy.
  * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 4 * rows * out + 4 * out * min(rows, 256) + 1024 (CDP_EINVAL if smaller), and as
  * above where it holds more: P times 4 * out * in bytes for dw, then P times 4 * rows * in for dx. */

@@ -11,10 +11,11 @@
 //   fp32 (exact_body): operands pass through registers, where each is cut into three bf16 planes (rounded: 2^-9, 2^-18 and 2^-27 of it are left), which lie in LDS as
 // the bf16 operands do; the six products of planes of which more than 2^-26 comes are added up, the smallest first.
 //   few tiles: the reduction is shared by `splits` workgroups, whose sums (fp32, in the workspace) are joined in order.
-// Forward of up to 16 rows (single tokens): bound by reading the weights once (token_few_kernel).
+// Forward of up to 16 rows (single tokens): bound by reading the weights once (token_few_kernel); backward of few outputs one launch (token_few_backward_kernel).
 #include "elem.h"
 #include "gelu.h"
 #include "kernels.h"
+#include "lane_sums.h"
 
 #include <algorithm>
 #include <climits>
@@ -852,6 +853,131 @@ template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_fe
   store(a.out);
 }
 
+// Backward of up to 16 rows and few outputs: bound by launches and round trips, so that it is one launch.  dz (dg, du) is made again by every workgroup that has it for a factor,
+// and stays fp32; products are of 16 x 16 x 4.
+struct FewBack {
+  const void *x, *w, *w2, *z, *u, *dy;  // gated: wg, wu, g, u, dh
+  void *dx, *dw, *dw2, *dbias;          // gated: dx, dwg, dwu; each may be null (dw and dw2 together)
+  int rows, in, out, act;
+  int dx_groups;
+};
+constexpr int FEW_BACK_WAVES = 8;
+template <typename T> struct alignas(4 * sizeof(T)) Four {
+  T e[4];
+  __device__ __forceinline__ float operator[](int i) const { return Elem<T>::to_f32(e[i]); }
+};
+template <typename T, bool DUAL> __global__ __launch_bounds__(FEW_BACK_WAVES * 64) void token_few_backward_kernel(const FewBack a) {
+  constexpr int STEPS = 8, SLAB = FEW_BACK_WAVES * 4 * STEPS;  // reduction indices that the wavefronts have at once
+  __shared__ v4f_t shares[FEW_BACK_WAVES][4][64];
+  __shared__ __attribute__((aligned(16))) float factors[DUAL ? 2 : 1][16][SLAB + 4];  // (rows on banks of their own)
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, quarter = lane >> 4;
+  const T *const z = static_cast<const T*>(a.z), *const u = static_cast<const T*>(a.u), *const dy = static_cast<const T*>(a.dy);
+  auto gradient = [&](float z, float u, float dy, float& p, float& q) {  // dg and du, or dz
+    float f = z, df = 1.f;
+    if (a.act != TOKEN_NONE) act_both<T>(a.act, z, f, df);
+    p = DUAL ? dy * u * df : dy * df;
+    q = dy * f;
+  };
+  if ((int)blockIdx.x < a.dx_groups) {
+    // 64 columns of dx; the wavefronts share the reduction.  lane: row c of dz, index `quarter` of four; columns 4 c .. of w
+    static_assert(FEW_BACK_WAVES * 64 == 16 * SLAB / 8, "eight values of a slab of dz a thread");
+    const int col = blockIdx.x * 64 + c * 4;
+    v4f_t acc[4] = {};
+    for (int o0 = 0; o0 < a.out; o0 += SLAB) {
+      Four<T> w[STEPS], w2[STEPS];
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int o = o0 + (wave * STEPS + i) * 4 + quarter;
+        const bool there = o < a.out && col < a.in;
+        const int64_t at = there ? (int64_t)o * a.in + col : 0;
+        w[i] = there ? *reinterpret_cast<const Four<T>*>(static_cast<const T*>(a.w) + at) : Four<T>{};
+        if (DUAL) w2[i] = there ? *reinterpret_cast<const Four<T>*>(static_cast<const T*>(a.w2) + at) : Four<T>{};
+      }
+      const int r = threadIdx.x / (SLAB / 8), o = threadIdx.x % (SLAB / 8) * 8;
+      float p[8] = {}, q[8] = {};
+      if (r < a.rows && o0 + o < a.out) {  // (out: a multiple of 8)
+        const int64_t at = (int64_t)r * a.out + o0 + o;
+        Eight<T> vz, vu, vd;
+        vd.load(dy + at);
+        if (DUAL || a.act != TOKEN_NONE) vz.load(z + at);
+        if (DUAL) vu.load(u + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) gradient(DUAL || a.act != TOKEN_NONE ? vz[e] : 0.f, DUAL ? vu[e] : 0.f, vd[e], p[e], q[e]);
+      }
+      if (o0) __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; e += 4) {
+        *reinterpret_cast<float4*>(&factors[0][r][o + e]) = make_float4(p[e], p[e + 1], p[e + 2], p[e + 3]);
+        if (DUAL) *reinterpret_cast<float4*>(&factors[DUAL ? 1 : 0][r][o + e]) = make_float4(q[e], q[e + 1], q[e + 2], q[e + 3]);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) {
+        const int k = (wave * STEPS + i) * 4 + quarter;
+        const float dg = factors[0][c][k], du = DUAL ? factors[DUAL ? 1 : 0][c][k] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(dg, w[i][e], acc[e], 0, 0, 0);
+          if (DUAL) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(du, w2[i][e], acc[e], 0, 0, 0);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) shares[wave][e][lane] = acc[e];
+    __syncthreads();
+    // row 4 (lane / 16) + k, columns 4 c ..
+    const int k = wave, r = 4 * quarter + k;
+    if (k >= 4 || r >= a.rows || col >= a.in) return;
+    Four<T> res;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float s = 0.f;
+#pragma unroll
+      for (int i = 0; i < FEW_BACK_WAVES; ++i) s += shares[i][e][lane][k];
+      res.e[e] = Elem<T>::from_f32(s);
+    }
+    *reinterpret_cast<Four<T>*>(static_cast<T*>(a.dx) + (int64_t)r * a.in + col) = res;
+    return;
+  }
+  // 16 rows of dw a wavefront, 64 columns.  lane: row c of them, rows of x quarter, quarter + 4, ..
+  const int columns = a.dw ? (a.in + 63) / 64 : 1, tile = (blockIdx.x - a.dx_groups) * FEW_BACK_WAVES + wave, o0 = tile / columns * 16, strip = tile % columns, col = strip * 64 + c * 4;
+  if (o0 >= a.out) return;
+  float p[4], q[4], sum = 0.f;
+  Four<T> x[4];
+#pragma unroll
+  for (int s = 0; s < 4; ++s) {
+    const int r = quarter + 4 * s;
+    const bool there = r < a.rows && o0 + c < a.out;
+    const int64_t at = there ? (int64_t)r * a.out + o0 + c : 0;
+    gradient(there && (DUAL || a.act != TOKEN_NONE) ? Elem<T>::to_f32(z[at]) : 0.f, DUAL && there ? Elem<T>::to_f32(u[at]) : 0.f, there ? Elem<T>::to_f32(dy[at]) : 0.f, p[s],
+             q[s]);
+    sum += p[s];
+    x[s] = a.dw && r < a.rows && col < a.in ? *reinterpret_cast<const Four<T>*>(static_cast<const T*>(a.x) + (int64_t)r * a.in + col) : Four<T>{};
+  }
+  if (!DUAL && a.dbias && strip == 0) {
+    sum = lanes_swap32(lanes_swap16(sum));
+    if (lane < 16 && o0 + c < a.out) static_cast<T*>(a.dbias)[o0 + c] = Elem<T>::from_f32(sum);
+  }
+  if (!a.dw) return;
+#pragma unroll
+  for (int which = 0; which < (DUAL ? 2 : 1); ++which) {
+    v4f_t acc[4] = {};
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(which ? q[s] : p[s], x[s][e], acc[e], 0, 0, 0);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int o = o0 + 4 * quarter + k;
+      if (o >= a.out || col >= a.in) continue;
+      Four<T> res;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) res.e[e] = Elem<T>::from_f32(acc[e][k]);
+      *reinterpret_cast<Four<T>*>(static_cast<T*>(which ? a.dw2 : a.dw) + (int64_t)o * a.in + col) = res;
+    }
+  }
+}
+
 // ---- launches ---------------------------------------------------------------------------------------------------------
 int slab_of(int what, int size, bool f32) { return f32 || size == 4 || (size == 3 && (what == DGRAD || what == WGRAD)) ? 32 : size == 0 ? 128 : 64; }
 int rows_of(int size) { return size == 3 ? 256 : size >= 2 ? 128 : 64; }
@@ -996,6 +1122,19 @@ template <bool DUAL> hipError_t launch_few(const Few& a, int dtype, hipStream_t 
   return hipGetLastError();
 }
 constexpr int FEW_ROWS = 16;
+// Whether a backward pass is one launch: while dx is one slab or two behind each other (us so / in the launches of more rows, 16 rows: bf16 256 x 256 7.6 / 10.3, with 512 outputs
+// 10.4 / 10.3, gated 13.5 / 12.0; fp32 256 x 64 8.5 / 14.3, 512 x 1024 15.4 / 19.6, gated 18.5 / 19.6; 16 x 512 x 12288 60 / 70).
+bool few_backward(int rows, int out, int dtype) { return rows <= FEW_ROWS && out <= (dtype == DT_F32 ? 512 : 256); }
+template <bool DUAL> hipError_t launch_few_backward(FewBack a, int dtype, hipStream_t stream) {
+  a.dx_groups = a.dx ? (a.in + 63) / 64 : 0;
+  const int64_t tiles = (int64_t)((a.out + 15) / 16) * (a.dw ? (a.in + 63) / 64 : 1);
+  const int64_t groups = a.dx_groups + (a.dw || a.dbias ? (tiles + FEW_BACK_WAVES - 1) / FEW_BACK_WAVES : 0);
+  if (!launchable(groups, FEW_BACK_WAVES * 64)) return hipErrorInvalidConfiguration;
+  const dim3 grid((unsigned)groups), block(FEW_BACK_WAVES * 64);
+  if (dtype == DT_BF16) hipLaunchKernelGGL((token_few_backward_kernel<uint16_t, DUAL>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((token_few_backward_kernel<float, DUAL>), grid, block, 0, stream, a);
+  return hipGetLastError();
+}
 
 template <typename T> hipError_t gated_backward(const GatedLinear& a, hipStream_t stream) {
   char* at = static_cast<char*>(a.workspace);
@@ -1084,6 +1223,8 @@ hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stre
   return dtype == DT_BF16 ? launch_forward<GATED, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<GATED, float>(p, a.workspace_bytes, stream);
 }
 hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream) {
+  if (few_backward(a.rows, a.hidden, dtype))
+    return launch_few_backward<true>({a.x, a.wg, a.wu, a.g, a.u, a.dh, a.dx, a.dwg, a.dwu, nullptr, a.rows, a.in, a.hidden, a.act, 0}, dtype, stream);
   return dtype == DT_BF16 ? gated_backward<uint16_t>(a, stream) : gated_backward<float>(a, stream);
 }
 hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream) {
@@ -1099,6 +1240,8 @@ hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stre
   return dtype == DT_BF16 ? launch_forward<LINEAR, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<LINEAR, float>(p, a.workspace_bytes, stream);
 }
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream) {
+  if (few_backward(a.rows, a.out, dtype))
+    return launch_few_backward<false>({a.x, a.w, nullptr, a.z, nullptr, a.dy, a.dx, a.dw, nullptr, a.dbias, a.rows, a.in, a.out, a.act, 0}, dtype, stream);
   return dtype == DT_BF16 ? linear_backward<uint16_t>(a, stream) : linear_backward<float>(a, stream);
 }
 

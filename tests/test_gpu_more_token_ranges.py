@@ -103,6 +103,15 @@ def test_linear_maps_of_any_size(seed, dtype):
     check_gated(R, I, O, int(g.integers(4)), dtype, room)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("act", range(4))
+@pytest.mark.parametrize("R,I,O", [(1, 8, 8), (3, 72, 248), (16, 64, 256), (16, 136, 264), (15, 200, 512), (1, 1000, 520), (17, 72, 256)])
+def test_linear_maps_of_few_rows(R, I, O, act, dtype):
+    """Around the sizes from which a backward pass is more than one launch."""
+    check_linear(R, I, O, act, dtype, 0)
+    check_gated(R, I, O, act, dtype, 0)
+
+
 # ---- offsets past 32 bits ---------------------------------------------------------------------------------------------
 def test_logprob_of_rows_far_apart():
     """Rows 2^31 elements apart, the third 8 GiB behind the first."""
