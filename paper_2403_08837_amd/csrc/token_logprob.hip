@@ -2,9 +2,10 @@
 //   lse = log sum exp z,  p = exp(z - lse),  logprob = z[target] - lse,  entropy = lse - sum p z;
 //   dlogits[j] = scale * (dlogprob * ((j == target) - p[j]) - dentropy * p[j] * (log p[j] + entropy)).
 //
-// Bound by memory: a row is read once forward, read and written once backward.  us of 4096 x 128000 in bf16, a quarter not wanted: forward 193 to 209 (3.8 to 4.1 TB/s; the
-// vector unit has some 100 of it: an exponential and six others a value), backward 350 (5.2 TB/s); 1500 x 50257 in fp32, rows that begin anywhere: with the 8 likeliest 94 to
-// 100, backward 92 to 95.  A lane keeps the maximum m of what it has seen with s = sum 2^y and
+// Bound by memory: a row is read once forward, read and written once backward.  us of 4096 x 128000 in bf16, a quarter
+// not wanted: forward 154 by itself (5.1 TB/s; without t 149), 193 to 209 right behind the backward, whose results are still on their way to memory, with the 8 likeliest 31
+// more; backward 350 (5.2 TB/s); 1500 x 50257 in fp32, rows that begin anywhere: 48 by itself (5.6 TB/s), with the 8 likeliest 61, backward 92 to 95.
+// A lane keeps the maximum m of what it has seen with s = sum 2^y and
 // t = sum 2^y y, y = (logit - m) scale log2(e): a new maximum multiplies s by f = 2^d and makes t = f (t + d s).  That maximum is raised once for eight values at most.
 // entropy = log s - (t / s) log 2 over the row.
 //
