@@ -192,7 +192,7 @@ int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const 
 /* Its gradients from dh[rows][hidden], x, wg, wu, and g, u as the forward wrote them:  dg = dh * u * act'(g) and du = dh * act(g), which bf16 rounds to the
  * element type (not always of up to 16 rows);  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
  * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 8 * rows * hidden + 1024 (CDP_EINVAL if smaller), and as above where it holds more: P times
- * 8 * hidden * in bytes for dwg and dwu, then P times 4 * rows * in for dx. */
+ * 8 * hidden * in bytes for dwg and dwu, then P times 4 * rows * in for dx.  Which results are wanted may, like the room, change their roundings. */
 int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
                                 void* dwg, void* dwu, void* workspace, size_t workspace_bytes, int rows, int in, int hidden, void* stream);
 
@@ -206,7 +206,7 @@ int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* b
  * to 16 rows);  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
  * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted).  The gradient of the residual is dy.
  * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 4 * rows * out + 4 * out * min(rows, 256) + 1024 (CDP_EINVAL if smaller), and as
- * above where it holds more: P times 4 * out * in bytes for dw, then P times 4 * rows * in for dx. */
+ * above where it holds more: P times 4 * out * in bytes for dw, then P times 4 * rows * in for dx.  Wanted results and roundings as above. */
 int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
                           size_t workspace_bytes, int rows, int in, int out, void* stream);
 

@@ -1174,7 +1174,6 @@ template <typename T> hipError_t gated_backward(const GatedLinear& a, hipStream_
 template <typename T> hipError_t linear_backward(const TokenLinear& a, hipStream_t stream) {
   char* at = static_cast<char*>(a.workspace);
   const int64_t n = (int64_t)a.rows * a.out;
-  // places in the workspace, whatever is wanted: a result does not depend on which others are
   T* const to = (a.dx || a.dw) && a.act != TOKEN_NONE ? reinterpret_cast<T*>(at) : nullptr;  // dz, where it is not dy
   at += rounded((int)sizeof(T) * n);
   float* const sums = reinterpret_cast<float*>(at);

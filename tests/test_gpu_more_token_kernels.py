@@ -406,6 +406,10 @@ def test_token_logprob(case, dtype, shared):
     same = dev.clone()
     b.cdp_k_token_logprob_backward(dtype, p(same), *given[2:], p(lse), p(entropy), p(dld), p(ded), p(same), rows, V)
     assert torch.equal(same[:, :V], dlogits[:, :V]) and torch.equal(same[:, V:].nan_to_num(), dev[:, V:].nan_to_num())
+    # at another alignment than the logits
+    other = hold(torch.full((rows, pitch), 5.0), t, shift + 1)
+    b.cdp_k_token_logprob_backward(*given, p(lse), p(entropy), p(dld), p(ded), p(other), rows, V)
+    assert torch.equal(other, dlogits)
     b.cdp_k_token_logprob_backward(*given, p(lse), 0, p(dld), 0, p(dlogits), rows, V)
     d1, s1 = scale * dl.double()[:, None] * (one - prob), scale * dl.double().abs()[:, None] * (one + prob)
     near(dlogits[:, :V], torch.where(some, d1, zero), half(dtype) * d1.abs() + left * s1 + 1e-37, "from logprob")
