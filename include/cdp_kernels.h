@@ -183,7 +183,8 @@ int cdp_k_head_norm_rotary_backward(int dtype, int accumulate, const void* qkv, 
  *   act 0: SiLU g * sigmoid(g)    1: exact GELU g * Phi(g)    2: sigmoid(g)    3: g
  * All in the element type, 16-byte aligned; in and hidden multiples of 8 up to 2^20, rows up to 2^30.  g and u (both or neither): written too, for the backward.
  * Sums are fp32.  fp32: factors are taken as three bf16 numbers that add up to them (2^-27 of a factor is left out, and what is below 2^-133) and the three
- * smallest products of those are left out (2^-26); up to 16 rows, forward and of few outputs backward: plain fp32.  What is infinite or NaN in x reaches its row, in wg or wu its column, as NaN in fp32.
+ * smallest products of those are left out (2^-26); of up to 64 rows forward, 16 backward, some are plain fp32.  What is infinite or
+ * NaN in x reaches its row, in wg or wu its column, what is infinite as NaN where factors are taken in three.
  * workspace: none needed (may be NULL).  Where there is one (16-byte aligned), of P times 8 * rows * hidden bytes, few tiles of long sums share their sums over up
  * to P workgroups: faster, other roundings. */
 int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const void* wu, void* h, void* g, void* u, void* workspace, size_t workspace_bytes,

@@ -11,7 +11,7 @@
 //   fp32 (exact_body): operands pass through registers, where each is cut into three bf16 planes (rounded: 2^-9, 2^-18 and 2^-27 of it are left), which lie in LDS as
 // the bf16 operands do; the six products of planes of which more than 2^-26 comes are added up, the smallest first.
 //   few tiles: the reduction is shared by `splits` workgroups, whose sums (fp32, in the workspace) are joined in order.
-// Forward of up to 16 rows (single tokens): bound by reading the weights once (token_few_kernel); backward of few outputs one launch (token_few_backward_kernel).
+// Forward of few rows (single tokens, up to 64): bound by reading the weights once and the rows from cache (token_few_kernel); backward of few outputs one launch (token_few_backward_kernel).
 #include "elem.h"
 #include "gelu.h"
 #include "kernels.h"
@@ -769,93 +769,109 @@ template <typename T> __global__ __launch_bounds__(256) void token_backward_join
 
 // ---- few rows ---------------------------------------------------------------------------------------------------------
 // Memory: 1 x 4096 x 12288 in bf16, gated, reads 201 MB in 29.6 to 37 us (5.4 to 6.8 TB/s, part of it from cache).
-// Up to 16 rows of x: the 16 rows of one operand are eight columns of wg and of wu each, or 16 of w, those of the other the rows of x; the four wavefronts of a
-// workgroup share the reduction.
+// Up to 64 rows of x: the 16 rows of one operand are eight columns of wg and of wu each, or 16 of w, those of the other 16 rows of x; RG groups of rows, CG of columns; the
+// wavefronts of a workgroup share the reduction.
 struct Few {
   const void *x, *w, *w2;       // gated: wg, wu
   void *out, *out2, *out3;      // gated: h, g, u; else y, z
   const void *bias, *residual;
   int rows, in, cols, act;
 };
-template <typename T, bool DUAL> __global__ __launch_bounds__(256) void token_few_kernel(const Few a) {
-  constexpr int V = Elem<T>::VEC, STEP = 4 * V, UNROLL = 8;  // reduction indices that the lanes of a wavefront have at once; such steps in flight
-  __shared__ v4f_t shares[4][64];
+template <typename T, bool DUAL, int RG, int CG, int WAVES> __global__ __launch_bounds__(WAVES * 64) void token_few_kernel(const Few a) {
+  constexpr int V = Elem<T>::VEC, STEP = 4 * V, UNROLL = RG * CG == 1 ? 8 : 4;  // reduction indices that the lanes of a wavefront have at once; such steps in flight
+  __shared__ v4f_t shares[WAVES][RG * CG][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, quarter = lane >> 4;
-  const int col0 = blockIdx.x * (DUAL ? 8 : 16);  // (cols: a multiple of 8)
-  const T* const w = static_cast<const T*>(DUAL && r >= 8 ? a.w2 : a.w) + (int64_t)(DUAL ? col0 + (r & 7) : min(col0 + r, a.cols - 1)) * a.in + quarter * V;
-  const T* const x = static_cast<const T*>(a.x) + (int64_t)min(r, a.rows - 1) * a.in + quarter * V;
-  v4f_t acc = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = wave * STEP * UNROLL; k0 < a.in; k0 += 4 * STEP * UNROLL) {
-    uint4 p[UNROLL], q[UNROLL];
+  const int col0 = blockIdx.x * (DUAL ? 8 : 16) * CG;
+  const T *w[CG], *x[RG];
+#pragma unroll
+  for (int g = 0; g < CG; ++g)
+    w[g] = static_cast<const T*>(DUAL && r >= 8 ? a.w2 : a.w) + (int64_t)min(col0 + (DUAL ? g * 8 + (r & 7) : g * 16 + r), a.cols - 1) * a.in + quarter * V;
+#pragma unroll
+  for (int g = 0; g < RG; ++g) x[g] = static_cast<const T*>(a.x) + (int64_t)min(g * 16 + r, a.rows - 1) * a.in + quarter * V;
+  v4f_t acc[RG][CG] = {};
+  for (int k0 = wave * STEP * UNROLL; k0 < a.in; k0 += WAVES * STEP * UNROLL) {
+    uint4 p[UNROLL][CG], q[UNROLL][RG];
 #pragma unroll
     for (int i = 0; i < UNROLL; ++i) {
       const int k = k0 + i * STEP;
       const bool in = k + quarter * V < a.in;
-      p[i] = in ? *reinterpret_cast<const uint4*>(w + k) : make_uint4(0, 0, 0, 0);
-      q[i] = in ? *reinterpret_cast<const uint4*>(x + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int g = 0; g < CG; ++g) p[i][g] = in ? *reinterpret_cast<const uint4*>(w[g] + k) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+      for (int g = 0; g < RG; ++g) q[i][g] = in ? *reinterpret_cast<const uint4*>(x[g] + k) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < UNROLL; ++i) {
-      if constexpr (sizeof(T) == 2) {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16_t, p[i]), __builtin_bit_cast(v8bf16_t, q[i]), acc, 0, 0, 0);
-      } else {
-        Chunk16<float> f, g;
-        f.v = p[i];
-        g.v = q[i];
+    for (int i = 0; i < UNROLL; ++i)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(f.e[e], g.e[e], acc, 0, 0, 0);
-      }
-    }
+      for (int m = 0; m < RG; ++m)
+#pragma unroll
+        for (int n = 0; n < CG; ++n) {
+          if constexpr (sizeof(T) == 2) {
+            acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf16_t, p[i][n]), __builtin_bit_cast(v8bf16_t, q[i][m]), acc[m][n], 0, 0, 0);
+          } else {
+            Chunk16<float> f, g;
+            f.v = p[i][n];
+            g.v = q[i][m];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x4f32(f.e[e], g.e[e], acc[m][n], 0, 0, 0);
+          }
+        }
   }
-  shares[wave][lane] = acc;
+#pragma unroll
+  for (int m = 0; m < RG; ++m)
+#pragma unroll
+    for (int n = 0; n < CG; ++n) shares[wave][m * CG + n][lane] = acc[m][n];
   __syncthreads();
-  if (wave) return;
-  // row of x lane % 16; columns 4 (lane / 16) .., gated: 4 (lane / 16 % 2) .. of wg (lanes below 32) or wu
-  acc = (shares[0][lane] + shares[1][lane]) + (shares[2][lane] + shares[3][lane]);
-  float u[4], v[4] = {acc[0], acc[1], acc[2], acc[3]};
-  if constexpr (DUAL)
+  for (int which = wave; which < RG * CG; which += WAVES) {
+    // row of x lane % 16; columns 4 (lane / 16) .., gated: 4 (lane / 16 % 2) .. of wg (lanes below 32) or wu
+    v4f_t sum = shares[0][which][lane];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) u[e] = __shfl(acc[e], lane + 32, 64);
-  const int col = col0 + 4 * (DUAL ? quarter & 1 : quarter);
-  if (r >= a.rows || col >= a.cols) return;
-  const int64_t at = (int64_t)r * a.cols + col;
-  auto store = [&](void* out) {
-    if constexpr (sizeof(T) == 2) {
-      Chunk16<T> c;
+    for (int i = 1; i < WAVES; ++i) sum += shares[i][which][lane];
+    float u[4], v[4] = {sum[0], sum[1], sum[2], sum[3]};
+    if constexpr (DUAL)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) c.e[e] = Elem<T>::from_f32(v[e]);
-      *reinterpret_cast<uint2*>(static_cast<T*>(out) + at) = c.h[0];
+      for (int e = 0; e < 4; ++e) u[e] = __shfl(sum[e], lane + 32, 64);
+    const int row = which / CG * 16 + r, col = col0 + which % CG * (DUAL ? 8 : 16) + 4 * (DUAL ? quarter & 1 : quarter);
+    if (row >= a.rows || col >= a.cols) continue;
+    const int64_t at = (int64_t)row * a.cols + col;
+    auto store = [&](void* out) {
+      if constexpr (sizeof(T) == 2) {
+        Chunk16<T> c;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c.e[e] = Elem<T>::from_f32(v[e]);
+        *reinterpret_cast<uint2*>(static_cast<T*>(out) + at) = c.h[0];
+      } else {
+        *reinterpret_cast<float4*>(static_cast<T*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+      }
+    };
+    auto add = [&](const void* from, int64_t i) {
+      if constexpr (sizeof(T) == 2) {
+        Chunk16<T> c;
+        c.h[0] = *reinterpret_cast<const uint2*>(static_cast<const T*>(from) + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += Elem<T>::to_f32(c.e[e]);
+      } else {
+        const float4 c = *reinterpret_cast<const float4*>(static_cast<const T*>(from) + i);
+        v[0] += c.x;
+        v[1] += c.y;
+        v[2] += c.z;
+        v[3] += c.w;
+      }
+    };
+    if constexpr (DUAL) {
+      if (a.out2) store(lane < 32 ? a.out2 : a.out3);
+      if (lane >= 32) continue;
+      act_all<T>(a.act, v);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= u[e];
     } else {
-      *reinterpret_cast<float4*>(static_cast<T*>(out) + at) = make_float4(v[0], v[1], v[2], v[3]);
+      if (a.bias) add(a.bias, col);
+      if (a.out2) store(a.out2);
+      act_all<T>(a.act, v);
+      if (a.residual) add(a.residual, at);
     }
-  };
-  auto add = [&](const void* from, int64_t i) {
-    if constexpr (sizeof(T) == 2) {
-      Chunk16<T> c;
-      c.h[0] = *reinterpret_cast<const uint2*>(static_cast<const T*>(from) + i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] += Elem<T>::to_f32(c.e[e]);
-    } else {
-      const float4 c = *reinterpret_cast<const float4*>(static_cast<const T*>(from) + i);
-      v[0] += c.x;
-      v[1] += c.y;
-      v[2] += c.z;
-      v[3] += c.w;
-    }
-  };
-  if constexpr (DUAL) {
-    if (a.out2) store(lane < 32 ? a.out2 : a.out3);
-    if (lane >= 32) return;
-    act_all<T>(a.act, v);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] *= u[e];
-  } else {
-    if (a.bias) add(a.bias, col);
-    if (a.out2) store(a.out2);
-    act_all<T>(a.act, v);
-    if (a.residual) add(a.residual, at);
+    store(a.out);
   }
-  store(a.out);
 }
 
 // Backward of up to 16 rows and few outputs: bound by launches and round trips, so that it is one launch.  dz (dg, du) is made again by every workgroup that has it for a factor,
@@ -1011,12 +1027,13 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
 struct Choice {
   int size;
   int64_t each;
+  double time;
 };
 template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room) {
   struct Cost { double slab, alone, tile; int resident; };
   static constexpr Cost BF16[5] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}, {0.57, 0.46, 2.0, 512}},
                         F32[3] = {{0.45, 0.53, 1.5, 768}, {0.78, 0.85, 2.0, 512}, {1.47, 1.47, 7.0, 256}};
-  Choice best = {0, INT32_MAX};
+  Choice best = {0, INT32_MAX, 0};
   double least = 1e30;
   for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 5); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
     const Cost& cost = f32 ? F32[size] : BF16[size];
@@ -1050,7 +1067,7 @@ template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N
       const double time = std::max(rounds * work / groups, longest) + std::ceil(groups / cost.resident) * cost.tile + join;
       if (time < least) {
         least = time;
-        best = {size, parts > 1 ? each : (int64_t)INT32_MAX};
+        best = {size, parts > 1 ? each : (int64_t)INT32_MAX, time};
       }
     }
   }
@@ -1063,12 +1080,56 @@ int64_t join_groups(const Product& p, int what) {
 template <int WHAT, typename T, int SIZE> void start_product(const Product& p, hipStream_t stream) {
   hipLaunchKernelGGL((token_product_kernel<WHAT, T, SIZE>), dim3(p.workgroups()), dim3(Tile<WHAT, T, SIZE>::THREADS), 0, stream, p);
 }
-// A forward product.
-template <int WHAT, typename T> hipError_t launch_forward(Product& p, int64_t room, hipStream_t stream) {
-  constexpr bool F32 = sizeof(T) == 4;
+// Few rows.  A CU reads 37 KB a us of weights and rows out of the caches, all of them 5 MB of weights out of memory.  Two groups of columns a workgroup read the rows half as
+// often (only of gated maps, whose groups have 8 of either matrix: us, 16 x 4096 x 12288 44 / 35, 32 x 1024 x 2816 7.4 / 5.8); of plain maps that are no more workgroups
+// than CUs those have eight wavefronts (1 x 4096 x 4096 7.7 / 6.9).
+struct FewChoice {
+  int groups;  // of columns
+  double time;
+};
+FewChoice choose_few(const Few& a, bool dual, bool f32) {
+  const double bytes = (f32 ? 4.0 : 2.0) * a.in, least = (dual ? 2 : 1) * bytes * a.cols / 5e6;
+  FewChoice best = {1, 1e30};
+  for (int groups = 1; groups <= (dual ? 2 : 1); ++groups) {
+    const int columns = (dual ? 8 : 16) * groups;
+    const double time = std::max(least, ((a.cols + columns - 1) / columns + 255) / 256 * bytes * (16 * groups + a.rows) / 37e3 * (groups == 2 ? 1.2 : 1.0));
+    if (time < best.time) best = {groups, time};
+  }
+  best.time *= !f32 ? 1.0 : a.rows <= 32 ? 1.25 : 1.6;
+  return best;
+}
+template <typename T, bool DUAL, int RG, int CG, int WAVES> void start_few(const Few& a, hipStream_t stream) {
+  constexpr int COLS = (DUAL ? 8 : 16) * CG;
+  hipLaunchKernelGGL((token_few_kernel<T, DUAL, RG, CG, WAVES>), dim3((a.cols + COLS - 1) / COLS), dim3(WAVES * 64), 0, stream, a);
+}
+template <typename T, bool DUAL, int RG> void start_few(const Few& a, int groups, hipStream_t stream) {
+  if constexpr (DUAL) {
+    if (groups == 2) return start_few<T, true, RG, 2, 4>(a, stream);
+  } else if constexpr (sizeof(T) == 2) {
+    if (a.cols <= 16 * 256) return start_few<T, false, RG, 1, 8>(a, stream);
+  }
+  start_few<T, DUAL, RG, 1, 4>(a, stream);
+}
+template <typename T, bool DUAL> hipError_t launch_few(const Few& a, int groups, hipStream_t stream) {
+  if (a.rows <= 16) start_few<T, DUAL, 1>(a, groups, stream);
+  else if (a.rows <= 32) start_few<T, DUAL, 2>(a, groups, stream);
+  else start_few<T, DUAL, 4>(a, groups, stream);
+  return hipGetLastError();
+}
+constexpr int FEW_ROWS = 16, FEW_MOST = 64;
+
+// A forward product, on tiles or, up to 16 rows and where its estimate is less, as one of few rows (us so / on tiles, bf16: 32 x 4096 x 4096 13.3 / 21.6, 64 x 12288 x 4096 55 / 64,
+// 32 x 4096 x 12288, which stays on tiles, 34 / 24; fp32: gated 32 x 1024 x 2816 12.8 / 17.4, 64 x 520 x 1000 7.7 / 13.8, 64 x 4096 x 4096, which stays, 41 / 25).  What tiles take
+// beside the estimate, at so few rows 1.1 (fp32) to 1.3 (bf16) of it, and a launch either way, are left out there.
+template <int WHAT, typename T> hipError_t launch_forward(Product& p, const Few& few, int64_t room, hipStream_t stream) {
+  constexpr bool F32 = sizeof(T) == 4, DUAL = WHAT == GATED;
+  FewChoice rows = {1, 1e30};
+  if (p.M <= FEW_MOST) rows = choose_few(few, DUAL, F32);
+  if (p.M <= FEW_ROWS) return launch_few<T, DUAL>(few, rows.groups, stream);
   const Product* const all[1] = {&p};
   const int what[1] = {WHAT};
   const Choice of = choose(all, what, F32, room);
+  if (rows.time < std::max((F32 ? 1.1 : 1.3) * of.time, (double)sizeof(T) * (DUAL ? 2 : 1) * p.K * p.N / 5e6)) return launch_few<T, DUAL>(few, rows.groups, stream);
   const int size = of.size;
   if (!plan(p, WHAT, size, F32, of.each, room)) return hipErrorInvalidConfiguration;
   if (size == 1) start_product<WHAT, T, 1>(p, stream);
@@ -1120,13 +1181,6 @@ template <typename T> hipError_t launch_backward(const Product& dw, const Produc
 }
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-template <bool DUAL> hipError_t launch_few(const Few& a, int dtype, hipStream_t stream) {
-  const dim3 grid((a.cols + (DUAL ? 7 : 15)) / (DUAL ? 8 : 16));
-  if (dtype == DT_BF16) hipLaunchKernelGGL((token_few_kernel<uint16_t, DUAL>), grid, dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((token_few_kernel<float, DUAL>), grid, dim3(256), 0, stream, a);
-  return hipGetLastError();
-}
-constexpr int FEW_ROWS = 16;
 // Whether a backward pass is one launch: while dx is one slab or two behind each other (us so / in the launches of more rows, 16 rows: bf16 256 x 256 7.6 / 10.3, with 512 outputs
 // 10.4 / 10.3, gated 13.5 / 12.0; fp32 256 x 64 8.5 / 14.3, 512 x 1024 15.4 / 19.6, gated 18.5 / 19.6; 16 x 512 x 12288 60 / 70).
 bool few_backward(int rows, int out, int dtype) { return rows <= FEW_ROWS && out <= (dtype == DT_F32 ? 512 : 256); }
@@ -1215,7 +1269,7 @@ int64_t token_linear_bwd_workspace_bytes(int rows, int out, int dtype) {
 }
 
 hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stream) {
-  if (a.rows <= FEW_ROWS) return launch_few<true>({a.x, a.wg, a.wu, a.h, a.g, a.u, nullptr, nullptr, a.rows, a.in, a.hidden, a.act}, dtype, stream);
+  const Few few = {a.x, a.wg, a.wu, a.h, a.g, a.u, nullptr, nullptr, a.rows, a.in, a.hidden, a.act};
   Product p;
   memset(&p, 0, sizeof(p));
   p.segments = 1;
@@ -1224,7 +1278,7 @@ hipError_t launch_gated_linear(const GatedLinear& a, int dtype, hipStream_t stre
   p.out = a.h; p.out2 = a.g; p.out3 = a.u;
   p.act = a.act;
   p.part = static_cast<float*>(a.workspace);
-  return dtype == DT_BF16 ? launch_forward<GATED, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<GATED, float>(p, a.workspace_bytes, stream);
+  return dtype == DT_BF16 ? launch_forward<GATED, uint16_t>(p, few, a.workspace_bytes, stream) : launch_forward<GATED, float>(p, few, a.workspace_bytes, stream);
 }
 hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t stream) {
   if (few_backward(a.rows, a.hidden, dtype))
@@ -1232,7 +1286,7 @@ hipError_t launch_gated_linear_bwd(const GatedLinear& a, int dtype, hipStream_t 
   return dtype == DT_BF16 ? gated_backward<uint16_t>(a, stream) : gated_backward<float>(a, stream);
 }
 hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stream) {
-  if (a.rows <= FEW_ROWS) return launch_few<false>({a.x, a.w, nullptr, a.y, a.z, nullptr, a.bias, a.residual, a.rows, a.in, a.out, a.act}, dtype, stream);
+  const Few few = {a.x, a.w, nullptr, a.y, a.z, nullptr, a.bias, a.residual, a.rows, a.in, a.out, a.act};
   Product p;
   memset(&p, 0, sizeof(p));
   p.segments = 1;
@@ -1241,7 +1295,7 @@ hipError_t launch_token_linear(const TokenLinear& a, int dtype, hipStream_t stre
   p.out = a.y; p.out2 = a.z; p.bias = a.bias; p.residual = a.residual;
   p.act = a.act;
   p.part = static_cast<float*>(a.workspace);
-  return dtype == DT_BF16 ? launch_forward<LINEAR, uint16_t>(p, a.workspace_bytes, stream) : launch_forward<LINEAR, float>(p, a.workspace_bytes, stream);
+  return dtype == DT_BF16 ? launch_forward<LINEAR, uint16_t>(p, few, a.workspace_bytes, stream) : launch_forward<LINEAR, float>(p, few, a.workspace_bytes, stream);
 }
 hipError_t launch_token_linear_bwd(const TokenLinear& a, int dtype, hipStream_t stream) {
   if (few_backward(a.rows, a.out, dtype))

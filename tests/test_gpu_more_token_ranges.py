@@ -104,6 +104,16 @@ def test_linear_maps_of_any_size(seed, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,I,O", [(16, 1032, 4096), (16, 1024, 4104), (17, 520, 1000), (31, 136, 40), (32, 1032, 2816), (33, 72, 24), (50, 264, 2824), (64, 1000, 1000), (64, 24, 5000), (65, 520, 1000), (9, 64, 20000),
+                                   (30, 64, 20008), (60, 64, 20008)])
+def test_linear_maps_of_some_rows(R, I, O, dtype):
+    """One to four groups of 16 rows, whole and not, with one and two groups of columns."""
+    check_linear(R, I, O, 0, dtype, 0)
+    check_linear(R, I, O, 3, dtype, 1 << 22)
+    check_gated(R, I, O, 1, dtype, 0)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("act", range(4))
 @pytest.mark.parametrize("R,I,O", [(1, 8, 8), (3, 72, 248), (16, 64, 256), (16, 136, 264), (15, 200, 512), (1, 1000, 520), (17, 72, 256)])
 def test_linear_maps_of_few_rows(R, I, O, act, dtype):
