@@ -678,10 +678,12 @@ __device__ __forceinline__ void exact_body(const Product& P, int block, unsigned
 // us, size 2 / 4: fewer tiles than CUs, forward 512 x 4096 x 4096 41 / 33, backward 1500 x 1536 x 6144 129 / 114; more, backward of 6272 x 768 x 2048, gated, 85 / 92.
 // us, products of 8192 x 4096 x 12288: 256 x 256 with two slabs of 64 / four of 32, gated forward 1357 / 1420, both backward 2563 / 2504; with four wavefronts of 128 x 128
 // instead of eight of 128 x 64 1418 / 2664 (and they spill).
+constexpr int threads_of(int what, int size) { return size == 3 ? 512 : size == 0 && what == GATED ? 128 : 256; }
 template <int WHAT, typename T, int SIZE> struct Tile {
   static constexpr bool EXACT = sizeof(T) == 4, DUAL = WHAT == GATED, BACK = WHAT == DGRAD || WHAT == WGRAD;
   static constexpr int BM = SIZE == 3 ? 256 : SIZE >= 2 ? 128 : 64, BN = SIZE == 3 ? 256 : SIZE >= 1 ? 128 : 64;
   static constexpr int WAVES_M = 2, WAVES_N = SIZE == 3 ? 4 : SIZE == 0 && DUAL ? 1 : 2, THREADS = WAVES_M * WAVES_N * 64;
+  static_assert(THREADS == threads_of(WHAT, SIZE), "");
   static constexpr int BK = EXACT || SIZE == 4 || (SIZE == 3 && BACK) ? 32 : SIZE == 0 ? 128 : 64, STAGES = SIZE == 4 || (SIZE == 3 && BACK) ? 4 : SIZE == 1 ? 3 : 2;
   static constexpr int AHEAD = 2;  // EXACT
   static constexpr int LDS = EXACT ? (BM + BN) * BK * 6 * 2 : (BM + BN) * BK * 2 * STAGES;
@@ -1014,22 +1016,24 @@ bool plan(Product& p, int what, int size, bool f32, int64_t slabs_each, int64_t 
   p.tiles_m = (int)(((int64_t)p.M + bm - 1) / bm);
   p.tiles_n = (p.N + bn - 1) / bn;
   const int64_t tiles = tiles_of(p, what, size), slabs = ((int64_t)p.K + bk - 1) / bk * p.segments, results = (int64_t)p.M * p.N * (what == GATED || p.pair ? 2 : 1);
-  if (!launchable(tiles, 512) || slabs > INT32_MAX) return false;
+  const int threads = threads_of(what, size);
+  if (!launchable(tiles, threads) || slabs > INT32_MAX) return false;
   p.tiles = (int)tiles;
   const int64_t splits = std::max<int64_t>(1, std::min(slabs / slabs_each, room / (4 * results)));
   p.slabs_per = (int)((slabs + splits - 1) / splits);
   p.splits = (int)((slabs + p.slabs_per - 1) / p.slabs_per);
-  return launchable((int64_t)p.tiles * p.splits, 512);
+  return launchable((int64_t)p.tiles * p.splits, threads);
 }
 // Tiles and slabs a workgroup for products of one launch: the least of the times that the following gives.  A CU takes `slab` us for a slab of a tile (`alone`: where it has one), and
 // `tile` us for what else there is to one (for those that it has at a time); `resident` tiles run at once.  Joining costs a launch and its memory.  The figures are fitted to products of 14
 // shapes at every size; of 20 others, of short and long sums, the tile taken is 3 % off the best of the five on average, 20 at most (3546 x 1312 x 2368 bf16 43 for 36 us).
+// Only what can be launched is taken, with `others` workgroups beside it: 2^29 rows are too many tiles of 64.
 struct Choice {
   int size;
   int64_t each;
   double time;
 };
-template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room) {
+template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N], bool f32, int64_t room, int64_t others) {
   struct Cost { double slab, alone, tile; int resident; };
   static constexpr Cost BF16[5] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}, {0.57, 0.46, 2.0, 512}},
                         F32[3] = {{0.45, 0.53, 1.5, 768}, {0.78, 0.85, 2.0, 512}, {1.47, 1.47, 7.0, 256}};
@@ -1063,6 +1067,7 @@ template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N
         longest = std::max(longest, slabs[i] / splits * unit[i] * cost.alone / cost.slab);
         groups += tiles[i] * splits;
       }
+      if (!launchable((int64_t)groups + others, threads_of(what[0], size))) break;
       // whole rounds of what is resident, then a last one of fewer a CU
       const double whole = std::floor(groups / cost.resident), last = std::ceil((groups - whole * cost.resident) / 256);
       const double tiles_a_cu = whole * (cost.resident / 256) + (last == 1 ? cost.alone / cost.slab : last);
@@ -1130,7 +1135,7 @@ template <int WHAT, typename T> hipError_t launch_forward(Product& p, const Few&
   if (p.M <= FEW_ROWS) return launch_few<T, DUAL>(few, rows.groups, stream);
   const Product* const all[1] = {&p};
   const int what[1] = {WHAT};
-  const Choice of = choose(all, what, F32, room);
+  const Choice of = choose(all, what, F32, room, 0);
   if (rows.time < std::max((F32 ? 1.1 : 1.3) * of.time, (double)sizeof(T) * (DUAL ? 2 : 1) * p.K * p.N / 5e6)) return launch_few<T, DUAL>(few, rows.groups, stream);
   const int size = of.size;
   if (!plan(p, WHAT, size, F32, of.each, room)) return hipErrorInvalidConfiguration;
@@ -1155,7 +1160,7 @@ template <typename T> int plan_backward(Product& dw, Product& dx, const BiasPart
   constexpr bool F32 = sizeof(T) == 4;
   const Product* const all[2] = {&dw, &dx};
   const int what[2] = {WGRAD, DGRAD};
-  const Choice of = choose(all, what, F32, room);
+  const Choice of = choose(all, what, F32, room, bias.out);
   const int size = of.size;
   const int64_t each = of.each;
   dw.part = reinterpret_cast<float*>(at);
@@ -1167,7 +1172,7 @@ template <typename T> int plan_backward(Product& dw, Product& dx, const BiasPart
   }
   dx.part = reinterpret_cast<float*>(at);
   if (dx.K && !plan(dx, DGRAD, size, F32, each, room)) return -1;
-  return launchable((int64_t)dw.workgroups() + dx.workgroups() + bias.out, 512) ? size : -1;
+  return launchable((int64_t)dw.workgroups() + dx.workgroups() + bias.out, threads_of(WGRAD, size)) ? size : -1;
 }
 // .. and launched.
 template <typename T> hipError_t launch_backward(const Product& dw, const Product& dx, const BiasParts& bias, int size, hipStream_t stream) {

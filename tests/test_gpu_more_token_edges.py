@@ -4,7 +4,7 @@ import math
 import pytest
 
 from paper_2403_08837_amd import binding as b
-from test_gpu_more_token_kernels import BF16, EPS, F32, TYPES, p
+from test_gpu_more_token_kernels import BF16, EPS, F32, TYPES, U, half, p, planes
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -52,3 +52,49 @@ def test_values_outside_the_rotation_stay(W, R, dtype, inter, gammas):
             for v in (out, dx):  # and reaches nothing that is rotated
                 assert bool(torch.isfinite(v[:, heads, :R].float()).all())
     assert same_bits(out[:, H + K:], x[:, H + K:]) and same_bits(dx[:, H + K:], d[:, H + K:])
+
+
+# ---- linear maps of many rows -----------------------------------------------------------------------------------------
+def fill(x, seed, scale=1.0):
+    """Normal numbers, a piece at a time."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    for v in x.split(max(1, (1 << 27) // x.shape[1])):
+        v.copy_(scale * torch.randn(v.shape, generator=g, device="cuda"))
+    return x
+
+
+def ends(n, m=40):
+    return torch.cat([torch.arange(min(n, m)), torch.arange(max(0, n - m), n)]).unique().cuda()
+
+
+def far(got, want, tol, what):
+    worst = float(((got.double() - want).abs() / tol).max())
+    assert got.shape == want.shape and worst <= 1, (what, worst)
+
+
+def product(v, o, n, dtype):
+    """v @ o with what its roundings come to: a result of n terms, and its own."""
+    want = v @ o
+    return want, half(dtype) * want.abs() + ((2 * n + 8) * U + planes(dtype)) * (v.abs() @ o.abs())
+
+
+def test_linear_of_more_rows_than_small_tiles_can_be_launched_for():
+    """2^29 rows and a few: rows at either end, and a gradient of the weights that only the last rows have."""
+    R, I, O, n, t = (1 << 29) + 3, 8, 16, 300, torch.bfloat16
+    empty = lambda *s: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    x, w, bias, y = fill(empty(R, I), 1), fill(empty(O, I), 2), fill(empty(1, O), 3), empty(R, O).fill_(math.nan)
+    b.cdp_k_linear(BF16, 3, p(x), p(w), p(bias), 0, p(y), 0, 0, 0, R, I, O)
+    rows = ends(R, 1000)
+    want, tol = product(x[rows].double(), w.double().t(), I + 1, BF16)
+    far(y[rows], want + bias.double(), tol + (half(BF16) + 20 * U) * bias.double().abs(), "y")
+    dy = y.zero_()
+    fill(dy[-n:], 4)
+    dx, dw, db = empty(R, I).fill_(math.nan), empty(O, I).fill_(math.nan), empty(O).fill_(math.nan)
+    ws = torch.empty(2 * R * O + 4 * O * 256 + 1024 + (1 << 20), dtype=torch.uint8, device="cuda")
+    b.cdp_k_linear_backward(BF16, 3, p(x), p(w), 0, p(dy), p(dx), p(dw), p(db), p(ws), ws.numel(), R, I, O)
+    far(dx[-n:], *product(dy[-n:].double(), w.double(), O, BF16), "dx")
+    assert bool((dx[rows][:1000] == 0).all())
+    far(dw, *product(dy[-n:].double().t(), x[-n:].double(), n, BF16), "dw")
+    d = dy[-n:].double()
+    far(db, d.sum(0), half(BF16) * d.sum(0).abs() + n * U * d.abs().sum(0), "dbias")
