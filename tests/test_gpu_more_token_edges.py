@@ -98,3 +98,59 @@ def test_linear_of_more_rows_than_small_tiles_can_be_launched_for():
     far(dw, *product(dy[-n:].double().t(), x[-n:].double(), n, BF16), "dw")
     d = dy[-n:].double()
     far(db, d.sum(0), half(BF16) * d.sum(0).abs() + n * U * d.abs().sum(0), "dbias")
+
+
+# rows, inputs, outputs: more than 2^31 elements of x, of w and dw, of y and dy
+MANY = [(1050000, 2056, 64), (40, 2056, 1048576), (4, 2056, 1048576), (1050000, 16, 2056)]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,I,O", MANY)
+def test_linear_gradients_from_behind_2_to_31_elements(R, I, O, dtype):
+    """dy is zero but for its last rows, or columns, whose x, or weights, lie behind 2^31 elements: what of them is lost or read elsewhere is all of the result."""
+    t, n = TYPES[dtype], 300
+    empty = lambda *s: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    rows, cols = min(n, R), O if R > O else n  # where dy is not zero: its last so many
+    x, w, dy = fill(empty(R, I), 1), fill(empty(O, I), 2, I ** -0.5), empty(R, O).zero_()
+    d = torch.randn((rows, cols), generator=torch.Generator("cuda").manual_seed(3), device="cuda").to(t)
+    dy[R - rows:, O - cols:] = d
+    assert max((R - rows) * I if R > O else 0, (O - cols) * I if O > R else 0, (R - rows) * O if R > O else 0) > 2 ** 31
+    dx, dw, db = empty(R, I).fill_(math.nan), empty(O, I).fill_(math.nan), empty(O).fill_(math.nan)
+    ws = torch.empty((4 if dtype == F32 else 2) * R * O + 4 * O * min(R, 256) + 1024 + (64 << 20), dtype=torch.uint8, device="cuda")
+    b.cdp_k_linear_backward(dtype, 3, p(x), p(w), 0, p(dy), p(dx), p(dw), p(db), p(ws), ws.numel(), R, I, O)
+    d = d.double()
+    far(dx[R - rows:], *product(d, w[O - cols:].double(), cols, dtype), "dx")
+    far(dw[O - cols:], *product(d.t(), x[R - rows:].double(), rows, dtype), "dw")
+    far(db[O - cols:], d.sum(0), half(dtype) * d.sum(0).abs() + (rows + 40) * U * d.abs().sum(0), "dbias")
+    for v, kept in ((dx, R - rows), (dw, O - cols), (db, O - cols)):  # and zeros elsewhere
+        for part in v[:kept].split(1 << 18):
+            assert not bool(part.any())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gated_gradients_from_behind_2_to_31_elements(dtype):
+    """The same of gated maps: dh behind 2^31 elements alone is not zero."""
+    t, n, (R, I, H) = TYPES[dtype], 300, (1050000, 16, 2056)
+    empty = lambda *s: torch.empty(s, dtype=t, device="cuda")  # noqa: E731
+    x, wg, wu = fill(empty(R, I), 1), fill(empty(H, I), 2, I ** -0.5), fill(empty(H, I), 3, I ** -0.5)
+    h, g, u = (empty(R, H).fill_(math.nan) for _ in range(3))
+    b.cdp_k_gated_linear(dtype, 3, p(x), p(wg), p(wu), p(h), p(g), p(u), 0, 0, R, I, H)
+    rows = ends(R, 1000)
+    for v, w in ((g, wg), (u, wu)):
+        far(v[rows], *product(x[rows].double(), w.double().t(), I, dtype), "g, u")
+    dh = h.zero_()
+    fill(dh[-n:], 4)
+    dx, dwg, dwu = empty(R, I).fill_(math.nan), empty(H, I).fill_(math.nan), empty(H, I).fill_(math.nan)
+    ws = torch.empty(2 * dh.element_size() * R * H + 1024 + (64 << 20), dtype=torch.uint8, device="cuda")
+    b.cdp_k_gated_linear_backward(dtype, 3, p(x), p(wg), p(wu), p(g), p(u), p(dh), p(dx), p(dwg), p(dwu), p(ws), ws.numel(), R, I, H)
+    gd, ud, d, xd = (v[-n:].double() for v in (g, u, dh, x))
+    dg, du = d * ud, d * gd
+    step = half(dtype) + 2 * U  # dg and du are rounded to the element type
+    want = dg @ wg.double() + du @ wu.double()
+    size = dg.abs() @ wg.double().abs() + du.abs() @ wu.double().abs()
+    far(dx[-n:], want, half(dtype) * want.abs() + (step + (4 * H + 8) * U + planes(dtype)) * (1 + step) * size, "dx")
+    for got, v, what in ((dwg, dg, "dwg"), (dwu, du, "dwu")):
+        want, size = v.t() @ xd, v.t().abs() @ xd.abs()
+        far(got, want, half(dtype) * want.abs() + (step + (2 * n + 8) * U + planes(dtype)) * (1 + step) * size, what)
+    for part in dx[:R - n].split(1 << 18):
+        assert not bool(part.any())
