@@ -54,6 +54,40 @@ def test_values_outside_the_rotation_stay(W, R, dtype, inter, gammas):
     assert same_bits(out[:, H + K:], x[:, H + K:]) and same_bits(dx[:, H + K:], d[:, H + K:])
 
 
+@pytest.mark.parametrize("inter", [0, 1])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_what_is_not_finite_reaches_its_own_head_and_stays_there(dtype, bad, inter):
+    """In x or in dout, of a normed head, of one without a gamma, of a v head (copied, bit for bit): every value of the head, the pair's two, that value.  A norm of an
+    infinite head is its values times 0, NaN where they are infinite."""
+    t, n, (H, K, W) = TYPES[dtype], 8, (3, 1, 40)
+    g = torch.Generator()
+    g.manual_seed(1)
+    x, d = (torch.randn((n, H + 2 * K, W), generator=g) for _ in range(2))
+    x[2, 1, 7] = x[3, 4, 5] = x[4, 3, 2] = bad
+    d[5, 1, 7] = d[6, 4, 5] = d[7, 3, 2] = bad
+    pair = [2, 3] if inter else [2, 22]
+    pos, freqs, gamma = torch.arange(1, n + 1).int().cuda(), torch.rand(W // 2, generator=g).cuda(), torch.ones(W).cuda()
+    x, d = x.to(t).cuda(), d.to(t).cuda()
+    out, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty(W, device="cuda")
+    ws = torch.empty(8 * W * n + 256, dtype=torch.uint8, device="cuda")
+    given = (p(x), p(pos), p(freqs), p(gamma), 0)
+    b.cdp_k_head_norm_rotary(dtype, *given, p(out), EPS, inter, n, H, K, W, W)
+    b.cdp_k_head_norm_rotary_backward(dtype, 0, *given, p(d), p(dx), p(dg), 0, EPS, inter, p(ws), ws.numel(), n, H, K, W, W)
+    assert same_bits(out[:, H + K:], x[:, H + K:]) and same_bits(dx[:, H + K:], d[:, H + K:])
+    fine, fine_d = (torch.isfinite(v.float().cpu()) for v in (out, dx))
+    for f, normed, plain in ((fine, 2, 4), (fine_d, 5, 7)):
+        assert not bool(f[normed, 1].all()) and not bool(f[plain, 3, pair].any())
+        if math.isnan(bad) or f is fine_d:
+            assert not bool(f[normed, 1].any())
+        f[normed, 1], f[plain, 3, pair] = True, True
+    assert not bool(fine_d[2, 1].any())  # the gradient of a head that was not finite
+    fine_d[2, 1] = True
+    fine[3, 4, 5], fine_d[6, 4, 5] = True, True
+    assert bool(fine.all()) and bool(fine_d.all())
+    assert not bool(torch.isfinite(dg.cpu()).all())
+
+
 # ---- linear maps of many rows -----------------------------------------------------------------------------------------
 def fill(x, seed, scale=1.0):
     """Normal numbers, a piece at a time."""
