@@ -188,3 +188,29 @@ def test_gated_gradients_from_behind_2_to_31_elements(dtype):
         far(got, want, half(dtype) * want.abs() + (step + (2 * n + 8) * U + planes(dtype)) * (1 + step) * size, what)
     for part in dx[:R - n].split(1 << 18):
         assert not bool(part.any())
+
+
+# ---- small and large fp32 values --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("R,I,O", [(5, 72, 136), (16, 200, 264), (40, 520, 136), (70, 264, 136), (300, 328, 520), (1030, 1032, 1544)])
+@pytest.mark.parametrize("small", ["x", "w"])
+@pytest.mark.parametrize("power", [100, 115, 125, 130])
+def test_linear_of_small_fp32_values(power, small, R, I, O):
+    """One factor of about 2^-power, the other of 2^power (2^125 at most): of a factor 2^-27 of itself and what is below 2^-133 may be left out, of a product 2^-26."""
+    up = min(power, 125)
+
+    def rand(seed, *shape, p):
+        return torch.ldexp(torch.randn(shape, generator=torch.Generator("cuda").manual_seed(seed), device="cuda"), torch.tensor(p, device="cuda"))
+    less, more = rand(1, R, I, p=-power), rand(2, O, I, p=up)
+    if small == "w":
+        less, more = rand(1, O, I, p=-power), rand(2, R, I, p=up)
+    x, w = (less, more) if small == "x" else (more, less)
+    dy = {k: rand(3, R, O, p=v) for k, v in (("dx", -power if small == "x" else up), ("dw", up if small == "x" else -power))}
+    y, dx, dw = torch.empty((R, O), device="cuda"), torch.empty((R, I), device="cuda"), torch.empty((O, I), device="cuda")
+    ws = torch.empty(4 * R * O + 4 * O * min(R, 256) + 1024 + (4 << 20), dtype=torch.uint8, device="cuda")
+    b.cdp_k_linear(F32, 3, p(x), p(w), 0, 0, p(y), 0, 0, 0, R, I, O)
+    b.cdp_k_linear_backward(F32, 3, 0, p(w), 0, p(dy["dx"]), p(dx), 0, 0, p(ws), ws.numel(), R, I, O)
+    b.cdp_k_linear_backward(F32, 3, p(x), 0, 0, p(dy["dw"]), 0, p(dw), 0, p(ws), ws.numel(), R, I, O)
+    x, w, dy = x.double(), w.double(), {k: v.double() for k, v in dy.items()}
+    for got, v, o, n, what in ((y, x, w.t(), I, "y"), (dx, dy["dx"], w, O, "dx"), (dw, dy["dw"].t(), x, R, "dw")):
+        want, tol = product(v, o, n, F32)
+        far(got, want, tol + 2.0 ** -133 * (v.abs().sum(1)[:, None] + o.abs().sum(0)), what)
