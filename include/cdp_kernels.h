@@ -211,7 +211,7 @@ int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* b
 int cdp_k_linear_backward(int dtype, int act, const void* x, const void* w, const void* z, const void* dy, void* dx, void* dw, void* dbias, void* workspace,
                           size_t workspace_bytes, int rows, int in, int out, void* stream);
 
-/* Of rows of logits, z = scale * logits[row * ld + 0 .. vocab) (scale > 0; ld >= vocab, up to 2^31; vocab up to 2^28; |z| within fp32), all fp32:
+/* Of rows of logits, z = scale * logits[row * ld + 0 .. vocab) (scale 1e-30 to 1e38; ld >= vocab, up to 2^31; vocab up to 2^28; |z| within fp32), all fp32:
  *   lse[row] = log sum exp z;  logprob[row] = z[targets[row]] - lse (with targets);  entropy[row] = - sum p log p, p = exp(z - lse) (may be NULL)
  *   top_ids[row][top] (int32), top_logprobs[row][top]: the likeliest tokens in order and their z - lse; of equal logits the lowest id first.
  *   top up to 64 and vocab (0: none)

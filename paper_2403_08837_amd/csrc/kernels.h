@@ -457,6 +457,8 @@ struct TokenLogprob {
   int rows, vocab, top, parts;
   float scale;
 };
+// scales whose product with log2(e) fp32 holds, and with which logits that are past fp32 apart are past its exponentials too
+constexpr float LOGPROB_MIN_SCALE = 1e-30f, LOGPROB_MAX_SCALE = 1e38f;
 constexpr int LOGPROB_MAX_TOP = 64, LOGPROB_MAX_SPLIT = 32, LOGPROB_MAX_VOCAB = 1 << 28, LOGPROB_BYTES = 1 << 20;
 hipError_t launch_token_logprob(const TokenLogprob& a, void* workspace, int dtype, hipStream_t stream);
 hipError_t launch_token_logprob_bwd(const TokenLogprob& a, int dtype, hipStream_t stream);

@@ -51,7 +51,7 @@ static bool linear_sizes(int dtype, int act, int rows, int in, int hidden) {
 }
 static bool logprob_sizes(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, int rows, int vocab) {
   return (dtype == DT_F32 || dtype == DT_BF16) && logits && aligned_to(logits, dtype == DT_BF16 ? 2 : 4) && aligned_to(targets, 4) && rows > 0 && vocab > 0 &&
-         vocab <= LOGPROB_MAX_VOCAB && ld >= vocab && ld <= (1ll << 31) && scale > 0.f && std::isfinite(scale);
+         vocab <= LOGPROB_MAX_VOCAB && ld >= vocab && ld <= (1ll << 31) && scale >= LOGPROB_MIN_SCALE && scale <= LOGPROB_MAX_SCALE;
 }
 
 extern "C" {

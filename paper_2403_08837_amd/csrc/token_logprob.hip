@@ -184,6 +184,11 @@ template <typename F> __device__ __forceinline__ void ranked(u64* keys, int n, i
   for (int i = threadIdx.x; i < min(n, top); i += THREADS) out(i, keys[i]);
 }
 
+// scale * (l - m) - ls, in 64 bits where the difference is past fp32 (logits of either sign near its end), which the product need not be.
+__device__ __forceinline__ float log_of(float scale, float l, float m, float ls) {
+  const float d = l - m;
+  return fabsf(d) < INFINITY ? fmaf(scale, d, -ls) : (float)((double)scale * ((double)l - (double)m) - (double)ls);
+}
 // What a row is, from its sums.
 __device__ __forceinline__ void write_row(const TokenLogprob& a, int64_t row, const Sums& w, float l) {  // l: the target's logit
   const bool none = w.m == -INFINITY && w.s == 0.f;  // everything masked
@@ -191,12 +196,12 @@ __device__ __forceinline__ void write_row(const TokenLogprob& a, int64_t row, co
   a.lse[row] = lse;
   if (a.entropy) a.entropy[row] = none ? 0.f : ls - LN2 * (w.t / w.s);
   if (a.logprob) {
-    a.logprob[row] = none || l == -INFINITY ? (w.s != w.s ? w.s : -INFINITY) : fmaf(a.scale, l - w.m, -ls);
+    a.logprob[row] = none || l == -INFINITY ? (w.s != w.s ? w.s : -INFINITY) : log_of(a.scale, l, w.m, ls);
   }
 }
 __device__ __forceinline__ float top_logprob(const TokenLogprob& a, const Sums& w, float l) {
   if (w.m == -INFINITY && w.s == 0.f) return -INFINITY;
-  return l == -INFINITY && w.s == w.s ? -INFINITY : fmaf(a.scale, l - w.m, -logf(w.s));
+  return l == -INFINITY && w.s == w.s ? -INFINITY : log_of(a.scale, l, w.m, logf(w.s));
 }
 // A row that is not wanted: nothing of it is read.
 __device__ __forceinline__ void write_none(const TokenLogprob& a, int64_t row) {

@@ -214,3 +214,56 @@ def test_linear_of_small_fp32_values(power, small, R, I, O):
     for got, v, o, n, what in ((y, x, w.t(), I, "y"), (dx, dy["dx"], w, O, "dx"), (dw, dy["dw"].t(), x, R, "dw")):
         want, tol = product(v, o, n, F32)
         far(got, want, tol + 2.0 ** -133 * (v.abs().sum(1)[:, None] + o.abs().sum(0)), what)
+
+
+# ---- log probabilities ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("shared", [0, 1 << 20])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_logprob_of_logits_whose_difference_overflows(dtype, shared):
+    """Logits of +-2e38 with a scale of 1/2: |z| is within fp32, and so are the log probabilities, up to -2e38 (their rounding: that of scale * logit, and one step)."""
+    t, V, top, scale = TYPES[dtype], 20011, 3, 0.5
+    x = torch.full((4, V), -2e38, dtype=torch.float64)
+    x[0, 5] = 2e38
+    x[1, [7, 9000]] = 2e38
+    x[2, 1] = 1e38
+    x[2, 2] = -3e38
+    x[3] = 2e38
+    x[3, 11] = -1.5e38
+    x = x.to(t)
+    targets = torch.tensor([6, 8, 2, 11], dtype=torch.int32)
+    xd, td = x.cuda(), targets.cuda()
+    lp, en, lse, best = (torch.empty(s, device="cuda") for s in (4, 4, 4, (4, top)))
+    ids, dx, ones, ws = torch.empty((4, top), dtype=torch.int32, device="cuda"), torch.empty_like(xd), torch.ones(4, device="cuda"), torch.empty(1 << 20, dtype=torch.uint8, device="cuda")
+    b.cdp_k_token_logprob(dtype, p(xd), V, p(td), scale, p(lp), p(en), p(lse), p(ids), p(best), top, p(ws) if shared else 0, shared, 4, V)
+    b.cdp_k_token_logprob_backward(dtype, p(xd), V, p(td), scale, p(lse), p(en), p(ones), p(ones), p(dx), 4, V)
+    z = scale * x.double()
+    z = z - z.amax(1, keepdim=True)  # (64 bits of 1e38 have no room for the logarithm beside it)
+    logp = z - torch.log(torch.exp(z).sum(1, keepdim=True))
+    want = logp.gather(1, targets.long()[:, None])[:, 0]
+    assert bool(torch.isfinite(lp).all())
+    far(lp.cpu(), want, 4 * U * want.abs(), "logprob")
+    order = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :top]
+    assert torch.equal(ids.cpu().long(), order)
+    wanted = logp.gather(1, order)
+    far(best.cpu(), wanted, 4 * U * wanted.abs() + 40 * U, "top")
+    entropy = torch.tensor([0.0, math.log(2), 0.0, math.log(V - 1)], dtype=torch.float64)
+    far(en.cpu(), entropy, U * (V / 64 + 200) * torch.ones(4, dtype=torch.float64), "entropy")
+    assert bool(torch.isfinite(dx.float()).all())
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-20, 1e30, 1e38])
+def test_logprob_of_any_scale(scale):
+    """The same z of logits that are that much larger or smaller."""
+    V = 3001
+    s = torch.tensor(scale).double()
+    x = (3 * torch.randn((3, V), generator=torch.Generator().manual_seed(1), dtype=torch.float64) / s).clamp(-3e38, 3e38).float()
+    targets = torch.tensor([0, 7, V - 1], dtype=torch.int32)
+    xd, td = x.cuda(), targets.cuda()
+    lp, en, lse = (torch.empty(3, device="cuda") for _ in range(3))
+    b.cdp_k_token_logprob(F32, p(xd), V, p(td), scale, p(lp), p(en), p(lse), 0, 0, 0, 0, 0, 3, V)
+    z = s * x.double()
+    want = torch.log_softmax(z, 1)
+    tol = U * (V / 64 + 200) * torch.ones(3, dtype=torch.float64)
+    far(lp.cpu(), want.gather(1, targets.long()[:, None])[:, 0], tol, "logprob")
+    far(lse.cpu(), torch.logsumexp(z, 1), tol, "lse")
+    far(en.cpu(), -(want.exp() * want).sum(1), 8 * tol, "entropy")

@@ -78,3 +78,12 @@ def test_numbers_of_other_kinds_go_through_ctypes(name, good):
 
 def test_in_the_list_of_exports():
     assert {name for name, _, _ in REFUSED} <= set(b.EXPORTS)
+
+
+@pytest.mark.parametrize("scale", [1e-45, 9e-31, 1.1e38, 3e38])
+@pytest.mark.parametrize("name,good", [("cdp_k_token_logprob", LOGP), ("cdp_k_token_logprob_backward", LOGP_B)])
+def test_scales_outside_of_what_is_exact_are_refused(name, good, scale):
+    args = list({**good, "scale": scale}.values()) + [0]
+    with pytest.raises(b.CdpError) as e:
+        getattr(b, name)(*args)
+    assert e.value.code == b.CDP_EINVAL and getattr(b.lib(), name)(*args) == b.CDP_EINVAL
