@@ -60,7 +60,6 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
   const int normed = a.heads + a.kv_heads, all = normed + a.kv_heads;
   const bool has = c * V < pairs;
   const Place at = place<V, INTER>(has ? c : 0, W, R);
-  const int turns_here = R / 2 - c * V;  // pairs of a lane that are turned: the first so many
   const float inv = 1.f / W;
   __shared__ __attribute__((aligned(16))) float gammas[2][2 * MAX_PAIRS];  // of q and k heads; ones where there is none
   if ((int)threadIdx.x < W) {
@@ -131,16 +130,6 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
         v[i] = has ? Elem<T>::to_f32(lo.e[i]) : 0.f;
         v[V + i] = has ? Elem<T>::to_f32(hi.e[i]) : 0.f;
       }
-      // what is behind the rotated pairs stays as it is: a product with a sine of zero would let an infinite value reach the one beside it
-      auto turn_pairs = [&] {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-          const float2 w = angles[j];
-          const float p = v[first_of<V, INTER>(j)], q = v[second_of<V, INTER>(j)];
-          v[first_of<V, INTER>(j)] = j < turns_here ? p * w.x - q * w.y : p;
-          v[second_of<V, INTER>(j)] = j < turns_here ? q * w.x + p * w.y : q;
-        }
-      };
       if constexpr (!BACKWARD) {
         if (norm) {
           float s = 0.f;
@@ -150,9 +139,23 @@ __global__ __launch_bounds__(THREADS) void head_rotary_kernel(const HeadRotary a
 #pragma unroll
           for (int i = 0; i < 2 * V; ++i) v[i] = v[i] * rho * gamma[i < V ? at.o0 + i : at.o1 + i - V];
         }
-        turn_pairs();
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float2 w = angles[j];
+          const float p = v[first_of<V, INTER>(j)], q = v[second_of<V, INTER>(j)];
+          const bool here = c * V + j < R / 2;  // (what is behind stays as it is: times a sine of zero, an infinite value would reach the one beside it)
+          v[first_of<V, INTER>(j)] = here ? p * w.x - q * w.y : p;
+          v[second_of<V, INTER>(j)] = here ? q * w.x + p * w.y : q;
+        }
       } else {
-        turn_pairs();
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const float2 w = angles[j];
+          const float p = v[first_of<V, INTER>(j)], q = v[second_of<V, INTER>(j)];
+          const bool here = c * V + j < R / 2;
+          v[first_of<V, INTER>(j)] = here ? p * w.x - q * w.y : p;
+          v[second_of<V, INTER>(j)] = here ? q * w.x + p * w.y : q;
+        }
         if (norm) {
           float x[2 * V], ss = 0.f, sa = 0.f;
 #pragma unroll
