@@ -191,7 +191,7 @@ int cdp_k_gated_linear(int dtype, int act, const void* x, const void* wg, const 
                        int rows, int in, int hidden, void* stream);
 
 /* Its gradients from dh[rows][hidden], x, wg, wu, and g, u as the forward wrote them:  dg = dh * u * act'(g) and du = dh * act(g), which bf16 rounds to the
- * element type (not always of up to 16 rows);  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
+ * element type (not of up to 16 rows and 256 of hidden: one launch then, in which they stay fp32);  dx[rows][in] = dg wg + du wu (NULL: not wanted), dwg[hidden][in] = dg^T x and dwu[hidden][in] = du^T x (both NULL: not wanted), in the element type.
  * workspace: bf16 4 * rows * hidden + 1024 bytes, fp32 8 * rows * hidden + 1024 (CDP_EINVAL if smaller), and as above where it holds more: P times
  * 8 * hidden * in bytes for dwg and dwu, then P times 4 * rows * in for dx.  Which results are wanted may, like the room, change their roundings. */
 int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* wg, const void* wu, const void* g, const void* u, const void* dh, void* dx,
@@ -199,12 +199,14 @@ int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* w
 
 /* y[rows][out] = act(z) + residual[rows][out], z = x w^T + bias[out], from x[rows][in], w[out][in]; bias and residual NULL: none.  Types, alignment, sizes, acts, exactness
  * as above.  z not NULL: written too, for the backward (which needs it unless act is 3).  y may be residual.
+ * A vocabulary that is no multiple of 8: weights with rows of zeros up to one; cdp_k_token_logprob takes vocab as it is, and that many columns as ld; of its gradient the
+ * columns between stay, so they are zeroed once, and their rows of dw come out zero.
  * workspace: none needed; where there is one of P times 4 * rows * out bytes, as above. */
 int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
                  size_t workspace_bytes, int rows, int in, int out, void* stream);
 
-/* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products (not always of up
- * to 16 rows);  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
+/* Its gradients from dy[rows][out]:  dz = dy * act'(z), which bf16 rounds to the element type for the products (not of up
+ * to 16 rows and 256 outputs, as above);  dx[rows][in] = dz w (with w), dw[out][in] = dz^T x
  * (with x), dbias[out] = the column sums of dz; each may be NULL (not wanted).  The gradient of the residual is dy.
  * workspace: bf16 2 * rows * out + 4 * out * min(rows, 256) + 1024 bytes, fp32 4 * rows * out + 4 * out * min(rows, 256) + 1024 (CDP_EINVAL if smaller), and as
  * above where it holds more: P times 4 * out * in bytes for dw, then P times 4 * rows * in for dx.  Wanted results and roundings as above. */

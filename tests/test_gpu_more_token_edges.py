@@ -267,3 +267,35 @@ def test_logprob_of_any_scale(scale):
     far(lp.cpu(), want.gather(1, targets.long()[:, None])[:, 0], tol, "logprob")
     far(lse.cpu(), torch.logsumexp(z, 1), tol, "lse")
     far(en.cpu(), -(want.exp() * want).sum(1), 8 * tol, "entropy")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R,C,V,top", [(1, 64, 50257, 5), (37, 64, 50, 3), (300, 128, 1001, 0)])
+def test_a_vocabulary_of_no_multiple_of_8(R, C, V, top, dtype):
+    """The projection with weights padded by rows of zeros, log probabilities of the vocabulary alone, and both gradients: nothing comes from the padding, and nothing goes to it."""
+    t, P = TYPES[dtype], -(-V // 8) * 8
+    g = torch.Generator().manual_seed(V)
+    x, w = torch.randn((R, C), generator=g).to(t).cuda(), torch.zeros((P, C), dtype=t, device="cuda")
+    w[:V] = torch.randn((V, C), generator=g).to(t).cuda() * C ** -0.5
+    targets = torch.randint(V, (R,), generator=g, dtype=torch.int32).cuda()
+    logits, dlogits = torch.empty((R, P), dtype=t, device="cuda"), torch.zeros((R, P), dtype=t, device="cuda")
+    lp, lse, ones = torch.empty(R, device="cuda"), torch.empty(R, device="cuda"), torch.ones(R, device="cuda")
+    ids, best = torch.empty((R, max(1, top)), dtype=torch.int32, device="cuda"), torch.empty((R, max(1, top)), device="cuda")
+    dx, dw, ws = torch.empty_like(x), torch.empty_like(w), torch.empty(1 << 26, dtype=torch.uint8, device="cuda")
+    b.cdp_k_linear(dtype, 3, p(x), p(w), 0, 0, p(logits), 0, p(ws), ws.numel(), R, C, P)
+    b.cdp_k_token_logprob(dtype, p(logits), P, p(targets), 1.0, p(lp), 0, p(lse), p(ids) if top else 0, p(best) if top else 0, top, p(ws), ws.numel(), R, V)
+    b.cdp_k_token_logprob_backward(dtype, p(logits), P, p(targets), 1.0, p(lse), 0, p(ones), 0, p(dlogits), R, V)
+    b.cdp_k_linear_backward(dtype, 3, p(x), p(w), 0, p(dlogits), p(dx), p(dw), 0, p(ws), ws.numel(), R, C, P)
+    far(logits[:, :V], *product(x.double(), w[:V].double().t(), C, dtype), "logits")
+    z = logits[:, :V].double()
+    logp = torch.log_softmax(z, 1)
+    far(lp, logp.gather(1, targets.long()[:, None])[:, 0], U * (V / 64 + 200) * torch.ones(R, dtype=torch.float64, device="cuda"), "logprob")
+    if top:
+        assert torch.equal(ids.long(), torch.sort(z, dim=1, descending=True, stable=True).indices[:, :top])
+    want = torch.zeros_like(z).scatter_(1, targets.long()[:, None], 1.0) - logp.exp()
+    # (probabilities by lse's rounding, sums of V terms in it, and a product's and a difference's)
+    far(dlogits[:, :V], want, half(dtype) * want.abs() + (U * (V / 64 + 200) + 2.0 ** -22 * 20) * logp.exp() + 2 * U, "dlogits")
+    assert not bool(dlogits[:, V:].any()) and not bool(dw[V:].any())
+    d = dlogits.double()
+    far(dx, *product(d, w.double(), P, dtype), "dx")
+    far(dw[:V], *product(d[:, :V].t(), x.double(), R, dtype), "dw")
