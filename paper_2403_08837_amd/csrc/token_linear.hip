@@ -118,7 +118,9 @@ template <typename T> __global__ __launch_bounds__(256) void gated_grad_kernel(c
   b.store(du + i);
 }
 // Memory: 1999 x 1368 in fp32 with its sums 9.6 us (3.4 TB/s; 1500 short workgroups).
-// dz from dy and z (null: not wanted, or it is dy; bf16 rounds it, as above), and its column sums: 256 columns of the rows blockIdx.y * share .. a workgroup, whose sums of dz as it
+// bf16: dz is rounded, as above: dx and dw are 2.4e-3 of their norm off (6272 x 768 x 2048, GELU), 1.7e-3 of that their own rounding; z as the forward rounded it is hardly any of it. The products
+// would take twice their time with two bf16 for dz (413 to 450 us for 8192 x 4096 x 4096).
+// dz from dy and z (null: not wanted, or it is dy), and its column sums: 256 columns of the rows blockIdx.y * share .. a workgroup, whose sums of dz as it
 // is before it is rounded go to part[blockIdx.y][out] (null: not wanted), or, where there is one part, to dbias.
 template <typename T>
 __global__ __launch_bounds__(256) void linear_grad_kernel(const T* z, const T* dy, T* dz, float* part, T* dbias, int rows, int out, int share, int act) {
@@ -1188,8 +1190,9 @@ template <typename T> hipError_t launch_backward(const Product& dw, const Produc
 }
 
 int64_t rounded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
-// Whether a backward pass is one launch: while dx is one slab or two behind each other (us so / in the launches of more rows, 16 rows: bf16 256 x 256 7.6 / 10.3, with 512 outputs
-// 10.4 / 10.3, gated 13.5 / 12.0; fp32 256 x 64 8.5 / 14.3, 512 x 1024 15.4 / 19.6, gated 18.5 / 19.6; 16 x 512 x 12288 60 / 70).
+// Whether a backward pass is one launch: while dx is one slab or two behind each other.  us so / in the launches of more rows, of rows x inputs x outputs: bf16 16 x 256 x 256 4.8 / 7.8,
+// gated 6.4 / 8.2, 16 x 4096 x 256 5.3 / 7.9, 7.1 / 10.0; 16 x 512 x 512, which is not, 7.7 / 8.2, 11.0 / 9.8, 16 x 512 x 1024 13.0 / 10.0, 20.0 / 12.5; fp32 16 x 512 x 512 8.1 / 13.2,
+// 11.3 / 12.8, 16 x 4096 x 512 10.5 / 16.2, 14.5 / 20.8; 16 x 512 x 1024, which is not, 14.2 / 13.1, 22.0 / 14.8, 16 x 512 x 12288 161 / 31.
 bool few_backward(int rows, int out, int dtype) { return rows <= FEW_ROWS && out <= (dtype == DT_F32 ? 512 : 256); }
 template <bool DUAL> hipError_t launch_few_backward(FewBack a, int dtype, hipStream_t stream) {
   a.dx_groups = a.dx ? (a.in + 63) / 64 : 0;
