@@ -299,3 +299,26 @@ def test_a_vocabulary_of_no_multiple_of_8(R, C, V, top, dtype):
     d = dlogits.double()
     far(dx, *product(d, w.double(), P, dtype), "dx")
     far(dw[:V], *product(d[:, :V].t(), x.double(), R, dtype), "dw")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_alternatives_of_rows_whose_large_logits_are_a_few_lanes(dtype):
+    """A quarter of a long row, what 64 lanes of a workgroup read, is large and ascending: nearly all of it is above the first border.  The time stays that of reading a few times (it had gone by the
+    square of the row: 60 and 100 times a random one's here)."""
+    t, V, top = TYPES[dtype], 1 << 24, 64
+    j = torch.arange(V, device="cuda")
+    x = torch.randn((2, V), generator=torch.Generator("cuda").manual_seed(1), device="cuda")
+    x[1] = torch.where((j * x.to(t).element_size() // 16) % 256 < 64, 1000 + j / 64, x[1])
+    x = x.to(t)
+    lse, ids, best = torch.empty(1, device="cuda"), torch.empty((1, top), dtype=torch.int32, device="cuda"), torch.empty((1, top), device="cuda")
+    us = []
+    for row in x:
+        events = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        for _ in range(2):
+            events[0].record()
+            b.cdp_k_token_logprob(dtype, p(row), V, 0, 1.0, 0, 0, p(lse), p(ids), p(best), top, 0, 0, 1, V)
+            events[1].record()
+        torch.cuda.synchronize()
+        us.append(events[0].elapsed_time(events[1]) * 1e3)
+        assert torch.equal(ids[0].long(), torch.sort(row, descending=True, stable=True).indices[:top])
+    assert us[1] < 20 * us[0], us
