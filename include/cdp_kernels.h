@@ -228,7 +228,7 @@ int cdp_k_token_logprob(int dtype, const void* logits, int64_t ld, const int32_t
 /* The gradient of the logits from those of logprob (dlogprob[rows]; NULL: none) and entropy (dentropy[rows], with entropy as the forward wrote it; NULL:
  * none) and the forward's lse:  dlogits[j] = scale * (dlogprob * ((j == target) - p[j]) - dentropy * p[j] * (log p[j] + entropy)), elem type, at the rows and
  * columns of logits (ld; what is between rows stays).  dlogits may be logits.  Zeros for a row whose target is outside [0, vocab) and for one of -infinity alone.
- * Probabilities are made from lse, with its rounding: |lse| * 2^-22 of themselves. */
+ * Probabilities are made from lse, with its rounding: |lse| * 2^-22 of themselves; those below 2^-126 count as zero. */
 int cdp_k_token_logprob_backward(int dtype, const void* logits, int64_t ld, const int32_t* targets, float scale, const float* lse, const float* entropy,
                                  const float* dlogprob, const float* dentropy, void* dlogits, int rows, int vocab, void* stream);
 
