@@ -10,6 +10,13 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 
+@pytest.fixture(autouse=True)
+def memory_goes_back():
+    """(Some of these take tens of gigabytes.)"""
+    yield
+    torch.cuda.empty_cache()
+
+
 def same_bits(x, y):
     i = {2: torch.int16, 4: torch.int32}[x.element_size()]
     return torch.equal(x.contiguous().view(i), y.contiguous().view(i))
