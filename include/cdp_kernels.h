@@ -199,8 +199,8 @@ int cdp_k_gated_linear_backward(int dtype, int act, const void* x, const void* w
 
 /* y[rows][out] = act(z) + residual[rows][out], z = x w^T + bias[out], from x[rows][in], w[out][in]; bias and residual NULL: none.  Types, alignment, sizes, acts, exactness
  * as above.  z not NULL: written too, for the backward (which needs it unless act is 3).  y may be residual.
- * A vocabulary that is no multiple of 8: weights with rows of zeros up to one; cdp_k_token_logprob takes vocab as it is, and that many columns as ld; of its gradient the
- * columns between stay, so they are zeroed once, and their rows of dw come out zero.
+ * A vocabulary that is no multiple of 8: weights with rows of zeros up to one; cdp_k_token_logprob takes vocab as it is, and the padded number of columns as ld; its gradient
+ * leaves the columns between as they are, so they are zeroed once, and their rows of dw come out zero.
  * workspace: none needed; where there is one of P times 4 * rows * out bytes, as above. */
 int cdp_k_linear(int dtype, int act, const void* x, const void* w, const void* bias, const void* residual, void* y, void* z, void* workspace,
                  size_t workspace_bytes, int rows, int in, int out, void* stream);

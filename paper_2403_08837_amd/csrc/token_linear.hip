@@ -1039,9 +1039,10 @@ template <int N> Choice choose(const Product* const (&p)[N], const int (&what)[N
   struct Cost { double slab, alone, tile; int resident; };
   static constexpr Cost BF16[5] = {{0.40, 0.43, 1.0, 512}, {0.30, 0.36, 1.6, 512}, {0.49, 0.68, 2.0, 512}, {1.60, 1.60, 5.0, 256}, {0.57, 0.46, 2.0, 512}},
                         F32[3] = {{0.45, 0.53, 1.5, 768}, {0.78, 0.85, 2.0, 512}, {1.47, 1.47, 7.0, 256}};
-  Choice best = {0, INT32_MAX, 0};
+  const int first = f32 && what[0] == GATED ? 1 : 0;  // (64 x 64 of a gated map in fp32 would be two wavefronts)
+  Choice best = {first, INT32_MAX, 0};
   double least = 1e30;
-  for (int size = f32 && what[0] == GATED ? 1 : 0; size < (f32 ? 3 : 5); ++size) {  // (64 x 64 of a gated map in fp32 would be two wavefronts)
+  for (int size = first; size < (f32 ? 3 : 5); ++size) {
     const Cost& cost = f32 ? F32[size] : BF16[size];
     int64_t tiles[N], slabs[N], most = 1;
     double unit[N];  // of a slab
